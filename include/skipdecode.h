@@ -50,7 +50,9 @@ typedef enum {
   SD_ERR_DEVICE = -6     /* the device status word is non-zero (see sd_status)                */
 } sd_error;
 
-enum { SD_DTYPE_FP32 = 0, SD_DTYPE_BF16 = 1 };
+/* Element types.  A model's storage (sd_config.dtype) is one of the first two; the others are types of a paged
+ * cache (fp32, bf16, int8, e4m3) or of the rows handed to its calls (fp32, bf16, fp16). */
+enum { SD_DTYPE_FP32 = 0, SD_DTYPE_BF16 = 1, SD_DTYPE_FP16 = 2, SD_DTYPE_INT8 = 3, SD_DTYPE_E4M3 = 4 };
 
 /* Model and limits.  Plain data, copied by sd_create.
  * dtype selects the storage type of weights and the KV cache; the residual
@@ -241,8 +243,132 @@ int sd_greedy(sd_handle *h, const float *d_logits, int B, int32_t *d_next);
 int sd_sample_top_p(sd_handle *h, const float *d_logits, int B, float temperature, float top_p,
                     const float *d_uniforms, int32_t *d_next);
 
+/* Token selection with each row's own settings.  Every member is a DEVICE array of B values or NULL (the setting is off
+ * for all rows).  With the tokens of row b in order of decreasing logit (equal logits: lower token id first) and
+ * w = exp((logit - maximum) / temperature), the row keeps a prefix of that order, the shortest that these leave:
+ *   top_k > 0:  the first top_k tokens (0 or less: off);
+ *   top_p < 1:  of those, the fewest first ones whose w sum to at least top_p of what the top_k tokens sum to;
+ *   min_p > 0:  the tokens with w >= min_p (the maximum has w = 1);
+ * never fewer than one token.  temperature 0 answers the lowest index of the maximum, whatever the other settings. */
+typedef struct {
+  const float *temperature;   /* >= 0, finite; NULL = 1 */
+  const int32_t *top_k;
+  const float *top_p;
+  const float *min_p;
+} sd_sampling;
+
+/* d_next[b] = the first kept token whose running sum of w exceeds d_uniforms[b] times the sum over the kept ones.
+ * d_uniforms: device fp32 [B], each in [0, 1) (values outside are clamped into the range).  The weights are computed in
+ * double precision and summed as fixed-point integers (2^-47 of the maximum's at 50 272 tokens, finer below): the result does not
+ * depend on thread order, and it is the one that 64-bit floating point gives unless a border is hit within about 1e-12 of it.  A logit that is NaN counts
+ * as minus infinity; a row without a finite maximum answers the lowest index of its maximum, or 0.  A setting
+ * that is NaN, or a temperature that is negative or infinite, sets the bad-setting bit of the status word, and that
+ * row answers the lowest index of its maximum.  sd_sample_top_p is the call for one scalar setting of temperature and top_p.
+ * d_logits: device fp32 [B, vocab]; d_next: device int32 [B].  Errors: SD_ERR_ARG, SD_ERR_CUDA. */
+int sd_sample(sd_handle *h, const float *d_logits, int B, const sd_sampling *settings, const float *d_uniforms,
+              int32_t *d_next);
+
+/* ---- paged cache ---------------------------------------------------------------------------
+ *
+ * A cache whose memory is handed out in pages, for sequences that come, grow and go at positions of their own (the
+ * batching limitation of Section 5 does not apply to it), in fp32, bf16, or 8 bits with a scale for each token and head.
+ * The object holds, per layer, a pool of K pages and one of V pages, [n_pages, n_kv_heads, page_len, head_dim], and in
+ * 8 bits a scale pool [n_pages, n_kv_heads, page_len] of fp32 for each.  Which page belongs to which sequence is the
+ * caller's to decide: every call brings a table.
+ *
+ * Streams and workspaces: work is enqueued on the stream given to sd_cache_create, calls return without synchronising,
+ * and every call may be captured into a CUDA graph on that stream.  All calls of one object share its workspace:
+ * they, and replays of graphs captured from them, must not run at the same time (one stream, or events between two). */
+typedef struct sd_cache sd_cache;
+
+typedef struct {
+  int32_t n_layers, n_heads, n_kv_heads, head_dim;  /* n_heads a multiple of n_kv_heads; head_dim 32, 64 or 128 */
+  int32_t page_len;                                  /* positions per page: 8, 16, 32, 64 or 128 */
+  int32_t n_pages;
+  int32_t max_seqs, max_tokens;                      /* most sequences and most new tokens of one call */
+  int32_t dtype;                                     /* SD_DTYPE_FP32, BF16, INT8 or E4M3 */
+} sd_cache_config;
+
+/* The sequences of one call and the new tokens each of them brings.  The first three are DEVICE arrays.  Row r of the new
+ * tokens, first[s] <= r < first[s + 1], belongs to sequence s and sits at position len[s] - first[s + 1] + r: the new
+ * tokens are the last ones of a sequence of len[s] positions.  Position p lives in page pages[s * pages_per_seq + p /
+ * page_len], slot p % page_len; table entries beyond a sequence's end are not read.  Rows from first[n_seqs] on are
+ * padding: left as they are in outputs, ignored in inputs.  A row whose position is negative (more new tokens than len[s])
+ * has no place: it is not stored, and its outputs are zeros.
+ * What the device finds wrong sets the bad-batch bit of the cache's status word and is skipped or read as zeros, never
+ * read or written out of range: a page number outside [0, n_pages), first not increasing or beyond n_tokens, len beyond
+ * the table, a sequence with more than max_new rows (the surplus is skipped). */
+typedef struct {
+  const int32_t *pages;      /* [n_seqs, pages_per_seq] */
+  const int32_t *first;      /* [n_seqs + 1], first[0] >= 0, not decreasing */
+  const int32_t *len;        /* [n_seqs] */
+  int32_t n_seqs, pages_per_seq;
+  int32_t n_tokens;          /* rows of the tensors; 0: the call does nothing */
+  int32_t max_new;           /* most new tokens of a sequence */
+  int32_t max_len;           /* longest len, or 0 when it is not known: pages_per_seq * page_len.  It only guides how the
+                                work is split: a longer sequence is still handled whole. */
+} sd_batch;
+
+/* Rows [n_tokens, heads, head_dim] on the device, fp32, bf16 or fp16; strides in elements, the elements of a head
+ * adjacent.  data: aligned to its element.  Strides of an input may be 0 (broadcast); rows and heads of an output must not
+ * overlap.  Outputs in fp16 saturate at 65504. */
+typedef struct {
+  void *data;
+  int64_t row_stride, head_stride;
+  int32_t dtype;
+} sd_heads;
+
+/* Bytes of device memory the arena must provide.  out: host.  Errors: SD_ERR_ARG. */
+int sd_cache_bytes(const sd_cache_config *cfg, size_t *out);
+
+/* Creates a cache in the caller's arena (device, 256-byte aligned).  Status word and counters are cleared on the stream;
+ * the pools are not.  Errors: SD_ERR_ARG, SD_ERR_CAPACITY (arena too small), SD_ERR_CUDA. */
+int sd_cache_create(const sd_cache_config *cfg, void *arena, size_t arena_bytes, void *stream, sd_cache **out);
+
+/* Device pointers of one layer's pools (scales NULL unless the cache is in 8 bits).  out pointers: host, may be NULL. */
+int sd_cache_layer(sd_cache *c, int layer, void **k, void **v, float **k_scale, float **v_scale);
+
+/* Writes the new tokens' keys and values (rows [n_tokens, n_kv_heads, head_dim]) into their places, rounded to nearest,
+ * ties to even.  In 8 bits the scale of a (token, head) is the largest magnitude of its head_dim elements divided by 127
+ * (int8) or 448 (e4m3), in fp32, and a code is the nearest to x / scale, decided exactly.  In every type elements that are
+ * not finite do not count for the scale and set the not-finite bit of the status word: infinities (and what rounds
+ * to one) are stored as the largest finite value, NaN as 0, so that a masked key never puts a NaN into a sum.  Whoever writes
+ * to the pools directly keeps to that.  Two rows of one call must
+ * not share a place (their contents would mix).  Errors: SD_ERR_ARG, SD_ERR_CAPACITY (beyond the configuration), SD_ERR_CUDA. */
+int sd_cache_append(sd_cache *c, int layer, const sd_batch *batch, const sd_heads *k, const sd_heads *v);
+
+/* Reads the keys and values at the new tokens' places back: code times scale in fp32, rounded once to the output's type.
+ * With first = prefix sums of len, whole sequences. */
+int sd_cache_read(sd_cache *c, int layer, const sd_batch *batch, const sd_heads *k, const sd_heads *v);
+
+/* Attention of the new tokens, whose keys and values have been appended, over their sequences: the row at position p
+ * attends to positions 0..p,
+ *   out[r, h] = sum_j softmax_j(scale * q[r, h] . K[j, g]) V[j, g],  g = h / (n_heads / n_kv_heads).
+ * q, out: rows [n_tokens, n_heads, head_dim].  scale: finite; 0 stands for head_dim^-1/2.  Single tokens, chunks
+ * and both in one call.  Sums and softmax statistics are fp32. */
+int sd_cache_attention(sd_cache *c, int layer, const sd_batch *batch, const sd_heads *q, float scale, const sd_heads *out);
+
+/* Synchronises the stream, reads the cache's status word and clears it.  Returns SD_ERR_DEVICE when it was not 0. */
+int sd_cache_status(sd_cache *c, int32_t *device_status);
+
+void sd_cache_destroy(sd_cache *c);
+
+/* Runs the new tokens of a batch through the model over a paged cache in place of the handle's own: embedding at each
+ * row's own position, then the layers [0, warmup) and [n_layers - (n_active - warmup), n_layers) (Section 2.4; n_active
+ * = n_layers for prompts), each appending to and attending over its layer of the cache, and the logits of every sequence's
+ * last new token.  Prompts in one piece or in chunks, single tokens, and both in one call.  As in sd_decode_step a
+ * layer's keys and values exist only at positions that ran it, so n_active must not grow along a sequence; sequences
+ * at one budget share a call.  The cache must have the model's layers, heads (n_kv_heads = n_heads) and head size, and
+ * the handle's stream.  Independent of sd_schedule, sd_prefill and the handle's own cache, which it leaves alone.
+ * d_tokens: device int32 [n_tokens] (padding rows too need valid ids), n_tokens at most the rows of a prompt pass,
+ * max(max_batch, 4096 / max_prompt * max_prompt, max_prompt), n_seqs at most max_batch.  d_logits: device fp32
+ * [n_seqs, vocab]; a sequence without new tokens gets a row of no meaning.
+ * Errors: SD_ERR_ARG, SD_ERR_CAPACITY, SD_ERR_CUDA. */
+int sd_extend(sd_handle *h, sd_cache *c, const sd_batch *batch, const int32_t *d_tokens, int n_active, int warmup,
+              float *d_logits);
+
 /* Synchronises the stream and reads the device status word (0 = no error; kernels
- * set bits on an out-of-range token id or a bounded wait that expired).
+ * set bits on an out-of-range token id, a sampling setting that is no number or a bounded wait that expired).
  * Returns SD_ERR_DEVICE when it is non-zero. */
 int sd_status(sd_handle *h, int32_t *device_status);
 

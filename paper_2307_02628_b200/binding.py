@@ -23,7 +23,9 @@ KERNEL_CLASSES = ("embed", "layernorm", "gemm_qkv", "kv_append", "attention", "l
 EXPORTS = ("sd_arena_bytes", "sd_create", "sd_schedule", "sd_schedule_compute", "sd_schedule_power_compute",
            "sd_schedule_custom", "sd_layer_capacity",
            "sd_prefill", "sd_decode_step", "sd_decode_step_static", "sd_rewind", "sd_launch_count", "sd_decode_step_host", "sd_greedy", "sd_sample_top_p", "sd_set_padding", "sd_set_rows", "sd_status", "sd_stats",
-           "sd_set_option", "sd_kernel_time", "sd_kernel_time_reset", "sd_strerror", "sd_destroy")
+           "sd_set_option", "sd_kernel_time", "sd_kernel_time_reset", "sd_strerror", "sd_destroy",
+           "sd_sample", "sd_cache_bytes", "sd_cache_create", "sd_cache_layer", "sd_cache_append", "sd_cache_read", "sd_cache_attention",
+           "sd_cache_status", "sd_cache_destroy", "sd_extend")
 
 
 class SdConfig(C.Structure):
@@ -42,6 +44,33 @@ class SdWeights(C.Structure):
 
 class SdPlan(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("max_layers", "min_layers", "warmup", "gen_len", "full_capacity")]
+
+
+class SdSampling(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p")]
+
+
+class SdCacheConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_heads", "n_kv_heads", "head_dim", "page_len", "n_pages",
+                                          "max_seqs", "max_tokens", "dtype")]
+
+
+class SdBatch(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("pages", "first", "len")] + \
+               [(n, C.c_int32) for n in ("n_seqs", "pages_per_seq", "n_tokens", "max_new", "max_len")]
+
+
+class SdHeads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64), ("dtype", C.c_int32)]
+
+
+# element types of a paged cache and of the rows handed to its calls
+SD_DTYPE_FP32, SD_DTYPE_BF16, SD_DTYPE_FP16, SD_DTYPE_INT8, SD_DTYPE_E4M3 = 0, 1, 2, 3, 4
+_CACHE_TYPES = {"fp32": (SD_DTYPE_FP32, torch.float32), "bf16": (SD_DTYPE_BF16, torch.bfloat16),
+                "int8": (SD_DTYPE_INT8, torch.int8), "e4m3": (SD_DTYPE_E4M3, torch.float8_e4m3fn)}
+_ROW_TYPES = {torch.float32: SD_DTYPE_FP32, torch.bfloat16: SD_DTYPE_BF16, torch.float16: SD_DTYPE_FP16}
+# bits of the status words
+STATUS_BAD_TOKEN, STATUS_WAIT_EXPIRED, STATUS_BAD_BATCH, STATUS_BAD_SETTING, STATUS_NOT_FINITE = 1, 2, 16, 32, 64
 
 
 class SdError(RuntimeError):
@@ -83,12 +112,23 @@ def lib() -> C.CDLL:
     L.sd_set_option.argtypes = [vp, C.c_int, C.c_int]
     L.sd_kernel_time.argtypes = [vp, C.c_int, C.POINTER(C.c_double), C.POINTER(C.c_int64)]
     L.sd_kernel_time_reset.argtypes = [vp]
+    L.sd_sample.argtypes = [vp, vp, C.c_int, C.POINTER(SdSampling), vp, vp]
+    L.sd_cache_bytes.argtypes = [C.POINTER(SdCacheConfig), C.POINTER(C.c_size_t)]
+    L.sd_cache_create.argtypes = [C.POINTER(SdCacheConfig), vp, C.c_size_t, vp, C.POINTER(vp)]
+    L.sd_cache_layer.argtypes = [vp, C.c_int, C.POINTER(vp), C.POINTER(vp), C.POINTER(vp), C.POINTER(vp)]
+    L.sd_cache_append.argtypes = [vp, C.c_int, C.POINTER(SdBatch), C.POINTER(SdHeads), C.POINTER(SdHeads)]
+    L.sd_cache_read.argtypes = L.sd_cache_append.argtypes
+    L.sd_cache_attention.argtypes = [vp, C.c_int, C.POINTER(SdBatch), C.POINTER(SdHeads), C.c_float, C.POINTER(SdHeads)]
+    L.sd_cache_status.argtypes = [vp, i32p]
+    L.sd_cache_destroy.argtypes = [vp]
+    L.sd_cache_destroy.restype = None
+    L.sd_extend.argtypes = [vp, vp, C.POINTER(SdBatch), vp, C.c_int, C.c_int, vp]
     L.sd_strerror.argtypes = [C.c_int]
     L.sd_strerror.restype = C.c_char_p
     L.sd_destroy.argtypes = [vp]
     L.sd_destroy.restype = None
     for name in EXPORTS:
-        if name not in ("sd_strerror", "sd_destroy"):
+        if name not in ("sd_strerror", "sd_destroy", "sd_cache_destroy"):
             getattr(L, name).restype = C.c_int
     _lib = L
     return L
@@ -131,6 +171,148 @@ def arena_bytes(cfg: SdConfig, plan: SdPlan) -> int:
     need = C.c_size_t(0)
     _check(lib().sd_arena_bytes(C.byref(cfg), C.byref(plan), C.byref(need)), "sd_arena_bytes")
     return need.value
+
+
+def cache_bytes(cfg: SdCacheConfig) -> int:
+    need = C.c_size_t(0)
+    _check(lib().sd_cache_bytes(C.byref(cfg), C.byref(need)), "sd_cache_bytes")
+    return need.value
+
+
+class CacheBatch:
+    """The sequences of a call and their new tokens (sd_batch).
+
+    pages [n_seqs, pages_per_seq], first [n_seqs + 1], length [n_seqs]: int32 CUDA tensors, read by the device at the call (their
+    contents may change between calls).  Rows first[s] .. first[s + 1] of the token tensors are the last positions of the
+    length[s] of sequence s.  n_tokens, max_new, max_len: the host's bounds on the rows, on a sequence's new tokens and on its
+    length (0: as far as the table reaches).
+    """
+
+    def __init__(self, pages: torch.Tensor, first: torch.Tensor, length: torch.Tensor, n_tokens: int, max_new: int, max_len: int = 0):
+        for name, t in (("pages", pages), ("first", first), ("length", length)):
+            if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous int32 CUDA tensor")
+        if pages.dim() != 2 or first.shape != (pages.shape[0] + 1,) or length.shape != (pages.shape[0],):
+            raise ValueError("shapes must be pages [n, pages_per_seq], first [n + 1], length [n]")
+        if not pages.device == first.device == length.device:
+            raise ValueError("pages, first and length must be on one device")
+        self.pages, self.first, self.length, self.n_tokens = pages, first, length, int(n_tokens)
+        self.device = pages.device
+        self.c = SdBatch(pages.data_ptr(), first.data_ptr(), length.data_ptr(), pages.shape[0], pages.shape[1], int(n_tokens), int(max_new), int(max_len))
+
+
+class PagedCache:
+    """A paged KV cache (sd_cache) in an arena of its own.
+
+    dtype: "fp32", "bf16", "int8" or "e4m3".  Calls are enqueued on `stream` (default: a stream of its own).  When torch's current
+    stream is another one, the two are ordered around every call, so tensors can be used as if the call ran on the current one.
+    """
+
+    def __init__(self, n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, page_len: int, n_pages: int,
+                 max_seqs: int, max_tokens: int, dtype: str = "int8", device: str = "cuda:0", stream=None):
+        if dtype not in _CACHE_TYPES:
+            raise ValueError(f"dtype must be one of {sorted(_CACHE_TYPES)}")
+        self.cfg = SdCacheConfig(n_layers, n_heads, n_kv_heads, head_dim, page_len, n_pages, max_seqs, max_tokens, _CACHE_TYPES[dtype][0])
+        self.arena_bytes = cache_bytes(self.cfg)
+        if not torch.cuda.is_available():
+            raise RuntimeError("no CUDA device: the cache has no CPU fallback")
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.stream = stream if stream is not None else torch.cuda.Stream(device=self.device)
+        self.arena = torch.empty(self.arena_bytes + 256, dtype=torch.uint8, device=self.device)
+        self._base = (self.arena.data_ptr() + 255) // 256 * 256 - self.arena.data_ptr()
+        self.h = C.c_void_p()
+        self._fork()
+        _check(lib().sd_cache_create(C.byref(self.cfg), self.arena.data_ptr() + self._base, self.arena_bytes,
+                                     self.stream.cuda_stream, C.byref(self.h)), "sd_cache_create")
+        self._join()
+
+    def layer(self, layer: int) -> dict:
+        """Views of one layer's pools: k, v [n_pages, n_kv_heads, page_len, head_dim], in 8 bits also k_scale, v_scale."""
+        p = [C.c_void_p() for _ in range(4)]
+        _check(lib().sd_cache_layer(self.h, layer, *[C.byref(x) for x in p]), "sd_cache_layer")
+        c = self.cfg
+        shape = (c.n_pages, c.n_kv_heads, c.page_len)
+        dt = next(t for code, t in _CACHE_TYPES.values() if code == c.dtype)
+        out = {}
+        for name, ptr, dtype, shp in (("k", p[0], dt, shape + (c.head_dim,)), ("v", p[1], dt, shape + (c.head_dim,)),
+                                      ("k_scale", p[2], torch.float32, shape), ("v_scale", p[3], torch.float32, shape)):
+            if ptr.value:
+                at = ptr.value - self.arena.data_ptr()
+                n = dtype.itemsize
+                for s in shp:
+                    n *= s
+                out[name] = self.arena[at:at + n].view(dtype).view(shp)
+        return out
+
+    def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, batch: CacheBatch):
+        """k, v: the new tokens' keys and values [n_tokens, n_kv_heads, head_dim], fp32, bf16 or fp16, elements of a head adjacent."""
+        n = self.cfg.n_kv_heads
+        self._call("sd_cache_append", layer, batch, self._rows("k", k, n, batch), self._rows("v", v, n, batch))
+
+    def read(self, layer: int, batch: CacheBatch, dtype: torch.dtype = torch.float32, k: torch.Tensor | None = None,
+             v: torch.Tensor | None = None):
+        """The keys and values at the new tokens' places, as (k, v) [n_tokens, n_kv_heads, head_dim] of `dtype`."""
+        shape = (batch.n_tokens, self.cfg.n_kv_heads, self.cfg.head_dim)
+        k = torch.empty(shape, dtype=dtype, device=self.device) if k is None else k
+        v = torch.empty(shape, dtype=dtype, device=self.device) if v is None else v
+        self._call("sd_cache_read", layer, batch, self._rows("k", k, shape[1], batch), self._rows("v", v, shape[1], batch))
+        return k, v
+
+    def attention(self, layer: int, q: torch.Tensor, batch: CacheBatch, scale: float | None = None, out: torch.Tensor | None = None):
+        """Causal attention of the new tokens' queries [n_tokens, n_heads, head_dim] over their sequences; out: like q unless given."""
+        if scale is not None and not (scale == scale and abs(scale) != float("inf") and scale != 0):
+            raise ValueError("scale must be a finite number other than 0")
+        n = self.cfg.n_heads
+        if out is None:
+            out = torch.empty(batch.n_tokens, n, self.cfg.head_dim, dtype=q.dtype, device=self.device)
+        self._call("sd_cache_attention", layer, batch, self._rows("q", q, n, batch), 0.0 if scale is None else scale, self._rows("out", out, n, batch))
+        return out
+
+    def status(self) -> int:
+        v = C.c_int32(0)
+        code = lib().sd_cache_status(self.h, C.byref(v))
+        if code not in (SD_OK, SD_ERR_DEVICE):
+            raise SdError(code, "sd_cache_status")
+        return v.value
+
+    def close(self):
+        if getattr(self, "h", None) is not None and self.h.value:
+            self.stream.synchronize()
+            lib().sd_cache_destroy(self.h)
+            self.h = C.c_void_p()
+        self.arena = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _rows(self, name: str, t: torch.Tensor, heads: int, batch: CacheBatch) -> SdHeads:
+        if t.dtype not in _ROW_TYPES or t.device != self.device or batch.device != self.device:
+            raise ValueError(f"{name} must be an fp32, bf16 or fp16 tensor on {self.device}, and so must the batch be there")
+        if t.shape != (batch.n_tokens, heads, self.cfg.head_dim) or (t.stride(2) != 1 and t.numel()):
+            raise ValueError(f"{name} must be [{batch.n_tokens}, {heads}, {self.cfg.head_dim}] with adjacent elements, got {tuple(t.shape)} strides {t.stride()}")
+        return SdHeads(t.data_ptr(), t.stride(0), t.stride(1), _ROW_TYPES[t.dtype])
+
+    def _call(self, name: str, layer: int, batch: CacheBatch, *args):
+        args = [C.byref(a) if isinstance(a, SdHeads) else a for a in args]
+        self._fork()
+        _check(getattr(lib(), name)(self.h, layer, C.byref(batch.c), *args), name)
+        self._join()
+
+    # work before the call on the current stream is seen by it, and work after the call sees its results (and reuses its memory)
+    def _fork(self):
+        cur = torch.cuda.current_stream(self.device)
+        if cur != self.stream:
+            self.stream.wait_stream(cur)
+
+    def _join(self):
+        cur = torch.cuda.current_stream(self.device)
+        if cur != self.stream:
+            cur.wait_stream(self.stream)
 
 
 class Decoder:
@@ -278,6 +460,42 @@ class Decoder:
                                      out.data_ptr()), "sd_sample_top_p")
         return out
 
+    def sample(self, logits: torch.Tensor, uniforms: torch.Tensor, temperature: torch.Tensor | None = None,
+               top_k: torch.Tensor | None = None, top_p: torch.Tensor | None = None, min_p: torch.Tensor | None = None,
+               out: torch.Tensor | None = None) -> torch.Tensor:
+        """One token per row with the row's own settings (CUDA tensors [B], fp32, top_k int32; None: off)."""
+        B = logits.shape[0]
+        if logits.dtype != torch.float32 or logits.shape != (B, self.shape.vocab) or not logits.is_contiguous() or logits.device != self.device:
+            raise ValueError(f"logits must be a contiguous fp32 [B, {self.shape.vocab}] on {self.device}")
+        if out is None:
+            out = torch.empty(B, dtype=torch.int32, device=self.device)
+        for name, t, dt in (("uniforms", uniforms, torch.float32), ("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                            ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32), ("out", out, torch.int32)):
+            if t is not None and (t.dtype != dt or t.shape != (B,) or not t.is_contiguous() or t.device != self.device):
+                raise ValueError(f"{name} must be a contiguous {dt} [{B}] on {self.device}")
+        ptr = [None if t is None else t.data_ptr() for t in (temperature, top_k, top_p, min_p)]
+        self._order()
+        _check(lib().sd_sample(self.h, logits.data_ptr(), B, C.byref(SdSampling(*ptr)), uniforms.data_ptr(), out.data_ptr()), "sd_sample")
+        self._after()
+        return out
+
+    def extend(self, cache: PagedCache, batch: CacheBatch, tokens: torch.Tensor, n_active: int | None = None, warmup: int = 0,
+               logits: torch.Tensor | None = None) -> torch.Tensor:
+        """The batch's new tokens [n_tokens] through the model over a paged cache made with this decoder's stream; n_active layers
+        (default all).  Returns the logits [n_seqs, vocab] of each sequence's last new token."""
+        tokens = self._dev_i32(tokens)
+        if tokens.shape != (batch.n_tokens,):
+            raise ValueError(f"tokens must be [{batch.n_tokens}]")
+        if logits is None:
+            logits = torch.empty(batch.c.n_seqs, self.shape.vocab, dtype=torch.float32, device=self.device)
+        elif logits.shape != (batch.c.n_seqs, self.shape.vocab) or logits.dtype != torch.float32 or not logits.is_contiguous():
+            raise ValueError(f"logits must be a contiguous fp32 [{batch.c.n_seqs}, {self.shape.vocab}]")
+        self._order()
+        _check(lib().sd_extend(self.h, cache.h, C.byref(batch.c), tokens.data_ptr(), self.shape.n_layers if n_active is None else n_active, warmup,
+                               logits.data_ptr()), "sd_extend")
+        self._after()
+        return logits
+
     def status(self) -> int:
         v = C.c_int32(0)
         code = lib().sd_status(self.h, C.byref(v))
@@ -329,3 +547,9 @@ class Decoder:
         cur = torch.cuda.current_stream(self.device)
         if cur != self.stream:
             self.stream.wait_stream(cur)
+
+    def _after(self):
+        # and what the library's stream wrote is seen, and its inputs' memory reused, only after it
+        cur = torch.cuda.current_stream(self.device)
+        if cur != self.stream:
+            cur.wait_stream(self.stream)

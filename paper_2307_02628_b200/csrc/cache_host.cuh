@@ -1,0 +1,378 @@
+// Host side of the paged cache and of sd_extend: argument checks, arena carving, kernel choice.  Part of skipdecode.cu.
+#pragma once
+
+struct sd_cache {
+  sd_cache_config cfg;
+  int esize, page_shift, group, device, sm_count;
+  bool scaled;
+  char* arena;
+  cudaStream_t stream;
+  size_t layer_bytes, v_off, ks_off, vs_off;   // K pool, V pool, K scales, V scales: offsets within a layer
+  size_t minus_pos, last_row, status_off, total;
+  char* layer(int l) const { return arena + (size_t)l * layer_bytes; }
+  template <typename T> T* at(size_t off) const { return reinterpret_cast<T*>(arena + off); }
+  int* status() const { return at<int>(status_off); }
+};
+
+namespace {
+
+// Makes `device` current for the length of a call.
+struct DeviceGuard {
+  int before = -1;
+  bool ok = true;
+  explicit DeviceGuard(int device) {
+    if (cudaGetDevice(&before) != cudaSuccess) { cudaGetLastError(); ok = false; return; }
+    if (before == device) { before = -1; return; }
+    if (cudaSetDevice(device) != cudaSuccess) { cudaGetLastError(); ok = false; }
+  }
+  ~DeviceGuard() { if (before >= 0) cudaSetDevice(before); }
+};
+
+int device_of(const void* p, int* device) {
+  cudaPointerAttributes attr;
+  if (cudaPointerGetAttributes(&attr, p) != cudaSuccess) { cudaGetLastError(); return SD_ERR_CUDA; }
+  if (attr.type != cudaMemoryTypeDevice && attr.type != cudaMemoryTypeManaged) return SD_ERR_ARG;
+  *device = attr.device;
+  return SD_OK;
+}
+
+bool valid_cache_config(const sd_cache_config* c) {
+  if (!c) return false;
+  if (c->n_layers < 1 || c->n_heads < 1 || c->n_kv_heads < 1 || c->n_pages < 1 || c->max_seqs < 1 || c->max_tokens < 1) return false;
+  if (c->n_heads % c->n_kv_heads || c->n_heads > 65535) return false;                // heads are a grid dimension
+  if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128) return false;
+  if (c->page_len < 8 || c->page_len > 128 || (c->page_len & (c->page_len - 1))) return false;
+  return c->dtype == SD_DTYPE_FP32 || c->dtype == SD_DTYPE_BF16 || c->dtype == SD_DTYPE_INT8 || c->dtype == SD_DTYPE_E4M3;
+}
+
+// Lays the arena out; false when a size does not fit 62 bits.
+bool carve_cache(const sd_cache_config& c, sd_cache& A) {
+  A.cfg = c;
+  A.scaled = c.dtype == SD_DTYPE_INT8 || c.dtype == SD_DTYPE_E4M3;
+  A.esize = c.dtype == SD_DTYPE_FP32 ? 4 : c.dtype == SD_DTYPE_BF16 ? 2 : 1;
+  A.page_shift = 0;
+  while ((1 << A.page_shift) < c.page_len) ++A.page_shift;
+  A.group = c.n_heads / c.n_kv_heads;
+  const unsigned __int128 entries = (unsigned __int128)c.n_pages * c.n_kv_heads * c.page_len;
+  const unsigned __int128 per_layer = 2 * entries * (c.head_dim * A.esize + (A.scaled ? 4 : 0)) + 4 * kAlign;
+  if (per_layer * c.n_layers > ((unsigned __int128)1 << 61)) return false;
+  size_t off = 0;
+  auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes); return o; };
+  const size_t values = (size_t)entries * c.head_dim * A.esize, scales = A.scaled ? (size_t)entries * 4 : 0;
+  take(values);
+  A.v_off = take(values);
+  A.ks_off = take(scales);
+  A.vs_off = take(scales);
+  A.layer_bytes = off;
+  off *= c.n_layers;
+  A.minus_pos = take((size_t)c.max_tokens * 4);
+  A.last_row = take((size_t)c.max_seqs * 4);
+  A.status_off = take(256);
+  A.total = off;
+  return true;
+}
+
+int check_batch(const sd_cache* c, const sd_batch* b) {
+  if (!b || !b->pages || !b->first || !b->len) return SD_ERR_ARG;
+  if (b->n_seqs < 1 || b->pages_per_seq < 1 || b->n_tokens < 0 || b->max_len < 0) return SD_ERR_ARG;
+  if ((int64_t)b->pages_per_seq * c->cfg.page_len > 0x7fffffff) return SD_ERR_ARG;
+  if (b->n_seqs > c->cfg.max_seqs || b->n_tokens > c->cfg.max_tokens) return SD_ERR_CAPACITY;
+  if (b->n_tokens > 0 && (b->max_new < 1 || b->max_new > b->n_tokens)) return SD_ERR_ARG;
+  return SD_OK;
+}
+
+int check_rows(const sd_cache* c, const sd_batch* b, const sd_heads* t, int heads, bool output) {
+  if (!t) return SD_ERR_ARG;
+  if (t->dtype != SD_DTYPE_FP32 && t->dtype != SD_DTYPE_BF16 && t->dtype != SD_DTYPE_FP16) return SD_ERR_ARG;
+  if (b->n_tokens == 0) return SD_OK;
+  if (!t->data || t->row_stride < 0 || t->head_stride < 0) return SD_ERR_ARG;
+  const int e = t->dtype == SD_DTYPE_FP32 ? 4 : 2;
+  if (reinterpret_cast<uintptr_t>(t->data) % e) return SD_ERR_ARG;
+  const int64_t far = (int64_t)1 << 50;                         // extents stay inside 64-bit byte offsets
+  if (t->row_stride > far / b->n_tokens || t->head_stride > far / heads) return SD_ERR_ARG;
+  if (output) {                                                 // rows of heads, or heads of rows, without overlap
+    const int64_t hd = c->cfg.head_dim, R = b->n_tokens, H = heads;
+    const bool by_row = (H == 1 || t->head_stride >= hd) && (R == 1 || t->row_stride >= (H - 1) * t->head_stride + hd);
+    const bool by_head = (R == 1 || t->row_stride >= hd) && (H == 1 || t->head_stride >= (R - 1) * t->row_stride + hd);
+    if (!by_row && !by_head) return SD_ERR_ARG;
+  }
+  return SD_OK;
+}
+
+bool wide(const sd_heads* t) {                                  // 16-byte accesses to eight elements at a time
+  const int64_t e = t->dtype == SD_DTYPE_FP32 ? 4 : 2;
+  return reinterpret_cast<uintptr_t>(t->data) % 16 == 0 && t->row_stride * e % 16 == 0 && t->head_stride * e % 16 == 0;
+}
+
+sd::Rows rows_of(const sd_heads* t) { return sd::Rows{t->data, t->row_stride, t->head_stride, t->dtype}; }
+
+sd::BatchView view_of(const sd_cache* c, const sd_batch* b) {
+  return sd::BatchView{b->pages, b->first, b->len, b->n_seqs, b->pages_per_seq, b->n_tokens, b->max_new,
+                       c->cfg.n_pages, c->cfg.page_len, c->page_shift, c->cfg.n_kv_heads, c->status()};
+}
+
+template <typename TC> struct LayerPools { TC *k, *v; float *ks, *vs; };
+template <typename TC>
+LayerPools<TC> pools(const sd_cache* c, int l) {
+  char* p = c->layer(l);
+  return {reinterpret_cast<TC*>(p), reinterpret_cast<TC*>(p + c->v_off), c->scaled ? reinterpret_cast<float*>(p + c->ks_off) : nullptr,
+          c->scaled ? reinterpret_cast<float*>(p + c->vs_off) : nullptr};
+}
+
+// Calls f with a value of the cache's element type, resp. the rows' element type, resp. the head size as a constant.
+template <typename F> int with_cache_type(int dtype, F f) {
+  switch (dtype) {
+    case SD_DTYPE_FP32: return f(float{});
+    case SD_DTYPE_BF16: return f(bf16{});
+    case SD_DTYPE_INT8: return f(int8_t{});
+    default: return f(sd::e4m3{});
+  }
+}
+template <typename F> int with_row_type(int dtype, F f) {
+  return dtype == SD_DTYPE_FP32 ? f(float{}) : dtype == SD_DTYPE_BF16 ? f(bf16{}) : f(__half{});
+}
+template <typename F> int with_head_dim(int hd, F f) {
+  return hd == 128 ? f(std::integral_constant<int, 128>{}) : hd == 64 ? f(std::integral_constant<int, 64>{}) : f(std::integral_constant<int, 32>{});
+}
+
+int launched() { return cudaGetLastError() == cudaSuccess ? SD_OK : SD_ERR_CUDA; }
+
+int cache_append(sd_cache* c, int l, const sd_batch* b, const sd_heads* k, const sd_heads* v) {
+  const bool vec = wide(k) && wide(v);
+  return with_cache_type(c->cfg.dtype, [&](auto tc) {
+    using TC = decltype(tc);
+    const auto P = pools<TC>(c, l);
+    return with_row_type(k->dtype, [&](auto ts) {
+      using TS = decltype(ts);
+      return with_head_dim(c->cfg.head_dim, [&](auto hd) {
+        constexpr int HD = decltype(hd)::value;
+        auto kernel = vec ? sd::cache_append_kernel<TS, TC, HD, true> : sd::cache_append_kernel<TS, TC, HD, false>;
+        kernel<<<b->n_tokens, 256, 0, c->stream>>>(view_of(c, b), rows_of(k), rows_of(v), P.k, P.v, P.ks, P.vs);
+        return launched();
+      });
+    });
+  });
+}
+
+int cache_read(sd_cache* c, int l, const sd_batch* b, const sd_heads* k, const sd_heads* v) {
+  const bool vec = wide(k) && wide(v);
+  return with_cache_type(c->cfg.dtype, [&](auto tc) {
+    using TC = decltype(tc);
+    const auto P = pools<TC>(c, l);
+    return with_row_type(k->dtype, [&](auto to) {
+      using TO = decltype(to);
+      return with_head_dim(c->cfg.head_dim, [&](auto hd) {
+        constexpr int HD = decltype(hd)::value;
+        auto kernel = vec ? sd::cache_read_kernel<TO, TC, HD, true> : sd::cache_read_kernel<TO, TC, HD, false>;
+        kernel<<<b->n_tokens, 256, 0, c->stream>>>(view_of(c, b), rows_of(k), rows_of(v), (const TC*)P.k, (const TC*)P.v,
+                                                   (const float*)P.ks, (const float*)P.vs);
+        return launched();
+      });
+    });
+  });
+}
+
+int cache_attention(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale, const sd_heads* out) {
+  if (scale == 0.f) scale = 1.f / sqrtf((float)c->cfg.head_dim);
+  const float scale_log2 = scale * 1.4426950408889634f;
+  return with_cache_type(c->cfg.dtype, [&](auto tc) {
+    using TC = decltype(tc);
+    const auto P = pools<TC>(c, l);
+    return with_head_dim(c->cfg.head_dim, [&](auto hd) {
+      constexpr int HD = decltype(hd)::value;
+      sd::paged_attn_row_kernel<TC, HD><<<dim3(b->n_tokens, c->cfg.n_heads), 128, 0, c->stream>>>(
+          view_of(c, b), rows_of(q), rows_of(out), (const TC*)P.k, (const TC*)P.v, (const float*)P.ks, (const float*)P.vs, c->group, scale_log2);
+      return launched();
+    });
+  });
+}
+
+// The layers of sd_extend.  The GEMM, LayerNorm and embedding launches are the decode step's; the K and V columns of the QKV
+// product go to the paged cache and the attention reads them from there.
+template <typename T>
+int extend_layers(sd_handle* h, sd_cache* c, const sd_batch* b, const int32_t* d_tokens, int n_active, int warmup, float* d_logits) {
+  Launcher Lc{h, false, h->at<float>(h->A.part_acc), h->at<float>(h->A.part_ml)};
+  const sd_config& m = h->cfg;
+  const int d = m.d_model, f = m.d_ffn, rows = b->n_tokens, top = m.n_layers - (n_active - warmup);
+  float* x = h->at<float>(h->A.x);
+  T* u = h->at<T>(h->A.u);
+  float* qkv = h->at<float>(h->A.qkv);
+  T* o = h->at<T>(h->A.o);
+  T* y = h->at<T>(h->A.y);
+  sd::cache_rows_kernel<<<rows, 128, 0, h->stream>>>(view_of(c, b), c->at<int>(c->minus_pos), c->at<int>(c->last_row));
+  Lc.end();
+  const sd::RowMap map{1, 0, 0, nullptr, nullptr, c->at<int>(c->minus_pos)};
+  enqueue_embed<T>(Lc, d_tokens, rows, map);
+  const sd_heads q{qkv, 3 * d, h->hd, SD_DTYPE_FP32}, k{qkv + d, 3 * d, h->hd, SD_DTYPE_FP32}, v{qkv + 2 * d, 3 * d, h->hd, SD_DTYPE_FP32};
+  // the out-projection's operand: fp32, or fp16 values (see Operand)
+  const sd_heads out{o, d, h->hd, std::is_same<T, float>::value ? SD_DTYPE_FP32 : SD_DTYPE_FP16};
+  auto norm = [&](const void* g, const void* be) {
+    sd::launch_kernel(pdl_for(h, SD_K_LAYERNORM), h->stream, sd::layernorm_kernel<T>, dim3(rows), dim3(ln_threads(d)), 0, x, (const T*)g, (const T*)be, u, d, m.ln_eps, nullptr);
+    Lc.end();
+  };
+  for (int l = 0; l < m.n_layers && !Lc.err; ++l) {
+    if (!(l < warmup || l >= top)) continue;
+    norm(h->ln1_g[l], h->ln1_b[l]);
+    launch_gemm<T>(Lc, SD_K_GEMM_QKV, u, (const T*)h->w_qkv[l], h->A.wp_qkv[l], (const T*)h->b_qkv[l], rows, 3 * d, d, qkv, 3 * d, sd::EPI_STORE_F32);
+    if (cache_append(c, l, b, &k, &v) != SD_OK || cache_attention(c, l, b, &q, 0.f, &out) != SD_OK) return SD_ERR_CUDA;
+    Lc.count += 2;
+    launch_gemm<T>(Lc, SD_K_GEMM_OUT, o, (const T*)h->w_o[l], h->A.wp_o[l], (const T*)h->b_o[l], rows, d, d, x, d, sd::EPI_RESIDUAL_F32);
+    norm(h->ln2_g[l], h->ln2_b[l]);
+    launch_gemm<T>(Lc, SD_K_GEMM_FC1, u, (const T*)h->w_fc1[l], h->A.wp_fc1[l], (const T*)h->b_fc1[l], rows, f, d, y, f * sd::Operand<T>::PARTS, sd::EPI_RELU_T);
+    launch_gemm<T>(Lc, SD_K_GEMM_FC2, y, (const T*)h->w_fc2[l], h->A.wp_fc2[l], (const T*)h->b_fc2[l], rows, d, f, x, d, sd::EPI_RESIDUAL_F32);
+  }
+  enqueue_head<T>(Lc, b->n_seqs, c->at<int>(c->last_row), d_logits);
+  h->launches += Lc.count;
+  return Lc.err;
+}
+
+}  // namespace
+
+extern "C" {
+
+int sd_cache_bytes(const sd_cache_config* cfg, size_t* out) {
+  if (!valid_cache_config(cfg) || !out) return SD_ERR_ARG;
+  sd_cache A;
+  if (!carve_cache(*cfg, A)) return SD_ERR_ARG;
+  *out = A.total;
+  return SD_OK;
+}
+
+int sd_cache_create(const sd_cache_config* cfg, void* arena, size_t arena_bytes, void* stream, sd_cache** out) {
+  if (!valid_cache_config(cfg) || !out || !arena || reinterpret_cast<uintptr_t>(arena) % kAlign) return SD_ERR_ARG;
+  sd_cache* c = new (std::nothrow) sd_cache();
+  if (!c) return SD_ERR_ARG;
+  if (!carve_cache(*cfg, *c)) { delete c; return SD_ERR_ARG; }
+  if (c->total > arena_bytes) { delete c; return SD_ERR_CAPACITY; }
+  c->arena = static_cast<char*>(arena);
+  c->stream = static_cast<cudaStream_t>(stream);
+  int rc = device_of(arena, &c->device);
+  if (rc != SD_OK) { delete c; return rc; }
+  DeviceGuard guard(c->device);
+  c->sm_count = 0;
+  if (!guard.ok || cudaDeviceGetAttribute(&c->sm_count, cudaDevAttrMultiProcessorCount, c->device) != cudaSuccess ||
+      cudaMemsetAsync(c->status(), 0, 256, c->stream) != cudaSuccess) {
+    cudaGetLastError();
+    delete c;
+    return SD_ERR_CUDA;
+  }
+  *out = c;
+  return SD_OK;
+}
+
+int sd_cache_layer(sd_cache* c, int layer, void** k, void** v, float** ks, float** vs) {
+  if (!c || layer < 0 || layer >= c->cfg.n_layers) return SD_ERR_ARG;
+  const auto P = pools<char>(c, layer);
+  if (k) *k = P.k;
+  if (v) *v = P.v;
+  if (ks) *ks = P.ks;
+  if (vs) *vs = P.vs;
+  return SD_OK;
+}
+
+int sd_cache_append(sd_cache* c, int layer, const sd_batch* b, const sd_heads* k, const sd_heads* v) {
+  if (!c || layer < 0 || layer >= c->cfg.n_layers) return SD_ERR_ARG;
+  int rc = check_batch(c, b);
+  if (rc == SD_OK) rc = check_rows(c, b, k, c->cfg.n_kv_heads, false);
+  if (rc == SD_OK) rc = check_rows(c, b, v, c->cfg.n_kv_heads, false);
+  if (rc != SD_OK) return rc;
+  if (k->dtype != v->dtype) return SD_ERR_ARG;
+  if (b->n_tokens == 0) return SD_OK;
+  DeviceGuard guard(c->device);
+  return guard.ok ? cache_append(c, layer, b, k, v) : SD_ERR_CUDA;
+}
+
+int sd_cache_read(sd_cache* c, int layer, const sd_batch* b, const sd_heads* k, const sd_heads* v) {
+  if (!c || layer < 0 || layer >= c->cfg.n_layers) return SD_ERR_ARG;
+  int rc = check_batch(c, b);
+  if (rc == SD_OK) rc = check_rows(c, b, k, c->cfg.n_kv_heads, true);
+  if (rc == SD_OK) rc = check_rows(c, b, v, c->cfg.n_kv_heads, true);
+  if (rc != SD_OK) return rc;
+  if (k->dtype != v->dtype) return SD_ERR_ARG;
+  if (b->n_tokens == 0) return SD_OK;
+  DeviceGuard guard(c->device);
+  return guard.ok ? cache_read(c, layer, b, k, v) : SD_ERR_CUDA;
+}
+
+int sd_cache_attention(sd_cache* c, int layer, const sd_batch* b, const sd_heads* q, float scale, const sd_heads* out) {
+  if (!c || layer < 0 || layer >= c->cfg.n_layers || !std::isfinite(scale)) return SD_ERR_ARG;
+  int rc = check_batch(c, b);
+  if (rc == SD_OK) rc = check_rows(c, b, q, c->cfg.n_heads, false);
+  if (rc == SD_OK) rc = check_rows(c, b, out, c->cfg.n_heads, true);
+  if (rc != SD_OK) return rc;
+  if (b->n_tokens == 0) return SD_OK;
+  DeviceGuard guard(c->device);
+  return guard.ok ? cache_attention(c, layer, b, q, scale, out) : SD_ERR_CUDA;
+}
+
+int sd_cache_status(sd_cache* c, int32_t* device_status) {
+  if (!c) return SD_ERR_ARG;
+  DeviceGuard guard(c->device);
+  int32_t v = 0;
+  if (!guard.ok || cudaMemcpyAsync(&v, c->status(), 4, cudaMemcpyDeviceToHost, c->stream) != cudaSuccess ||
+      cudaMemsetAsync(c->status(), 0, 4, c->stream) != cudaSuccess || cudaStreamSynchronize(c->stream) != cudaSuccess) {
+    cudaGetLastError();
+    return SD_ERR_CUDA;
+  }
+  if (device_status) *device_status = v;
+  return v ? SD_ERR_DEVICE : SD_OK;
+}
+
+void sd_cache_destroy(sd_cache* c) { delete c; }
+
+int sd_extend(sd_handle* h, sd_cache* c, const sd_batch* b, const int32_t* d_tokens, int n_active, int warmup, float* d_logits) {
+  if (!h || !c || !d_tokens || !d_logits) return SD_ERR_ARG;
+  const sd_config& m = h->cfg;
+  if (c->cfg.n_layers != m.n_layers || c->cfg.n_heads != m.n_heads || c->cfg.n_kv_heads != m.n_heads || c->cfg.head_dim != h->hd) return SD_ERR_ARG;
+  if (c->stream != h->stream || warmup < 0 || n_active <= warmup || n_active > m.n_layers) return SD_ERR_ARG;
+  const int rc = check_batch(c, b);
+  if (rc != SD_OK) return rc;
+  if (b->n_tokens > h->A.rows_max || b->n_seqs > m.max_batch) return SD_ERR_CAPACITY;
+  if (b->n_tokens == 0) return SD_OK;
+  DeviceGuard guard(c->device);
+  if (!guard.ok) return SD_ERR_CUDA;
+  return m.dtype == SD_DTYPE_BF16 ? extend_layers<bf16>(h, c, b, d_tokens, n_active, warmup, d_logits)
+                                  : extend_layers<float>(h, c, b, d_tokens, n_active, warmup, d_logits);
+}
+
+int sd_sample(sd_handle* h, const float* d_logits, int B, const sd_sampling* s, const float* d_uniforms, int32_t* d_next) {
+  if (!h || !d_logits || B < 1 || !s || !d_uniforms || !d_next) return SD_ERR_ARG;
+  int device = 0;
+  const int rc = device_of(h->arena, &device);
+  if (rc != SD_OK) return rc;
+  DeviceGuard guard(device);
+  if (!guard.ok) return SD_ERR_CUDA;
+  const int vocab = h->cfg.vocab;
+  const int C = vocab <= 4096 ? 1 : 8;
+  if ((int64_t)B * C > 0x7fffffff) return SD_ERR_ARG;
+  const int part = (vocab + 4 * C - 1) / (4 * C) * 4;          // a multiple of 4: parts keep the row's 16-byte alignment
+  int bits = 0;                                                // sums of vocab weights of at most 2^fraction stay below 2^63
+  while ((1ll << bits) < vocab) ++bits;
+  const int fraction = std::min(52, 63 - bits);
+  const size_t staged = sizeof(sd::sr::Shared) + (size_t)part * 4;
+  const bool in_smem = staged <= (size_t)sd::sr::MAX_SMEM;
+  auto kernel = in_smem ? sd::sample_rows_kernel<true> : sd::sample_rows_kernel<false>;
+  const size_t smem = in_smem ? staged : sizeof(sd::sr::Shared);
+  if (!h->sample_rows_ready) {               // per handle: the attribute belongs to the handle's device
+    if (cudaFuncSetAttribute(sd::sample_rows_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, sd::sr::MAX_SMEM) != cudaSuccess ||
+        cudaFuncSetAttribute(sd::sample_rows_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, sd::sr::MAX_SMEM) != cudaSuccess) {
+      cudaGetLastError();
+      return SD_ERR_CUDA;
+    }
+    h->sample_rows_ready = true;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(B * C); cfg.blockDim = dim3(sd::sr::THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = h->stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, kernel, d_logits, vocab, part, fraction, d_uniforms, s->temperature, s->top_k, s->top_p, s->min_p, d_next, h->status()) != cudaSuccess) {
+    cudaGetLastError();
+    return SD_ERR_CUDA;
+  }
+  h->launches += 1;
+  return SD_OK;
+}
+
+}  // extern "C"

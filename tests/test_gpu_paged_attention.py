@@ -1,0 +1,246 @@
+"""Attention of new tokens over a paged cache against the 64-bit form on the cache's own contents.
+
+Tolerances.  With fp32 arithmetic a score is a sum of head_dim products in some order, off by at most (head_dim + 2) 2^-24 of
+the sum of their magnitudes, plus 2^-22 for the scaling of q, the scales of an 8-bit cache and the base change; a weight's
+exponential and the running rescalings cost at most 2^-19 (one 2^-22 step per key tile would be needed to pass it), sums of
+up to 2^12 weights in a tree or in tiles 2^-19.  Queries and weights that enter the tensor cores as a high and a low 16-bit
+part lose 2^-17 of themselves at most (bf16 parts; fp16 parts less).  Where they enter as one bf16, each product loses
+2^-8 of itself and each weight 2^-8.
+"""
+import pytest
+import torch
+
+import paged_reference as P
+from paper_2307_02628_b200 import binding
+
+pytestmark = pytest.mark.gpu
+
+
+def rels(hd, cache_dtype, q_dtype, out_dtype):
+    """(score_rel, weight_rel) of the arithmetic that the library documents for these types."""
+    score, weight = (hd + 2 + 8) * 2.0 ** -24, 2.0 ** -18
+    if cache_dtype != "fp32":
+        score += 2.0 ** -16
+        weight += 2.0 ** -16
+        if out_dtype != torch.float32:                          # a 16-bit result may be computed with bf16 queries and weights
+            score += 2.0 ** -8
+            weight += 2.0 ** -8
+    return score, weight
+
+
+def run(cache_dtype, io, heads, kv_heads, hd, page, new, length, scale=None, out_dtype=None, seed=0, gain=1.0, **kw):
+    lay = P.Layout(new, length, page, seed=seed, **kw)
+    cache = P.make_cache(lay, heads, kv_heads, hd, cache_dtype)
+    contents = P.fill(cache, lay, seed=seed + 1, k_gain=gain)
+    g = torch.Generator().manual_seed(seed + 2)
+    q = torch.randn(lay.n_tokens, heads, hd, generator=g).to(P.TORCH[io])
+    out_dtype = P.TORCH[out_dtype or io]
+    out = torch.full((lay.n_tokens, heads, hd), 9.0, dtype=out_dtype, device="cuda")
+    cache.attention(0, q.cuda(), lay.batch(), scale=scale, out=out)
+    assert cache.status() == 0
+    cache.close()
+    want, spread, terms = P.attention(q, contents, lay, hd ** -0.5 if scale is None else scale, heads // kv_heads)
+    lim = P.bound(want, spread, terms, *rels(hd, cache_dtype, q.dtype, out_dtype), out_dtype)
+    got = out.cpu().double()
+    own = torch.zeros(lay.n_tokens, dtype=torch.bool)
+    for s in range(len(new)):
+        own[int(lay.first[s]):int(lay.first[s + 1])] = True
+    assert bool((got[~own] == 9).all())                         # padding rows are left as they were
+    err = ((got - want).abs() - lim)[own]
+    assert not bool(torch.isnan(got).any())
+    assert float(err.max()) <= 0, (float(err.max()), float((got - want)[own].abs().max()))
+
+
+CACHES = ("fp32", "bf16", "int8", "e4m3")
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
+@pytest.mark.parametrize("heads,kv_heads,hd", [(4, 4, 64), (8, 2, 128), (3, 1, 32), (7, 1, 64), (12, 12, 128)])
+def test_single_tokens(cache_dtype, heads, kv_heads, hd):
+    run(cache_dtype, "fp32", heads, kv_heads, hd, 16, [1] * 7, [1, 2, 15, 16, 17, 100, 333], seed=heads)
+    run(cache_dtype, "bf16", heads, kv_heads, hd, 8, [1, 0, 1], [9, 5, 64], seed=heads + 1, start=1, tail=2)
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
+@pytest.mark.parametrize("io", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("heads,kv_heads,hd,page", [(2, 2, 64, 16), (4, 1, 128, 64), (2, 1, 32, 8)])
+def test_chunks(cache_dtype, io, heads, kv_heads, hd, page):
+    # whole prompts, chunks after a prefix, single tokens, a sequence without new tokens and one shorter than its new tokens
+    run(cache_dtype, io, heads, kv_heads, hd, page, [1, 33, 64, 130, 0, 5, 2], [70, 33, 65, 200, 40, 3, 0], seed=hd, tail=1)
+
+
+@pytest.mark.parametrize("cache_dtype", ["bf16", "int8", "e4m3"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("new,length", [([128], [128]), ([127], [255]), ([129], [129]), ([256, 1], [513, 511]), ([300], [700]), ([1, 257], [1, 258])])
+def test_chunk_borders(cache_dtype, hd, new, length):
+    run(cache_dtype, "bf16", 2, 2, hd, 32, new, length, seed=sum(new))
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
+def test_long_sequences(cache_dtype):
+    run(cache_dtype, "fp32", 4, 2, 64, 64, [1, 1], [4001, 63], seed=5)
+    run(cache_dtype, "bf16", 8, 1, 128, 128, [2], [2500], seed=6)
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
+@pytest.mark.parametrize("page", [8, 16, 32, 64, 128])
+def test_page_lengths(cache_dtype, page):
+    run(cache_dtype, "bf16", 2, 2, 64, page, [1, 40], [page * 3 + 1, 150], seed=page)
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
+@pytest.mark.parametrize("scale,gain", [(0.05, 1.0), (-0.3, 1.0), (1.0, 4.0), (None, 1e-6), (1e-7, 1e6)])
+def test_scales_and_magnitudes(cache_dtype, scale, gain):
+    # scores from nearly equal to dominated by one key; keys of tiny and of large magnitude
+    run(cache_dtype, "fp32", 2, 1, 64, 16, [1, 20], [50, 64], scale=scale, gain=gain, seed=11)
+
+
+@pytest.mark.parametrize("io,out", [("fp32", "fp16"), ("fp32", "bf16"), ("bf16", "fp32"), ("fp16", "bf16")])
+@pytest.mark.parametrize("cache_dtype", CACHES)
+def test_output_types(cache_dtype, io, out):
+    run(cache_dtype, io, 2, 2, 64, 16, [1, 70], [30, 100], out_dtype=out, seed=21)
+
+
+def test_scales_of_very_different_sizes():
+    # values whose scales differ by 2^60 between neighbouring tokens, and tokens whose values are all zero
+    lay = P.Layout([1, 1], [77, 16], 16, seed=3)
+    cache = P.make_cache(lay, 2, 2, 64, "int8")
+    contents = P.fill(cache, lay, seed=4)
+    pool = cache.layer(0)
+    for s, l in enumerate(lay.length):
+        for p in range(l):
+            page, slot = lay.slot(s, p)
+            f = 0.0 if (p % 5 == 0 or s == 1) else 2.0 ** (12 * (p % 6) - 30)
+            pool["v_scale"][page, :, slot] *= f
+            contents[s][1][:, p] *= f
+    q = torch.randn(2, 2, 64, generator=torch.Generator().manual_seed(1))
+    got = cache.attention(0, q.cuda(), lay.batch()).cpu().double()
+    want, spread, terms = P.attention(q, contents, lay, 0.125, 1)
+    lim = P.bound(want, spread, terms, *rels(64, "int8", torch.float32, torch.float32), torch.float32)
+    assert bool(((got - want).abs() <= lim).all())
+    assert bool((got[1] == 0).all())
+    cache.close()
+
+
+@pytest.mark.parametrize("cache_dtype", ["bf16", "int8"])
+def test_strided_queries_and_outputs(cache_dtype):
+    lay = P.Layout([3, 1, 70], [30, 17, 90], 16, seed=8)
+    H, hd, n = 4, 64, 74
+    cache = P.make_cache(lay, H, H, hd, cache_dtype)
+    contents = P.fill(cache, lay, seed=9)
+    g = torch.Generator().manual_seed(10)
+    for make in (lambda: torch.randn(n, 3 * H * hd, generator=g)[:, :H * hd].unflatten(1, (H, hd)),
+                 lambda: torch.randn(n, H, hd + 3, generator=g)[..., 3:],
+                 lambda: torch.randn(H, n, hd, generator=g).transpose(0, 1),
+                 lambda: torch.randn(n, 1, hd, generator=g).expand(n, H, hd)):
+        q = make()
+        dev = torch.empty_strided(q.shape, q.stride(), device="cuda") if q.stride(1) else q[:, :1].cuda().expand(n, H, hd)
+        if q.stride(1):
+            dev.copy_(q)
+        out = torch.zeros(H, n, hd + 1, device="cuda").transpose(0, 1)[..., 1:]
+        cache.attention(0, dev, lay.batch(), out=out)
+        want, spread, terms = P.attention(q, contents, lay, hd ** -0.5, 1)
+        lim = P.bound(want, spread, terms, *rels(hd, cache_dtype, torch.float32, torch.float32), torch.float32)
+        assert bool(((out.cpu().double() - want).abs() <= lim).all())
+    cache.close()
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
+def test_bad_pages_are_masked_and_reported(cache_dtype):
+    # the keys of a page that does not exist are left out of the sums; a row that has no other keys is zero
+    lay = P.Layout([1, 1, 20], [40, 10, 40], 16, seed=2)
+    cache = P.make_cache(lay, 2, 2, 64, cache_dtype)
+    contents = P.fill(cache, lay, seed=3)
+    q = torch.randn(22, 2, 64, generator=torch.Generator().manual_seed(1))
+    pages = lay.pages.clone()
+    pages[0, 1], pages[1, 0], pages[2, 0] = lay.n_pages, -1, 1 << 30
+    out = cache.attention(0, q.cuda(), binding.CacheBatch(pages.cuda(), lay.first.cuda(), lay.len.cuda(), 22, 20)).cpu().double()
+    assert cache.status() == binding.STATUS_BAD_BATCH
+    keep = [torch.arange(40) // 16 != 1, torch.zeros(10, dtype=torch.bool), torch.arange(40) >= 16]
+    score_rel, weight_rel = rels(64, cache_dtype, torch.float32, torch.float32)
+    for r, s, p in lay.places():
+        k, v = contents[s]
+        seen = keep[s] & (torch.arange(len(keep[s])) <= p)
+        if not bool(seen.any()):
+            assert bool((out[r] == 0).all())
+            continue
+        w = torch.softmax(torch.einsum("hd,hjd->hj", q[r].double(), k[:, seen]) * 0.125, -1)
+        want = torch.einsum("hj,hjd->hd", w, v[:, seen])
+        assert float((out[r] - want).abs().max()) <= 40 * (score_rel + weight_rel)      # terms stay below 10, values below 5
+    cache.close()
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
+def test_steps_replayed_from_a_graph(cache_dtype):
+    # append + attention captured once, replayed with other lengths, pages and inputs in the same device arrays
+    H, hd, page, steps = 4, 64, 16, 24
+    lay = P.Layout([1, 1], [30 + steps, 5 + steps], page, seed=1)
+    cache = P.make_cache(lay, H, H, hd, cache_dtype)
+    eager = P.make_cache(lay, H, H, hd, cache_dtype)
+    for c in (cache, eager):
+        P.fill(c, lay, seed=2)
+    length = torch.tensor([30, 5], dtype=torch.int32, device="cuda")
+    b = binding.CacheBatch(lay.pages.cuda(), lay.first.cuda(), length, 2, 1, max(lay.length))
+    q, k, v = (torch.zeros(2, H, hd, device="cuda") for _ in range(3))
+    out = torch.zeros(2, H, hd, device="cuda")
+    eager.append(0, k, v, b)                                    # the warm-up below writes the same place of the other cache
+    torch.cuda.synchronize()
+    with torch.cuda.stream(cache.stream):
+        cache.append(0, k, v, b)
+        cache.attention(0, q, b, out=out)
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=cache.stream):
+            cache.append(0, k, v, b)
+            cache.attention(0, q, b, out=out)
+    g = torch.Generator().manual_seed(7)
+    for t in range(steps):
+        for x in (q, k, v):
+            x.copy_(torch.randn(2, H, hd, generator=g))
+        length += 1
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        eager.append(0, k, v, b)
+        want = eager.attention(0, q, b)
+        assert torch.equal(got, want), t
+    for n, t in cache.layer(0).items():
+        assert torch.equal(t.view(torch.uint8), eager.layer(0)[n].view(torch.uint8))
+    assert cache.status() == 0 and eager.status() == 0
+    cache.close()
+    eager.close()
+
+
+def test_another_stream_and_two_caches_at_once():
+    lay = P.Layout([1, 50], [600, 130], 16, seed=6)
+    caches = [P.make_cache(lay, 4, 2, 64, "int8") for _ in range(2)]
+    contents = [P.fill(c, lay, seed=s) for s, c in enumerate(caches)]
+    q = torch.randn(51, 4, 64, generator=torch.Generator().manual_seed(1))
+    side = torch.cuda.Stream()
+    outs = []
+    with torch.cuda.stream(side):
+        dev = q.cuda()
+        b = lay.batch()
+        for _ in range(20):                                     # both in flight together, inputs and outputs from a third stream
+            outs = [c.attention(0, dev * 1.0, b) for c in caches]
+        outs = [o * 1.0 for o in outs]
+    side.synchronize()
+    for o, con in zip(outs, contents):
+        want, spread, terms = P.attention(q, con, lay, 0.125, 2)
+        lim = P.bound(want, spread, terms, *rels(64, "int8", torch.float32, torch.float32), torch.float32)
+        assert bool(((o.cpu().double() - want).abs() <= lim).all())
+    for c in caches:
+        c.close()
+
+
+def test_same_call_twice_gives_the_same_bits():
+    for cache_dtype in CACHES:
+        lay = P.Layout([1, 90, 1], [3000, 200, 5], 32, seed=6)
+        cache = P.make_cache(lay, 4, 2, 128, cache_dtype)
+        P.fill(cache, lay)
+        q = torch.randn(92, 4, 128, generator=torch.Generator().manual_seed(1)).cuda()
+        one = cache.attention(0, q, lay.batch())
+        for _ in range(5):
+            assert torch.equal(one, cache.attention(0, q, lay.batch()))
+        cache.close()
