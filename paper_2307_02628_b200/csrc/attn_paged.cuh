@@ -1,0 +1,435 @@
+// Attention of few query rows over a paged cache in bf16 or 8 bits: single tokens, and chunks whose results are wanted in
+// fp32.  One block per (sequence, key head, tile of 8 query rows, split of the keys); a query row is a (token, head of the group)
+// pair, so grouped heads share the keys they read.
+//
+// What bounds it is the cache's bytes.  The products run on the tensor cores (m16n8k16, fp32 accumulation) because the CUDA
+// cores could not convert and multiply 8-bit elements at the rate at which the memory delivers them (23 per clock and SM).  The
+// 16 rows of a tile are the 8 query rows twice: once the upper and once the lower half of each query element (and of
+// each softmax weight), two 16-bit numbers that together keep 16 bits in bf16 and 22 in fp16, so the operands' rounding stays
+// near fp32 at no cost: with 8 rows or fewer the other half of the tile would be empty.  8-bit codes are fp16 numbers exactly.
+// bf16 caches multiply in bf16.
+//
+// Each of the four warps walks its own 16-key tiles with a ring of its own in shared memory, filled by 16-byte asynchronous copies: no
+// block-wide synchronisation until the end, and every warp keeps STAGES - 1 tiles in flight.  The fragments are read in the order
+// in which the bytes lie: the sum over the head's elements may run in any order, so a thread takes whole 16-byte pieces of a key
+// and the queries are laid out to match; for the values, a thread takes a run of elements of four keys, and the
+// accumulator's columns stand for the elements that order implies.  Pieces are XOR-swizzled against bank conflicts.
+//
+// 8-bit scales.  A key's scale multiplies its score.  A value's scale joins its weight: weights are kept relative to the
+// largest weight-times-scale seen (running maximum mv), the sum of weights relative to the largest weight (m), so scales of
+// any size keep the weights inside fp16.  Both maxima are only raised when they would be passed by 2^8, which keeps most tiles
+// free of rescaling; in 8 bits a weight is 2^7 times its ratio to the maximum, so that with that slack it stays below fp16's
+// 65504 and a weight far below the largest keeps bits (the grid of fp16 ends at 2^-24).
+#pragma once
+#include "attn_prefill.cuh"
+#include "paged.cuh"
+
+namespace sd {
+namespace ap {
+
+constexpr int NW = 4, THREADS = 128, ROWS = 8, KEYS = 16;
+
+template <typename TC, int HD> struct Shape {
+  static constexpr bool SCALED = CacheType<TC>::TOP > 0.f;
+  static constexpr int E = sizeof(TC);
+  static constexpr int ROW = HD * E;                         // bytes of a key
+  static constexpr int PIECES = ROW / 16;
+  static constexpr int SWZ = PIECES < 8 ? PIECES - 1 : 7;
+  static constexpr int EC = 16 / E < HD / 4 ? 16 / E : HD / 4;   // elements a thread reads at a time for the scores
+  static constexpr int NCH = HD / (4 * EC);
+  static constexpr int KS = HD / 16, NT = HD / 8;
+  static constexpr int STAGE = 2 * KEYS * ROW + (SCALED ? 2 * KEYS * 4 : 0);
+  // enough stages that an SM holds at least 96 KB of ring, shared by the blocks its registers allow
+  static constexpr int STAGES = STAGE >= 8192 ? 3 : STAGE >= 4096 ? 4 : 6;
+  static constexpr int MERGE = NW * ROWS * (HD + 2) * 4;
+  static constexpr int SMEM = NW * STAGES * STAGE > MERGE ? NW * STAGES * STAGE : MERGE;
+};
+
+__device__ __forceinline__ int swz(int key) { return ((key & 1) << 2) | ((key >> 1) & 3); }
+
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __nv_bfloat16) { pf_mma(c, a, b0, b1); }
+template <typename T>
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, T) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// two floats as packed 16-bit pairs: the values rounded, and what the rounding left
+__device__ __forceinline__ void split(float x, float y, uint32_t& hi, uint32_t& lo, __nv_bfloat16) { pf_split(x, y, hi, lo); }
+template <typename T> __device__ __forceinline__ void split(float x, float y, uint32_t& hi, uint32_t& lo, T) {
+  const __half hx = __float2half_rn(x), hy = __float2half_rn(y);
+  hi = (uint32_t)__half_as_ushort(hx) | ((uint32_t)__half_as_ushort(hy) << 16);
+  lo = pack_f16(x - __half2float(hx), y - __half2float(hy));
+}
+
+// Codes to fp16 pairs.  flip() prepares a word of four codes; lower(), upper() give its first and last two as fp16.  An int8
+// with its sign bit flipped is the code plus 128, and 0x64 above a byte makes it the fp16 number 1024 + byte.
+__device__ __forceinline__ uint32_t flip(uint32_t w, int8_t) { return w ^ 0x80808080u; }
+__device__ __forceinline__ uint32_t flip(uint32_t w, e4m3) { return w; }
+__device__ __forceinline__ uint32_t minus_1152(uint32_t v) {
+  const uint32_t c = 0x64806480u;
+  const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&c));
+  return *reinterpret_cast<const uint32_t*>(&d);
+}
+__device__ __forceinline__ uint32_t lower(uint32_t w, int8_t) { return minus_1152(__byte_perm(w, 0x64646464u, 0x4140)); }
+__device__ __forceinline__ uint32_t upper(uint32_t w, int8_t) { return minus_1152(__byte_perm(w, 0x64646464u, 0x4342)); }
+__device__ __forceinline__ uint32_t widen(uint32_t w) {
+  const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)w, __NV_E4M3);
+  return (uint32_t)r.x | ((uint32_t)r.y << 16);
+}
+__device__ __forceinline__ uint32_t lower(uint32_t w, e4m3) { return widen(w & 0xffffu); }
+__device__ __forceinline__ uint32_t upper(uint32_t w, e4m3) { return widen(w >> 16); }
+
+template <int B> __device__ __forceinline__ void lds(uint32_t addr, uint32_t (&r)[B / 4]) {
+  if constexpr (B == 16) asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+  else if constexpr (B == 8) asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(addr));
+  else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(r[0]) : "r"(addr));
+}
+__device__ __forceinline__ float lds_f32(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr));
+  return v;
+}
+
+// N consecutive elements of a row, any type; vec: 16-byte accesses are allowed
+template <int N> __device__ __forceinline__ void load_run(const Rows& t, long long at, bool vec, float (&o)[N]) {
+  if (vec) {
+#pragma unroll
+    for (int i = 0; i < N; i += 8) {
+      float x[8];
+      if (t.dtype == DT_FP32) load8<true>(static_cast<const float*>(t.data) + at + i, x);
+      else if (t.dtype == DT_BF16) load8<true>(static_cast<const __nv_bfloat16*>(t.data) + at + i, x);
+      else load8<true>(static_cast<const __half*>(t.data) + at + i, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[i + j] = x[j];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = load_elem(t, at + i);
+  }
+}
+
+}  // namespace ap
+
+// grid (tiles_per_seq * n_kv_heads * n_seqs, splits).  Split z takes keys [z * chunk, (z + 1) * chunk), the last one all that follow.
+// Several splits leave partial results (accumulator, maximum, sum) of the rows they see and the block that arrives last at a
+// unit's counter adds them in split order, so the result does not depend on who came when.
+template <typename TC, int HD>
+__global__ void __launch_bounds__(ap::THREADS)
+paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC* __restrict__ Kp, const TC* __restrict__ Vp,
+                       const float* __restrict__ Ksc, const float* __restrict__ Vsc, int group, float scale_log2, bool q_vec,
+                       int tiles_per_seq, int chunk, float* part_acc, float* part_ml, int* __restrict__ counters) {
+  using namespace ap;
+  using S = Shape<TC, HD>;
+  extern __shared__ __align__(128) unsigned char ap_smem[];
+  __shared__ int sm_last;
+
+  const int unit = blockIdx.x, tile = unit % tiles_per_seq, g_head = (unit / tiles_per_seq) % b.n_kv_heads, seq = unit / tiles_per_seq / b.n_kv_heads;
+  const int splits = gridDim.y, z = blockIdx.y;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+
+  // the sequence's rows; whatever does not fit the tensors is reported and left out
+  const int f0 = b.first[seq], f1 = b.first[seq + 1], len = b.seq_len(seq);
+  int n_new = f1 - f0;
+  if (f0 < 0 || n_new < 0 || f1 > b.n_tokens || n_new > b.max_new) {
+    if (threadIdx.x == 0) b.bad();
+    if (f0 < 0 || n_new < 0) return;
+    n_new = min(n_new, min(b.max_new, b.n_tokens - f0));
+  }
+  const int n_rows = min(ROWS, n_new * group - tile * ROWS);
+  if (n_rows <= 0) return;
+  const long long pos_first = (long long)b.len[seq] - (f1 - f0);            // position of the first new token, negative without a place
+  const int last_token = (tile * ROWS + n_rows - 1) / group;
+  const int key_end = (int)min(max(pos_first + last_token + 1, 0ll), (long long)len);      // keys that any row of the tile sees
+  const int used_splits = max(1, min(splits, (key_end + chunk - 1) / chunk));
+  if (z >= used_splits) return;
+  const int k0 = z * chunk, k1 = z == splits - 1 ? key_end : min(k0 + chunk, key_end);
+
+  // this thread's query row (rows past the tile repeat the last one and are not stored) and the last key it sees
+  const int row = tile * ROWS + min(g, n_rows - 1);
+  const int token = row / group, head = g_head * group + row % group;
+  const int row_last = (int)max(min(pos_first + token, (long long)len - 1), -1ll);         // -1: none
+  const int all_see = (int)max(min(pos_first + (tile * ROWS) / group, (long long)len - 1), -1ll);   // the last key that every row sees
+
+  uint32_t qf[S::KS][4];
+  float row_scale = scale_log2;
+  {
+    constexpr int PER = S::EC;
+    float x[S::NCH][PER];
+    const long long at = (long long)(f0 + token) * q.row_stride + head * q.head_stride;
+    float top = 0.f;
+#pragma unroll
+    for (int c = 0; c < S::NCH; ++c) {
+      load_run<PER>(q, at + (t + 4 * c) * PER, q_vec, x[c]);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) top = fmaxf(top, fabsf(x[c][i]));
+    }
+    float down = 1.f;
+    if constexpr (S::SCALED) {                     // queries enter as fp16: brought near 1 by a power of two
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const int e = min(max((int)((__float_as_uint(top) >> 23) & 0xff), 2), 252);
+      down = __uint_as_float((uint32_t)(254 - e) << 23);           // 2^(127 - e)
+      row_scale *= __uint_as_float((uint32_t)e << 23);             // 2^(e - 127)
+    }
+#pragma unroll
+    for (int ks = 0; ks < S::KS; ++ks) {
+      const float* v = x[ks / (PER / 4)] + 4 * (ks % (PER / 4));
+      split(v[0] * down, v[1] * down, qf[ks][0], qf[ks][1], TC{});
+      split(v[2] * down, v[3] * down, qf[ks][2], qf[ks][3], TC{});
+    }
+  }
+
+  float acc[S::NT][4];
+#pragma unroll
+  for (int n = 0; n < S::NT; ++n) { acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f; }
+  float m = -INFINITY, mv = -INFINITY, l = 0.f;    // maxima are a row's, the sum is this thread's share
+
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(ap_smem) + warp * (S::STAGES * S::STAGE);
+  const int tile0 = k0 / KEYS + warp, n_tiles = (k1 + KEYS - 1) / KEYS;      // this warp's tiles: tile0, tile0 + NW, ...
+  const int* table = b.pages + (size_t)seq * b.pages_per_seq;
+  uint32_t valid = 0u;                             // two bits per stage: the halves of the tile whose page exists
+  int next_page[2] = {-1, -1};                     // table entries of the tile to be issued next
+  auto look_up = [&](int kt) {
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      const int key = kt * KEYS + 8 * hf;
+      next_page[hf] = key < k1 ? table[key >> b.page_shift] : 0;
+    }
+  };
+  auto issue = [&](int kt, int stage) {
+    const uint32_t dst = ring + stage * S::STAGE;
+    size_t e[2];
+    uint32_t ok = 0u;
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      const int key = kt * KEYS + 8 * hf;
+      const bool there = (unsigned)next_page[hf] < (unsigned)b.n_pages;
+      if (!there && key < k1 && lane == 0) b.bad();
+      e[hf] = there ? b.entry(next_page[hf], g_head, key) : 0;
+      ok |= there ? 1u << hf : 0u;
+    }
+    valid = (valid & ~(3u << (2 * stage))) | (ok << (2 * stage));
+#pragma unroll
+    for (int i = 0; i < KEYS * S::PIECES / 32; ++i) {
+      const int c = i * 32 + lane, key = c / S::PIECES, piece = c % S::PIECES, hf = key >> 3;
+      const bool on = kt * KEYS + key < k1 && ((ok >> hf) & 1u);             // off: zeros, nothing is read
+      const size_t src = on ? (e[hf] + (key & 7)) * HD + piece * (16 / S::E) : 0;
+      const uint32_t at = dst + key * S::ROW + ((piece ^ (swz(key) & S::SWZ)) << 4);
+      pf_cp16(at, Kp + src, on ? 16 : 0);
+      pf_cp16(at + KEYS * S::ROW, Vp + src, on ? 16 : 0);
+    }
+    if constexpr (S::SCALED) {
+      if (lane < 8) {                              // 16 scales of each: four pieces of four
+        const int key = (lane & 3) * 4, hf = key >> 3;
+        const bool on = kt * KEYS + key < k1 && ((ok >> hf) & 1u);
+        const float* src = (lane < 4 ? Ksc : Vsc) + (on ? e[hf] + (key & 7) : 0);
+        pf_cp16(dst + 2 * KEYS * S::ROW + lane * 16, src, on ? 16 : 0);
+      }
+    }
+  };
+  static_assert(KEYS * S::PIECES % 32 == 0, "whole warps of copies");
+
+  look_up(tile0);
+#pragma unroll
+  for (int s = 0; s < S::STAGES - 1; ++s) {
+    const int kt = tile0 + s * NW;
+    if (kt < n_tiles) { issue(kt, s); look_up(kt + NW); }
+    pf_commit();
+  }
+  int stage = 0, fill = S::STAGES - 1;
+  for (int kt = tile0; kt < n_tiles; kt += NW) {
+    {
+      const int ahead = kt + (S::STAGES - 1) * NW;
+      if (ahead < n_tiles) { issue(ahead, fill); look_up(ahead + NW); }
+      pf_commit();
+      fill = fill + 1 == S::STAGES ? 0 : fill + 1;
+    }
+    pf_wait<S::STAGES - 1>();
+    __syncwarp();
+    const uint32_t ks_base = ring + stage * S::STAGE, vs_base = ks_base + KEYS * S::ROW, sc_base = vs_base + KEYS * S::ROW;
+
+    // scores: 8 query rows (twice) x 16 keys
+    float s[2][4];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+      const int key = n * 8 + g;
+#pragma unroll
+      for (int c = 0; c < S::NCH; ++c) {
+        constexpr int B = S::EC * S::E;                                       // 16 bytes, or 8
+        uint32_t w[B / 4];
+        const int off = (t + 4 * c) * B;
+        lds<B>(ks_base + key * S::ROW + (((off >> 4) ^ (swz(key) & S::SWZ)) << 4) + (off & 15), w);
+#pragma unroll
+        for (int k = 0; k < S::EC / 4; ++k) {
+          if constexpr (S::SCALED) {
+            const uint32_t f = flip(w[k], TC{});
+            mma(s[n], qf[c * (S::EC / 4) + k], lower(f, TC{}), upper(f, TC{}), TC{});
+          } else {
+            mma(s[n], qf[c * (S::EC / 4) + k], w[2 * k], w[2 * k + 1], TC{});
+          }
+        }
+      }
+    }
+    float sc[2][2], sv[2][2];
+    const uint32_t ok = valid >> (2 * stage);
+    const bool edge = kt * KEYS + KEYS - 1 > all_see || kt * KEYS + KEYS > k1 || (ok & 3u) != 3u;
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int key = n * 8 + 2 * t + i;
+        float v = (s[n][i] + s[n][2 + i]) * row_scale, lv = 0.f;
+        if constexpr (S::SCALED) {
+          v *= lds_f32(sc_base + key * 4);
+          lv = __log2f(lds_f32(sc_base + KEYS * 4 + key * 4));
+        }
+        const int at = kt * KEYS + key;
+        const bool seen = !edge || (at <= row_last && at < k1 && ((ok >> n) & 1u));
+        sc[n][i] = seen ? v : -INFINITY;
+        sv[n][i] = seen ? v + lv : -INFINITY;
+      }
+    float mx = fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[1][0], sc[1][1]));
+    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+    float mxv = mx;
+    if constexpr (S::SCALED) {
+      mxv = fmaxf(fmaxf(sv[0][0], sv[0][1]), fmaxf(sv[1][0], sv[1][1]));
+      mxv = fmaxf(mxv, __shfl_xor_sync(0xffffffffu, mxv, 1));
+      mxv = fmaxf(mxv, __shfl_xor_sync(0xffffffffu, mxv, 2));
+    }
+    if (__any_sync(0xffffffffu, mx > m + 8.f || mxv > mv + 8.f)) {
+      const float m_new = fmaxf(m, mx);
+      l *= exp2_safe(m, m_new);
+      m = m_new;
+      const float mv_new = fmaxf(mv, mxv), a = exp2_safe(mv, mv_new);
+      mv = mv_new;
+#pragma unroll
+      for (int n = 0; n < S::NT; ++n) { acc[n][0] *= a; acc[n][1] *= a; acc[n][2] *= a; acc[n][3] *= a; }
+    }
+    // weights: the sum's, and the ones that multiply the values.  A row that has seen nothing has m = -inf and only masked scores.
+    const float mb = m == -INFINITY ? 0.f : m, mvb = mv == -INFINITY ? 0.f : mv;
+    uint32_t pf[4];
+    float p[2][2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        p[n][i] = exp2f(sc[n][i] - mb);
+        l += p[n][i];
+        if constexpr (S::SCALED) p[n][i] = exp2f(sv[n][i] - mvb + 7.f);
+      }
+      split(p[n][0], p[n][1], pf[2 * n], pf[2 * n + 1], TC{});
+    }
+
+    // values
+    if constexpr (S::SCALED) {
+      constexpr int B = HD / 8;                                               // bytes of a thread's run: elements [run * B, +B)
+      const int run = ((g & 1) << 2) | (g >> 1);
+      uint32_t w[4][B / 4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int key = 2 * t + (i & 1) + (i >> 1) * 8, off = run * B;
+        lds<B>(vs_base + key * S::ROW + (((off >> 4) ^ (swz(key) & S::SWZ)) << 4) + (off & 15), w[i]);
+      }
+#pragma unroll
+      for (int k = 0; k < B / 4; ++k) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i][k] = flip(w[i][k], TC{});
+        // bytes of keys 0 and 1 (2 and 3) side by side, element by element
+        const uint32_t a0 = __byte_perm(w[0][k], w[1][k], 0x5140), a1 = __byte_perm(w[0][k], w[1][k], 0x7362);
+        const uint32_t b0 = __byte_perm(w[2][k], w[3][k], 0x5140), b1 = __byte_perm(w[2][k], w[3][k], 0x7362);
+        mma(acc[4 * k + 0], pf, lower(a0, TC{}), lower(b0, TC{}), TC{});
+        mma(acc[4 * k + 1], pf, upper(a0, TC{}), upper(b0, TC{}), TC{});
+        mma(acc[4 * k + 2], pf, lower(a1, TC{}), lower(b1, TC{}), TC{});
+        mma(acc[4 * k + 3], pf, upper(a1, TC{}), upper(b1, TC{}), TC{});
+      }
+    } else {
+      const int mi = lane >> 3, mr = lane & 7, key = ((mi & 1) << 3) + mr;
+#pragma unroll
+      for (int n = 0; n < S::NT; n += 2) {
+        uint32_t v[4];
+        pf_ldmatrix_t(v, vs_base + key * S::ROW + (((n + (mi >> 1)) ^ (swz(key) & S::SWZ)) << 4));
+        mma(acc[n], pf, v[0], v[1], TC{});
+        mma(acc[n + 1], pf, v[2], v[3], TC{});
+      }
+    }
+    __syncwarp();                                                             // the stage is refilled in the next round
+    stage = stage + 1 == S::STAGES ? 0 : stage + 1;
+  }
+  pf_wait<0>();
+
+  // this warp's rows: accumulators in units of 2^m, sums over the quad
+  l += __shfl_xor_sync(0xffffffffu, l, 1);
+  l += __shfl_xor_sync(0xffffffffu, l, 2);
+  const float back = S::SCALED ? (mv == -INFINITY ? 0.f : exp2f(mv - m - 7.f)) : 1.f;
+  __syncthreads();                                                            // every warp is done with its ring
+  float* sm_acc = reinterpret_cast<float*>(ap_smem);                          // [NW][ROWS][HD]
+  float* sm_m = sm_acc + NW * ROWS * HD;                                      // [NW][ROWS]
+  float* sm_l = sm_m + NW * ROWS;
+#pragma unroll
+  for (int n = 0; n < S::NT; ++n)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int col = 2 * t + i;
+      const int d = S::SCALED ? (((col & 1) << 2) | (col >> 1)) * (HD / 8) + n : n * 8 + col;
+      sm_acc[(warp * ROWS + g) * HD + d] = (acc[n][i] + acc[n][2 + i]) * back;
+    }
+  if (t == 0) { sm_m[warp * ROWS + g] = m; sm_l[warp * ROWS + g] = l; }
+  __syncthreads();
+
+  auto place = [&](int r, int& tok, int& hd) {
+    const int rr = tile * ROWS + r;
+    tok = f0 + rr / group;
+    hd = g_head * group + rr % group;
+  };
+  for (int i = threadIdx.x; i < n_rows * HD; i += THREADS) {
+    const int r = i / HD, c = i % HD;
+    float M = -INFINITY, L = 0.f, a = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) M = fmaxf(M, sm_m[w * ROWS + r]);
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float f = exp2_safe(sm_m[w * ROWS + r], M);
+      L += sm_l[w * ROWS + r] * f;
+      a += sm_acc[(w * ROWS + r) * HD + c] * f;
+    }
+    int tok, hd;
+    place(r, tok, hd);
+    if (used_splits == 1) {
+      store_elem(out, (long long)tok * out.row_stride + hd * out.head_stride + c, L > 0.f ? a / L : 0.f);
+    } else {
+      const size_t slot = ((size_t)tok * (group * b.n_kv_heads) + hd) * splits + z;
+      __stcg(part_acc + slot * HD + c, a);
+      if (c == 0) { __stcg(part_ml + slot * 2, M); __stcg(part_ml + slot * 2 + 1, L); }
+    }
+  }
+  if (used_splits == 1) return;
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const int done = atomicAdd(&counters[unit], 1);
+    sm_last = done == used_splits - 1;
+    if (sm_last) counters[unit] = 0;                                          // ready for the next launch
+  }
+  __syncthreads();
+  if (!sm_last) return;
+  __threadfence();
+  for (int i = threadIdx.x; i < n_rows * HD; i += THREADS) {
+    const int r = i / HD, c = i % HD;
+    int tok, hd;
+    place(r, tok, hd);
+    const size_t slot0 = ((size_t)tok * (group * b.n_kv_heads) + hd) * splits;
+    float M = -INFINITY, L = 0.f, a = 0.f;
+    for (int s = 0; s < used_splits; ++s) M = fmaxf(M, __ldcg(part_ml + (slot0 + s) * 2));
+    for (int s = 0; s < used_splits; ++s) {
+      const float f = exp2_safe(__ldcg(part_ml + (slot0 + s) * 2), M);
+      L += __ldcg(part_ml + (slot0 + s) * 2 + 1) * f;
+      a += __ldcg(part_acc + (slot0 + s) * HD + c) * f;
+    }
+    store_elem(out, (long long)tok * out.row_stride + hd * out.head_stride + c, L > 0.f ? a / L : 0.f);
+  }
+}
+
+}  // namespace sd

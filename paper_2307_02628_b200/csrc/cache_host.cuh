@@ -8,13 +8,16 @@ struct sd_cache {
   char* arena;
   cudaStream_t stream;
   size_t layer_bytes, v_off, ks_off, vs_off;   // K pool, V pool, K scales, V scales: offsets within a layer
-  size_t minus_pos, last_row, status_off, total;
+  size_t minus_pos, last_row, part_acc, part_ml, counters, status_off, total;
+  unsigned tile_ready = 0;    // bit per kernel whose shared-memory size has been allowed on this device
   char* layer(int l) const { return arena + (size_t)l * layer_bytes; }
   template <typename T> T* at(size_t off) const { return reinterpret_cast<T*>(arena + off); }
   int* status() const { return at<int>(status_off); }
 };
 
 namespace {
+
+constexpr int kPartSlots = 32768;      // 17 MB of head size 128
 
 // Makes `device` current for the length of a call.
 struct DeviceGuard {
@@ -67,6 +70,10 @@ bool carve_cache(const sd_cache_config& c, sd_cache& A) {
   off *= c.n_layers;
   A.minus_pos = take((size_t)c.max_tokens * 4);
   A.last_row = take((size_t)c.max_seqs * 4);
+  // partial results of attention over split keys: a fixed number of (row, split) slots, which bounds the splits of a call
+  A.part_acc = take((size_t)kPartSlots * c.head_dim * 4);
+  A.part_ml = take((size_t)kPartSlots * 8);
+  A.counters = take((size_t)kPartSlots * 4);
   A.status_off = take(256);
   A.total = off;
   return true;
@@ -172,17 +179,60 @@ int cache_read(sd_cache* c, int l, const sd_batch* b, const sd_heads* k, const s
   });
 }
 
+// Keys per split for `units` blocks over up to max_len keys each, `rows` query rows in all.  The blocks that an SM holds (three)
+// should all have work, and the last wave should not be long: splitting stops at 256 keys, below which a block's start
+// and end outweigh its walk.
+int pick_split(const sd_cache* c, long units, long rows, int64_t max_len) {
+  const long slots = 3L * c->sm_count;
+  int best = 1;
+  double best_cost = 1e30;
+  for (int splits = 1; splits <= 512; splits = splits < 4 ? splits + 1 : splits + splits / 4) {
+    const int64_t chunk = (max_len + splits * 64 - 1) / (splits * 64) * 64;
+    if (splits > 1 && (chunk < 256 || rows * splits > kPartSlots || units > kPartSlots)) break;
+    const double waves = (double)((units * splits + slots - 1) / slots);
+    const double cost = waves * (chunk + 160);
+    if (cost < best_cost * 0.999) { best_cost = cost; best = splits; }
+  }
+  return (int)std::min<int64_t>((max_len + best * 64 - 1) / (best * 64) * 64, 0x7fffffc0);
+}
+
+template <typename TC, int HD>
+int attention_tiles(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale_log2, const sd_heads* out) {
+  using S = sd::ap::Shape<TC, HD>;
+  constexpr unsigned bit = 1u << ((HD == 128 ? 0 : HD == 64 ? 1 : 2) + 3 * (std::is_same<TC, bf16>::value ? 0 : std::is_same<TC, int8_t>::value ? 1 : 2));
+  auto kernel = sd::paged_attn_tile_kernel<TC, HD>;
+  if (!(c->tile_ready & bit)) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) != cudaSuccess) { cudaGetLastError(); return SD_ERR_CUDA; }
+    c->tile_ready |= bit;
+  }
+  const auto P = pools<TC>(c, l);
+  const int tiles = (int)(((int64_t)b->max_new * c->group + sd::ap::ROWS - 1) / sd::ap::ROWS);
+  const int64_t units = (int64_t)tiles * c->cfg.n_kv_heads * b->n_seqs;
+  if (units > 0x7fffffff) return SD_ERR_ARG;
+  const int max_len = b->max_len > 0 ? b->max_len : b->pages_per_seq * c->cfg.page_len;
+  const int chunk = pick_split(c, (long)units, (long)b->n_tokens * c->cfg.n_heads, max_len);
+  const int splits = (int)(((int64_t)max_len + chunk - 1) / chunk);
+  kernel<<<dim3((unsigned)units, splits), sd::ap::THREADS, S::SMEM, c->stream>>>(
+      view_of(c, b), rows_of(q), rows_of(out), (const TC*)P.k, (const TC*)P.v, (const float*)P.ks, (const float*)P.vs, c->group, scale_log2, wide(q),
+      tiles, chunk, c->at<float>(c->part_acc), c->at<float>(c->part_ml), c->at<int>(c->counters));
+  return launched();
+}
+
 int cache_attention(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale, const sd_heads* out) {
   if (scale == 0.f) scale = 1.f / sqrtf((float)c->cfg.head_dim);
   const float scale_log2 = scale * 1.4426950408889634f;
   return with_cache_type(c->cfg.dtype, [&](auto tc) {
     using TC = decltype(tc);
-    const auto P = pools<TC>(c, l);
     return with_head_dim(c->cfg.head_dim, [&](auto hd) {
       constexpr int HD = decltype(hd)::value;
-      sd::paged_attn_row_kernel<TC, HD><<<dim3(b->n_tokens, c->cfg.n_heads), 128, 0, c->stream>>>(
-          view_of(c, b), rows_of(q), rows_of(out), (const TC*)P.k, (const TC*)P.v, (const float*)P.ks, (const float*)P.vs, c->group, scale_log2);
-      return launched();
+      if constexpr (std::is_same<TC, float>::value) {
+        const auto P = pools<TC>(c, l);
+        sd::paged_attn_row_kernel<TC, HD><<<dim3(b->n_tokens, c->cfg.n_heads), 128, 0, c->stream>>>(
+            view_of(c, b), rows_of(q), rows_of(out), (const TC*)P.k, (const TC*)P.v, (const float*)P.ks, (const float*)P.vs, c->group, scale_log2);
+        return launched();
+      } else {
+        return attention_tiles<TC, HD>(c, l, b, q, scale_log2, out);
+      }
     });
   });
 }
@@ -251,7 +301,8 @@ int sd_cache_create(const sd_cache_config* cfg, void* arena, size_t arena_bytes,
   DeviceGuard guard(c->device);
   c->sm_count = 0;
   if (!guard.ok || cudaDeviceGetAttribute(&c->sm_count, cudaDevAttrMultiProcessorCount, c->device) != cudaSuccess ||
-      cudaMemsetAsync(c->status(), 0, 256, c->stream) != cudaSuccess) {
+      cudaMemsetAsync(c->status(), 0, 256, c->stream) != cudaSuccess ||
+      cudaMemsetAsync(c->at<int>(c->counters), 0, (size_t)kPartSlots * 4, c->stream) != cudaSuccess) {
     cudaGetLastError();
     delete c;
     return SD_ERR_CUDA;

@@ -20,6 +20,7 @@
 #include "attn_prefill.cuh"
 #include "attn_stream.cuh"
 #include "paged.cuh"
+#include "attn_paged.cuh"
 #include "sample_rows.cuh"
 
 namespace {

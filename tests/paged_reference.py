@@ -117,11 +117,11 @@ def fill(cache, layout, layer=0, seed=1, k_gain=1.0, v_gain=1.0):
 
 
 def attention(q, contents, layout, scale, group):
-    """out [n_tokens, n_heads, head_dim] in 64 bits (rows without a place: zeros), and a bound on what an error of `rel` in a score's
-    terms and of `rel` in a weight may do to each output: see `bound`."""
+    """out [n_tokens, n_heads, head_dim] in 64 bits (rows without a place: zeros), and what `bound` needs."""
     out = torch.zeros(q.shape, dtype=torch.float64)
     spread = torch.zeros(q.shape, dtype=torch.float64)        # sum_j p_j |v_j|
     terms = torch.zeros(q.shape[:2], dtype=torch.float64)     # largest scale * sum_d |q_d k_jd| of a row
+    reach = torch.zeros(q.shape[:2], dtype=torch.float64)     # number of keys times their largest |v|
     for r, s, p in layout.places():
         k, v = contents[s]
         k, v = k[:, :p + 1], v[:, :p + 1]
@@ -130,15 +130,22 @@ def attention(q, contents, layout, scale, group):
         out[r] = torch.einsum("kgj,kjd->kgd", w, v).reshape(out[r].shape)
         spread[r] = torch.einsum("kgj,kjd->kgd", w, v.abs()).reshape(out[r].shape)
         terms[r] = (torch.einsum("kgd,kjd->kgj", qr.abs(), k.abs()) * abs(scale)).amax(-1).reshape(-1)
-    return out, spread, terms
+        reach[r] = (v.abs().amax((1, 2)) * (p + 1)).repeat_interleave(group)
+    return out, (spread, terms, reach)
 
 
-def bound(out, spread, terms, score_rel, weight_rel, out_dtype):
+def bound(out, parts, score_rel, weight_rel, out_dtype):
     """Largest error of an output.  A score is off by at most score_rel * terms, so every weight p_j by a factor within
     exp(+-2 score_rel terms) (numerator and sum), times 1 +- weight_rel: |error| <= spread * (e^(2 score_rel terms) - 1 + weight_rel) to first
-    order (doubled for the rest), and the rounding to the output's type is half a step."""
+    order (doubled for the rest), and the rounding to the output's type is half a step.
+
+    Where weights enter as sums of two fp16 numbers (8-bit caches), weights below 2^-14 lie on fp16's fixed grid of 2^-24, so each is also
+    off by up to 2^-25 of the unit, in which the largest weight times scale is at least 2^7: with a largest code c that key's
+    weight moves by at most 2^-32 and its contribution by 2^-32 times the largest |v| (w_j scale_j c <= the largest |v| after
+    the division by the sum), for each of the keys: reach * 2^-32 in all."""
+    spread, terms, reach = parts
     rel = torch.expm1(2 * score_rel * terms).unsqueeze(-1) + weight_rel
-    return 2 * spread * rel + (out.abs() + spread * rel) * torch.finfo(out_dtype).eps / 2 + 1e-30
+    return 2 * spread * rel + (out.abs() + spread * rel) * torch.finfo(out_dtype).eps / 2 + reach.unsqueeze(-1) * 2.0 ** -32 + 1e-30
 
 
 def select(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):

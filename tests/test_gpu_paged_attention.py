@@ -39,8 +39,8 @@ def run(cache_dtype, io, heads, kv_heads, hd, page, new, length, scale=None, out
     cache.attention(0, q.cuda(), lay.batch(), scale=scale, out=out)
     assert cache.status() == 0
     cache.close()
-    want, spread, terms = P.attention(q, contents, lay, hd ** -0.5 if scale is None else scale, heads // kv_heads)
-    lim = P.bound(want, spread, terms, *rels(hd, cache_dtype, q.dtype, out_dtype), out_dtype)
+    want, parts = P.attention(q, contents, lay, hd ** -0.5 if scale is None else scale, heads // kv_heads)
+    lim = P.bound(want, parts, *rels(hd, cache_dtype, q.dtype, out_dtype), out_dtype)
     got = out.cpu().double()
     own = torch.zeros(lay.n_tokens, dtype=torch.bool)
     for s in range(len(new)):
@@ -115,8 +115,8 @@ def test_scales_of_very_different_sizes():
             contents[s][1][:, p] *= f
     q = torch.randn(2, 2, 64, generator=torch.Generator().manual_seed(1))
     got = cache.attention(0, q.cuda(), lay.batch()).cpu().double()
-    want, spread, terms = P.attention(q, contents, lay, 0.125, 1)
-    lim = P.bound(want, spread, terms, *rels(64, "int8", torch.float32, torch.float32), torch.float32)
+    want, parts = P.attention(q, contents, lay, 0.125, 1)
+    lim = P.bound(want, parts, *rels(64, "int8", torch.float32, torch.float32), torch.float32)
     assert bool(((got - want).abs() <= lim).all())
     assert bool((got[1] == 0).all())
     cache.close()
@@ -139,8 +139,8 @@ def test_strided_queries_and_outputs(cache_dtype):
             dev.copy_(q)
         out = torch.zeros(H, n, hd + 1, device="cuda").transpose(0, 1)[..., 1:]
         cache.attention(0, dev, lay.batch(), out=out)
-        want, spread, terms = P.attention(q, contents, lay, hd ** -0.5, 1)
-        lim = P.bound(want, spread, terms, *rels(hd, cache_dtype, torch.float32, torch.float32), torch.float32)
+        want, parts = P.attention(q, contents, lay, hd ** -0.5, 1)
+        lim = P.bound(want, parts, *rels(hd, cache_dtype, torch.float32, torch.float32), torch.float32)
         assert bool(((out.cpu().double() - want).abs() <= lim).all())
     cache.close()
 
@@ -227,8 +227,8 @@ def test_another_stream_and_two_caches_at_once():
         outs = [o * 1.0 for o in outs]
     side.synchronize()
     for o, con in zip(outs, contents):
-        want, spread, terms = P.attention(q, con, lay, 0.125, 2)
-        lim = P.bound(want, spread, terms, *rels(64, "int8", torch.float32, torch.float32), torch.float32)
+        want, parts = P.attention(q, con, lay, 0.125, 2)
+        lim = P.bound(want, parts, *rels(64, "int8", torch.float32, torch.float32), torch.float32)
         assert bool(((o.cpu().double() - want).abs() <= lim).all())
     for c in caches:
         c.close()
