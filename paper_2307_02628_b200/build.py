@@ -11,7 +11,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libskipdecode.so")
 SOURCES = [os.path.join(CSRC, "skipdecode.cu")]
 HEADERS = [os.path.join(CSRC, n) for n in ("kernels.cuh", "gemm_tc.cuh", "sample.cuh", "attn_prefill.cuh", "gemm_persist.cuh", "attn_stream.cuh",
-                                              "paged.cuh", "attn_paged.cuh", "sample_rows.cuh", "cache_host.cuh")] + \
+                                              "paged.cuh", "attn_paged.cuh", "attn_chunk.cuh", "sample_rows.cuh", "cache_host.cuh")] + \
           [os.path.join(os.path.dirname(PKG), "include", "skipdecode.h")]
 
 

@@ -1,0 +1,455 @@
+// Attention of chunks of new tokens over a paged cache in bf16 or 8 bits, on the fifth-generation tensor cores.
+//
+// One block per (sequence, key head, 256 query rows); a query row is a (token, head of the group) pair, so grouped heads share
+// the keys they read.  The 256 rows are two tiles of 128 that take turns: while one tile's softmax runs on the CUDA cores, the
+// tensor core works on the other's products.  For every 128 keys and each tile t:
+//     S_t = Q_t K^T        (both operands in shared memory, result in tensor memory)
+//     P_t = 2^(S_t - m)    (one thread per row: maximum, exponentials, sum; P_t in bf16 over S_t's own columns)
+//     O_t += P_t V         (P_t from tensor memory, V from shared memory as it lies: keys are the product's inner axis)
+// Tensor memory holds S_0, S_1 (128 columns each) and O_0, O_1 (HD columns each).  The products of one block are issued by one
+// thread and execute in order, so S_t of the next keys may overwrite P_t as soon as its product is issued.
+//
+// Operands are bf16: queries and weights are rounded once to 8 bits of significand, codes of 8-bit caches are bf16 numbers
+// exactly.  A result in 16 bits keeps no more; results wanted in fp32 go to the kernel for few rows.  A key's scale (8-bit
+// caches) multiplies its score in the softmax, a value's scale its weight, before the rounding.
+//
+// The running maximum is raised only when it would be passed by 2^8 (weights then reach 256, well inside bf16 and the fp32
+// sums): O_t is rescaled in tensor memory in the first tiles and hardly ever after.
+//
+// What bounds it: 2 x 128 x 128 weights take 2048 clocks on the unit that computes exponentials, and 2 x 2 products take 2048 clocks
+// (HD = 128) of the tensor core.
+//
+// Warps: 0-3 and 4-7 softmax of tile 0 and 1 (one thread per row, which is a lane of tensor memory), 8-11 loaders (page
+// look-up, copies into the swizzled layout the tensor core reads, conversion of codes), 12 issues the products.
+// Every wait is bounded; on expiry the block records it, waits (bounded) for the products in flight and frees its tensor memory.
+#pragma once
+#include "attn_paged.cuh"
+#include "gemm_tc.cuh"
+
+namespace sd {
+namespace ac {
+
+constexpr int THREADS = 416, ROWS = 256, KEYS = 128, TILE_ROWS = 128, STAGES = 2, SIDE = 4;
+constexpr float SLACK = 8.f;
+
+template <int HD> struct Layout {
+  static constexpr int TILE = 128 * HD * 2;                    // a tile of Q, K or V: blocks of 64 elements, 128 rows of 128 bytes each
+  static constexpr int Q = 0, K = 2 * TILE, V = K + STAGES * TILE, END = V + STAGES * TILE;
+  static constexpr int SIDE_OFF = END;                         // per key tile: 128 key scales, 128 value scales, mask of existing pages
+  static constexpr int SIDE_BYTES = 2 * KEYS * 4 + 16;
+  static constexpr int NEED = END + SIDE * SIDE_BYTES + 1024;  // + alignment
+  static constexpr int SMEM = NEED > 116 * 1024 ? NEED : 116 * 1024;   // one block per SM: each takes all of the tensor memory
+  static constexpr int O_COL = 256;                            // tensor memory: S_0 at 0, S_1 at 128, O_0, O_1 from 256
+};
+
+// bf16 x bf16 -> fp32, 128 rows; b_mn: B is stored with its output axis contiguous
+__host__ __device__ constexpr uint32_t idesc(int n, bool b_mn) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
+}
+// V as it lies: 64-element blocks `lead` bytes apart, groups of 8 keys 1024 bytes apart, 128-byte swizzle
+__device__ __forceinline__ uint64_t v_desc(uint32_t addr, uint32_t lead) {
+  return (uint64_t)((addr >> 4) & 0x3FFF) | ((uint64_t)(lead >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t acc) { tc::umma(d, a, b, id, acc); }
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t acc) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
+               ::"r"(d), "r"(a), "l"(b), "r"(id), "r"(acc) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+               ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+                 "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&r)[32]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+               "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+               ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+                 "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+                 "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+                 "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void sts16(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+// byte offset of 16-byte piece c (8 elements) of row r in a tile
+__device__ __forceinline__ uint32_t piece(int r, int c) { return (uint32_t)((c >> 3) * (128 * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)); }
+
+// Four codes (a word) to two bf16 pairs.  int8: the lower seven bits under the exponent of 128 are 128 + those bits; the sign bit
+// lands in the exponent of the subtrahend and makes 128 of it 256.
+__device__ __forceinline__ uint32_t int8_pair(uint32_t two) {              // two codes in the lower bytes of the halves
+  const uint32_t a = (two & 0x007f007fu) | 0x43004300u, s = (two & 0x00800080u) | 0xc300c300u;
+  const __nv_bfloat162 d = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&s));
+  return *reinterpret_cast<const uint32_t*>(&d);
+}
+__device__ __forceinline__ void to_bf16(uint32_t w, uint32_t& lo, uint32_t& hi, int8_t) {
+  lo = int8_pair(__byte_perm(w, 0u, 0x4140));
+  hi = int8_pair(__byte_perm(w, 0u, 0x4342));
+}
+__device__ __forceinline__ void to_bf16(uint32_t w, uint32_t& lo, uint32_t& hi, e4m3) {
+  const float2 a = e4m3_widen(w & 0xffffu), b = e4m3_widen(w >> 16);
+  lo = pack_bf16(a.x, a.y);
+  hi = pack_bf16(b.x, b.y);
+}
+
+}  // namespace ac
+
+// grid: blocks_per_seq * n_kv_heads * n_seqs.  Sequences with fewer than rows_from query rows are another kernel's.
+template <typename TC, int HD>
+__global__ void __launch_bounds__(ac::THREADS, 1)
+paged_attn_chunk_kernel(const BatchView b, const Rows q, const Rows out, const TC* __restrict__ Kp, const TC* __restrict__ Vp,
+                        const float* __restrict__ Ksc, const float* __restrict__ Vsc, int group, float scale_log2, bool q_vec, bool out_vec,
+                        int blocks_per_seq, int rows_from) {
+  using namespace ac;
+  using L = Layout<HD>;
+  constexpr bool SCALED = CacheType<TC>::TOP > 0.f;
+  extern __shared__ unsigned char ac_smem[];
+  __shared__ uint64_t bars[4 * STAGES + 8];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_word;
+
+  // the block's rows
+  const int blk = blockIdx.x % blocks_per_seq, rest = blockIdx.x / blocks_per_seq;
+  const int g_head = rest % b.n_kv_heads, seq = rest / b.n_kv_heads;
+  const int f0 = b.first[seq], f1 = b.first[seq + 1], len = b.seq_len(seq);
+  int n_new = f1 - f0;
+  if (f0 < 0 || n_new < 0 || f1 > b.n_tokens || n_new > b.max_new) {
+    if (threadIdx.x == 0) b.bad();
+    if (f0 < 0 || n_new < 0) return;
+    n_new = min(n_new, min(b.max_new, b.n_tokens - f0));
+  }
+  const int rows_all = n_new * group;
+  if (rows_all < rows_from) return;
+  const int blocks = (rows_all + ROWS - 1) / ROWS;
+  const int row0 = (blocks - 1 - blk) * ROWS;                   // the rows that see most keys first
+  if (row0 < 0) return;
+  const long long pos_first = (long long)b.len[seq] - (f1 - f0);
+  int n_keys[2], n_rows[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    n_rows[t] = max(0, min(TILE_ROWS, rows_all - row0 - t * TILE_ROWS));
+    const int last = (row0 + t * TILE_ROWS + n_rows[t] - 1) / group;
+    const int keys = n_rows[t] ? (int)min(max(pos_first + last + 1, 0ll), (long long)len) : 0;
+    n_keys[t] = (keys + KEYS - 1) / KEYS;                       // tiles of keys; a later tile of rows sees no fewer
+  }
+  const int n_tiles = max(n_keys[0], n_keys[1]);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t raw = (uint32_t)__cvta_generic_to_shared(ac_smem), base = (raw + 1023u) & ~1023u;
+  unsigned char* base_ptr = ac_smem + (base - raw);
+  const uint32_t bar0 = (uint32_t)__cvta_generic_to_shared(bars);
+  const uint32_t kfull = bar0, kempty = kfull + 8 * STAGES, vfull = kempty + 8 * STAGES, vempty = vfull + 8 * STAGES;
+  const uint32_t sfull = vempty + 8 * STAGES, pready = sfull + 16, odone = pready + 16, qfull = odone + 16, drain = qfull + 8;
+  volatile int* abort_flag = &abort_word;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) {
+      tc::mbar_init(kfull + 8 * s, 4); tc::mbar_init(kempty + 8 * s, 1);
+      tc::mbar_init(vfull + 8 * s, 4); tc::mbar_init(vempty + 8 * s, 1);
+    }
+    for (int t = 0; t < 2; ++t) { tc::mbar_init(sfull + 8 * t, 1); tc::mbar_init(pready + 8 * t, 4); tc::mbar_init(odone + 8 * t, 1); }
+    tc::mbar_init(qfull, 8);
+    tc::mbar_init(drain, 1);
+    abort_word = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 12) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"((uint32_t)__cvta_generic_to_shared(&tmem_slot)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = tmem_slot;
+
+  if (warp < 8) {
+    // ---- softmax: one thread per query row
+    const int t = warp >> 2, r = (warp & 3) * 32 + lane;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t s_addr = tmem + lanes + t * 128, o_addr = tmem + lanes + L::O_COL + t * HD;
+    const int row = row0 + t * TILE_ROWS + min(r, max(n_rows[t] - 1, 0));
+    const int token = row / group, head = g_head * group + row % group;
+    const int row_last = (int)max(min(pos_first + token, (long long)len - 1), -1ll);        // last key this row sees
+    if (n_rows[t] > 0) {
+      const long long at = (long long)(f0 + token) * q.row_stride + head * q.head_stride;
+      const uint32_t dst = base + L::Q + t * L::TILE;
+#pragma unroll 4
+      for (int c = 0; c < HD / 8; ++c) {
+        float x[8];
+        ap::load_run<8>(q, at + c * 8, q_vec, x);
+        sts16(dst + piece(r, c), pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+      }
+    }
+    fence_async();
+    __syncwarp();
+    if (lane == 0) arrive(qfull);
+
+    // the keys that all 32 rows of the warp see: tiles below need no mask
+    const int first_token = (row0 + t * TILE_ROWS + min((warp & 3) * 32, max(n_rows[t] - 1, 0))) / group;
+    const int all_see = (int)max(min(pos_first + first_token, (long long)len - 1), -1ll);
+    float m = -INFINITY, l = 0.f;
+    bool ok = true;
+    for (int j = 0; j < n_keys[t]; ++j) {
+      // the loaders' own barrier orders their plain stores (scales, mask); it cannot run a phase ahead of this wait, because the
+      // next keys of the stage are announced only after this tile's product with its values
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(sfull + 8 * t, j & 1, abort_flag, b.status) &&
+                                   tc::mbar_wait(kfull + 8 * (j % STAGES), (j / STAGES) & 1, abort_flag, b.status));
+      if (!ok) break;
+      fence_after();
+      const float* side = reinterpret_cast<const float*>(base_ptr + L::SIDE_OFF + (j & (SIDE - 1)) * L::SIDE_BYTES);
+      const uint32_t pages_ok = *reinterpret_cast<const uint32_t*>(side + 2 * KEYS);
+      const bool edge = j * KEYS + KEYS - 1 > all_see || pages_ok != 0xffffu;
+      // a column's score, in base-2 units; -inf where the row does not see the key
+      auto score = [&](uint32_t bits, int c) {
+        float s = __uint_as_float(bits);
+        if (SCALED) s *= side[c];
+        s *= scale_log2;
+        if (edge && (j * KEYS + c > row_last || !((pages_ok >> (c >> 3)) & 1u))) s = -INFINITY;
+        return s;
+      };
+      float mx = -INFINITY;
+#pragma unroll 1
+      for (int c0 = 0; c0 < KEYS; c0 += 32) {
+        uint32_t v[32];
+        tc::tmem_ld32(s_addr + c0, v);
+        tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 32; ++i) mx = fmaxf(mx, score(v[i], c0 + i));
+      }
+      if (__any_sync(0xffffffffu, mx > m + SLACK)) {
+        const float m_new = fmaxf(m, mx), a = exp2_safe(m, m_new);
+        m = m_new;
+        l *= a;
+        if (j > 0) {
+          ok = __all_sync(0xffffffffu, tc::mbar_wait(odone + 8 * t, (j - 1) & 1, abort_flag, b.status));
+          if (!ok) break;
+          fence_after();
+#pragma unroll 1
+          for (int c0 = 0; c0 < HD; c0 += 32) {
+            uint32_t v[32];
+            tc::tmem_ld32(o_addr + c0, v);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * a);
+            tmem_st32(o_addr + c0, v);
+          }
+          tmem_wait_st();
+        }
+      }
+      const float mb = m == -INFINITY ? 0.f : m;
+      float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll 1
+      for (int c0 = 0; c0 < KEYS; c0 += 32) {
+        uint32_t v[32], w[16];
+        tc::tmem_ld32(s_addr + c0, v);
+        tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float p0 = ex2(score(v[2 * i], c0 + 2 * i) - mb), p1 = ex2(score(v[2 * i + 1], c0 + 2 * i + 1) - mb);
+          sum0 += p0;
+          sum1 += p1;
+          if (SCALED) { p0 *= side[KEYS + c0 + 2 * i]; p1 *= side[KEYS + c0 + 2 * i + 1]; }
+          w[i] = pack_bf16(p0, p1);
+        }
+        tmem_st16(s_addr + (c0 >> 1), w);                        // over columns that have been read
+      }
+      l += sum0 + sum1;
+      tmem_wait_st();
+      fence_before();
+      __syncwarp();
+      if (lane == 0) arrive(pready + 8 * t);
+    }
+    if (n_rows[t] > 0 && ok) {
+      if (n_keys[t] > 0) {
+        ok = __all_sync(0xffffffffu, tc::mbar_wait(odone + 8 * t, (n_keys[t] - 1) & 1, abort_flag, b.status));
+        fence_after();
+      }
+      if (ok) {
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const long long at = (long long)(f0 + token) * out.row_stride + head * out.head_stride;
+#pragma unroll 1
+        for (int c0 = 0; c0 < HD; c0 += 32) {
+          uint32_t v[32];
+          if (n_keys[t] > 0) {
+            tc::tmem_ld32(o_addr + c0, v);
+            tmem_wait_ld();
+          }
+          if (r < n_rows[t]) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) {
+              float x[8];
+#pragma unroll
+              for (int k = 0; k < 8; ++k) x[k] = l > 0.f ? __uint_as_float(v[i + k]) * inv : (l == 0.f ? 0.f : l);   // l NaN: NaN
+              const long long e = at + c0 + i;
+              if (out_vec && out.dtype == DT_BF16) store8<true>(static_cast<__nv_bfloat16*>(out.data) + e, x);
+              else if (out_vec && out.dtype == DT_FP16) store8<true>(static_cast<__half*>(out.data) + e, x);
+              else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) store_elem(out, e + k, x[k]);
+              }
+            }
+          }
+        }
+      }
+    }
+  } else if (warp < 12) {
+    // ---- loaders
+    const int w = warp - 8, tid = w * 32 + lane;
+    const int* table = b.pages + (size_t)seq * b.pages_per_seq;
+    constexpr int E = sizeof(TC), PER_ROW = HD * E / 16;          // 16-byte pieces of a stored key
+    constexpr int ROWS_AT_ONCE = 32 / PER_ROW;                    // of a warp
+    constexpr int STEPS = KEYS / (4 * ROWS_AT_ONCE);
+    const int most = min(len, n_tiles * KEYS);                    // keys past it are filled with zeros
+    // lane i < 16 looks up the page of keys [8 i, 8 i + 8) of a tile
+    auto look_up = [&](int j) {
+      const int key = j * KEYS + (lane & 15) * 8;
+      return j < n_tiles && key < most ? table[key >> b.page_shift] : 0;
+    };
+    auto entry_of = [&](int page, int j, int key) { return b.entry(page, g_head, j * KEYS + key); };
+    int entry_next = look_up(0);
+    bool ok = true;
+    for (int j = 0; j < n_tiles && ok; ++j) {
+      const int s = j % STAGES, round = j / STAGES;
+      const int my_page = entry_next;
+      entry_next = look_up(j + 1);
+      const bool there = (unsigned)my_page < (unsigned)b.n_pages;
+      const uint32_t pages_ok = __ballot_sync(0xffffffffu, there || (j * KEYS + (lane & 15) * 8) >= most) & 0xffffu;
+      if (!there && lane < 16 && w == 0) b.bad();
+      if (round > 0) {
+        ok = __all_sync(0xffffffffu, tc::mbar_wait(kempty + 8 * s, (round - 1) & 1, abort_flag, b.status));
+        if (!ok) break;
+      }
+      const uint32_t kt = base + L::K + s * L::TILE, vt = base + L::V + s * L::TILE;
+      float* side = reinterpret_cast<float*>(base_ptr + L::SIDE_OFF + (j & (SIDE - 1)) * L::SIDE_BYTES);
+      if (tid == 0) *reinterpret_cast<uint32_t*>(side + 2 * KEYS) = pages_ok;
+      if (SCALED) {
+        const int page = __shfl_sync(0xffffffffu, my_page, tid >> 3 & 15);
+        const bool on = j * KEYS + tid < most && (pages_ok >> (tid >> 3) & 1u);
+        const size_t e = on ? entry_of(page, j, tid) : 0;
+        side[tid] = on ? Ksc[e] : 0.f;
+        side[KEYS + tid] = on ? Vsc[e] : 0.f;
+      }
+      // keys, then values: pieces go to their swizzled places; rows that are not there become zeros
+      auto fill = [&](const TC* __restrict__ pool, uint32_t dst) {
+        if constexpr (!SCALED) {
+#pragma unroll
+          for (int i = 0; i < STEPS; ++i) {
+            const int key = (i * 4 + w) * ROWS_AT_ONCE + lane / PER_ROW, c = lane % PER_ROW;
+            const int page = __shfl_sync(0xffffffffu, my_page, key >> 3);
+            const bool on = j * KEYS + key < most && ((pages_ok >> (key >> 3)) & 1u);
+            const TC* src = on ? pool + entry_of(page, j, key) * HD + c * 8 : pool;
+            pf_cp16(dst + piece(key, c), src, on ? 16 : 0);
+          }
+        } else {
+          uint4 v[STEPS];
+#pragma unroll
+          for (int i = 0; i < STEPS; ++i) {
+            const int key = (i * 4 + w) * ROWS_AT_ONCE + lane / PER_ROW, c = lane % PER_ROW;
+            const int page = __shfl_sync(0xffffffffu, my_page, key >> 3);
+            const bool on = j * KEYS + key < most && ((pages_ok >> (key >> 3)) & 1u);
+            v[i] = on ? __ldg(reinterpret_cast<const uint4*>(pool + entry_of(page, j, key) * HD + c * 16)) : make_uint4(0u, 0u, 0u, 0u);
+          }
+#pragma unroll
+          for (int i = 0; i < STEPS; ++i) {
+            const int key = (i * 4 + w) * ROWS_AT_ONCE + lane / PER_ROW, c = lane % PER_ROW;
+            uint32_t o[8];
+            to_bf16(v[i].x, o[0], o[1], TC{});
+            to_bf16(v[i].y, o[2], o[3], TC{});
+            to_bf16(v[i].z, o[4], o[5], TC{});
+            to_bf16(v[i].w, o[6], o[7], TC{});
+            sts16(dst + piece(key, 2 * c), o[0], o[1], o[2], o[3]);
+            sts16(dst + piece(key, 2 * c + 1), o[4], o[5], o[6], o[7]);
+          }
+        }
+      };
+      fill(Kp, kt);
+      if constexpr (!SCALED) pf_commit();
+      if (round > 0) {
+        ok = __all_sync(0xffffffffu, tc::mbar_wait(vempty + 8 * s, (round - 1) & 1, abort_flag, b.status));
+        if (!ok) break;
+      }
+      if constexpr (SCALED) { fence_async(); __syncwarp(); if (lane == 0) arrive(kfull + 8 * s); }
+      fill(Vp, vt);
+      if constexpr (!SCALED) {
+        pf_commit();
+        pf_wait<1>();
+        fence_async();
+        __syncwarp();
+        if (lane == 0) arrive(kfull + 8 * s);
+        pf_wait<0>();
+      }
+      fence_async();
+      __syncwarp();
+      if (lane == 0) arrive(vfull + 8 * s);
+    }
+    if constexpr (!SCALED) pf_wait<0>();
+  } else if (lane == 0 && n_tiles > 0) {
+    // ---- products
+    constexpr uint32_t id_s = idesc(KEYS, false), id_o = idesc(HD, true);
+    bool ok = tc::mbar_wait(qfull, 0, abort_flag, b.status);
+    auto product_s = [&](int t, int j) {
+      const uint32_t qa = base + L::Q + t * L::TILE, ka = base + L::K + (j % STAGES) * L::TILE;
+#pragma unroll
+      for (int k = 0; k < HD / 16; ++k) {
+        const uint32_t off = (k >> 2) * (128 * 128) + (k & 3) * 32;
+        mma_ss(tmem + t * 128, tc::smem_desc(qa + off), tc::smem_desc(ka + off), id_s, k > 0);
+      }
+      tc::umma_commit(sfull + 8 * t);
+    };
+    auto product_o = [&](int t, int j) {
+      const uint32_t va = base + L::V + (j % STAGES) * L::TILE;
+#pragma unroll
+      for (int k = 0; k < KEYS / 16; ++k)
+        mma_ts(tmem + L::O_COL + t * HD, tmem + t * 128 + k * 8, v_desc(va + k * 2048, 128 * 128), id_o, (j > 0 || k > 0) ? 1u : 0u);
+      tc::umma_commit(odone + 8 * t);
+    };
+    if (ok) ok = tc::mbar_wait(kfull, 0, abort_flag, b.status);
+    if (ok) {
+      fence_after();
+      for (int t = 0; t < 2; ++t)
+        if (n_keys[t] > 0) product_s(t, 0);
+      tc::umma_commit(kempty);
+    }
+    for (int j = 0; j < n_tiles && ok; ++j) {
+      const int s = j % STAGES, sn = (j + 1) % STAGES;
+      ok = tc::mbar_wait(vfull + 8 * s, (j / STAGES) & 1, abort_flag, b.status);
+      if (ok && j + 1 < n_tiles) ok = tc::mbar_wait(kfull + 8 * sn, ((j + 1) / STAGES) & 1, abort_flag, b.status);
+      for (int t = 0; t < 2 && ok; ++t) {
+        if (j < n_keys[t]) {
+          ok = tc::mbar_wait(pready + 8 * t, j & 1, abort_flag, b.status);
+          if (!ok) break;
+          fence_after();
+          product_o(t, j);
+        }
+        if (j + 1 < n_keys[t]) product_s(t, j + 1);
+      }
+      if (ok) {
+        tc::umma_commit(vempty + 8 * s);
+        if (j + 1 < n_tiles) tc::umma_commit(kempty + 8 * sn);
+      }
+    }
+    if (!ok) {                                                    // let what has been issued finish before the memory goes
+      tc::umma_commit(drain);
+      const long long t0 = clock64();
+      while (!tc::mbar_try(drain, 0) && clock64() - t0 < tc::kWaitLimit) {}
+    }
+  }
+  fence_before();
+  __syncthreads();
+  if (warp == 12) {
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  }
+}
+
+}  // namespace sd

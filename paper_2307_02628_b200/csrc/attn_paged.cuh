@@ -111,14 +111,14 @@ template <int N> __device__ __forceinline__ void load_run(const Rows& t, long lo
 
 }  // namespace ap
 
-// grid (tiles_per_seq * n_kv_heads * n_seqs, splits).  Split z takes keys [z * chunk, (z + 1) * chunk), the last one all that follow.
+// grid (tiles_per_seq * n_kv_heads * n_seqs, splits).  Sequences with rows_below query rows or more are another kernel's.  Split z takes keys [z * chunk, (z + 1) * chunk), the last one all that follow.
 // Several splits leave partial results (accumulator, maximum, sum) of the rows they see and the block that arrives last at a
 // unit's counter adds them in split order, so the result does not depend on who came when.
 template <typename TC, int HD>
 __global__ void __launch_bounds__(ap::THREADS)
 paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC* __restrict__ Kp, const TC* __restrict__ Vp,
                        const float* __restrict__ Ksc, const float* __restrict__ Vsc, int group, float scale_log2, bool q_vec,
-                       int tiles_per_seq, int chunk, float* part_acc, float* part_ml, int* __restrict__ counters) {
+                       int tiles_per_seq, int rows_below, int chunk, float* part_acc, float* part_ml, int* __restrict__ counters) {
   using namespace ap;
   using S = Shape<TC, HD>;
   extern __shared__ __align__(128) unsigned char ap_smem[];
@@ -137,7 +137,7 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
     n_new = min(n_new, min(b.max_new, b.n_tokens - f0));
   }
   const int n_rows = min(ROWS, n_new * group - tile * ROWS);
-  if (n_rows <= 0) return;
+  if (n_rows <= 0 || n_new * group >= rows_below) return;
   const long long pos_first = (long long)b.len[seq] - (f1 - f0);            // position of the first new token, negative without a place
   const int last_token = (tile * ROWS + n_rows - 1) / group;
   const int key_end = (int)min(max(pos_first + last_token + 1, 0ll), (long long)len);      // keys that any row of the tile sees

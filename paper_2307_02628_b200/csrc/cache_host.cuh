@@ -196,8 +196,9 @@ int pick_split(const sd_cache* c, long units, long rows, int64_t max_len) {
   return (int)std::min<int64_t>((max_len + best * 64 - 1) / (best * 64) * 64, 0x7fffffc0);
 }
 
+// Sequences of rows_below query rows per key head or more are left out (another kernel takes them).
 template <typename TC, int HD>
-int attention_tiles(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale_log2, const sd_heads* out) {
+int attention_tiles(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale_log2, const sd_heads* out, int64_t rows_below) {
   using S = sd::ap::Shape<TC, HD>;
   constexpr unsigned bit = 1u << ((HD == 128 ? 0 : HD == 64 ? 1 : 2) + 3 * (std::is_same<TC, bf16>::value ? 0 : std::is_same<TC, int8_t>::value ? 1 : 2));
   auto kernel = sd::paged_attn_tile_kernel<TC, HD>;
@@ -206,7 +207,7 @@ int attention_tiles(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, fl
     c->tile_ready |= bit;
   }
   const auto P = pools<TC>(c, l);
-  const int tiles = (int)(((int64_t)b->max_new * c->group + sd::ap::ROWS - 1) / sd::ap::ROWS);
+  const int tiles = (int)((std::min((int64_t)b->max_new * c->group, rows_below - 1) + sd::ap::ROWS - 1) / sd::ap::ROWS);
   const int64_t units = (int64_t)tiles * c->cfg.n_kv_heads * b->n_seqs;
   if (units > 0x7fffffff) return SD_ERR_ARG;
   const int max_len = b->max_len > 0 ? b->max_len : b->pages_per_seq * c->cfg.page_len;
@@ -214,9 +215,30 @@ int attention_tiles(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, fl
   const int splits = (int)(((int64_t)max_len + chunk - 1) / chunk);
   kernel<<<dim3((unsigned)units, splits), sd::ap::THREADS, S::SMEM, c->stream>>>(
       view_of(c, b), rows_of(q), rows_of(out), (const TC*)P.k, (const TC*)P.v, (const float*)P.ks, (const float*)P.vs, c->group, scale_log2, wide(q),
-      tiles, chunk, c->at<float>(c->part_acc), c->at<float>(c->part_ml), c->at<int>(c->counters));
+      tiles, (int)std::min<int64_t>(rows_below, 0x7fffffff), chunk, c->at<float>(c->part_acc), c->at<float>(c->part_ml), c->at<int>(c->counters));
   return launched();
 }
+
+template <typename TC, int HD>
+int attention_chunks(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale_log2, const sd_heads* out, int rows_from) {
+  using L = sd::ac::Layout<HD>;
+  constexpr unsigned bit = 1u << (16 + (HD == 128 ? 0 : 1) + 2 * (std::is_same<TC, bf16>::value ? 0 : std::is_same<TC, int8_t>::value ? 1 : 2));
+  auto kernel = sd::paged_attn_chunk_kernel<TC, HD>;
+  if (!(c->tile_ready & bit)) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM) != cudaSuccess) { cudaGetLastError(); return SD_ERR_CUDA; }
+    c->tile_ready |= bit;
+  }
+  const auto P = pools<TC>(c, l);
+  const int blocks = (int)(((int64_t)b->max_new * c->group + sd::ac::ROWS - 1) / sd::ac::ROWS);
+  const int64_t grid = (int64_t)blocks * c->cfg.n_kv_heads * b->n_seqs;
+  if (grid > 0x7fffffff) return SD_ERR_ARG;
+  kernel<<<(unsigned)grid, sd::ac::THREADS, L::SMEM, c->stream>>>(
+      view_of(c, b), rows_of(q), rows_of(out), (const TC*)P.k, (const TC*)P.v, (const float*)P.ks, (const float*)P.vs, c->group, scale_log2, wide(q), wide(out),
+      blocks, rows_from);
+  return launched();
+}
+
+constexpr int kChunkRows = 33;   // query rows per key head from which a sequence goes to the kernel for chunks
 
 int cache_attention(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale, const sd_heads* out) {
   if (scale == 0.f) scale = 1.f / sqrtf((float)c->cfg.head_dim);
@@ -231,7 +253,17 @@ int cache_attention(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, fl
             view_of(c, b), rows_of(q), rows_of(out), (const TC*)P.k, (const TC*)P.v, (const float*)P.ks, (const float*)P.vs, c->group, scale_log2);
         return launched();
       } else {
-        return attention_tiles<TC, HD>(c, l, b, q, scale_log2, out);
+        const int64_t most = (int64_t)b->max_new * c->group;
+        if (most > 0x7fffff00) return (int)SD_ERR_ARG;
+        if constexpr (HD >= 64) {
+          if (most >= kChunkRows && out->dtype != SD_DTYPE_FP32) {
+            // max_new is only a bound: which kernel takes a sequence is decided on the device, by its own rows
+            const int rc = attention_chunks<TC, HD>(c, l, b, q, scale_log2, out, b->n_seqs == 1 ? 1 : kChunkRows);
+            if (rc != SD_OK || b->n_seqs == 1) return rc;
+            return attention_tiles<TC, HD>(c, l, b, q, scale_log2, out, kChunkRows);
+          }
+        }
+        return attention_tiles<TC, HD>(c, l, b, q, scale_log2, out, most + 1);
       }
     });
   });

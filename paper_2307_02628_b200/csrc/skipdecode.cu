@@ -21,6 +21,7 @@
 #include "attn_stream.cuh"
 #include "paged.cuh"
 #include "attn_paged.cuh"
+#include "attn_chunk.cuh"
 #include "sample_rows.cuh"
 
 namespace {
