@@ -29,8 +29,12 @@
 namespace sd {
 namespace ac {
 
-constexpr int THREADS = 416, ROWS = 256, KEYS = 128, TILE_ROWS = 128, STAGES = 2, SIDE = 4;
+constexpr int THREADS = 512, ROWS = 256, KEYS = 128, TILE_ROWS = 128, STAGES = 2, SIDE = 4;
 constexpr float SLACK = 8.f;
+// Registers per thread of the softmax, the loader and the product warpgroups; the block is launched with 128 for each of its
+// 512 threads, and the shares add up to no more: 2 x 128 x 184 + 128 x 104 + 128 x 40 = 65 536.
+constexpr int LAUNCH_REGS = 128, SOFTMAX_REGS = 184, LOADER_REGS = 104, PRODUCT_REGS = 40;
+static_assert(2 * 128 * SOFTMAX_REGS + 128 * LOADER_REGS + 128 * PRODUCT_REGS <= THREADS * LAUNCH_REGS, "a larger share would wait forever");
 
 template <int HD> struct Layout {
   static constexpr int TILE = 128 * HD * 2;                    // a tile of Q, K or V: blocks of 64 elements, 128 rows of 128 bytes each
@@ -82,6 +86,17 @@ __device__ __forceinline__ float ex2(float x) {
 __device__ __forceinline__ void sts16(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+               ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+// two floats at a time
+struct F2 { unsigned long long v; };
+__device__ __forceinline__ F2 f2(float a, float b) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void un2(F2 x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v)); }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
+__device__ __forceinline__ F2 add2(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
 // byte offset of 16-byte piece c (8 elements) of row r in a tile
 __device__ __forceinline__ uint32_t piece(int r, int c) { return (uint32_t)((c >> 3) * (128 * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)); }
 
@@ -105,16 +120,18 @@ __device__ __forceinline__ void to_bf16(uint32_t w, uint32_t& lo, uint32_t& hi, 
 }  // namespace ac
 
 // grid: blocks_per_seq * n_kv_heads * n_seqs.  Sequences with fewer than rows_from query rows are another kernel's.
+// map_k, map_v: the pools as [n_pages * n_kv_heads][page_len][HD] with boxes of a page by 64 elements (bf16 only; use_maps 0: not made).
 template <typename TC, int HD>
 __global__ void __launch_bounds__(ac::THREADS, 1)
-paged_attn_chunk_kernel(const BatchView b, const Rows q, const Rows out, const TC* __restrict__ Kp, const TC* __restrict__ Vp,
+paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, int use_maps,
+                        const BatchView b, const Rows q, const Rows out, const TC* __restrict__ Kp, const TC* __restrict__ Vp,
                         const float* __restrict__ Ksc, const float* __restrict__ Vsc, int group, float scale_log2, bool q_vec, bool out_vec,
                         int blocks_per_seq, int rows_from) {
   using namespace ac;
   using L = Layout<HD>;
   constexpr bool SCALED = CacheType<TC>::TOP > 0.f;
   extern __shared__ unsigned char ac_smem[];
-  __shared__ uint64_t bars[4 * STAGES + 8];
+  __shared__ uint64_t bars[4 * STAGES + 8 + SIDE];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_word;
 
@@ -149,7 +166,7 @@ paged_attn_chunk_kernel(const BatchView b, const Rows q, const Rows out, const T
   unsigned char* base_ptr = ac_smem + (base - raw);
   const uint32_t bar0 = (uint32_t)__cvta_generic_to_shared(bars);
   const uint32_t kfull = bar0, kempty = kfull + 8 * STAGES, vfull = kempty + 8 * STAGES, vempty = vfull + 8 * STAGES;
-  const uint32_t sfull = vempty + 8 * STAGES, pready = sfull + 16, odone = pready + 16, qfull = odone + 16, drain = qfull + 8;
+  const uint32_t sfull = vempty + 8 * STAGES, pready = sfull + 16, odone = pready + 16, qfull = odone + 16, drain = qfull + 8, sidefull = drain + 8;
   volatile int* abort_flag = &abort_word;
 
   if (threadIdx.x == 0) {
@@ -160,6 +177,7 @@ paged_attn_chunk_kernel(const BatchView b, const Rows q, const Rows out, const T
     for (int t = 0; t < 2; ++t) { tc::mbar_init(sfull + 8 * t, 1); tc::mbar_init(pready + 8 * t, 4); tc::mbar_init(odone + 8 * t, 1); }
     tc::mbar_init(qfull, 8);
     tc::mbar_init(drain, 1);
+    for (int i = 0; i < SIDE; ++i) tc::mbar_init(sidefull + 8 * i, 4);
     abort_word = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -174,12 +192,14 @@ paged_attn_chunk_kernel(const BatchView b, const Rows q, const Rows out, const T
 
   if (warp < 8) {
     // ---- softmax: one thread per query row
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFTMAX_REGS));
     const int t = warp >> 2, r = (warp & 3) * 32 + lane;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t s_addr = tmem + lanes + t * 128, o_addr = tmem + lanes + L::O_COL + t * HD;
     const int row = row0 + t * TILE_ROWS + min(r, max(n_rows[t] - 1, 0));
     const int token = row / group, head = g_head * group + row % group;
     const int row_last = (int)max(min(pos_first + token, (long long)len - 1), -1ll);        // last key this row sees
+    const float scale = fabsf(scale_log2), sign = scale_log2 < 0.f ? -1.f : 1.f;            // a negative scale turns the queries round
     if (n_rows[t] > 0) {
       const long long at = (long long)(f0 + token) * q.row_stride + head * q.head_stride;
       const uint32_t dst = base + L::Q + t * L::TILE;
@@ -187,6 +207,8 @@ paged_attn_chunk_kernel(const BatchView b, const Rows q, const Rows out, const T
       for (int c = 0; c < HD / 8; ++c) {
         float x[8];
         ap::load_run<8>(q, at + c * 8, q_vec, x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= sign;
         sts16(dst + piece(r, c), pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
       }
     }
@@ -197,37 +219,48 @@ paged_attn_chunk_kernel(const BatchView b, const Rows q, const Rows out, const T
     // the keys that all 32 rows of the warp see: tiles below need no mask
     const int first_token = (row0 + t * TILE_ROWS + min((warp & 3) * 32, max(n_rows[t] - 1, 0))) / group;
     const int all_see = (int)max(min(pos_first + first_token, (long long)len - 1), -1ll);
-    float m = -INFINITY, l = 0.f;
+    float m = -INFINITY, l = 0.f;                                // m in the units of the scores (bf16) or base-2 (8 bits)
+    const float unit = SCALED ? 1.f : scale;                     // base-2 units per unit of m
     bool ok = true;
     for (int j = 0; j < n_keys[t]; ++j) {
-      // the loaders' own barrier orders their plain stores (scales, mask); it cannot run a phase ahead of this wait, because the
-      // next keys of the stage are announced only after this tile's product with its values
+      // scales and mask have a barrier of their own; it cannot run a phase ahead of this wait, because the loaders reach tile
+      // j + SIDE only after the scores of tile j + 2, which follow this tile's weights
       ok = __all_sync(0xffffffffu, tc::mbar_wait(sfull + 8 * t, j & 1, abort_flag, b.status) &&
-                                   tc::mbar_wait(kfull + 8 * (j % STAGES), (j / STAGES) & 1, abort_flag, b.status));
+                                   tc::mbar_wait(sidefull + 8 * (j % SIDE), (j / SIDE) & 1, abort_flag, b.status));
       if (!ok) break;
       fence_after();
       const float* side = reinterpret_cast<const float*>(base_ptr + L::SIDE_OFF + (j & (SIDE - 1)) * L::SIDE_BYTES);
       const uint32_t pages_ok = *reinterpret_cast<const uint32_t*>(side + 2 * KEYS);
-      const bool edge = j * KEYS + KEYS - 1 > all_see || pages_ok != 0xffffu;
-      // a column's score, in base-2 units; -inf where the row does not see the key
-      auto score = [&](uint32_t bits, int c) {
-        float s = __uint_as_float(bits);
-        if (SCALED) s *= side[c];
-        s *= scale_log2;
-        if (edge && (j * KEYS + c > row_last || !((pages_ok >> (c >> 3)) & 1u))) s = -INFINITY;
-        return s;
-      };
-      float mx = -INFINITY;
-#pragma unroll 1
-      for (int c0 = 0; c0 < KEYS; c0 += 32) {
-        uint32_t v[32];
-        tc::tmem_ld32(s_addr + c0, v);
-        tmem_wait_ld();
+
+      uint32_t s[4][32];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) mx = fmaxf(mx, score(v[i], c0 + i));
+      for (int c = 0; c < 4; ++c) tc::tmem_ld32(s_addr + 32 * c, s[c]);
+      tmem_wait_ld();
+      if (SCALED) {                                              // the key's scale (with the softmax scale and log2 e)
+#pragma unroll
+        for (int c = 0; c < 128; c += 4) {
+          const float4 k = *reinterpret_cast<const float4*>(side + c);
+          uint32_t* x = &s[c >> 5][c & 31];
+          float y0, y1, y2, y3;
+          un2(mul2(f2(__uint_as_float(x[0]), __uint_as_float(x[1])), f2(k.x, k.y)), y0, y1);
+          un2(mul2(f2(__uint_as_float(x[2]), __uint_as_float(x[3])), f2(k.z, k.w)), y2, y3);
+          x[0] = __float_as_uint(y0); x[1] = __float_as_uint(y1); x[2] = __float_as_uint(y2); x[3] = __float_as_uint(y3);
+        }
       }
-      if (__any_sync(0xffffffffu, mx > m + SLACK)) {
-        const float m_new = fmaxf(m, mx), a = exp2_safe(m, m_new);
+      if (j * KEYS + KEYS - 1 > all_see || pages_ok != 0xffffu) {
+        const int left = row_last - j * KEYS;                    // columns up to here are seen
+#pragma unroll
+        for (int c = 0; c < 128; ++c)
+          if (c > left || !((pages_ok >> (c >> 3)) & 1u)) s[c >> 5][c & 31] = 0xff800000u;
+      }
+      float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int i = 0; i < 32; i += 2)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) mx[c] = fmaxf(mx[c], fmaxf(__uint_as_float(s[c][i]), __uint_as_float(s[c][i + 1])));
+      const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+      if (__any_sync(0xffffffffu, (top - m) * unit > SLACK)) {   // -inf - -inf is NaN: not greater
+        const float m_new = fmaxf(m, top), a = m == -INFINITY ? 0.f : ex2((m - m_new) * unit);
         m = m_new;
         l *= a;
         if (j > 0) {
@@ -235,35 +268,44 @@ paged_attn_chunk_kernel(const BatchView b, const Rows q, const Rows out, const T
           if (!ok) break;
           fence_after();
 #pragma unroll 1
-          for (int c0 = 0; c0 < HD; c0 += 32) {
-            uint32_t v[32];
-            tc::tmem_ld32(o_addr + c0, v);
+          for (int c0 = 0; c0 < HD; c0 += 16) {
+            uint32_t v[32], o16[16];
+            tc::tmem_ld16(o_addr + c0, v);
             tmem_wait_ld();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * a);
-            tmem_st32(o_addr + c0, v);
+            for (int i = 0; i < 16; ++i) o16[i] = __float_as_uint(__uint_as_float(v[i]) * a);
+            tmem_st16(o_addr + c0, o16);
           }
           tmem_wait_st();
         }
       }
-      const float mb = m == -INFINITY ? 0.f : m;
-      float sum0 = 0.f, sum1 = 0.f;
-#pragma unroll 1
-      for (int c0 = 0; c0 < KEYS; c0 += 32) {
-        uint32_t v[32], w[16];
-        tc::tmem_ld32(s_addr + c0, v);
-        tmem_wait_ld();
+      const float mb = m == -INFINITY ? 0.f : -m * unit;
+      const F2 unit2 = f2(unit, unit), mb2 = f2(mb, mb);
+      F2 sum[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t w[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          float p0 = ex2(score(v[2 * i], c0 + 2 * i) - mb), p1 = ex2(score(v[2 * i + 1], c0 + 2 * i + 1) - mb);
-          sum0 += p0;
-          sum1 += p1;
-          if (SCALED) { p0 *= side[KEYS + c0 + 2 * i]; p1 *= side[KEYS + c0 + 2 * i + 1]; }
+          F2 x = f2(__uint_as_float(s[c][2 * i]), __uint_as_float(s[c][2 * i + 1]));
+          x = SCALED ? add2(x, mb2) : fma2(x, unit2, mb2);
+          float p0, p1;
+          un2(x, p0, p1);
+          p0 = ex2(p0);
+          p1 = ex2(p1);
+          x = f2(p0, p1);
+          sum[i & 1] = add2(sum[i & 1], x);
+          if (SCALED) {
+            const float2 v = *reinterpret_cast<const float2*>(side + KEYS + c * 32 + 2 * i);
+            un2(mul2(x, f2(v.x, v.y)), p0, p1);
+          }
           w[i] = pack_bf16(p0, p1);
         }
-        tmem_st16(s_addr + (c0 >> 1), w);                        // over columns that have been read
+        tmem_st16(s_addr + 16 * c, w);                           // over columns that have been read
       }
-      l += sum0 + sum1;
+      float a0, a1;
+      un2(add2(sum[0], sum[1]), a0, a1);
+      l += a0 + a1;
       tmem_wait_st();
       fence_before();
       __syncwarp();
@@ -304,6 +346,7 @@ paged_attn_chunk_kernel(const BatchView b, const Rows q, const Rows out, const T
     }
   } else if (warp < 12) {
     // ---- loaders
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LOADER_REGS));
     const int w = warp - 8, tid = w * 32 + lane;
     const int* table = b.pages + (size_t)seq * b.pages_per_seq;
     constexpr int E = sizeof(TC), PER_ROW = HD * E / 16;          // 16-byte pieces of a stored key
@@ -315,133 +358,194 @@ paged_attn_chunk_kernel(const BatchView b, const Rows q, const Rows out, const T
       const int key = j * KEYS + (lane & 15) * 8;
       return j < n_tiles && key < most ? table[key >> b.page_shift] : 0;
     };
-    auto entry_of = [&](int page, int j, int key) { return b.entry(page, g_head, j * KEYS + key); };
-    int entry_next = look_up(0);
-    bool ok = true;
-    for (int j = 0; j < n_tiles && ok; ++j) {
-      const int s = j % STAGES, round = j / STAGES;
-      const int my_page = entry_next;
-      entry_next = look_up(j + 1);
-      const bool there = (unsigned)my_page < (unsigned)b.n_pages;
-      const uint32_t pages_ok = __ballot_sync(0xffffffffu, there || (j * KEYS + (lane & 15) * 8) >= most) & 0xffffu;
-      if (!there && lane < 16 && w == 0) b.bad();
-      if (round > 0) {
-        ok = __all_sync(0xffffffffu, tc::mbar_wait(kempty + 8 * s, (round - 1) & 1, abort_flag, b.status));
-        if (!ok) break;
-      }
-      const uint32_t kt = base + L::K + s * L::TILE, vt = base + L::V + s * L::TILE;
+    auto exists = [&](int j, int page) {
+      return __ballot_sync(0xffffffffu, (unsigned)page < (unsigned)b.n_pages || j * KEYS + (lane & 15) * 8 >= most) & 0xffffu;
+    };
+    // this thread's piece in step i: row `key`, piece c
+    auto key_of = [&](int i) { return (i * 4 + w) * ROWS_AT_ONCE + lane / PER_ROW; };
+    const int c = lane % PER_ROW;
+    auto source = [&](const TC* pool, int j, int key, int page, uint32_t pages_ok) -> const TC* {
+      page = __shfl_sync(0xffffffffu, page, key >> 3);
+      const bool on = j * KEYS + key < most && ((pages_ok >> (key >> 3)) & 1u);
+      return on ? pool + b.entry(page, g_head, j * KEYS + key) * HD + c * (16 / E) : nullptr;
+    };
+    auto begin_side = [&](int j, int page, uint32_t pages_ok) {
       float* side = reinterpret_cast<float*>(base_ptr + L::SIDE_OFF + (j & (SIDE - 1)) * L::SIDE_BYTES);
       if (tid == 0) *reinterpret_cast<uint32_t*>(side + 2 * KEYS) = pages_ok;
+      if (pages_ok != 0xffffu && w == 0 && lane == 0) b.bad();
       if (SCALED) {
-        const int page = __shfl_sync(0xffffffffu, my_page, tid >> 3 & 15);
-        const bool on = j * KEYS + tid < most && (pages_ok >> (tid >> 3) & 1u);
-        const size_t e = on ? entry_of(page, j, tid) : 0;
-        side[tid] = on ? Ksc[e] : 0.f;
+        page = __shfl_sync(0xffffffffu, page, (tid >> 3) & 15);
+        const bool on = j * KEYS + tid < most && ((pages_ok >> (tid >> 3)) & 1u);
+        const size_t e = on ? b.entry(page, g_head, j * KEYS + tid) : 0;
+        side[tid] = on ? Ksc[e] * fabsf(scale_log2) : 0.f;
         side[KEYS + tid] = on ? Vsc[e] : 0.f;
       }
-      // keys, then values: pieces go to their swizzled places; rows that are not there become zeros
-      auto fill = [&](const TC* __restrict__ pool, uint32_t dst) {
-        if constexpr (!SCALED) {
-#pragma unroll
-          for (int i = 0; i < STEPS; ++i) {
-            const int key = (i * 4 + w) * ROWS_AT_ONCE + lane / PER_ROW, c = lane % PER_ROW;
-            const int page = __shfl_sync(0xffffffffu, my_page, key >> 3);
-            const bool on = j * KEYS + key < most && ((pages_ok >> (key >> 3)) & 1u);
-            const TC* src = on ? pool + entry_of(page, j, key) * HD + c * 8 : pool;
-            pf_cp16(dst + piece(key, c), src, on ? 16 : 0);
-          }
-        } else {
-          uint4 v[STEPS];
-#pragma unroll
-          for (int i = 0; i < STEPS; ++i) {
-            const int key = (i * 4 + w) * ROWS_AT_ONCE + lane / PER_ROW, c = lane % PER_ROW;
-            const int page = __shfl_sync(0xffffffffu, my_page, key >> 3);
-            const bool on = j * KEYS + key < most && ((pages_ok >> (key >> 3)) & 1u);
-            v[i] = on ? __ldg(reinterpret_cast<const uint4*>(pool + entry_of(page, j, key) * HD + c * 16)) : make_uint4(0u, 0u, 0u, 0u);
-          }
-#pragma unroll
-          for (int i = 0; i < STEPS; ++i) {
-            const int key = (i * 4 + w) * ROWS_AT_ONCE + lane / PER_ROW, c = lane % PER_ROW;
-            uint32_t o[8];
-            to_bf16(v[i].x, o[0], o[1], TC{});
-            to_bf16(v[i].y, o[2], o[3], TC{});
-            to_bf16(v[i].z, o[4], o[5], TC{});
-            to_bf16(v[i].w, o[6], o[7], TC{});
-            sts16(dst + piece(key, 2 * c), o[0], o[1], o[2], o[3]);
-            sts16(dst + piece(key, 2 * c + 1), o[4], o[5], o[6], o[7]);
-          }
-        }
-      };
-      fill(Kp, kt);
-      if constexpr (!SCALED) pf_commit();
-      if (round > 0) {
-        ok = __all_sync(0xffffffffu, tc::mbar_wait(vempty + 8 * s, (round - 1) & 1, abort_flag, b.status));
-        if (!ok) break;
-      }
-      if constexpr (SCALED) { fence_async(); __syncwarp(); if (lane == 0) arrive(kfull + 8 * s); }
-      fill(Vp, vt);
-      if constexpr (!SCALED) {
-        pf_commit();
-        pf_wait<1>();
-        fence_async();
-        __syncwarp();
-        if (lane == 0) arrive(kfull + 8 * s);
-        pf_wait<0>();
-      }
+      __syncwarp();
+      if (lane == 0) arrive(sidefull + 8 * (j % SIDE));
+    };
+    auto wait_free = [&](uint32_t bar, int j) {
+      return j < STAGES || __all_sync(0xffffffffu, tc::mbar_wait(bar + 8 * (j % STAGES), (j / STAGES - 1) & 1, abort_flag, b.status));
+    };
+    auto announce = [&](uint32_t bar, int j) {                    // plain stores or asynchronous copies that have landed
       fence_async();
       __syncwarp();
-      if (lane == 0) arrive(vfull + 8 * s);
-    }
-    if constexpr (!SCALED) pf_wait<0>();
-  } else if (lane == 0 && n_tiles > 0) {
-    // ---- products
-    constexpr uint32_t id_s = idesc(KEYS, false), id_o = idesc(HD, true);
-    bool ok = tc::mbar_wait(qfull, 0, abort_flag, b.status);
-    auto product_s = [&](int t, int j) {
-      const uint32_t qa = base + L::Q + t * L::TILE, ka = base + L::K + (j % STAGES) * L::TILE;
-#pragma unroll
-      for (int k = 0; k < HD / 16; ++k) {
-        const uint32_t off = (k >> 2) * (128 * 128) + (k & 3) * 32;
-        mma_ss(tmem + t * 128, tc::smem_desc(qa + off), tc::smem_desc(ka + off), id_s, k > 0);
-      }
-      tc::umma_commit(sfull + 8 * t);
+      if (lane == 0) arrive(bar + 8 * (j % STAGES));
     };
-    auto product_o = [&](int t, int j) {
-      const uint32_t va = base + L::V + (j % STAGES) * L::TILE;
-#pragma unroll
-      for (int k = 0; k < KEYS / 16; ++k)
-        mma_ts(tmem + L::O_COL + t * HD, tmem + t * 128 + k * 8, v_desc(va + k * 2048, 128 * 128), id_o, (j > 0 || k > 0) ? 1u : 0u);
-      tc::umma_commit(odone + 8 * t);
-    };
-    if (ok) ok = tc::mbar_wait(kfull, 0, abort_flag, b.status);
-    if (ok) {
-      fence_after();
-      for (int t = 0; t < 2; ++t)
-        if (n_keys[t] > 0) product_s(t, 0);
-      tc::umma_commit(kempty);
-    }
-    for (int j = 0; j < n_tiles && ok; ++j) {
-      const int s = j % STAGES, sn = (j + 1) % STAGES;
-      ok = tc::mbar_wait(vfull + 8 * s, (j / STAGES) & 1, abort_flag, b.status);
-      if (ok && j + 1 < n_tiles) ok = tc::mbar_wait(kfull + 8 * sn, ((j + 1) / STAGES) & 1, abort_flag, b.status);
-      for (int t = 0; t < 2 && ok; ++t) {
-        if (j < n_keys[t]) {
-          ok = tc::mbar_wait(pready + 8 * t, j & 1, abort_flag, b.status);
-          if (!ok) break;
-          fence_after();
-          product_o(t, j);
+    bool ok = true;
+    int page_next = look_up(0);
+    if constexpr (!SCALED) {
+      auto copy = [&](const TC* pool, uint32_t dst, int j, int page, uint32_t pages_ok) {
+#pragma unroll 4
+        for (int i = 0; i < STEPS; ++i) {
+          const int key = key_of(i);
+          const TC* src = source(pool, j, key, page, pages_ok);
+          pf_cp16(dst + piece(key, c), src ? src : pool, src ? 16 : 0);
         }
-        if (j + 1 < n_keys[t]) product_s(t, j + 1);
+        pf_commit();
+      };
+      // whole pages by tensor copies, a page's half (64 elements) per copy, lane i the page of keys [8 i, ...)
+      auto fetch = [&](const CUtensorMap* map, uint32_t dst, uint32_t bar, int j, int page) {
+        const uint32_t full = bar + 8 * (j % STAGES);
+        if (w == 0) {
+          if (lane == 0) tc::mbar_expect_tx(full, L::TILE);
+          __syncwarp();
+          if (lane < 16 && ((lane * 8) & (b.page_len - 1)) == 0) {
+#pragma unroll
+            for (int h = 0; h < HD / 64; ++h)
+              tma_load_3d(dst + h * (128 * 128) + lane * 1024, map, h * 64, 0, page * b.n_kv_heads + g_head, full);
+          }
+        } else if (lane == 0) arrive(full);
+      };
+      for (int j = 0; j < n_tiles; ++j) {
+        const int page = page_next;
+        page_next = look_up(j + 1);
+        const uint32_t pages_ok = exists(j, page);
+        const bool whole = use_maps && (j + 1) * KEYS <= most && pages_ok == 0xffffu;
+        const uint32_t kt = base + L::K + (j % STAGES) * L::TILE, vt = base + L::V + (j % STAGES) * L::TILE;
+        if (!(ok = wait_free(kempty, j))) break;
+        begin_side(j, page, pages_ok);
+        if (whole) fetch(&map_k, kt, kfull, j, page);
+        else copy(Kp, kt, j, page, pages_ok);
+        if (!(ok = wait_free(vempty, j))) break;
+        if (whole) fetch(&map_v, vt, vfull, j, page);
+        else {
+          copy(Vp, vt, j, page, pages_ok);
+          pf_wait<1>();
+          announce(kfull, j);
+          pf_wait<0>();
+          announce(vfull, j);
+        }
       }
-      if (ok) {
-        tc::umma_commit(vempty + 8 * s);
-        if (j + 1 < n_tiles) tc::umma_commit(kempty + 8 * sn);
+      pf_wait<0>();
+      if (!ok && w == 0) {
+        // giving up: tensor copies may still be on their way into this block's memory; wait (bounded) for every stage to come to rest
+        for (int i = 0; i < 2 * STAGES; ++i) {
+          const uint32_t full = (i < STAGES ? kfull : vfull) + 8 * (i % STAGES);
+          const long long t0 = clock64();
+          while (!(tc::mbar_try(full, 0) && tc::mbar_try(full, 1)) && clock64() - t0 < tc::kWaitLimit / 4) {}
+        }
+      }
+    } else {
+      uint4 k[STEPS], v[STEPS];                                   // the next tile's codes, on their way
+      auto request = [&](const TC* pool, uint4 (&x)[STEPS], int j, int page, uint32_t pages_ok) {
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+          const TC* src = source(pool, j, key_of(i), page, pages_ok);
+          x[i] = src ? __ldg(reinterpret_cast<const uint4*>(src)) : make_uint4(0u, 0u, 0u, 0u);
+        }
+      };
+      auto convert = [&](const uint4 (&x)[STEPS], uint32_t dst) {
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+          const int key = key_of(i);
+          uint32_t o[8];
+          to_bf16(x[i].x, o[0], o[1], TC{});
+          to_bf16(x[i].y, o[2], o[3], TC{});
+          to_bf16(x[i].z, o[4], o[5], TC{});
+          to_bf16(x[i].w, o[6], o[7], TC{});
+          sts16(dst + piece(key, 2 * c), o[0], o[1], o[2], o[3]);
+          sts16(dst + piece(key, 2 * c + 1), o[4], o[5], o[6], o[7]);
+        }
+      };
+      int page = page_next;
+      uint32_t pages_ok = exists(0, page);
+      request(Kp, k, 0, page, pages_ok);
+      request(Vp, v, 0, page, pages_ok);
+      page_next = look_up(1);
+      for (int j = 0; j < n_tiles; ++j) {
+        const uint32_t pages_next = exists(j + 1, page_next);
+        if (!(ok = wait_free(kempty, j))) break;
+        begin_side(j, page, pages_ok);
+        convert(k, base + L::K + (j % STAGES) * L::TILE);
+        announce(kfull, j);
+        if (j + 1 < n_tiles) request(Kp, k, j + 1, page_next, pages_next);
+        if (!(ok = wait_free(vempty, j))) break;
+        convert(v, base + L::V + (j % STAGES) * L::TILE);
+        announce(vfull, j);
+        if (j + 1 < n_tiles) request(Vp, v, j + 1, page_next, pages_next);
+        page = page_next;
+        pages_ok = pages_next;
+        page_next = look_up(j + 2);
       }
     }
-    if (!ok) {                                                    // let what has been issued finish before the memory goes
-      tc::umma_commit(drain);
-      const long long t0 = clock64();
-      while (!tc::mbar_try(drain, 0) && clock64() - t0 < tc::kWaitLimit) {}
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PRODUCT_REGS));
+    if (warp == 12 && lane == 0 && n_tiles > 0) {
+      // ---- products
+      constexpr uint32_t id_s = idesc(KEYS, false), id_o = idesc(HD, true);
+      bool ok = tc::mbar_wait(qfull, 0, abort_flag, b.status);
+      auto product_s = [&](int t, int j) {
+        const uint32_t qa = base + L::Q + t * L::TILE, ka = base + L::K + (j % STAGES) * L::TILE;
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k) {
+          const uint32_t off = (k >> 2) * (128 * 128) + (k & 3) * 32;
+          mma_ss(tmem + t * 128, tc::smem_desc(qa + off), tc::smem_desc(ka + off), id_s, k > 0);
+        }
+        tc::umma_commit(sfull + 8 * t);
+      };
+      auto product_o = [&](int t, int j) {
+        const uint32_t va = base + L::V + (j % STAGES) * L::TILE;
+#pragma unroll
+        for (int k = 0; k < KEYS / 16; ++k)
+          mma_ts(tmem + L::O_COL + t * HD, tmem + t * 128 + k * 8, v_desc(va + k * 2048, 128 * 128), id_o, (j > 0 || k > 0) ? 1u : 0u);
+        tc::umma_commit(odone + 8 * t);
+      };
+      if (ok) ok = tc::mbar_wait(kfull, 0, abort_flag, b.status);
+      if (ok) {
+        fence_after();
+        for (int t = 0; t < 2; ++t)
+          if (n_keys[t] > 0) product_s(t, 0);
+        tc::umma_commit(kempty);
+      }
+      for (int j = 0; j < n_tiles && ok; ++j) {
+        const int s = j % STAGES, sn = (j + 1) % STAGES;
+        ok = tc::mbar_wait(vfull + 8 * s, (j / STAGES) & 1, abort_flag, b.status);
+        bool k_there = false;
+        for (int t = 0; t < 2 && ok; ++t) {
+          if (j < n_keys[t]) {
+            ok = tc::mbar_wait(pready + 8 * t, j & 1, abort_flag, b.status);
+            if (!ok) break;
+            fence_after();
+            product_o(t, j);
+          }
+          if (j + 1 < n_keys[t]) {
+            if (!k_there) ok = tc::mbar_wait(kfull + 8 * sn, ((j + 1) / STAGES) & 1, abort_flag, b.status);
+            if (!ok) break;
+            k_there = true;
+            fence_after();
+            product_s(t, j + 1);
+          }
+        }
+        if (ok) {
+          tc::umma_commit(vempty + 8 * s);
+          if (j + 1 < n_tiles) tc::umma_commit(kempty + 8 * sn);
+        }
+      }
+      if (!ok) {                                                  // let what has been issued finish before the memory goes
+        tc::umma_commit(drain);
+        const long long t0 = clock64();
+        while (!tc::mbar_try(drain, 0) && clock64() - t0 < tc::kWaitLimit) {}
+      }
     }
   }
   fence_before();

@@ -9,6 +9,7 @@ struct sd_cache {
   cudaStream_t stream;
   size_t layer_bytes, v_off, ks_off, vs_off;   // K pool, V pool, K scales, V scales: offsets within a layer
   size_t minus_pos, last_row, part_acc, part_ml, counters, status_off, total;
+  sd::EncodeTiledFn encode = nullptr;
   unsigned tile_ready = 0;    // bit per kernel whose shared-memory size has been allowed on this device
   char* layer(int l) const { return arena + (size_t)l * layer_bytes; }
   template <typename T> T* at(size_t off) const { return reinterpret_cast<T*>(arena + off); }
@@ -219,21 +220,37 @@ int attention_tiles(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, fl
   return launched();
 }
 
+// A bf16 pool as [n_pages * n_kv_heads][page_len][HD], boxes of one page by 64 elements (128 bytes, swizzled).
+template <int HD>
+bool pool_map(const sd_cache* c, void* pool, CUtensorMap* out) {
+  const int64_t planes = (int64_t)c->cfg.n_pages * c->cfg.n_kv_heads;
+  if (!c->encode || planes > 0x7fffffff) return false;          // coordinates are 32-bit
+  const cuuint64_t dims[3] = {HD, (cuuint64_t)c->cfg.page_len, (cuuint64_t)planes};
+  const cuuint64_t strides[2] = {HD * 2, (cuuint64_t)c->cfg.page_len * HD * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)c->cfg.page_len, 1}, estr[3] = {1, 1, 1};
+  return c->encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, pool, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <typename TC, int HD>
 int attention_chunks(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale_log2, const sd_heads* out, int rows_from) {
   using L = sd::ac::Layout<HD>;
   constexpr unsigned bit = 1u << (16 + (HD == 128 ? 0 : 1) + 2 * (std::is_same<TC, bf16>::value ? 0 : std::is_same<TC, int8_t>::value ? 1 : 2));
   auto kernel = sd::paged_attn_chunk_kernel<TC, HD>;
   if (!(c->tile_ready & bit)) {
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM) != cudaSuccess) { cudaGetLastError(); return SD_ERR_CUDA; }
+    cudaFuncAttributes attr;                 // the warpgroups redistribute what the block is launched with: it must be that much
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM) != cudaSuccess ||
+        cudaFuncGetAttributes(&attr, kernel) != cudaSuccess || attr.numRegs != sd::ac::LAUNCH_REGS) { cudaGetLastError(); return SD_ERR_CUDA; }
     c->tile_ready |= bit;
   }
   const auto P = pools<TC>(c, l);
+  CUtensorMap mk = {}, mv = {};
+  const int use_maps = std::is_same<TC, bf16>::value && pool_map<HD>(c, P.k, &mk) && pool_map<HD>(c, P.v, &mv);
   const int blocks = (int)(((int64_t)b->max_new * c->group + sd::ac::ROWS - 1) / sd::ac::ROWS);
   const int64_t grid = (int64_t)blocks * c->cfg.n_kv_heads * b->n_seqs;
   if (grid > 0x7fffffff) return SD_ERR_ARG;
   kernel<<<(unsigned)grid, sd::ac::THREADS, L::SMEM, c->stream>>>(
-      view_of(c, b), rows_of(q), rows_of(out), (const TC*)P.k, (const TC*)P.v, (const float*)P.ks, (const float*)P.vs, c->group, scale_log2, wide(q), wide(out),
+      mk, mv, use_maps, view_of(c, b), rows_of(q), rows_of(out), (const TC*)P.k, (const TC*)P.v, (const float*)P.ks, (const float*)P.vs, c->group, scale_log2, wide(q), wide(out),
       blocks, rows_from);
   return launched();
 }
@@ -339,6 +356,11 @@ int sd_cache_create(const sd_cache_config* cfg, void* arena, size_t arena_bytes,
     delete c;
     return SD_ERR_CUDA;
   }
+  void* fn = nullptr;
+  cudaDriverEntryPointQueryResult found;
+  if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) == cudaSuccess && found == cudaDriverEntryPointSuccess)
+    c->encode = reinterpret_cast<sd::EncodeTiledFn>(fn);
+  else cudaGetLastError();                                      // without it keys and values come by plain asynchronous copies
   *out = c;
   return SD_OK;
 }
