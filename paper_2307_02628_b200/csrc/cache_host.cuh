@@ -448,26 +448,31 @@ int sd_sample(sd_handle* h, const float* d_logits, int B, const sd_sampling* s, 
   DeviceGuard guard(device);
   if (!guard.ok) return SD_ERR_CUDA;
   const int vocab = h->cfg.vocab;
-  const int C = vocab <= 4096 ? 1 : 8;
+  // Blocks per row: as many as leave each SM at most one block and each block 6000 logits.  Measured at 50 272 logits, 1, 2, 4, 8
+  // blocks: one row 31, 25, 19, 18 us; 32 rows 35, 29, 24, 28 us; 148 rows 38, 45, 65, 110 us; 64 rows of 8000: 16, 17, 20, 45 us.
+  int C = 8;
+  while (C > 1 && ((int64_t)B * C > h->tc.sm_count || vocab < 6000 * C)) C >>= 1;
   if ((int64_t)B * C > 0x7fffffff) return SD_ERR_ARG;
-  const int part = (vocab + 4 * C - 1) / (4 * C) * 4;          // a multiple of 4: parts keep the row's 16-byte alignment
+  const int part = (vocab + 8 * C - 1) / (8 * C) * 8;          // a multiple of 8: parts keep the row's 16-byte alignment
   int bits = 0;                                                // sums of vocab weights of at most 2^fraction stay below 2^63
   while ((1ll << bits) < vocab) ++bits;
   const int fraction = std::min(52, 63 - bits);
-  const size_t staged = sizeof(sd::sr::Shared) + (size_t)part * 4;
-  const bool in_smem = staged <= (size_t)sd::sr::MAX_SMEM;
-  auto kernel = in_smem ? sd::sample_rows_kernel<true> : sd::sample_rows_kernel<false>;
-  const size_t smem = in_smem ? staged : sizeof(sd::sr::Shared);
-  if (!h->sample_rows_ready) {               // per handle: the attribute belongs to the handle's device
-    if (cudaFuncSetAttribute(sd::sample_rows_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, sd::sr::MAX_SMEM) != cudaSuccess ||
-        cudaFuncSetAttribute(sd::sample_rows_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, sd::sr::MAX_SMEM) != cudaSuccess) {
+  const size_t with_slices = sizeof(sd::sr::Shared) + (size_t)part * 2;
+  const bool slices = with_slices <= (size_t)sd::sr::MAX_SMEM;
+  const size_t smem = slices ? with_slices : sizeof(sd::sr::Shared);
+  auto kernel = C == 1 ? (slices ? sd::sample_rows_kernel<1024, true, true> : sd::sample_rows_kernel<1024, true, false>)
+                       : (slices ? sd::sample_rows_kernel<512, false, true> : sd::sample_rows_kernel<512, false, false>);
+  const unsigned bit = (C == 1 ? 1u : 4u) << (slices ? 0 : 1);
+  if (!(h->sample_rows_ready & bit)) {       // per handle: the attributes belong to the handle's device
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sd::sr::MAX_SMEM) != cudaSuccess ||
+        cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 100) != cudaSuccess) {
       cudaGetLastError();
       return SD_ERR_CUDA;
     }
-    h->sample_rows_ready = true;
+    h->sample_rows_ready |= bit;
   }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(B * C); cfg.blockDim = dim3(sd::sr::THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = h->stream;
+  cfg.gridDim = dim3(B * C); cfg.blockDim = dim3(C == 1 ? 1024 : 512); cfg.dynamicSmemBytes = smem; cfg.stream = h->stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;

@@ -66,7 +66,8 @@ struct sd_handle {
   // ragged batches: left padding per row (host copy; device copy in the arena) and the rows still generating
   std::vector<int> pad, rows;
   bool have_pad = false, have_rows = false;
-  bool prefill_attn_ready = false, sample_ready = false, sample_rows_ready = false;   // large dynamic shared memory enabled for these kernels
+  bool prefill_attn_ready = false, sample_ready = false;   // large dynamic shared memory enabled for these kernels
+  unsigned sample_rows_ready = 0;                          // the same, a bit per form of the kernel
   int n_rows() const { return have_rows ? (int)rows.size() : B; }
   const int* d_pad() const { return have_pad ? at<int>(A.pad) : nullptr; }
   const int* d_rows() const { return have_rows ? at<int>(A.rows) : nullptr; }

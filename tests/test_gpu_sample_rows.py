@@ -84,6 +84,26 @@ def test_equal_and_extreme_logits(vocab):
     dec.close()
 
 
+@pytest.mark.parametrize("vocab", [700, 50272])
+def test_logits_masked_with_the_lowest_value(vocab):
+    low = torch.finfo(torch.float32).min
+    x = torch.randn(6, vocab, generator=torch.Generator().manual_seed(5))
+    x[0] = low                                                  # nothing is left
+    x[1, 1:] = low                                              # one token is
+    x[2, ::2] = low
+    x[3, 10:] = low
+    x[4] = low
+    x[4, 17] = torch.nextafter(torch.tensor(low), torch.tensor(0.0))
+    x[5, 3:] = float("-inf")
+    dec = make(vocab, 6)
+    for u in (0.0, 0.4, 0.9999):
+        for T in (1e-30, 0.7, 3e38):
+            for s in ({}, dict(top_k=torch.full((6,), 3)), dict(top_p=torch.full((6,), 0.6)), dict(min_p=torch.full((6,), 1.0))):
+                check(dec, x, torch.full((6,), u), temperature=torch.full((6,), T), **s)
+    assert dec.status() == 0
+    dec.close()
+
+
 def test_more_equal_elements_than_fit_a_list_next_to_others():
     # dense clusters of nearly equal logits: the search has to cut its slice again, several times
     vocab = 50272
