@@ -116,9 +116,9 @@ def lib() -> C.CDLL:
     L.sd_cache_bytes.argtypes = [C.POINTER(SdCacheConfig), C.POINTER(C.c_size_t)]
     L.sd_cache_create.argtypes = [C.POINTER(SdCacheConfig), vp, C.c_size_t, vp, C.POINTER(vp)]
     L.sd_cache_layer.argtypes = [vp, C.c_int, C.POINTER(vp), C.POINTER(vp), C.POINTER(vp), C.POINTER(vp)]
-    L.sd_cache_append.argtypes = [vp, C.c_int, C.POINTER(SdBatch), C.POINTER(SdHeads), C.POINTER(SdHeads)]
+    L.sd_cache_append.argtypes = [vp, C.c_int, vp, vp, vp]          # structures by address
     L.sd_cache_read.argtypes = L.sd_cache_append.argtypes
-    L.sd_cache_attention.argtypes = [vp, C.c_int, C.POINTER(SdBatch), C.POINTER(SdHeads), C.c_float, C.POINTER(SdHeads)]
+    L.sd_cache_attention.argtypes = [vp, C.c_int, vp, vp, C.c_float, vp]
     L.sd_cache_status.argtypes = [vp, i32p]
     L.sd_cache_destroy.argtypes = [vp]
     L.sd_cache_destroy.restype = None
@@ -179,6 +179,11 @@ def cache_bytes(cfg: SdCacheConfig) -> int:
     return need.value
 
 
+def _raw_stream(index: int) -> int:
+    """The handle of torch's current stream on a device (a plain integer; building a Stream object takes ten times as long)."""
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
 class CacheBatch:
     """The sequences of a call and their new tokens (sd_batch).
 
@@ -197,8 +202,9 @@ class CacheBatch:
         if not pages.device == first.device == length.device:
             raise ValueError("pages, first and length must be on one device")
         self.pages, self.first, self.length, self.n_tokens = pages, first, length, int(n_tokens)
-        self.device = pages.device
+        self.device, self.index = pages.device, pages.device.index
         self.c = SdBatch(pages.data_ptr(), first.data_ptr(), length.data_ptr(), pages.shape[0], pages.shape[1], int(n_tokens), int(max_new), int(max_len))
+        self.ref = C.addressof(self.c)
 
 
 class PagedCache:
@@ -220,6 +226,7 @@ class PagedCache:
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self.stream = stream if stream is not None else torch.cuda.Stream(device=self.device)
+        self._index, self._raw = self.device.index, self.stream.cuda_stream
         self.arena = torch.empty(self.arena_bytes + 256, dtype=torch.uint8, device=self.device)
         self._base = (self.arena.data_ptr() + 255) // 256 * 256 - self.arena.data_ptr()
         self.h = C.c_void_p()
@@ -227,6 +234,11 @@ class PagedCache:
         _check(lib().sd_cache_create(C.byref(self.cfg), self.arena.data_ptr() + self._base, self.arena_bytes,
                                      self.stream.cuda_stream, C.byref(self.h)), "sd_cache_create")
         self._join()
+        L = lib()
+        self._append, self._read, self._attention = L.sd_cache_append, L.sd_cache_read, L.sd_cache_attention
+        self._heads, self._kv_heads, self._head_dim = n_heads, n_kv_heads, head_dim
+        self._tensors = (SdHeads(), SdHeads())
+        self._refs = tuple(C.addressof(t) for t in self._tensors)
 
     def layer(self, layer: int) -> dict:
         """Views of one layer's pools: k, v [n_pages, n_kv_heads, page_len, head_dim], in 8 bits also k_scale, v_scale."""
@@ -248,26 +260,36 @@ class PagedCache:
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, batch: CacheBatch):
         """k, v: the new tokens' keys and values [n_tokens, n_kv_heads, head_dim], fp32, bf16 or fp16, elements of a head adjacent."""
-        n = self.cfg.n_kv_heads
-        self._call("sd_cache_append", layer, batch, self._rows("k", k, n, batch), self._rows("v", v, n, batch))
+        n = self._kv_heads
+        self._rows(0, "k", k, n, batch)
+        self._rows(1, "v", v, n, batch)
+        self._call(self._append, "sd_cache_append", layer, batch)
 
     def read(self, layer: int, batch: CacheBatch, dtype: torch.dtype = torch.float32, k: torch.Tensor | None = None,
              v: torch.Tensor | None = None):
         """The keys and values at the new tokens' places, as (k, v) [n_tokens, n_kv_heads, head_dim] of `dtype`."""
-        shape = (batch.n_tokens, self.cfg.n_kv_heads, self.cfg.head_dim)
-        k = torch.empty(shape, dtype=dtype, device=self.device) if k is None else k
-        v = torch.empty(shape, dtype=dtype, device=self.device) if v is None else v
-        self._call("sd_cache_read", layer, batch, self._rows("k", k, shape[1], batch), self._rows("v", v, shape[1], batch))
+        n = self._kv_heads
+        if k is None:
+            k = torch.empty(batch.n_tokens, n, self._head_dim, dtype=dtype, device=self.device)
+        if v is None:
+            v = torch.empty(batch.n_tokens, n, self._head_dim, dtype=dtype, device=self.device)
+        self._rows(0, "k", k, n, batch)
+        self._rows(1, "v", v, n, batch)
+        self._call(self._read, "sd_cache_read", layer, batch)
         return k, v
 
     def attention(self, layer: int, q: torch.Tensor, batch: CacheBatch, scale: float | None = None, out: torch.Tensor | None = None):
         """Causal attention of the new tokens' queries [n_tokens, n_heads, head_dim] over their sequences; out: like q unless given."""
-        if scale is not None and not (scale == scale and abs(scale) != float("inf") and scale != 0):
+        if scale is None:
+            scale = 0.0                                        # the library's default, head_dim^-1/2
+        elif not (scale == scale and abs(scale) != float("inf") and scale != 0):
             raise ValueError("scale must be a finite number other than 0")
-        n = self.cfg.n_heads
+        n = self._heads
         if out is None:
-            out = torch.empty(batch.n_tokens, n, self.cfg.head_dim, dtype=q.dtype, device=self.device)
-        self._call("sd_cache_attention", layer, batch, self._rows("q", q, n, batch), 0.0 if scale is None else scale, self._rows("out", out, n, batch))
+            out = torch.empty(batch.n_tokens, n, self._head_dim, dtype=q.dtype, device=self.device)
+        self._rows(0, "q", q, n, batch)
+        self._rows(1, "out", out, n, batch)
+        self._call(self._attention, "sd_cache_attention", layer, batch, scale)
         return out
 
     def status(self) -> int:
@@ -290,18 +312,29 @@ class PagedCache:
         except Exception:
             pass
 
-    def _rows(self, name: str, t: torch.Tensor, heads: int, batch: CacheBatch) -> SdHeads:
-        if t.dtype not in _ROW_TYPES or t.device != self.device or batch.device != self.device:
+    # describes a tensor in one of the two structures that a call passes on (they are read during the call only)
+    def _rows(self, which: int, name: str, t: torch.Tensor, heads: int, batch: CacheBatch):
+        code = _ROW_TYPES.get(t.dtype)
+        if code is None or t.get_device() != self._index or batch.index != self._index:
             raise ValueError(f"{name} must be an fp32, bf16 or fp16 tensor on {self.device}, and so must the batch be there")
-        if t.shape != (batch.n_tokens, heads, self.cfg.head_dim) or (t.stride(2) != 1 and t.numel()):
-            raise ValueError(f"{name} must be [{batch.n_tokens}, {heads}, {self.cfg.head_dim}] with adjacent elements, got {tuple(t.shape)} strides {t.stride()}")
-        return SdHeads(t.data_ptr(), t.stride(0), t.stride(1), _ROW_TYPES[t.dtype])
+        if t.shape != (batch.n_tokens, heads, self._head_dim):
+            raise ValueError(f"{name} must be [{batch.n_tokens}, {heads}, {self._head_dim}], got {tuple(t.shape)}")
+        r = self._tensors[which]
+        r.row_stride, r.head_stride, step = t.stride()
+        if step != 1 and t.numel():
+            raise ValueError(f"{name}'s elements of a head must be adjacent, got strides {t.stride()}")
+        r.data = t.data_ptr()
+        r.dtype = code
 
-    def _call(self, name: str, layer: int, batch: CacheBatch, *args):
-        args = [C.byref(a) if isinstance(a, SdHeads) else a for a in args]
-        self._fork()
-        _check(getattr(lib(), name)(self.h, layer, C.byref(batch.c), *args), name)
-        self._join()
+    def _call(self, fn, name: str, layer: int, batch: CacheBatch, *scale):
+        other = _raw_stream(self._index) != self._raw
+        if other:
+            self._fork()
+        code = fn(self.h, layer, batch.ref, self._refs[0], *scale, self._refs[1])
+        if code != SD_OK:
+            raise SdError(code, name)
+        if other:
+            self._join()
 
     # work before the call on the current stream is seen by it, and work after the call sees its results (and reuses its memory)
     def _fork(self):
@@ -465,18 +498,26 @@ class Decoder:
                out: torch.Tensor | None = None) -> torch.Tensor:
         """One token per row with the row's own settings (CUDA tensors [B], fp32, top_k int32; None: off)."""
         B = logits.shape[0]
-        if logits.dtype != torch.float32 or logits.shape != (B, self.shape.vocab) or not logits.is_contiguous() or logits.device != self.device:
-            raise ValueError(f"logits must be a contiguous fp32 [B, {self.shape.vocab}] on {self.device}")
+        index = self.device.index
+        if logits.dtype != torch.float32 or logits.shape != (B, self.shape.vocab) or not logits.is_contiguous() or logits.get_device() != index:
+            raise ValueError(f"logits must be a contiguous fp32 [{B}, {self.shape.vocab}] on {self.device}")
         if out is None:
             out = torch.empty(B, dtype=torch.int32, device=self.device)
-        for name, t, dt in (("uniforms", uniforms, torch.float32), ("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
-                            ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32), ("out", out, torch.int32)):
-            if t is not None and (t.dtype != dt or t.shape != (B,) or not t.is_contiguous() or t.device != self.device):
+        ptr = []
+        for name, t, dt in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
+                            ("min_p", min_p, torch.float32), ("uniforms", uniforms, torch.float32), ("out", out, torch.int32)):
+            if t is None and name not in ("uniforms", "out"):
+                ptr.append(None)
+            elif t.dtype != dt or t.shape != (B,) or not t.is_contiguous() or t.get_device() != index:
                 raise ValueError(f"{name} must be a contiguous {dt} [{B}] on {self.device}")
-        ptr = [None if t is None else t.data_ptr() for t in (temperature, top_k, top_p, min_p)]
-        self._order()
-        _check(lib().sd_sample(self.h, logits.data_ptr(), B, C.byref(SdSampling(*ptr)), uniforms.data_ptr(), out.data_ptr()), "sd_sample")
-        self._after()
+            else:
+                ptr.append(t.data_ptr())
+        other = _raw_stream(index) != self.stream.cuda_stream
+        if other:
+            self._order()
+        _check(lib().sd_sample(self.h, logits.data_ptr(), B, SdSampling(*ptr[:4]), ptr[4], ptr[5]), "sd_sample")
+        if other:
+            self._after()
         return out
 
     def extend(self, cache: PagedCache, batch: CacheBatch, tokens: torch.Tensor, n_active: int | None = None, warmup: int = 0,

@@ -9,17 +9,16 @@
 // near fp32 at no cost: with 8 rows or fewer the other half of the tile would be empty.  8-bit codes are fp16 numbers exactly.
 // bf16 caches multiply in bf16.
 //
-// Each of the four warps walks its own 16-key tiles with a ring of its own in shared memory, filled by 16-byte asynchronous copies: no
+// Each of the block's NW warps walks its own 16-key tiles with a ring of its own in shared memory, filled by 16-byte asynchronous copies: no
 // block-wide synchronisation until the end, and every warp keeps STAGES - 1 tiles in flight.  The fragments are read in the order
 // in which the bytes lie: the sum over the head's elements may run in any order, so a thread takes whole 16-byte pieces of a key
 // and the queries are laid out to match; for the values, a thread takes a run of elements of four keys, and the
 // accumulator's columns stand for the elements that order implies.  Pieces are XOR-swizzled against bank conflicts.
 //
-// 8-bit scales.  A key's scale multiplies its score.  A value's scale joins its weight: weights are kept relative to the
-// largest weight-times-scale seen (running maximum mv), the sum of weights relative to the largest weight (m), so scales of
-// any size keep the weights inside fp16.  Both maxima are only raised when they would be passed by 2^8, which keeps most tiles
-// free of rescaling; in 8 bits a weight is 2^7 times its ratio to the maximum, so that with that slack it stays below fp16's
-// 65504 and a weight far below the largest keeps bits (the grid of fp16 ends at 2^-24).
+// 8-bit scales.  A key's scale multiplies its score.  A value's scale joins its weight, relative to a power of two that no scale
+// seen so far exceeds (ve) and times 2^7.  That power and the running maximum (m) are raised only when a scale passes the one or a
+// score the other by 2^8, so most tiles need no reduction across lanes and no rescaling: weights stay below 2^15, inside fp16, whose
+// grid ends at 2^-24: a weight is exact to 2^-32 of the largest |value| of the sequence.
 #pragma once
 #include "attn_prefill.cuh"
 #include "paged.cuh"
@@ -27,9 +26,9 @@
 namespace sd {
 namespace ap {
 
-constexpr int NW = 4, THREADS = 128, ROWS = 8, KEYS = 16;
+constexpr int ROWS = 8, KEYS = 16;
 
-template <typename TC, int HD> struct Shape {
+template <typename TC, int HD, int NW> struct Shape {
   static constexpr bool SCALED = CacheType<TC>::TOP > 0.f;
   static constexpr int E = sizeof(TC);
   static constexpr int ROW = HD * E;                         // bytes of a key
@@ -85,10 +84,15 @@ template <int B> __device__ __forceinline__ void lds(uint32_t addr, uint32_t (&r
   else if constexpr (B == 8) asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(addr));
   else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(r[0]) : "r"(addr));
 }
-__device__ __forceinline__ float lds_f32(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr));
+__device__ __forceinline__ float2 lds_f32x2(uint32_t addr) {
+  float2 v;
+  asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr));
   return v;
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
 // N consecutive elements of a row, any type; vec: 16-byte accesses are allowed
@@ -114,13 +118,14 @@ template <int N> __device__ __forceinline__ void load_run(const Rows& t, long lo
 // grid (tiles_per_seq * n_kv_heads * n_seqs, splits).  Sequences with rows_below query rows or more are another kernel's.  Split z takes keys [z * chunk, (z + 1) * chunk), the last one all that follow.
 // Several splits leave partial results (accumulator, maximum, sum) of the rows they see and the block that arrives last at a
 // unit's counter adds them in split order, so the result does not depend on who came when.
-template <typename TC, int HD>
-__global__ void __launch_bounds__(ap::THREADS)
+template <typename TC, int HD, int NW>
+__global__ void __launch_bounds__(32 * NW)
 paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC* __restrict__ Kp, const TC* __restrict__ Vp,
                        const float* __restrict__ Ksc, const float* __restrict__ Vsc, int group, float scale_log2, bool q_vec,
                        int tiles_per_seq, int rows_below, int chunk, float* part_acc, float* part_ml, int* __restrict__ counters) {
   using namespace ap;
-  using S = Shape<TC, HD>;
+  using S = Shape<TC, HD, NW>;
+  constexpr int THREADS = 32 * NW;
   extern __shared__ __align__(128) unsigned char ap_smem[];
   __shared__ int sm_last;
 
@@ -151,6 +156,86 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
   const int row_last = (int)max(min(pos_first + token, (long long)len - 1), -1ll);         // -1: none
   const int all_see = (int)max(min(pos_first + (tile * ROWS) / group, (long long)len - 1), -1ll);   // the last key that every row sees
 
+  float acc[S::NT][4];
+#pragma unroll
+  for (int n = 0; n < S::NT; ++n) { acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f; }
+  float m = -INFINITY, l = 0.f;                    // the maximum is a row's, the sum is this thread's share
+  float ve = 0.f, inv_ve = 0.f;                    // 2^7 over it; 0: no value has had a scale yet
+
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(ap_smem) + warp * (S::STAGES * S::STAGE);
+  const int tile0 = k0 / KEYS + warp, n_tiles = (k1 + KEYS - 1) / KEYS;      // this warp's tiles: tile0, tile0 + NW, ...
+  const int* table = b.pages + (size_t)seq * b.pages_per_seq;
+  uint32_t valid = 0u;                             // two bits per stage: the halves of the tile whose page exists
+  int next_page[2] = {-1, -1};                     // table entries of the tile to be issued next (one page holds it unless pages have 8 keys)
+  const bool split_tile = b.page_len < KEYS;
+  auto look_up = [&](int kt) {
+    const int key = kt * KEYS;
+    next_page[0] = key < k1 ? table[key >> b.page_shift] : 0;
+    next_page[1] = !split_tile ? next_page[0] : key + 8 < k1 ? table[(key + 8) >> b.page_shift] : 0;
+  };
+  // this lane's piece of the first keys of a tile: the others follow at fixed distances
+  const int lane_key = lane / S::PIECES, lane_piece = lane % S::PIECES;
+  constexpr int STEPS = KEYS * S::PIECES / 32, STEP_KEYS = 32 / S::PIECES;
+  static_assert(KEYS * S::PIECES % 32 == 0, "whole warps of copies");
+  auto issue = [&](int kt, int stage) {
+    const uint32_t dst = ring + stage * S::STAGE;
+    const int key0 = kt * KEYS;
+    if (!split_tile && key0 + KEYS <= k1 && (unsigned)next_page[0] < (unsigned)b.n_pages) {
+      // a whole tile inside one page
+      const size_t e = b.entry(next_page[0], g_head, key0);
+      const TC* ks = Kp + e * HD + lane * (16 / S::E);
+      const TC* vs = Vp + e * HD + lane * (16 / S::E);
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) {
+        const int key = lane_key + i * STEP_KEYS;
+        const uint32_t at = dst + key * S::ROW + ((lane_piece ^ (swz(key) & S::SWZ)) << 4);
+        pf_cp16(at, ks + i * 32 * (16 / S::E), 16);
+        pf_cp16(at + KEYS * S::ROW, vs + i * 32 * (16 / S::E), 16);
+      }
+      if constexpr (S::SCALED) {
+        if (lane < 8) pf_cp16(dst + 2 * KEYS * S::ROW + lane * 16, (lane < 4 ? Ksc : Vsc) + e + (lane & 3) * 4, 16);
+      }
+      valid |= 3u << (2 * stage);
+      return;
+    }
+    size_t e[2];
+    uint32_t ok = 0u;
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      const int key = key0 + 8 * hf;
+      const bool there = (unsigned)next_page[hf] < (unsigned)b.n_pages;
+      if (!there && key < k1 && lane == 0) b.bad();
+      e[hf] = there ? b.entry(next_page[hf], g_head, key) : 0;
+      ok |= there ? 1u << hf : 0u;
+    }
+    valid = (valid & ~(3u << (2 * stage))) | (ok << (2 * stage));
+#pragma unroll 1
+    for (int i = 0; i < STEPS; ++i) {
+      const int key = lane_key + i * STEP_KEYS, hf = key >> 3;
+      const bool on = key0 + key < k1 && ((ok >> hf) & 1u);                  // off: zeros, nothing is read
+      const size_t src = on ? ((hf ? e[1] : e[0]) + (key & 7)) * HD + lane_piece * (16 / S::E) : 0;
+      const uint32_t at = dst + key * S::ROW + ((lane_piece ^ (swz(key) & S::SWZ)) << 4);
+      pf_cp16(at, Kp + src, on ? 16 : 0);
+      pf_cp16(at + KEYS * S::ROW, Vp + src, on ? 16 : 0);
+    }
+    if constexpr (S::SCALED) {
+      if (lane < 8) {                              // 16 scales of each: four pieces of four
+        const int key = (lane & 3) * 4, hf = key >> 3;
+        const bool on = key0 + key < k1 && ((ok >> hf) & 1u);
+        const float* src = (lane < 4 ? Ksc : Vsc) + (on ? (hf ? e[1] : e[0]) + (key & 7) : 0);
+        pf_cp16(dst + 2 * KEYS * S::ROW + lane * 16, src, on ? 16 : 0);
+      }
+    }
+  };
+
+  look_up(tile0);
+#pragma unroll
+  for (int s = 0; s < S::STAGES - 1; ++s) {
+    const int kt = tile0 + s * NW;
+    if (kt < n_tiles) { issue(kt, s); look_up(kt + NW); }
+    pf_commit();
+  }
+  // the query row, while the first keys are on their way
   uint32_t qf[S::KS][4];
   float row_scale = scale_log2;
   {
@@ -180,63 +265,6 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
     }
   }
 
-  float acc[S::NT][4];
-#pragma unroll
-  for (int n = 0; n < S::NT; ++n) { acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f; }
-  float m = -INFINITY, mv = -INFINITY, l = 0.f;    // maxima are a row's, the sum is this thread's share
-
-  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(ap_smem) + warp * (S::STAGES * S::STAGE);
-  const int tile0 = k0 / KEYS + warp, n_tiles = (k1 + KEYS - 1) / KEYS;      // this warp's tiles: tile0, tile0 + NW, ...
-  const int* table = b.pages + (size_t)seq * b.pages_per_seq;
-  uint32_t valid = 0u;                             // two bits per stage: the halves of the tile whose page exists
-  int next_page[2] = {-1, -1};                     // table entries of the tile to be issued next
-  auto look_up = [&](int kt) {
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      const int key = kt * KEYS + 8 * hf;
-      next_page[hf] = key < k1 ? table[key >> b.page_shift] : 0;
-    }
-  };
-  auto issue = [&](int kt, int stage) {
-    const uint32_t dst = ring + stage * S::STAGE;
-    size_t e[2];
-    uint32_t ok = 0u;
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      const int key = kt * KEYS + 8 * hf;
-      const bool there = (unsigned)next_page[hf] < (unsigned)b.n_pages;
-      if (!there && key < k1 && lane == 0) b.bad();
-      e[hf] = there ? b.entry(next_page[hf], g_head, key) : 0;
-      ok |= there ? 1u << hf : 0u;
-    }
-    valid = (valid & ~(3u << (2 * stage))) | (ok << (2 * stage));
-#pragma unroll
-    for (int i = 0; i < KEYS * S::PIECES / 32; ++i) {
-      const int c = i * 32 + lane, key = c / S::PIECES, piece = c % S::PIECES, hf = key >> 3;
-      const bool on = kt * KEYS + key < k1 && ((ok >> hf) & 1u);             // off: zeros, nothing is read
-      const size_t src = on ? (e[hf] + (key & 7)) * HD + piece * (16 / S::E) : 0;
-      const uint32_t at = dst + key * S::ROW + ((piece ^ (swz(key) & S::SWZ)) << 4);
-      pf_cp16(at, Kp + src, on ? 16 : 0);
-      pf_cp16(at + KEYS * S::ROW, Vp + src, on ? 16 : 0);
-    }
-    if constexpr (S::SCALED) {
-      if (lane < 8) {                              // 16 scales of each: four pieces of four
-        const int key = (lane & 3) * 4, hf = key >> 3;
-        const bool on = kt * KEYS + key < k1 && ((ok >> hf) & 1u);
-        const float* src = (lane < 4 ? Ksc : Vsc) + (on ? e[hf] + (key & 7) : 0);
-        pf_cp16(dst + 2 * KEYS * S::ROW + lane * 16, src, on ? 16 : 0);
-      }
-    }
-  };
-  static_assert(KEYS * S::PIECES % 32 == 0, "whole warps of copies");
-
-  look_up(tile0);
-#pragma unroll
-  for (int s = 0; s < S::STAGES - 1; ++s) {
-    const int kt = tile0 + s * NW;
-    if (kt < n_tiles) { issue(kt, s); look_up(kt + NW); }
-    pf_commit();
-  }
   int stage = 0, fill = S::STAGES - 1;
   for (int kt = tile0; kt < n_tiles; kt += NW) {
     {
@@ -272,55 +300,84 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
         }
       }
     }
-    float sc[2][2], sv[2][2];
-    const uint32_t ok = valid >> (2 * stage);
-    const bool edge = kt * KEYS + KEYS - 1 > all_see || kt * KEYS + KEYS > k1 || (ok & 3u) != 3u;
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int key = n * 8 + 2 * t + i;
-        float v = (s[n][i] + s[n][2 + i]) * row_scale, lv = 0.f;
-        if constexpr (S::SCALED) {
-          v *= lds_f32(sc_base + key * 4);
-          lv = __log2f(lds_f32(sc_base + KEYS * 4 + key * 4));
-        }
-        const int at = kt * KEYS + key;
-        const bool seen = !edge || (at <= row_last && at < k1 && ((ok >> n) & 1u));
-        sc[n][i] = seen ? v : -INFINITY;
-        sv[n][i] = seen ? v + lv : -INFINITY;
-      }
-    float mx = fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[1][0], sc[1][1]));
-    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-    float mxv = mx;
-    if constexpr (S::SCALED) {
-      mxv = fmaxf(fmaxf(sv[0][0], sv[0][1]), fmaxf(sv[1][0], sv[1][1]));
-      mxv = fmaxf(mxv, __shfl_xor_sync(0xffffffffu, mxv, 1));
-      mxv = fmaxf(mxv, __shfl_xor_sync(0xffffffffu, mxv, 2));
-    }
-    if (__any_sync(0xffffffffu, mx > m + 8.f || mxv > mv + 8.f)) {
-      const float m_new = fmaxf(m, mx);
-      l *= exp2_safe(m, m_new);
-      m = m_new;
-      const float mv_new = fmaxf(mv, mxv), a = exp2_safe(mv, mv_new);
-      mv = mv_new;
-#pragma unroll
-      for (int n = 0; n < S::NT; ++n) { acc[n][0] *= a; acc[n][1] *= a; acc[n][2] *= a; acc[n][3] *= a; }
-    }
-    // weights: the sum's, and the ones that multiply the values.  A row that has seen nothing has m = -inf and only masked scores.
-    const float mb = m == -INFINITY ? 0.f : m, mvb = mv == -INFINITY ? 0.f : mv;
-    uint32_t pf[4];
-    float p[2][2];
+    // this thread's four: keys n * 8 + 2 t + {0, 1}
+    float sc[2][2], vsc[2][2];
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
+      sc[n][0] = s[n][0] + s[n][2];
+      sc[n][1] = s[n][1] + s[n][3];
+      if constexpr (S::SCALED) {
+        const float2 k = lds_f32x2(sc_base + (n * 8 + 2 * t) * 4), v = lds_f32x2(sc_base + (KEYS + n * 8 + 2 * t) * 4);
+        sc[n][0] *= k.x; sc[n][1] *= k.y;
+        vsc[n][0] = v.x; vsc[n][1] = v.y;
+      }
+    }
+    const uint32_t ok = valid >> (2 * stage);
+    uint32_t hidden = 0u;                           // of the four: keys that the row does not see
+    if (kt * KEYS + KEYS - 1 > all_see || kt * KEYS + KEYS > k1 || (ok & 3u) != 3u) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int at = kt * KEYS + n * 8 + 2 * t + i;
+          const bool there = at < k1 && ((ok >> n) & 1u);
+          if (!there || at > row_last) hidden |= 1u << (2 * n + i);
+          if (!there) vsc[n][i] = 0.f;              // past the end or on a page that does not exist: it may be anything
+        }
+    }
+    float mb = m == -INFINITY ? 0.f : m;
+    float x[2][2];                                  // scores relative to the maximum, base 2
+    auto relative = [&] {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          x[n][i] = fmaf(sc[n][i], row_scale, -mb);
+          if (hidden && ((hidden >> (2 * n + i)) & 1u)) x[n][i] = -INFINITY;
+        }
+    };
+    relative();
+    const float mx = fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[1][0], x[1][1]));
+    bool raise = mx > 8.f || m == -INFINITY;
+    if constexpr (S::SCALED) raise = raise || fmaxf(fmaxf(vsc[0][0], vsc[0][1]), fmaxf(vsc[1][0], vsc[1][1])) > ve;
+    if (__any_sync(0xffffffffu, raise)) {
+      float top = mx;
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const float m_new = fmaxf(m, top + mb);
+      float a = exp2_safe(m, m_new);
+      l *= a;
+      m = m_new;
+      if constexpr (S::SCALED) {
+        float v = fmaxf(fmaxf(vsc[0][0], vsc[0][1]), fmaxf(vsc[1][0], vsc[1][1]));
+        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
+        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));       // the four lanes of a row see all 16 keys
+        if (v > ve) {
+          // the next power of two, kept where 2^7 over it is a normal number too
+          const int e = min(max((int)((__float_as_uint(v) >> 23) & 0xff) + 1, 14), 254);
+          const float ve_new = __uint_as_float((uint32_t)e << 23);
+          a *= ve / ve_new;
+          ve = ve_new;
+          inv_ve = __uint_as_float((uint32_t)(254 - e + 7) << 23);
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < S::NT; ++n) { acc[n][0] *= a; acc[n][1] *= a; acc[n][2] *= a; acc[n][3] *= a; }
+      mb = m == -INFINITY ? 0.f : m;
+      relative();
+    }
+    // weights: the sum's, and the ones that multiply the values
+    uint32_t pf[4];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      float p[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        p[n][i] = exp2f(sc[n][i] - mb);
-        l += p[n][i];
-        if constexpr (S::SCALED) p[n][i] = exp2f(sv[n][i] - mvb + 7.f);
+        p[i] = ex2(x[n][i]);
+        l += p[i];
+        if constexpr (S::SCALED) p[i] *= vsc[n][i] * inv_ve;
       }
-      split(p[n][0], p[n][1], pf[2 * n], pf[2 * n + 1], TC{});
+      split(p[0], p[1], pf[2 * n], pf[2 * n + 1], TC{});
     }
 
     // values
@@ -335,11 +392,9 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
       }
 #pragma unroll
       for (int k = 0; k < B / 4; ++k) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i][k] = flip(w[i][k], TC{});
         // bytes of keys 0 and 1 (2 and 3) side by side, element by element
-        const uint32_t a0 = __byte_perm(w[0][k], w[1][k], 0x5140), a1 = __byte_perm(w[0][k], w[1][k], 0x7362);
-        const uint32_t b0 = __byte_perm(w[2][k], w[3][k], 0x5140), b1 = __byte_perm(w[2][k], w[3][k], 0x7362);
+        const uint32_t a0 = flip(__byte_perm(w[0][k], w[1][k], 0x5140), TC{}), a1 = flip(__byte_perm(w[0][k], w[1][k], 0x7362), TC{});
+        const uint32_t b0 = flip(__byte_perm(w[2][k], w[3][k], 0x5140), TC{}), b1 = flip(__byte_perm(w[2][k], w[3][k], 0x7362), TC{});
         mma(acc[4 * k + 0], pf, lower(a0, TC{}), lower(b0, TC{}), TC{});
         mma(acc[4 * k + 1], pf, upper(a0, TC{}), upper(b0, TC{}), TC{});
         mma(acc[4 * k + 2], pf, lower(a1, TC{}), lower(b1, TC{}), TC{});
@@ -360,10 +415,10 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
   }
   pf_wait<0>();
 
-  // this warp's rows: accumulators in units of 2^m, sums over the quad
+  // this warp's rows: accumulators and sums in units of 2^m, sums over the quad
   l += __shfl_xor_sync(0xffffffffu, l, 1);
   l += __shfl_xor_sync(0xffffffffu, l, 2);
-  const float back = S::SCALED ? (mv == -INFINITY ? 0.f : exp2f(mv - m - 7.f)) : 1.f;
+  const float back = S::SCALED ? ve * 0.0078125f : 1.f;                       // the unit of the values' weights
   __syncthreads();                                                            // every warp is done with its ring
   float* sm_acc = reinterpret_cast<float*>(ap_smem);                          // [NW][ROWS][HD]
   float* sm_m = sm_acc + NW * ROWS * HD;                                      // [NW][ROWS]
