@@ -54,6 +54,15 @@ __host__ __device__ constexpr uint32_t idesc(int n, bool b_mn) {
 __device__ __forceinline__ uint64_t v_desc(uint32_t addr, uint32_t lead) {
   return (uint64_t)((addr >> 4) & 0x3FFF) | ((uint64_t)(lead >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
+// One lane of a warp, chosen so that the compiler knows it to be one: what it issues takes its operands from uniform registers, and
+// a product goes out every 64 clocks (128 x 128 x 16).  Under a branch on the lane's number, with operands that the compiler cannot
+// show to be uniform, it took 130.
+__device__ __forceinline__ bool elect() {
+  uint32_t p;
+  asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n selp.b32 %0, 1, 0, q;\n}\n" : "=r"(p));
+  return p != 0;
+}
+template <typename T> __device__ __forceinline__ T uniform(T v) { return __shfl_sync(0xffffffffu, v, 0); }
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t acc) { tc::umma(d, a, b, id, acc); }
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t acc) {
   asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
@@ -161,7 +170,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   }
   const int n_tiles = max(n_keys[0], n_keys[1]);
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
   const uint32_t raw = (uint32_t)__cvta_generic_to_shared(ac_smem), base = (raw + 1023u) & ~1023u;
   unsigned char* base_ptr = ac_smem + (base - raw);
   const uint32_t bar0 = (uint32_t)__cvta_generic_to_shared(bars);
@@ -203,13 +212,23 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     if (n_rows[t] > 0) {
       const long long at = (long long)(f0 + token) * q.row_stride + head * q.head_stride;
       const uint32_t dst = base + L::Q + t * L::TILE;
-#pragma unroll 4
-      for (int c = 0; c < HD / 8; ++c) {
-        float x[8];
-        ap::load_run<8>(q, at + c * 8, q_vec, x);
+      if (q_vec && q.dtype == DT_BF16) {
+        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(q.data) + at);
+        const uint32_t turn = scale_log2 < 0.f ? 0x80008000u : 0u;
+        uint4 x[HD / 8];                                          // all on their way together
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] *= sign;
-        sts16(dst + piece(r, c), pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+        for (int c = 0; c < HD / 8; ++c) x[c] = __ldg(src + c);
+#pragma unroll
+        for (int c = 0; c < HD / 8; ++c) sts16(dst + piece(r, c), x[c].x ^ turn, x[c].y ^ turn, x[c].z ^ turn, x[c].w ^ turn);
+      } else {
+#pragma unroll 8
+        for (int c = 0; c < HD / 8; ++c) {
+          float x[8];
+          ap::load_run<8>(q, at + c * 8, q_vec, x);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] *= sign;
+          sts16(dst + piece(r, c), pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+        }
       }
     }
     fence_async();
@@ -490,46 +509,64 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PRODUCT_REGS));
-    if (warp == 12 && lane == 0 && n_tiles > 0) {
+    if (warp == 12 && n_tiles > 0) {
       // ---- products
       constexpr uint32_t id_s = idesc(KEYS, false), id_o = idesc(HD, true);
-      bool ok = tc::mbar_wait(qfull, 0, abort_flag, b.status);
+      const int tiles = uniform(n_tiles), keys[2] = {uniform(n_keys[0]), uniform(n_keys[1])};
+      const uint32_t tm = uniform(tmem), at = uniform(base), bar = uniform(bar0);
+      auto wait = [&](uint32_t which, int phase) { return __all_sync(0xffffffffu, tc::mbar_wait(bar + (which - bar0), phase & 1, abort_flag, b.status)) != 0; };
+      // each of these announces its completion, and that of everything before it, on the barriers named
       auto product_s = [&](int t, int j) {
-        const uint32_t qa = base + L::Q + t * L::TILE, ka = base + L::K + (j % STAGES) * L::TILE;
+        const uint64_t qa = tc::smem_desc(at + L::Q + t * L::TILE), ka = tc::smem_desc(at + L::K + (j % STAGES) * L::TILE);
+        if (elect()) {
 #pragma unroll
-        for (int k = 0; k < HD / 16; ++k) {
-          const uint32_t off = (k >> 2) * (128 * 128) + (k & 3) * 32;
-          mma_ss(tmem + t * 128, tc::smem_desc(qa + off), tc::smem_desc(ka + off), id_s, k > 0);
+          for (int k = 0; k < HD / 16; ++k) {                     // descriptors count 16-byte units
+            const uint32_t off = ((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4;
+            mma_ss(tm + t * 128, qa + off, ka + off, id_s, k > 0);
+          }
+          tc::umma_commit(bar + (sfull - bar0) + 8 * t);
         }
-        tc::umma_commit(sfull + 8 * t);
+        __syncwarp();
       };
       auto product_o = [&](int t, int j) {
-        const uint32_t va = base + L::V + (j % STAGES) * L::TILE;
+        const uint64_t va = v_desc(at + L::V + (j % STAGES) * L::TILE, 128 * 128);
+        const uint32_t first = j > 0;
+        if (elect()) {
 #pragma unroll
-        for (int k = 0; k < KEYS / 16; ++k)
-          mma_ts(tmem + L::O_COL + t * HD, tmem + t * 128 + k * 8, v_desc(va + k * 2048, 128 * 128), id_o, (j > 0 || k > 0) ? 1u : 0u);
-        tc::umma_commit(odone + 8 * t);
+          for (int k = 0; k < KEYS / 16; ++k)
+            mma_ts(tm + L::O_COL + t * HD, tm + t * 128 + k * 8, va + k * (2048 >> 4), id_o, k > 0 ? 1u : first);
+          tc::umma_commit(bar + (odone - bar0) + 8 * t);
+        }
+        __syncwarp();
       };
-      if (ok) ok = tc::mbar_wait(kfull, 0, abort_flag, b.status);
+      auto announce = [&](uint32_t which) {
+        if (elect()) tc::umma_commit(bar + (which - bar0));
+        __syncwarp();
+      };
+      bool ok = wait(qfull, 0);
+      if (ok) ok = wait(kfull, 0);
       if (ok) {
         fence_after();
+#pragma unroll
         for (int t = 0; t < 2; ++t)
-          if (n_keys[t] > 0) product_s(t, 0);
-        tc::umma_commit(kempty);
+          if (keys[t] > 0) product_s(t, 0);
+        announce(kempty);
       }
-      for (int j = 0; j < n_tiles && ok; ++j) {
+      for (int j = 0; j < tiles && ok; ++j) {
         const int s = j % STAGES, sn = (j + 1) % STAGES;
-        ok = tc::mbar_wait(vfull + 8 * s, (j / STAGES) & 1, abort_flag, b.status);
+        ok = wait(vfull + 8 * s, j / STAGES);
         bool k_there = false;
-        for (int t = 0; t < 2 && ok; ++t) {
-          if (j < n_keys[t]) {
-            ok = tc::mbar_wait(pready + 8 * t, j & 1, abort_flag, b.status);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          if (!ok) break;
+          if (j < keys[t]) {
+            ok = wait(pready + 8 * t, j);
             if (!ok) break;
             fence_after();
             product_o(t, j);
           }
-          if (j + 1 < n_keys[t]) {
-            if (!k_there) ok = tc::mbar_wait(kfull + 8 * sn, ((j + 1) / STAGES) & 1, abort_flag, b.status);
+          if (j + 1 < keys[t]) {
+            if (!k_there) ok = wait(kfull + 8 * sn, (j + 1) / STAGES);
             if (!ok) break;
             k_there = true;
             fence_after();
@@ -537,12 +574,12 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
           }
         }
         if (ok) {
-          tc::umma_commit(vempty + 8 * s);
-          if (j + 1 < n_tiles) tc::umma_commit(kempty + 8 * sn);
+          announce(vempty + 8 * s);
+          if (j + 1 < tiles) announce(kempty + 8 * sn);
         }
       }
       if (!ok) {                                                  // let what has been issued finish before the memory goes
-        tc::umma_commit(drain);
+        announce(drain);
         const long long t0 = clock64();
         while (!tc::mbar_try(drain, 0) && clock64() - t0 < tc::kWaitLimit) {}
       }
