@@ -1,13 +1,15 @@
 // Attention of chunks of new tokens over a paged cache in bf16 or 8 bits, on the fifth-generation tensor cores.
 //
 // One block per (sequence, key head, 256 query rows); a query row is a (token, head of the group) pair, so grouped heads share
-// the keys they read.  The 256 rows are two tiles of 128 that take turns: while one tile's softmax runs on the CUDA cores, the
-// tensor core works on the other's products.  For every 128 keys and each tile t:
-//     S_t = Q_t K^T        (both operands in shared memory, result in tensor memory)
-//     P_t = 2^(S_t - m)    (one thread per row: maximum, exponentials, sum; P_t in bf16 over S_t's own columns)
-//     O_t += P_t V         (P_t from tensor memory, V from shared memory as it lies: keys are the product's inner axis)
-// Tensor memory holds S_0, S_1 (128 columns each) and O_0, O_1 (HD columns each).  The products of one block are issued by one
-// thread and execute in order, so S_t of the next keys may overwrite P_t as soon as its product is issued.
+// the keys they read.  The 256 rows are two tiles of 128.  Keys come in tiles of 128; for every half i of one (64 keys) and each tile t:
+//     S_t,i = Q_t K_i^T    (both operands in shared memory, result in tensor memory)
+//     P_t,i = 2^(S - m)    (one thread per row: maximum, exponentials, sum; P in bf16 over S's own columns)
+//     O_t += P_t,i V_i     (P from tensor memory, V from shared memory as it lies: keys are the product's inner axis)
+// Tensor memory holds for each tile S of two halves (64 columns each) and O (HD columns).  S of half i + 2 takes the columns of half i
+// once the product that reads P there has completed, so the scores of the next half are there when a softmax is done with one, and the
+// tensor core works through both tiles' softmax.  (Scores of 128 keys at a time leave no columns for a second set: every
+// softmax then waited for its two products, 1500 of 3700 clocks.)  The order of issue, PV_0(i) S_1(i+1) PV_1(i) S_0(i+2), keeps a product of
+// the other tile between a PV and the S that waits for it.
 //
 // Operands are bf16: queries and weights are rounded once to 8 bits of significand, codes of 8-bit caches are bf16 numbers
 // exactly.  A result in 16 bits keeps no more; results wanted in fp32 go to the kernel for few rows.  A key's scale (8-bit
@@ -16,8 +18,8 @@
 // The running maximum is raised only when it would be passed by 2^8 (weights then reach 256, well inside bf16 and the fp32
 // sums): O_t is rescaled in tensor memory in the first tiles and hardly ever after.
 //
-// What bounds it: 2 x 128 x 128 weights take 2048 clocks on the unit that computes exponentials, and 2 x 2 products take 2048 clocks
-// (HD = 128) of the tensor core.
+// What bounds it: for 128 keys the 2 x 128 x 128 weights take 2048 clocks on the unit that computes exponentials, and the products
+// 2 x (768 + 512) clocks of the tensor core at HD = 128 (64 x 128 x 16 reads its operands for 48 clocks, not 32).
 //
 // Warps: 0-3 and 4-7 softmax of tile 0 and 1 (one thread per row, which is a lane of tensor memory), 8-11 loaders (page
 // look-up, copies into the swizzled layout the tensor core reads, conversion of codes), 12 issues the products.
@@ -29,12 +31,13 @@
 namespace sd {
 namespace ac {
 
-constexpr int THREADS = 512, ROWS = 256, KEYS = 128, TILE_ROWS = 128, STAGES = 2, SIDE = 4;
+constexpr int THREADS = 512, ROWS = 256, KEYS = 128, TILE_ROWS = 128, STAGES = 2, SIDE = 4, HALF = 64;
 constexpr float SLACK = 8.f;
 // Registers per thread of the softmax, the loader and the product warpgroups; the block is launched with 128 for each of its
-// 512 threads, and the shares add up to no more: 2 x 128 x 184 + 128 x 104 + 128 x 40 = 65 536.
-constexpr int LAUNCH_REGS = 128, SOFTMAX_REGS = 184, LOADER_REGS = 104, PRODUCT_REGS = 40;
+// 512 threads, and the shares add up to no more: 2 x 128 x 168 + 128 x 120 + 128 x 40 = 63 488.
+constexpr int LAUNCH_REGS = 128, SOFTMAX_REGS = 168, LOADER_REGS = 120, PRODUCT_REGS = 40;
 static_assert(2 * 128 * SOFTMAX_REGS + 128 * LOADER_REGS + 128 * PRODUCT_REGS <= THREADS * LAUNCH_REGS, "a larger share would wait forever");
+static_assert(SOFTMAX_REGS >= LAUNCH_REGS && LOADER_REGS <= LAUNCH_REGS && PRODUCT_REGS <= LAUNCH_REGS, "the first is raised, the others are lowered");
 
 template <int HD> struct Layout {
   static constexpr int TILE = 128 * HD * 2;                    // a tile of Q, K or V: blocks of 64 elements, 128 rows of 128 bytes each
@@ -43,7 +46,7 @@ template <int HD> struct Layout {
   static constexpr int SIDE_BYTES = 2 * KEYS * 4 + 16;
   static constexpr int NEED = END + SIDE * SIDE_BYTES + 1024;  // + alignment
   static constexpr int SMEM = NEED > 116 * 1024 ? NEED : 116 * 1024;   // one block per SM: each takes all of the tensor memory
-  static constexpr int O_COL = 256;                            // tensor memory: S_0 at 0, S_1 at 128, O_0, O_1 from 256
+  static constexpr int O_COL = 256;                            // tensor memory: S_0 at 0 and 64, S_1 at 128 and 192, O_0, O_1 from 256
 };
 
 // bf16 x bf16 -> fp32, 128 rows; b_mn: B is stored with its output axis contiguous
@@ -140,13 +143,28 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   using L = Layout<HD>;
   constexpr bool SCALED = CacheType<TC>::TOP > 0.f;
   extern __shared__ unsigned char ac_smem[];
-  __shared__ uint64_t bars[4 * STAGES + 8 + SIDE];
+  __shared__ uint64_t bars[4 * STAGES + 12 + SIDE];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_word;
 
-  // the block's rows
-  const int blk = blockIdx.x % blocks_per_seq, rest = blockIdx.x / blocks_per_seq;
-  const int g_head = rest % b.n_kv_heads, seq = rest / b.n_kv_heads;
+  // the block's rows.  The longest sequences come first, so that no long block is left to the end: sequence number `turn` in
+  // order of decreasing length (a block counts for each of up to THREADS sequences how many are longer; more keep their order)
+  const int g_head = blockIdx.x % b.n_kv_heads, rest = blockIdx.x / b.n_kv_heads;
+  const int blk = rest % blocks_per_seq, turn = rest / blocks_per_seq;
+  __shared__ int lens[THREADS];
+  __shared__ int turn_seq;
+  if (b.n_seqs > 1 && b.n_seqs <= THREADS) {
+    const int mine = threadIdx.x < b.n_seqs ? b.len[threadIdx.x] : 0;
+    lens[threadIdx.x] = mine;
+    __syncthreads();
+    if (threadIdx.x < b.n_seqs) {
+      int ahead = 0;
+      for (int i = 0; i < b.n_seqs; ++i) ahead += lens[i] > mine || (lens[i] == mine && i < (int)threadIdx.x);
+      if (ahead == turn) turn_seq = threadIdx.x;
+    }
+    __syncthreads();
+  }
+  const int seq = b.n_seqs > 1 && b.n_seqs <= THREADS ? turn_seq : turn;
   const int f0 = b.first[seq], f1 = b.first[seq + 1], len = b.seq_len(seq);
   int n_new = f1 - f0;
   if (f0 < 0 || n_new < 0 || f1 > b.n_tokens || n_new > b.max_new) {
@@ -166,16 +184,16 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     n_rows[t] = max(0, min(TILE_ROWS, rows_all - row0 - t * TILE_ROWS));
     const int last = (row0 + t * TILE_ROWS + n_rows[t] - 1) / group;
     const int keys = n_rows[t] ? (int)min(max(pos_first + last + 1, 0ll), (long long)len) : 0;
-    n_keys[t] = (keys + KEYS - 1) / KEYS;                       // tiles of keys; a later tile of rows sees no fewer
+    n_keys[t] = (keys + HALF - 1) / HALF;                       // halves of key tiles; a later tile of rows sees no fewer
   }
-  const int n_tiles = max(n_keys[0], n_keys[1]);
+  const int n_tiles = (max(n_keys[0], n_keys[1]) + 1) / 2;
 
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
   const uint32_t raw = (uint32_t)__cvta_generic_to_shared(ac_smem), base = (raw + 1023u) & ~1023u;
   unsigned char* base_ptr = ac_smem + (base - raw);
   const uint32_t bar0 = (uint32_t)__cvta_generic_to_shared(bars);
   const uint32_t kfull = bar0, kempty = kfull + 8 * STAGES, vfull = kempty + 8 * STAGES, vempty = vfull + 8 * STAGES;
-  const uint32_t sfull = vempty + 8 * STAGES, pready = sfull + 16, odone = pready + 16, qfull = odone + 16, drain = qfull + 8, sidefull = drain + 8;
+  const uint32_t sfull = vempty + 8 * STAGES, pready = sfull + 32, odone = pready + 32, qfull = odone + 16, drain = qfull + 8, sidefull = drain + 8;
   volatile int* abort_flag = &abort_word;
 
   if (threadIdx.x == 0) {
@@ -183,7 +201,8 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       tc::mbar_init(kfull + 8 * s, 4); tc::mbar_init(kempty + 8 * s, 1);
       tc::mbar_init(vfull + 8 * s, 4); tc::mbar_init(vempty + 8 * s, 1);
     }
-    for (int t = 0; t < 2; ++t) { tc::mbar_init(sfull + 8 * t, 1); tc::mbar_init(pready + 8 * t, 4); tc::mbar_init(odone + 8 * t, 1); }
+    for (int i = 0; i < 4; ++i) { tc::mbar_init(sfull + 8 * i, 1); tc::mbar_init(pready + 8 * i, 4); }      // tile t, half h: 2 t + h
+    for (int t = 0; t < 2; ++t) tc::mbar_init(odone + 8 * t, 1);
     tc::mbar_init(qfull, 8);
     tc::mbar_init(drain, 1);
     for (int i = 0; i < SIDE; ++i) tc::mbar_init(sidefull + 8 * i, 4);
@@ -241,23 +260,26 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     float m = -INFINITY, l = 0.f;                                // m in the units of the scores (bf16) or base-2 (8 bits)
     const float unit = SCALED ? 1.f : scale;                     // base-2 units per unit of m
     bool ok = true;
-    for (int j = 0; j < n_keys[t]; ++j) {
+    for (int i = 0; i < n_keys[t]; ++i) {
+      const int j = i >> 1, h = i & 1;
       // scales and mask have a barrier of their own; it cannot run a phase ahead of this wait, because the loaders reach tile
-      // j + SIDE only after the scores of tile j + 2, which follow this tile's weights
-      ok = __all_sync(0xffffffffu, tc::mbar_wait(sfull + 8 * t, j & 1, abort_flag, b.status) &&
+      // j + SIDE only after the scores of tile j + 2, which follow this half's weights
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(sfull + 8 * (2 * t + h), j & 1, abort_flag, b.status) &&
                                    tc::mbar_wait(sidefull + 8 * (j % SIDE), (j / SIDE) & 1, abort_flag, b.status));
       if (!ok) break;
       fence_after();
       const float* side = reinterpret_cast<const float*>(base_ptr + L::SIDE_OFF + (j & (SIDE - 1)) * L::SIDE_BYTES);
-      const uint32_t pages_ok = *reinterpret_cast<const uint32_t*>(side + 2 * KEYS);
+      const uint32_t pages_ok = *reinterpret_cast<const uint32_t*>(side + 2 * KEYS) >> (8 * h) & 0xffu;
+      side += h * HALF;
+      const uint32_t s_half = s_addr + h * HALF;
 
-      uint32_t s[4][32];
+      uint32_t s[2][32];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) tc::tmem_ld32(s_addr + 32 * c, s[c]);
+      for (int c = 0; c < 2; ++c) tc::tmem_ld32(s_half + 32 * c, s[c]);
       tmem_wait_ld();
       if (SCALED) {                                              // the key's scale (with the softmax scale and log2 e)
 #pragma unroll
-        for (int c = 0; c < 128; c += 4) {
+        for (int c = 0; c < HALF; c += 4) {
           const float4 k = *reinterpret_cast<const float4*>(side + c);
           uint32_t* x = &s[c >> 5][c & 31];
           float y0, y1, y2, y3;
@@ -266,24 +288,24 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
           x[0] = __float_as_uint(y0); x[1] = __float_as_uint(y1); x[2] = __float_as_uint(y2); x[3] = __float_as_uint(y3);
         }
       }
-      if (j * KEYS + KEYS - 1 > all_see || pages_ok != 0xffffu) {
-        const int left = row_last - j * KEYS;                    // columns up to here are seen
+      if (i * HALF + HALF - 1 > all_see || pages_ok != 0xffu) {
+        const int left = row_last - i * HALF;                    // columns up to here are seen
 #pragma unroll
-        for (int c = 0; c < 128; ++c)
+        for (int c = 0; c < HALF; ++c)
           if (c > left || !((pages_ok >> (c >> 3)) & 1u)) s[c >> 5][c & 31] = 0xff800000u;
       }
       float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-      for (int i = 0; i < 32; i += 2)
+      for (int k = 0; k < 16; k += 2)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) mx[c] = fmaxf(mx[c], fmaxf(__uint_as_float(s[c][i]), __uint_as_float(s[c][i + 1])));
+        for (int c = 0; c < 4; ++c) mx[c] = fmaxf(mx[c], fmaxf(__uint_as_float(s[c >> 1][(c & 1) * 16 + k]), __uint_as_float(s[c >> 1][(c & 1) * 16 + k + 1])));
       const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
       if (__any_sync(0xffffffffu, (top - m) * unit > SLACK)) {   // -inf - -inf is NaN: not greater
         const float m_new = fmaxf(m, top), a = m == -INFINITY ? 0.f : ex2((m - m_new) * unit);
         m = m_new;
         l *= a;
-        if (j > 0) {
-          ok = __all_sync(0xffffffffu, tc::mbar_wait(odone + 8 * t, (j - 1) & 1, abort_flag, b.status));
+        if (i > 0) {
+          ok = __all_sync(0xffffffffu, tc::mbar_wait(odone + 8 * t, (i - 1) & 1, abort_flag, b.status));
           if (!ok) break;
           fence_after();
 #pragma unroll 1
@@ -292,7 +314,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
             tc::tmem_ld16(o_addr + c0, v);
             tmem_wait_ld();
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o16[i] = __float_as_uint(__uint_as_float(v[i]) * a);
+            for (int k = 0; k < 16; ++k) o16[k] = __float_as_uint(__uint_as_float(v[k]) * a);
             tmem_st16(o_addr + c0, o16);
           }
           tmem_wait_st();
@@ -302,25 +324,25 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       const F2 unit2 = f2(unit, unit), mb2 = f2(mb, mb);
       F2 sum[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
+      for (int c = 0; c < 2; ++c) {
         uint32_t w[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          F2 x = f2(__uint_as_float(s[c][2 * i]), __uint_as_float(s[c][2 * i + 1]));
+        for (int k = 0; k < 16; ++k) {
+          F2 x = f2(__uint_as_float(s[c][2 * k]), __uint_as_float(s[c][2 * k + 1]));
           x = SCALED ? add2(x, mb2) : fma2(x, unit2, mb2);
           float p0, p1;
           un2(x, p0, p1);
           p0 = ex2(p0);
           p1 = ex2(p1);
           x = f2(p0, p1);
-          sum[i & 1] = add2(sum[i & 1], x);
+          sum[k & 1] = add2(sum[k & 1], x);
           if (SCALED) {
-            const float2 v = *reinterpret_cast<const float2*>(side + KEYS + c * 32 + 2 * i);
+            const float2 v = *reinterpret_cast<const float2*>(side + KEYS + c * 32 + 2 * k);
             un2(mul2(x, f2(v.x, v.y)), p0, p1);
           }
-          w[i] = pack_bf16(p0, p1);
+          w[k] = pack_bf16(p0, p1);
         }
-        tmem_st16(s_addr + 16 * c, w);                           // over columns that have been read
+        tmem_st16(s_half + 16 * c, w);                           // over columns that have been read
       }
       float a0, a1;
       un2(add2(sum[0], sum[1]), a0, a1);
@@ -328,7 +350,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       tmem_wait_st();
       fence_before();
       __syncwarp();
-      if (lane == 0) arrive(pready + 8 * t);
+      if (lane == 0) arrive(pready + 8 * (2 * t + h));
     }
     if (n_rows[t] > 0 && ok) {
       if (n_keys[t] > 0) {
@@ -511,30 +533,32 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PRODUCT_REGS));
     if (warp == 12 && n_tiles > 0) {
       // ---- products
-      constexpr uint32_t id_s = idesc(KEYS, false), id_o = idesc(HD, true);
-      const int tiles = uniform(n_tiles), keys[2] = {uniform(n_keys[0]), uniform(n_keys[1])};
+      constexpr uint32_t id_s = idesc(HALF, false), id_o = idesc(HD, true);
+      const int halves[2] = {uniform(n_keys[0]), uniform(n_keys[1])};
       const uint32_t tm = uniform(tmem), at = uniform(base), bar = uniform(bar0);
       auto wait = [&](uint32_t which, int phase) { return __all_sync(0xffffffffu, tc::mbar_wait(bar + (which - bar0), phase & 1, abort_flag, b.status)) != 0; };
-      // each of these announces its completion, and that of everything before it, on the barriers named
-      auto product_s = [&](int t, int j) {
-        const uint64_t qa = tc::smem_desc(at + L::Q + t * L::TILE), ka = tc::smem_desc(at + L::K + (j % STAGES) * L::TILE);
+      // each of these announces its completion, and that of everything before it, on the barrier named
+      auto product_s = [&](int t, int i) {
+        const int h = i & 1;
+        const uint64_t qa = tc::smem_desc(at + L::Q + t * L::TILE), ka = tc::smem_desc(at + L::K + ((i >> 1) % STAGES) * L::TILE + h * (HALF * 128));
         if (elect()) {
 #pragma unroll
           for (int k = 0; k < HD / 16; ++k) {                     // descriptors count 16-byte units
             const uint32_t off = ((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4;
-            mma_ss(tm + t * 128, qa + off, ka + off, id_s, k > 0);
+            mma_ss(tm + t * 128 + h * HALF, qa + off, ka + off, id_s, k > 0);
           }
-          tc::umma_commit(bar + (sfull - bar0) + 8 * t);
+          tc::umma_commit(bar + (sfull - bar0) + 8 * (2 * t + h));
         }
         __syncwarp();
       };
-      auto product_o = [&](int t, int j) {
-        const uint64_t va = v_desc(at + L::V + (j % STAGES) * L::TILE, 128 * 128);
-        const uint32_t first = j > 0;
+      auto product_o = [&](int t, int i) {
+        const int h = i & 1;
+        const uint64_t va = v_desc(at + L::V + ((i >> 1) % STAGES) * L::TILE + h * (HALF * 128), 128 * 128);
+        const uint32_t first = i > 0;
         if (elect()) {
 #pragma unroll
-          for (int k = 0; k < KEYS / 16; ++k)
-            mma_ts(tm + L::O_COL + t * HD, tm + t * 128 + k * 8, va + k * (2048 >> 4), id_o, k > 0 ? 1u : first);
+          for (int k = 0; k < HALF / 16; ++k)
+            mma_ts(tm + L::O_COL + t * HD, tm + t * 128 + h * HALF + k * 8, va + k * (2048 >> 4), id_o, k > 0 ? 1u : first);
           tc::umma_commit(bar + (odone - bar0) + 8 * t);
         }
         __syncwarp();
@@ -548,35 +572,42 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       if (ok) {
         fence_after();
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-          if (keys[t] > 0) product_s(t, 0);
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+            if (i < halves[t]) product_s(t, i);
         announce(kempty);
       }
-      for (int j = 0; j < tiles && ok; ++j) {
-        const int s = j % STAGES, sn = (j + 1) % STAGES;
-        ok = wait(vfull + 8 * s, j / STAGES);
-        bool k_there = false;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          if (!ok) break;
-          if (j < keys[t]) {
-            ok = wait(pready + 8 * t, j);
-            if (!ok) break;
-            fence_after();
-            product_o(t, j);
-          }
-          if (j + 1 < keys[t]) {
-            if (!k_there) ok = wait(kfull + 8 * sn, (j + 1) / STAGES);
-            if (!ok) break;
-            k_there = true;
-            fence_after();
-            product_s(t, j + 1);
-          }
+      int k_there = 0;                                            // the last tile of keys known to have arrived
+      // the scores of half i, i >= 2, in the columns of half i - 2.  Products with other accumulators are not ordered among each
+      // other: its product with the values must have completed.
+      auto next_s = [&](int t, int i) {
+        const int j = i >> 1;
+        if (j > k_there) {
+          if (!wait(kfull + 8 * (j % STAGES), j / STAGES)) return false;
+          k_there = j;
         }
-        if (ok) {
-          announce(vempty + 8 * s);
-          if (j + 1 < tiles) announce(kempty + 8 * sn);
-        }
+        if (!wait(odone + 8 * t, i - 2)) return false;
+        fence_after();
+        product_s(t, i);
+        return true;
+      };
+      auto next_o = [&](int t, int i) {
+        if (!wait(pready + 8 * (2 * t + (i & 1)), i >> 1)) return false;
+        fence_after();
+        product_o(t, i);
+        return true;
+      };
+      const int most = max(halves[0], halves[1]);
+      for (int i = 0; i < most && ok; ++i) {
+        const int j = i >> 1;
+        if (!(i & 1)) ok = wait(vfull + 8 * (j % STAGES), j / STAGES);
+        if (ok && i < halves[0]) ok = next_o(0, i);
+        if (ok && i > 0 && i + 1 < halves[1]) ok = next_s(1, i + 1);
+        if (ok && i > 0 && !(i & 1)) announce(kempty + 8 * (j % STAGES));
+        if (ok && i < halves[1]) ok = next_o(1, i);
+        if (ok && i + 2 < halves[0]) ok = next_s(0, i + 2);
+        if (ok && ((i & 1) || i + 1 == most)) announce(vempty + 8 * (j % STAGES));
       }
       if (!ok) {                                                  // let what has been issued finish before the memory goes
         announce(drain);
