@@ -80,6 +80,48 @@ __device__ __forceinline__ int locate_row(const BatchView& b, int r, int& seq, i
   return ROW_OK;
 }
 
+// The same for up to MOST_ROWS consecutive rows of a block at once, one lane of the first warp per row (its owner by bisection): the
+// chain of dependent loads (owner, length, table) is paid once for all of them.  Block 0 also checks the whole description.
+constexpr int MOST_ROWS = 2;
+struct Places {
+  int state[MOST_ROWS], pos[MOST_ROWS], page[MOST_ROWS];         // ROW_*; position; page, -1 where the row has none
+};
+__device__ __forceinline__ void locate_rows(const BatchView& b, int r0, int n, Places& p) {
+  if (threadIdx.x < n) {
+    const int r = r0 + threadIdx.x;
+    int lo = 0, hi = b.n_seqs + 1;                               // how many of first[0..n_seqs] are at most r
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (b.first[mid] <= r) lo = mid + 1;
+      else hi = mid;
+    }
+    const int seq = lo - 1;
+    int state = ROW_PADDING, pos = -1, page = -1;
+    if (seq >= 0 && seq < b.n_seqs) {
+      const int f0 = b.first[seq], f1 = b.first[seq + 1];
+      if (f0 < 0 || f0 > r || r >= f1 || r - f0 >= b.max_new) b.bad();
+      else {
+        const long long at = (long long)b.len[seq] - f1 + r;
+        state = ROW_NOWHERE;
+        if (at >= (long long)b.pages_per_seq << b.page_shift) b.bad();
+        else if (at >= 0) {
+          state = ROW_OK;
+          pos = (int)at;
+          page = b.page_of(seq, pos);
+        }
+      }
+    }
+    p.state[threadIdx.x] = state;
+    p.pos[threadIdx.x] = pos;
+    p.page[threadIdx.x] = page;
+  }
+  if (blockIdx.x == 0) {
+    for (int i = threadIdx.x; i <= b.n_seqs; i += blockDim.x)
+      if (b.first[i] < (i ? b.first[i - 1] : 0) || (i == b.n_seqs && b.first[i] > b.n_tokens)) b.bad();
+  }
+  __syncthreads();
+}
+
 // Rows handed in by the caller: [n_tokens, heads, head_dim] with strides in elements.
 struct Rows {
   void* data;
@@ -176,8 +218,7 @@ __device__ __forceinline__ float2 e4m3_widen(uint32_t pair) {          // exact:
   return __half22float2(*reinterpret_cast<const __half2*>(&r));
 }
 
-// The code nearest to x / s, ties to even, for one element whose fast quotient is too close to a border (or s to the
-// smallest floats) to decide.  The quotient of two 24-bit numbers is either a border or at least 2^-25 (relative) away from
+// The code nearest to x / s, ties to even.  The quotient of two 24-bit numbers is either a border or at least 2^-25 (relative) away from
 // it, so the 53-bit quotient decides exactly; on the way to e4m3 it passes through a float that is rounded to odd, which
 // keeps a later rounding to fewer bits correct.
 __device__ __noinline__ float quotient_int8(float x, float s) { return (float)fmin(fmax(rint((double)x / (double)s), -127.0), 127.0); }
@@ -187,40 +228,51 @@ __device__ __noinline__ float quotient_sticky(float x, float s) {
   return (double)f == q ? f : __uint_as_float(__float_as_uint(f) | 1u);
 }
 
-// Eight codes of x / s.  inv = 1 / s, or 0 to send every element through the exact route.  The fast quotient x * inv is off
-// by less than 2^-22 of itself.
-__device__ __forceinline__ uint2 encode8(const float (&x)[8], float s, float inv, int8_t) {
+// Eight codes of x / s the exact way, for rows whose fast quotients do not decide, with a tiny scale or with elements that are not finite.
+__device__ __forceinline__ uint2 encode8_exact(const float (&x)[8], float s, int8_t) {
   uint32_t w[2] = {0u, 0u};
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    float c;
-    if (x[i] != x[i] || s == 0.f) c = 0.f;
-    else {
-      const float y = fminf(fmaxf(x[i] * inv, -127.f), 127.f);
-      c = rintf(y);
-      if (fabsf(y - c) > 0.4999f || inv == 0.f) c = quotient_int8(x[i], s);      // 127 * 2^-22 = 3e-5 < 1e-4
-    }
+    const float c = (x[i] != x[i] || s == 0.f) ? 0.f : quotient_int8(x[i], s);
     w[i >> 2] |= ((uint32_t)(int)c & 0xffu) << (8 * (i & 3));
   }
   return make_uint2(w[0], w[1]);
 }
-__device__ __forceinline__ uint2 encode8(const float (&x)[8], float s, float inv, e4m3) {
+__device__ __forceinline__ uint2 encode8_exact(const float (&x)[8], float s, e4m3) {
   uint32_t w[2] = {0u, 0u};
 #pragma unroll
-  for (int i = 0; i < 8; i += 2) {
-    float y[2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) y[j] = (x[i + j] != x[i + j] || s == 0.f) ? 0.f : x[i + j] * inv;
-    constexpr float UP = 1.f + 4.f / 16777216.f, DOWN = 1.f - 4.f / 16777216.f;        // 1 +- 2^-22
-    uint32_t c = e4m3_pair(y[0] * DOWN, y[1] * DOWN);
-    if (c != e4m3_pair(y[0] * UP, y[1] * UP) || inv == 0.f) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j) y[j] = (x[i + j] != x[i + j] || s == 0.f) ? 0.f : quotient_sticky(x[i + j], s);
-      c = e4m3_pair(y[0], y[1]);
-    }
-    w[i >> 2] |= c << (16 * ((i >> 1) & 1));
+  for (int i = 0; i < 8; ++i) {
+    const float y = (x[i] != x[i] || s == 0.f) ? 0.f : quotient_sticky(x[i], s);
+    w[i >> 2] |= (e4m3_pair(y, 0.f) & 0xffu) << (8 * (i & 3));
   }
   return make_uint2(w[0], w[1]);
+}
+// Eight codes of x / s by the fast quotient x * inv, which is off by less than 2^-22 of itself; false where an element is too close
+// to a border between two codes for that.  x: finite, inv = 1 / s.
+__device__ __forceinline__ bool encode8_fast(const float (&x)[8], float inv, uint2& code, int8_t) {
+  uint32_t w[2] = {0u, 0u};
+  float far = 0.f;                                 // largest distance from the code
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float y = x[i] * inv;
+    const float t = y + 12582912.f;                // 1.5 * 2^23: the code in the low bits
+    far = fmaxf(far, fabsf(y - (t - 12582912.f)));
+    w[i >> 2] |= (__float_as_uint(t) & 0xffu) << (8 * (i & 3));
+  }
+  code = make_uint2(w[0], w[1]);
+  return far < 0.4999f;                            // 127 * 2^-22 = 3e-5 < 1e-4; at most 127 + 3e-5, so within the codes
+}
+__device__ __forceinline__ bool encode8_fast(const float (&x)[8], float inv, uint2& code, e4m3) {
+  constexpr float UP = 1.f + 4.f / 16777216.f, DOWN = 1.f - 4.f / 16777216.f;          // 1 +- 2^-22
+  uint32_t lo[4], hi[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float a = x[2 * i] * inv, b = x[2 * i + 1] * inv;
+    lo[i] = e4m3_pair(a * DOWN, b * DOWN);
+    hi[i] = e4m3_pair(a * UP, b * UP);
+  }
+  code = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+  return ((code.x ^ (hi[0] | hi[1] << 16)) | (code.y ^ (hi[2] | hi[3] << 16))) == 0u;
 }
 __device__ __forceinline__ void decode8(uint2 v, float s, float (&o)[8], int8_t) {
   const uint32_t w[2] = {v.x, v.y};
@@ -237,55 +289,72 @@ __device__ __forceinline__ void decode8(uint2 v, float s, float (&o)[8], e4m3) {
 }
 
 // ---- append -----------------------------------------------------------------------------------
-// One block per row.  A group of HD / 8 lanes owns one (head, K or V) of it: each lane holds eight elements, the largest
+// One block per few rows.  A group of HD / 8 lanes owns one (row, head, K or V): each lane holds eight elements, the largest
 // magnitude goes round the group by shuffles, and the codes leave as one 8-byte store per lane (16 or 32 bytes in bf16 or
 // fp32).  The bytes are read once and written once; there is no other work to speak of.
 template <typename TS, typename TC, int HD, bool VEC>
 __global__ void __launch_bounds__(256)
-cache_append_kernel(const BatchView b, const Rows ks, const Rows vs, TC* __restrict__ Kp, TC* __restrict__ Vp,
+cache_append_kernel(const BatchView b, int row_shift, const Rows ks, const Rows vs, TC* __restrict__ Kp, TC* __restrict__ Vp,
                     float* __restrict__ Ksc, float* __restrict__ Vsc) {
   constexpr int LANES = HD / 8;
-  int seq, pos;
-  if (locate_row(b, blockIdx.x, seq, pos) != ROW_OK) return;
-  const int page = b.page_of(seq, pos);
-  if (page < 0) return;
-  const int total = 2 * b.n_kv_heads * LANES;
-  for (int i0 = 0; i0 < total; i0 += blockDim.x) {              // uniform: the shuffles need whole warps
-    const int i = i0 + threadIdx.x;
-    const bool on = i < total;
-    const int unit = on ? i / LANES : 0, sub = i % LANES;
-    const bool is_v = unit >= b.n_kv_heads;
-    const int g = is_v ? unit - b.n_kv_heads : unit;
-    const Rows& src = is_v ? vs : ks;
-    float x[8];
-    load8<VEC>(static_cast<const TS*>(src.data) + (long long)blockIdx.x * src.row_stride + g * src.head_stride + sub * 8, x);
-    const size_t e = b.entry(page, g, pos);
-    TC* dst = (is_v ? Vp : Kp) + e * HD + sub * 8;
-    float top = 0.f;                                             // of the finite elements
-    bool finite = true;
+  __shared__ Places place;
+  const int rows = 1 << row_shift, r0 = blockIdx.x << row_shift, n = min(rows, b.n_tokens - r0);
+  locate_rows(b, r0, n, place);
+  // lanes go over a head's elements, then over the block's rows, then over heads: neighbouring rows are neighbours in a page
+  const int total = 2 * b.n_kv_heads * LANES << row_shift;
+  constexpr int AT_ONCE = 4;                                     // pieces of a thread whose loads are on their way together
+  for (int i0 = 0; i0 < total; i0 += AT_ONCE * blockDim.x) {     // uniform: the shuffles need whole warps
+    float x[AT_ONCE][8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float a = fabsf(x[j]);
-      if (a < INFINITY) top = fmaxf(top, a);
-      else finite = false;                                       // NaN too
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const int i = i0 + u * blockDim.x + threadIdx.x;
+      const int row = i / LANES & (rows - 1), unit = i / LANES >> row_shift;
+      if (i >= total || row >= n || place.page[row] < 0) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[u][j] = 0.f;
+        continue;
+      }
+      const bool is_v = unit >= b.n_kv_heads;
+      const Rows& src = is_v ? vs : ks;
+      load8<VEC>(static_cast<const TS*>(src.data) + (long long)(r0 + row) * src.row_stride + (is_v ? unit - b.n_kv_heads : unit) * src.head_stride + i % LANES * 8, x[u]);
     }
-    if (!finite && on) atomicOr(b.status, STATUS_NOT_FINITE);
-    if constexpr (CacheType<TC>::TOP > 0.f) {
 #pragma unroll
-      for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      const float s = __fdiv_rn(top, CacheType<TC>::TOP);
-      const float inv = s > 1e-30f ? __fdiv_rn(1.f, s) : 0.f;
-      if (on) {
-        *reinterpret_cast<uint2*>(dst) = encode8(x, s, inv, TC{});
-        if (sub == 0) (is_v ? Vsc : Ksc)[e] = s;
-      }
-    } else if (on) {
-      constexpr float MOST = CacheType<TC>::MOST;
-      if (!finite || top > MOST) {                               // in bf16 the last half step below 2^128 would round to infinity
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const int i = i0 + u * blockDim.x + threadIdx.x;
+      if (i0 + u * (int)blockDim.x >= total) break;              // the same for all threads
+      const int row = i / LANES & (rows - 1), unit = i / LANES >> row_shift, sub = i % LANES;
+      const bool on = i < total && row < n && place.page[row] >= 0;
+      const bool is_v = unit >= b.n_kv_heads;
+      const size_t e = on ? b.entry(place.page[row], is_v ? unit - b.n_kv_heads : unit, place.pos[row]) : 0;
+      TC* dst = (is_v ? Vp : Kp) + e * HD + sub * 8;
+      float top = 0.f;                                           // of the finite elements
+      bool finite = true;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = x[j] != x[j] ? 0.f : fminf(fmaxf(x[j], -MOST), MOST);
+      for (int j = 0; j < 8; ++j) {
+        const float a = fabsf(x[u][j]);
+        if (a < INFINITY) top = fmaxf(top, a);
+        else finite = false;                                     // NaN too
       }
-      store8<true>(dst, x);                                      // pools are 256-byte aligned, rows multiples of 64 bytes
+      if (!finite) atomicOr(b.status, STATUS_NOT_FINITE);
+      if constexpr (CacheType<TC>::TOP > 0.f) {
+#pragma unroll
+        for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float s = __fdiv_rn(top, CacheType<TC>::TOP);
+        const float inv = s > 1e-30f ? __fdiv_rn(1.f, s) : 0.f;
+        if (on) {
+          uint2 code;
+          if (!finite || inv == 0.f || !encode8_fast(x[u], inv, code, TC{})) code = encode8_exact(x[u], s, TC{});
+          *reinterpret_cast<uint2*>(dst) = code;
+          if (sub == 0) (is_v ? Vsc : Ksc)[e] = s;
+        }
+      } else if (on) {
+        constexpr float MOST = CacheType<TC>::MOST;
+        if (!finite || top > MOST) {                             // in bf16 the last half step below 2^128 would round to infinity
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[u][j] = x[u][j] != x[u][j] ? 0.f : fminf(fmaxf(x[u][j], -MOST), MOST);
+        }
+        store8<true>(dst, x[u]);                                 // pools are 256-byte aligned, rows multiples of 64 bytes
+      }
     }
   }
 }
@@ -294,27 +363,50 @@ cache_append_kernel(const BatchView b, const Rows ks, const Rows vs, TC* __restr
 // The same walk the other way.  A row without a place reads as zeros.
 template <typename TO, typename TC, int HD, bool VEC>
 __global__ void __launch_bounds__(256)
-cache_read_kernel(const BatchView b, const Rows ko, const Rows vo, const TC* __restrict__ Kp, const TC* __restrict__ Vp,
+cache_read_kernel(const BatchView b, int row_shift, const Rows ko, const Rows vo, const TC* __restrict__ Kp, const TC* __restrict__ Vp,
                   const float* __restrict__ Ksc, const float* __restrict__ Vsc) {
   constexpr int LANES = HD / 8;
-  int seq, pos;
-  const int where = locate_row(b, blockIdx.x, seq, pos);
-  if (where == ROW_PADDING) return;
-  const int page = where == ROW_OK ? b.page_of(seq, pos) : -1;
-  const int total = 2 * b.n_kv_heads * LANES;
-  for (int i = threadIdx.x; i < total; i += blockDim.x) {
-    const int unit = i / LANES, sub = i % LANES;
-    const bool is_v = unit >= b.n_kv_heads;
-    const int g = is_v ? unit - b.n_kv_heads : unit;
-    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (page >= 0) {
-      const size_t e = b.entry(page, g, pos);
-      const TC* src = (is_v ? Vp : Kp) + e * HD + sub * 8;
-      if constexpr (CacheType<TC>::TOP > 0.f) decode8(*reinterpret_cast<const uint2*>(src), (is_v ? Vsc : Ksc)[e], x, TC{});
-      else load8<true>(src, x);
+  __shared__ Places place;
+  const int rows = 1 << row_shift, r0 = blockIdx.x << row_shift, n = min(rows, b.n_tokens - r0);
+  locate_rows(b, r0, n, place);
+  // lanes go over a head's elements, then over the block's rows, then over heads: neighbouring rows are neighbours in a page
+  const int total = 2 * b.n_kv_heads * LANES << row_shift;
+  constexpr int AT_ONCE = 4;                                     // pieces of a thread whose loads are on their way together
+  for (int i0 = threadIdx.x; i0 < total; i0 += AT_ONCE * blockDim.x) {
+    constexpr bool SCALED = CacheType<TC>::TOP > 0.f;
+    uint2 code[AT_ONCE];
+    float scale[AT_ONCE], x[AT_ONCE][8];
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const int i = i0 + u * blockDim.x;
+      code[u] = make_uint2(0u, 0u);
+      scale[u] = 0.f;
+      if constexpr (!SCALED) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[u][j] = 0.f;
+      }
+      const int row = i / LANES & (rows - 1), unit = i / LANES >> row_shift;
+      if (i >= total || row >= n || place.page[row] < 0) continue;
+      const bool is_v = unit >= b.n_kv_heads;
+      const size_t e = b.entry(place.page[row], is_v ? unit - b.n_kv_heads : unit, place.pos[row]);
+      const TC* src = (is_v ? Vp : Kp) + e * HD + i % LANES * 8;
+      if constexpr (SCALED) {
+        code[u] = __ldg(reinterpret_cast<const uint2*>(src));
+        scale[u] = __ldg((is_v ? Vsc : Ksc) + e);
+      } else {
+        load8<true>(src, x[u]);
+      }
     }
-    const Rows& dst = is_v ? vo : ko;
-    store8<VEC>(static_cast<TO*>(dst.data) + (long long)blockIdx.x * dst.row_stride + g * dst.head_stride + sub * 8, x);
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const int i = i0 + u * blockDim.x;
+      const int row = i / LANES & (rows - 1), unit = i / LANES >> row_shift;
+      if (i >= total || row >= n || place.state[row] == ROW_PADDING) continue;
+      const bool is_v = unit >= b.n_kv_heads;
+      if constexpr (SCALED) decode8(code[u], scale[u], x[u], TC{});
+      const Rows& dst = is_v ? vo : ko;
+      store8<VEC>(static_cast<TO*>(dst.data) + (long long)(r0 + row) * dst.row_stride + (is_v ? unit - b.n_kv_heads : unit) * dst.head_stride + i % LANES * 8, x[u]);
+    }
   }
 }
 

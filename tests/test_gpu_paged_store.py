@@ -243,7 +243,7 @@ def test_refusals():
         with pytest.raises(ValueError):
             call()
     L = binding.lib()
-    rows = cache._rows("k", k, 2, b)
+    rows = binding.SdHeads(k.data_ptr(), k.stride(0), k.stride(1), binding.SD_DTYPE_FP32)
     for field, value, code in (("pages", None, binding.SD_ERR_ARG), ("first", None, binding.SD_ERR_ARG), ("len", None, binding.SD_ERR_ARG),
                                ("n_seqs", 0, binding.SD_ERR_ARG), ("n_seqs", 9, binding.SD_ERR_CAPACITY), ("pages_per_seq", 0, binding.SD_ERR_ARG),
                                ("pages_per_seq", 1 << 30, binding.SD_ERR_ARG), ("n_tokens", -1, binding.SD_ERR_ARG), ("n_tokens", 9, binding.SD_ERR_CAPACITY),
