@@ -166,23 +166,29 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
   const int tile0 = k0 / KEYS + warp, n_tiles = (k1 + KEYS - 1) / KEYS;      // this warp's tiles: tile0, tile0 + NW, ...
   const int* table = b.pages + (size_t)seq * b.pages_per_seq;
   uint32_t valid = 0u;                             // two bits per stage: the halves of the tile whose page exists
-  int next_page[2] = {-1, -1};                     // table entries of the tile to be issued next (one page holds it unless pages have 8 keys)
-  const bool split_tile = b.page_len < KEYS;
-  auto look_up = [&](int kt) {
-    const int key = kt * KEYS;
-    next_page[0] = key < k1 ? table[key >> b.page_shift] : 0;
-    next_page[1] = !split_tile ? next_page[0] : key + 8 < k1 ? table[(key + 8) >> b.page_shift] : 0;
+  const bool split_tile = b.page_len < KEYS;       // else one page holds a tile
+  // Table entries of this warp's next 32 tiles (from number win on), one per lane and half: one round of loads instead of one per tile.
+  int window[2] = {0, 0}, win = -32;
+  auto look_up = [&](int n) {                      // n: the warp's n-th tile, in order
+    if (n < win + 32) return;
+    win = n;
+    const int key = (tile0 + (n + lane) * NW) * KEYS;
+    window[0] = key < k1 ? table[key >> b.page_shift] : 0;
+    window[1] = !split_tile ? window[0] : key + 8 < k1 ? table[(key + 8) >> b.page_shift] : 0;
   };
   // this lane's piece of the first keys of a tile: the others follow at fixed distances
   const int lane_key = lane / S::PIECES, lane_piece = lane % S::PIECES;
   constexpr int STEPS = KEYS * S::PIECES / 32, STEP_KEYS = 32 / S::PIECES;
   static_assert(KEYS * S::PIECES % 32 == 0, "whole warps of copies");
-  auto issue = [&](int kt, int stage) {
+  auto issue = [&](int n, int stage) {
+    look_up(n);
+    const int kt = tile0 + n * NW;
+    const int page[2] = {__shfl_sync(0xffffffffu, window[0], n - win), __shfl_sync(0xffffffffu, window[1], n - win)};
     const uint32_t dst = ring + stage * S::STAGE;
     const int key0 = kt * KEYS;
-    if (!split_tile && key0 + KEYS <= k1 && (unsigned)next_page[0] < (unsigned)b.n_pages) {
+    if (!split_tile && key0 + KEYS <= k1 && (unsigned)page[0] < (unsigned)b.n_pages) {
       // a whole tile inside one page
-      const size_t e = b.entry(next_page[0], g_head, key0);
+      const size_t e = b.entry(page[0], g_head, key0);
       const TC* ks = Kp + e * HD + lane * (16 / S::E);
       const TC* vs = Vp + e * HD + lane * (16 / S::E);
 #pragma unroll
@@ -203,9 +209,9 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
       const int key = key0 + 8 * hf;
-      const bool there = (unsigned)next_page[hf] < (unsigned)b.n_pages;
+      const bool there = (unsigned)page[hf] < (unsigned)b.n_pages;
       if (!there && key < k1 && lane == 0) b.bad();
-      e[hf] = there ? b.entry(next_page[hf], g_head, key) : 0;
+      e[hf] = there ? b.entry(page[hf], g_head, key) : 0;
       ok |= there ? 1u << hf : 0u;
     }
     valid = (valid & ~(3u << (2 * stage))) | (ok << (2 * stage));
@@ -228,27 +234,29 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
     }
   };
 
-  look_up(tile0);
+  // the query row is asked for, then the first keys, and both are on their way together
+  constexpr int PER = S::EC;
+  float q_raw[S::NCH][PER];
+  {
+    const long long at = (long long)(f0 + token) * q.row_stride + head * q.head_stride;
+#pragma unroll
+    for (int c = 0; c < S::NCH; ++c) load_run<PER>(q, at + (t + 4 * c) * PER, q_vec, q_raw[c]);
+  }
+  const int mine = tile0 < n_tiles ? (n_tiles - tile0 + NW - 1) / NW : 0;     // this warp's tiles
+  look_up(0);
 #pragma unroll
   for (int s = 0; s < S::STAGES - 1; ++s) {
-    const int kt = tile0 + s * NW;
-    if (kt < n_tiles) { issue(kt, s); look_up(kt + NW); }
+    if (s < mine) issue(s, s);
     pf_commit();
   }
-  // the query row, while the first keys are on their way
   uint32_t qf[S::KS][4];
   float row_scale = scale_log2;
   {
-    constexpr int PER = S::EC;
-    float x[S::NCH][PER];
-    const long long at = (long long)(f0 + token) * q.row_stride + head * q.head_stride;
     float top = 0.f;
 #pragma unroll
-    for (int c = 0; c < S::NCH; ++c) {
-      load_run<PER>(q, at + (t + 4 * c) * PER, q_vec, x[c]);
+    for (int c = 0; c < S::NCH; ++c)
 #pragma unroll
-      for (int i = 0; i < PER; ++i) top = fmaxf(top, fabsf(x[c][i]));
-    }
+      for (int i = 0; i < PER; ++i) top = fmaxf(top, fabsf(q_raw[c][i]));
     float down = 1.f;
     if constexpr (S::SCALED) {                     // queries enter as fp16: brought near 1 by a power of two
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
@@ -259,20 +267,18 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
     }
 #pragma unroll
     for (int ks = 0; ks < S::KS; ++ks) {
-      const float* v = x[ks / (PER / 4)] + 4 * (ks % (PER / 4));
+      const float* v = q_raw[ks / (PER / 4)] + 4 * (ks % (PER / 4));
       split(v[0] * down, v[1] * down, qf[ks][0], qf[ks][1], TC{});
       split(v[2] * down, v[3] * down, qf[ks][2], qf[ks][3], TC{});
     }
   }
 
   int stage = 0, fill = S::STAGES - 1;
-  for (int kt = tile0; kt < n_tiles; kt += NW) {
-    {
-      const int ahead = kt + (S::STAGES - 1) * NW;
-      if (ahead < n_tiles) { issue(ahead, fill); look_up(ahead + NW); }
-      pf_commit();
-      fill = fill + 1 == S::STAGES ? 0 : fill + 1;
-    }
+  for (int n = 0; n < mine; ++n) {
+    const int kt = tile0 + n * NW;
+    if (n + S::STAGES - 1 < mine) issue(n + S::STAGES - 1, fill);
+    pf_commit();
+    fill = fill + 1 == S::STAGES ? 0 : fill + 1;
     pf_wait<S::STAGES - 1>();
     __syncwarp();
     const uint32_t ks_base = ring + stage * S::STAGE, vs_base = ks_base + KEYS * S::ROW, sc_base = vs_base + KEYS * S::ROW;
