@@ -536,37 +536,29 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       constexpr uint32_t id_s = idesc(HALF, false), id_o = idesc(HD, true);
       const int halves[2] = {uniform(n_keys[0]), uniform(n_keys[1])};
       const uint32_t tm = uniform(tmem), at = uniform(base), bar = uniform(bar0);
-      auto wait = [&](uint32_t which, int phase) { return __all_sync(0xffffffffu, tc::mbar_wait(bar + (which - bar0), phase & 1, abort_flag, b.status)) != 0; };
+      auto wait = [&](uint32_t which, int phase) { return tc::mbar_wait(bar + (which - bar0), phase & 1, abort_flag, b.status); };
+      if (elect()) {
       // each of these announces its completion, and that of everything before it, on the barrier named
       auto product_s = [&](int t, int i) {
         const int h = i & 1;
         const uint64_t qa = tc::smem_desc(at + L::Q + t * L::TILE), ka = tc::smem_desc(at + L::K + ((i >> 1) % STAGES) * L::TILE + h * (HALF * 128));
-        if (elect()) {
 #pragma unroll
-          for (int k = 0; k < HD / 16; ++k) {                     // descriptors count 16-byte units
-            const uint32_t off = ((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4;
-            mma_ss(tm + t * 128 + h * HALF, qa + off, ka + off, id_s, k > 0);
-          }
-          tc::umma_commit(bar + (sfull - bar0) + 8 * (2 * t + h));
+        for (int k = 0; k < HD / 16; ++k) {                       // descriptors count 16-byte units
+          const uint32_t off = ((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4;
+          mma_ss(tm + t * 128 + h * HALF, qa + off, ka + off, id_s, k > 0);
         }
-        __syncwarp();
+        tc::umma_commit(bar + (sfull - bar0) + 8 * (2 * t + h));
       };
       auto product_o = [&](int t, int i) {
         const int h = i & 1;
         const uint64_t va = v_desc(at + L::V + ((i >> 1) % STAGES) * L::TILE + h * (HALF * 128), 128 * 128);
         const uint32_t first = i > 0;
-        if (elect()) {
 #pragma unroll
-          for (int k = 0; k < HALF / 16; ++k)
-            mma_ts(tm + L::O_COL + t * HD, tm + t * 128 + h * HALF + k * 8, va + k * (2048 >> 4), id_o, k > 0 ? 1u : first);
-          tc::umma_commit(bar + (odone - bar0) + 8 * t);
-        }
-        __syncwarp();
+        for (int k = 0; k < HALF / 16; ++k)
+          mma_ts(tm + L::O_COL + t * HD, tm + t * 128 + h * HALF + k * 8, va + k * (2048 >> 4), id_o, k > 0 ? 1u : first);
+        tc::umma_commit(bar + (odone - bar0) + 8 * t);
       };
-      auto announce = [&](uint32_t which) {
-        if (elect()) tc::umma_commit(bar + (which - bar0));
-        __syncwarp();
-      };
+      auto announce = [&](uint32_t which) { tc::umma_commit(bar + (which - bar0)); };
       bool ok = wait(qfull, 0);
       if (ok) ok = wait(kfull, 0);
       if (ok) {
@@ -614,6 +606,8 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         const long long t0 = clock64();
         while (!tc::mbar_try(drain, 0) && clock64() - t0 < tc::kWaitLimit) {}
       }
+      }
+      __syncwarp();
     }
   }
   fence_before();

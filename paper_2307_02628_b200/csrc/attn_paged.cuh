@@ -9,7 +9,7 @@
 // near fp32 at no cost: with 8 rows or fewer the other half of the tile would be empty.  8-bit codes are fp16 numbers exactly.
 // bf16 caches multiply in bf16.
 //
-// Each of the block's NW warps walks its own 16-key tiles with a ring of its own in shared memory, filled by 16-byte asynchronous copies: no
+// Each of the block's four warps walks its own 16-key tiles with a ring of its own in shared memory, filled by 16-byte asynchronous copies: no
 // block-wide synchronisation until the end, and every warp keeps STAGES - 1 tiles in flight.  The fragments are read in the order
 // in which the bytes lie: the sum over the head's elements may run in any order, so a thread takes whole 16-byte pieces of a key
 // and the queries are laid out to match; for the values, a thread takes a run of elements of four keys, and the
@@ -26,9 +26,9 @@
 namespace sd {
 namespace ap {
 
-constexpr int ROWS = 8, KEYS = 16;
+constexpr int NW = 4, THREADS = 32 * NW, ROWS = 8, KEYS = 16;
 
-template <typename TC, int HD, int NW> struct Shape {
+template <typename TC, int HD> struct Shape {
   static constexpr bool SCALED = CacheType<TC>::TOP > 0.f;
   static constexpr int E = sizeof(TC);
   static constexpr int ROW = HD * E;                         // bytes of a key
@@ -38,7 +38,7 @@ template <typename TC, int HD, int NW> struct Shape {
   static constexpr int NCH = HD / (4 * EC);
   static constexpr int KS = HD / 16, NT = HD / 8;
   static constexpr int STAGE = 2 * KEYS * ROW + (SCALED ? 2 * KEYS * 4 : 0);
-  // enough stages that an SM holds at least 96 KB of ring, shared by the blocks its registers allow
+  // two blocks of 98 KB per SM (bf16, 128 elements), else three or four of 50 to 66 KB, as registers allow
   static constexpr int STAGES = STAGE >= 8192 ? 3 : STAGE >= 4096 ? 4 : 6;
   static constexpr int MERGE = NW * ROWS * (HD + 2) * 4;
   static constexpr int SMEM = NW * STAGES * STAGE > MERGE ? NW * STAGES * STAGE : MERGE;
@@ -118,14 +118,13 @@ template <int N> __device__ __forceinline__ void load_run(const Rows& t, long lo
 // grid (tiles_per_seq * n_kv_heads * n_seqs, splits).  Sequences with rows_below query rows or more are another kernel's.  Split z takes keys [z * chunk, (z + 1) * chunk), the last one all that follow.
 // Several splits leave partial results (accumulator, maximum, sum) of the rows they see and the block that arrives last at a
 // unit's counter adds them in split order, so the result does not depend on who came when.
-template <typename TC, int HD, int NW>
-__global__ void __launch_bounds__(32 * NW)
+template <typename TC, int HD>
+__global__ void __launch_bounds__(ap::THREADS)
 paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC* __restrict__ Kp, const TC* __restrict__ Vp,
                        const float* __restrict__ Ksc, const float* __restrict__ Vsc, int group, float scale_log2, bool q_vec,
                        int tiles_per_seq, int rows_below, int chunk, float* part_acc, float* part_ml, int* __restrict__ counters) {
   using namespace ap;
-  using S = Shape<TC, HD, NW>;
-  constexpr int THREADS = 32 * NW;
+  using S = Shape<TC, HD>;
   extern __shared__ __align__(128) unsigned char ap_smem[];
   __shared__ int sm_last;
 

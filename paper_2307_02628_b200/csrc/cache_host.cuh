@@ -10,6 +10,7 @@ struct sd_cache {
   size_t layer_bytes, v_off, ks_off, vs_off;   // K pool, V pool, K scales, V scales: offsets within a layer
   size_t minus_pos, last_row, part_acc, part_ml, counters, status_off, total;
   sd::EncodeTiledFn encode = nullptr;
+  int tile_blocks[9] = {};   // blocks per SM of each form of the kernel for few rows
   unsigned long long tile_ready = 0;    // bit per kernel whose shared-memory size has been allowed on this device
   char* layer(int l) const { return arena + (size_t)l * layer_bytes; }
   template <typename T> T* at(size_t off) const { return reinterpret_cast<T*>(arena + off); }
@@ -188,11 +189,11 @@ int cache_read(sd_cache* c, int l, const sd_batch* b, const sd_heads* k, const s
   });
 }
 
-// Keys per split for `units` blocks over up to max_len keys each, `rows` query rows in all.  The blocks that an SM holds (three)
-// should all have work, and the last wave should not be long: splitting stops at 256 keys, below which a block's start
-// and end outweigh its walk.
-int pick_split(const sd_cache* c, long units, long rows, int64_t max_len) {
-  const long slots = 3L * c->sm_count;
+// Keys per split for `units` blocks over up to max_len keys each, `rows` query rows in all, `slots` blocks at a time on the device.
+// All of them should have work, and the last wave should not be long: three single tokens over 50 000..61 000 positions in
+// bf16 take 120 us with 12 splits (288 blocks, 296 slots), 135 with 18, 149 with 32; splitting stops at 256 keys, below which
+// a block's start and end outweigh its walk.
+int pick_split(long slots, long units, long rows, int64_t max_len) {
   int best = 1;
   double best_cost = 1e30;
   for (int splits = 1; splits <= 512; splits = splits < 4 ? splits + 1 : splits + splits / 4) {
@@ -206,13 +207,18 @@ int pick_split(const sd_cache* c, long units, long rows, int64_t max_len) {
 }
 
 // Sequences of rows_below query rows per key head or more are left out (another kernel takes them).
-template <typename TC, int HD, int NW>
+template <typename TC, int HD>
 int attention_tiles(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale_log2, const sd_heads* out, int64_t rows_below) {
-  using S = sd::ap::Shape<TC, HD, NW>;
-  constexpr unsigned long long bit = 1ull << ((NW == 4 ? 0 : 9) + (HD == 128 ? 0 : HD == 64 ? 1 : 2) + 3 * (std::is_same<TC, bf16>::value ? 0 : std::is_same<TC, int8_t>::value ? 1 : 2));
-  auto kernel = sd::paged_attn_tile_kernel<TC, HD, NW>;
+  using S = sd::ap::Shape<TC, HD>;
+  constexpr int index = (HD == 128 ? 0 : HD == 64 ? 1 : 2) + 3 * (std::is_same<TC, bf16>::value ? 0 : std::is_same<TC, int8_t>::value ? 1 : 2);
+  constexpr unsigned long long bit = 1ull << index;
+  auto kernel = sd::paged_attn_tile_kernel<TC, HD>;
   if (!(c->tile_ready & bit)) {
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) != cudaSuccess) { cudaGetLastError(); return SD_ERR_CUDA; }
+    int per_sm = 0;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) != cudaSuccess ||
+        cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 100) != cudaSuccess ||
+        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, sd::ap::THREADS, S::SMEM) != cudaSuccess) { cudaGetLastError(); return SD_ERR_CUDA; }
+    c->tile_blocks[index] = std::max(per_sm, 1);
     c->tile_ready |= bit;
   }
   const auto P = pools<TC>(c, l);
@@ -220,18 +226,12 @@ int attention_tiles(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, fl
   const int64_t units = (int64_t)tiles * c->cfg.n_kv_heads * b->n_seqs;
   if (units > 0x7fffffff) return SD_ERR_ARG;
   const int max_len = b->max_len > 0 ? b->max_len : b->pages_per_seq * c->cfg.page_len;
-  const int chunk = getenv("SD_CH") ? atoi(getenv("SD_CH")) : pick_split(c, (long)units, (long)b->n_tokens * c->cfg.n_heads, max_len);
+  const int chunk = pick_split((long)c->tile_blocks[index] * c->sm_count, (long)units, (long)b->n_tokens * c->cfg.n_heads, max_len);
   const int splits = (int)(((int64_t)max_len + chunk - 1) / chunk);
-  kernel<<<dim3((unsigned)units, splits), 32 * NW, S::SMEM, c->stream>>>(
+  kernel<<<dim3((unsigned)units, splits), sd::ap::THREADS, S::SMEM, c->stream>>>(
       view_of(c, b), rows_of(q), rows_of(out), (const TC*)P.k, (const TC*)P.v, (const float*)P.ks, (const float*)P.vs, c->group, scale_log2, wide(q),
       tiles, (int)std::min<int64_t>(rows_below, 0x7fffffff), chunk, c->at<float>(c->part_acc), c->at<float>(c->part_ml), c->at<int>(c->counters));
   return launched();
-}
-
-template <typename TC, int HD>
-int attention_few(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale_log2, const sd_heads* out, int64_t rows_below) {
-  if (getenv("SD_NW2")) return attention_tiles<TC, HD, 2>(c, l, b, q, scale_log2, out, rows_below);
-  return attention_tiles<TC, HD, 4>(c, l, b, q, scale_log2, out, rows_below);
 }
 
 // A bf16 pool as [n_pages * n_kv_heads][page_len][HD], boxes of one page by 64 elements (128 bytes, swizzled).
@@ -291,10 +291,10 @@ int cache_attention(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, fl
             // max_new is only a bound: which kernel takes a sequence is decided on the device, by its own rows
             const int rc = attention_chunks<TC, HD>(c, l, b, q, scale_log2, out, b->n_seqs == 1 ? 1 : kChunkRows);
             if (rc != SD_OK || b->n_seqs == 1) return rc;
-            return attention_few<TC, HD>(c, l, b, q, scale_log2, out, kChunkRows);
+            return attention_tiles<TC, HD>(c, l, b, q, scale_log2, out, kChunkRows);
           }
         }
-        return attention_few<TC, HD>(c, l, b, q, scale_log2, out, most + 1);
+        return attention_tiles<TC, HD>(c, l, b, q, scale_log2, out, most + 1);
       }
     });
   });
