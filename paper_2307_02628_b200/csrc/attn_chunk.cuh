@@ -8,8 +8,7 @@
 // Tensor memory holds for each tile S of two halves (64 columns each) and O (HD columns).  S of half i + 2 takes the columns of half i
 // once the product that reads P there has completed, so the scores of the next half are there when a softmax is done with one, and the
 // tensor core works through both tiles' softmax.  (Scores of 128 keys at a time leave no columns for a second set: every
-// softmax then waited for its two products, 1500 of 3700 clocks.)  The order of issue, PV_0(i) S_1(i+1) PV_1(i) S_0(i+2), keeps a product of
-// the other tile between a PV and the S that waits for it.
+// softmax then waited for its two products, 1500 of 3700 clocks.)
 //
 // Operands are bf16: queries and weights are rounded once to 8 bits of significand, codes of 8-bit caches are bf16 numbers
 // exactly.  A result in 16 bits keeps no more; results wanted in fp32 go to the kernel for few rows.  A key's scale (8-bit
@@ -22,7 +21,7 @@
 // 2 x (768 + 512) clocks of the tensor core at HD = 128 (64 x 128 x 16 reads its operands for 48 clocks, not 32).
 //
 // Warps: 0-3 and 4-7 softmax of tile 0 and 1 (one thread per row, which is a lane of tensor memory), 8-11 loaders (page
-// look-up, copies into the swizzled layout the tensor core reads, conversion of codes), 12 issues the products.
+// look-up, copies into the swizzled layout the tensor core reads, conversion of codes), 12 and 13 issue the products of tile 0 and 1.
 // Every wait is bounded; on expiry the block records it, waits (bounded) for the products in flight and frees its tensor memory.
 #pragma once
 #include "attn_paged.cuh"
@@ -143,7 +142,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   using L = Layout<HD>;
   constexpr bool SCALED = CacheType<TC>::TOP > 0.f;
   extern __shared__ unsigned char ac_smem[];
-  __shared__ uint64_t bars[4 * STAGES + 12 + SIDE];
+  __shared__ uint64_t bars[4 * STAGES + 13 + SIDE];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_word;
 
@@ -193,18 +192,18 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   unsigned char* base_ptr = ac_smem + (base - raw);
   const uint32_t bar0 = (uint32_t)__cvta_generic_to_shared(bars);
   const uint32_t kfull = bar0, kempty = kfull + 8 * STAGES, vfull = kempty + 8 * STAGES, vempty = vfull + 8 * STAGES;
-  const uint32_t sfull = vempty + 8 * STAGES, pready = sfull + 32, odone = pready + 32, qfull = odone + 16, drain = qfull + 8, sidefull = drain + 8;
+  const uint32_t sfull = vempty + 8 * STAGES, pready = sfull + 32, odone = pready + 32, qfull = odone + 16, drain = qfull + 8, sidefull = drain + 16;
   volatile int* abort_flag = &abort_word;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
-      tc::mbar_init(kfull + 8 * s, 4); tc::mbar_init(kempty + 8 * s, 1);
-      tc::mbar_init(vfull + 8 * s, 4); tc::mbar_init(vempty + 8 * s, 1);
+      tc::mbar_init(kfull + 8 * s, 4); tc::mbar_init(kempty + 8 * s, 2);
+      tc::mbar_init(vfull + 8 * s, 4); tc::mbar_init(vempty + 8 * s, 2);
     }
     for (int i = 0; i < 4; ++i) { tc::mbar_init(sfull + 8 * i, 1); tc::mbar_init(pready + 8 * i, 4); }      // tile t, half h: 2 t + h
     for (int t = 0; t < 2; ++t) tc::mbar_init(odone + 8 * t, 1);
     tc::mbar_init(qfull, 8);
-    tc::mbar_init(drain, 1);
+    tc::mbar_init(drain, 1); tc::mbar_init(drain + 8, 1);
     for (int i = 0; i < SIDE; ++i) tc::mbar_init(sidefull + 8 * i, 4);
     abort_word = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -353,7 +352,10 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       if (lane == 0) arrive(pready + 8 * (2 * t + h));
     }
     if (n_rows[t] > 0 && ok) {
-      if (n_keys[t] > 0) {
+      // the last two products with the values one after the other: a wait looks at a phase's parity, and while the one before the last
+      // is running, the last one's parity is that of a phase long past
+      if (n_keys[t] > 1) ok = __all_sync(0xffffffffu, tc::mbar_wait(odone + 8 * t, (n_keys[t] - 2) & 1, abort_flag, b.status));
+      if (ok && n_keys[t] > 0) {
         ok = __all_sync(0xffffffffu, tc::mbar_wait(odone + 8 * t, (n_keys[t] - 1) & 1, abort_flag, b.status));
         fence_after();
       }
@@ -410,16 +412,20 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       const bool on = j * KEYS + key < most && ((pages_ok >> (key >> 3)) & 1u);
       return on ? pool + b.entry(page, g_head, j * KEYS + key) * HD + c * (16 / E) : nullptr;
     };
-    auto begin_side = [&](int j, int page, uint32_t pages_ok) {
+    // this thread's key's scales, zeros where there is none
+    auto ask_scales = [&](int j, int page, uint32_t pages_ok) {
+      page = __shfl_sync(0xffffffffu, page, (tid >> 3) & 15);
+      if (!(j * KEYS + tid < most && ((pages_ok >> (tid >> 3)) & 1u))) return make_float2(0.f, 0.f);
+      const size_t e = b.entry(page, g_head, j * KEYS + tid);
+      return make_float2(__ldg(Ksc + e), __ldg(Vsc + e));
+    };
+    auto begin_side = [&](int j, float2 scales, uint32_t pages_ok) {
       float* side = reinterpret_cast<float*>(base_ptr + L::SIDE_OFF + (j & (SIDE - 1)) * L::SIDE_BYTES);
       if (tid == 0) *reinterpret_cast<uint32_t*>(side + 2 * KEYS) = pages_ok;
       if (pages_ok != 0xffffu && w == 0 && lane == 0) b.bad();
       if (SCALED) {
-        page = __shfl_sync(0xffffffffu, page, (tid >> 3) & 15);
-        const bool on = j * KEYS + tid < most && ((pages_ok >> (tid >> 3)) & 1u);
-        const size_t e = on ? b.entry(page, g_head, j * KEYS + tid) : 0;
-        side[tid] = on ? Ksc[e] * fabsf(scale_log2) : 0.f;
-        side[KEYS + tid] = on ? Vsc[e] : 0.f;
+        side[tid] = scales.x * fabsf(scale_log2);
+        side[KEYS + tid] = scales.y;
       }
       __syncwarp();
       if (lane == 0) arrive(sidefull + 8 * (j % SIDE));
@@ -464,7 +470,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         const bool whole = use_maps && (j + 1) * KEYS <= most && pages_ok == 0xffffu;
         const uint32_t kt = base + L::K + (j % STAGES) * L::TILE, vt = base + L::V + (j % STAGES) * L::TILE;
         if (!(ok = wait_free(kempty, j))) break;
-        begin_side(j, page, pages_ok);
+        begin_side(j, make_float2(0.f, 0.f), pages_ok);
         if (whole) fetch(&map_k, kt, kfull, j, page);
         else copy(Kp, kt, j, page, pages_ok);
         if (!(ok = wait_free(vempty, j))) break;
@@ -510,16 +516,20 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       };
       int page = page_next;
       uint32_t pages_ok = exists(0, page);
+      float2 scales = ask_scales(0, page, pages_ok);
       request(Kp, k, 0, page, pages_ok);
       request(Vp, v, 0, page, pages_ok);
       page_next = look_up(1);
       for (int j = 0; j < n_tiles; ++j) {
         const uint32_t pages_next = exists(j + 1, page_next);
         if (!(ok = wait_free(kempty, j))) break;
-        begin_side(j, page, pages_ok);
+        begin_side(j, scales, pages_ok);
         convert(k, base + L::K + (j % STAGES) * L::TILE);
         announce(kfull, j);
-        if (j + 1 < n_tiles) request(Kp, k, j + 1, page_next, pages_next);
+        if (j + 1 < n_tiles) {
+          scales = ask_scales(j + 1, page_next, pages_next);
+          request(Kp, k, j + 1, page_next, pages_next);
+        }
         if (!(ok = wait_free(vempty, j))) break;
         convert(v, base + L::V + (j % STAGES) * L::TILE);
         announce(vfull, j);
@@ -531,81 +541,75 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PRODUCT_REGS));
-    if (warp == 12 && n_tiles > 0) {
-      // ---- products
+    if (warp < 14 && n_tiles > 0) {
+      // ---- products: one warp per tile of rows, so that neither waits for the other's softmax
       constexpr uint32_t id_s = idesc(HALF, false), id_o = idesc(HD, true);
-      const int halves[2] = {uniform(n_keys[0]), uniform(n_keys[1])};
+      const int t = warp - 12, tiles = uniform(n_tiles), halves = uniform(t ? n_keys[1] : n_keys[0]);
       const uint32_t tm = uniform(tmem), at = uniform(base), bar = uniform(bar0);
       auto wait = [&](uint32_t which, int phase) { return tc::mbar_wait(bar + (which - bar0), phase & 1, abort_flag, b.status); };
       if (elect()) {
-      // each of these announces its completion, and that of everything before it, on the barrier named
-      auto product_s = [&](int t, int i) {
-        const int h = i & 1;
-        const uint64_t qa = tc::smem_desc(at + L::Q + t * L::TILE), ka = tc::smem_desc(at + L::K + ((i >> 1) % STAGES) * L::TILE + h * (HALF * 128));
+        // each of these announces its completion, and that of everything before it, on the barrier named
+        const uint64_t qa = tc::smem_desc(at + L::Q + t * L::TILE);
+        auto product_s = [&](int i) {
+          const int h = i & 1;
+          const uint64_t ka = tc::smem_desc(at + L::K + ((i >> 1) % STAGES) * L::TILE + h * (HALF * 128));
 #pragma unroll
-        for (int k = 0; k < HD / 16; ++k) {                       // descriptors count 16-byte units
-          const uint32_t off = ((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4;
-          mma_ss(tm + t * 128 + h * HALF, qa + off, ka + off, id_s, k > 0);
+          for (int k = 0; k < HD / 16; ++k) {                     // descriptors count 16-byte units
+            const uint32_t off = ((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4;
+            mma_ss(tm + t * 128 + h * HALF, qa + off, ka + off, id_s, k > 0);
+          }
+          tc::umma_commit(bar + (sfull - bar0) + 8 * (2 * t + h));
+        };
+        auto product_o = [&](int i) {
+          const int h = i & 1;
+          const uint64_t va = v_desc(at + L::V + ((i >> 1) % STAGES) * L::TILE + h * (HALF * 128), 128 * 128);
+          const uint32_t first = i > 0;
+#pragma unroll
+          for (int k = 0; k < HALF / 16; ++k)
+            mma_ts(tm + L::O_COL + t * HD, tm + t * 128 + h * HALF + k * 8, va + k * (2048 >> 4), id_o, k > 0 ? 1u : first);
+          tc::umma_commit(bar + (odone - bar0) + 8 * t);
+        };
+        auto announce = [&](uint32_t which) { tc::umma_commit(bar + (which - bar0)); };
+        // the scores of half i, i >= 2, in the columns of half i - 2.  Products with other accumulators are not ordered among each
+        // other: its product with the values must have completed.
+        auto next_s = [&](int i) {
+          if (!wait(odone + 8 * t, i - 2)) return false;
+          fence_after();
+          product_s(i);
+          return true;
+        };
+        auto next_o = [&](int i) {
+          if (!wait(pready + 8 * (2 * t + (i & 1)), i >> 1)) return false;
+          fence_after();
+          product_o(i);
+          return true;
+        };
+        bool ok = wait(qfull, 0) && wait(kfull, 0);
+        if (ok) {
+          fence_after();
+          if (halves > 0) product_s(0);
+          if (halves > 1) product_s(1);
+          announce(kempty);
         }
-        tc::umma_commit(bar + (sfull - bar0) + 8 * (2 * t + h));
-      };
-      auto product_o = [&](int t, int i) {
-        const int h = i & 1;
-        const uint64_t va = v_desc(at + L::V + ((i >> 1) % STAGES) * L::TILE + h * (HALF * 128), 128 * 128);
-        const uint32_t first = i > 0;
-#pragma unroll
-        for (int k = 0; k < HALF / 16; ++k)
-          mma_ts(tm + L::O_COL + t * HD, tm + t * 128 + h * HALF + k * 8, va + k * (2048 >> 4), id_o, k > 0 ? 1u : first);
-        tc::umma_commit(bar + (odone - bar0) + 8 * t);
-      };
-      auto announce = [&](uint32_t which) { tc::umma_commit(bar + (which - bar0)); };
-      bool ok = wait(qfull, 0);
-      if (ok) ok = wait(kfull, 0);
-      if (ok) {
-        fence_after();
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int t = 0; t < 2; ++t)
-            if (i < halves[t]) product_s(t, i);
-        announce(kempty);
-      }
-      int k_there = 0;                                            // the last tile of keys known to have arrived
-      // the scores of half i, i >= 2, in the columns of half i - 2.  Products with other accumulators are not ordered among each
-      // other: its product with the values must have completed.
-      auto next_s = [&](int t, int i) {
-        const int j = i >> 1;
-        if (j > k_there) {
-          if (!wait(kfull + 8 * (j % STAGES), j / STAGES)) return false;
-          k_there = j;
+        // every tile of keys is waited for and given back by both warps, also where this one's rows see no more: a warp that
+        // gave stages back ahead of the loaders would stand in for the other
+        for (int j = 0; j < tiles && ok; ++j) {
+          ok = wait(vfull + 8 * (j % STAGES), j / STAGES);
+          if (ok && 2 * j < halves) ok = next_o(2 * j);
+          if (ok && j + 1 < tiles) {
+            ok = wait(kfull + 8 * ((j + 1) % STAGES), (j + 1) / STAGES);
+            if (ok && 2 * j + 2 < halves) ok = next_s(2 * j + 2);
+          }
+          if (ok && 2 * j + 1 < halves) ok = next_o(2 * j + 1);
+          if (ok) announce(vempty + 8 * (j % STAGES));
+          if (ok && 2 * j + 3 < halves) ok = next_s(2 * j + 3);
+          if (ok && j + 1 < tiles) announce(kempty + 8 * ((j + 1) % STAGES));
         }
-        if (!wait(odone + 8 * t, i - 2)) return false;
-        fence_after();
-        product_s(t, i);
-        return true;
-      };
-      auto next_o = [&](int t, int i) {
-        if (!wait(pready + 8 * (2 * t + (i & 1)), i >> 1)) return false;
-        fence_after();
-        product_o(t, i);
-        return true;
-      };
-      const int most = max(halves[0], halves[1]);
-      for (int i = 0; i < most && ok; ++i) {
-        const int j = i >> 1;
-        if (!(i & 1)) ok = wait(vfull + 8 * (j % STAGES), j / STAGES);
-        if (ok && i < halves[0]) ok = next_o(0, i);
-        if (ok && i > 0 && i + 1 < halves[1]) ok = next_s(1, i + 1);
-        if (ok && i > 0 && !(i & 1)) announce(kempty + 8 * (j % STAGES));
-        if (ok && i < halves[1]) ok = next_o(1, i);
-        if (ok && i + 2 < halves[0]) ok = next_s(0, i + 2);
-        if (ok && ((i & 1) || i + 1 == most)) announce(vempty + 8 * (j % STAGES));
-      }
-      if (!ok) {                                                  // let what has been issued finish before the memory goes
-        announce(drain);
-        const long long t0 = clock64();
-        while (!tc::mbar_try(drain, 0) && clock64() - t0 < tc::kWaitLimit) {}
-      }
+        if (!ok) {                                                // let what has been issued finish before the memory goes
+          announce(drain + 8 * t);
+          const long long t0 = clock64();
+          while (!tc::mbar_try(drain + 8 * t, 0) && clock64() - t0 < tc::kWaitLimit) {}
+        }
       }
       __syncwarp();
     }

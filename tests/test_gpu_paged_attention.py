@@ -244,3 +244,24 @@ def test_same_call_twice_gives_the_same_bits():
         for _ in range(5):
             assert torch.equal(one, cache.attention(0, q, lay.batch()))
         cache.close()
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
+@pytest.mark.parametrize("hd,page", [(64, 16), (128, 8), (128, 64)])
+def test_many_runs_of_a_mixed_batch_agree(cache_dtype, hd, page):
+    # blocks of every length side by side, two hundred times: a result that is read before its last product shows here
+    new, length = [1, 33, 64, 130, 0, 5, 2, 300, 256, 129], [70, 33, 65, 200, 40, 3, 0, 900, 1024, 3000]
+    lay = P.Layout(new, length, page, seed=1)
+    cache = P.make_cache(lay, 4, 1, hd, cache_dtype)
+    contents = P.fill(cache, lay, seed=2)
+    q = torch.randn(lay.n_tokens, 4, hd, generator=torch.Generator().manual_seed(3)).bfloat16()
+    dev, b = q.cuda(), lay.batch()
+    one = cache.attention(0, dev, b)
+    want, parts = P.attention(q, contents, lay, hd ** -0.5, 4)
+    lim = P.bound(want, parts, *rels(hd, cache_dtype, torch.bfloat16, torch.bfloat16), torch.bfloat16)
+    assert bool(((one.cpu().double() - want).abs() <= lim).all())
+    out = torch.empty_like(one)
+    for _ in range(20 if cache_dtype == "fp32" else 200):
+        assert torch.equal(cache.attention(0, dev, b, out=out), one)
+    assert cache.status() == 0
+    cache.close()
