@@ -348,14 +348,17 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       l += a0 + a1;
       tmem_wait_st();
       fence_before();
+      // The last half waits here for the product before its own, so that the wait after the loop is for the phase in progress or
+      // the one before: a wait looks at a phase's parity only, and one for a phase two back would never end.
+      if (i > 0 && i + 1 == n_keys[t]) {
+        ok = __all_sync(0xffffffffu, tc::mbar_wait(odone + 8 * t, (i - 1) & 1, abort_flag, b.status));
+        if (!ok) break;
+      }
       __syncwarp();
       if (lane == 0) arrive(pready + 8 * (2 * t + h));
     }
     if (n_rows[t] > 0 && ok) {
-      // the last two products with the values one after the other: a wait looks at a phase's parity, and while the one before the last
-      // is running, the last one's parity is that of a phase long past
-      if (n_keys[t] > 1) ok = __all_sync(0xffffffffu, tc::mbar_wait(odone + 8 * t, (n_keys[t] - 2) & 1, abort_flag, b.status));
-      if (ok && n_keys[t] > 0) {
+      if (n_keys[t] > 0) {
         ok = __all_sync(0xffffffffu, tc::mbar_wait(odone + 8 * t, (n_keys[t] - 1) & 1, abort_flag, b.status));
         fence_after();
       }

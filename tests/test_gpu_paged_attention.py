@@ -265,3 +265,19 @@ def test_many_runs_of_a_mixed_batch_agree(cache_dtype, hd, page):
         assert torch.equal(cache.attention(0, dev, b, out=out), one)
     assert cache.status() == 0
     cache.close()
+
+
+@pytest.mark.parametrize("cache_dtype,hd", [("bf16", 128), ("e4m3", 64)])
+def test_no_wait_runs_out_when_the_gpu_is_full(cache_dtype, hd):
+    # more blocks than processors and several heads, a hundred times: a wait for a phase that has been passed shows as a bad status
+    new = [40 + (37 * i) % 290 for i in range(32)]
+    lay = P.Layout(new, [n + (211 * i) % 1200 for i, n in enumerate(new)], 32, seed=4)
+    cache = P.make_cache(lay, 8, 4, hd, cache_dtype)
+    P.fill(cache, lay, seed=5)
+    dev, b = torch.randn(lay.n_tokens, 8, hd, generator=torch.Generator().manual_seed(6)).bfloat16().cuda(), lay.batch()
+    one = cache.attention(0, dev, b)
+    out = torch.empty_like(one)
+    for _ in range(100):
+        assert torch.equal(cache.attention(0, dev, b, out=out), one)
+    assert cache.status() == 0
+    cache.close()
