@@ -345,10 +345,13 @@ int sd_cache_read(sd_cache *c, int layer, const sd_batch *batch, const sd_heads 
  * attends to positions 0..p,
  *   out[r, h] = sum_j softmax_j(scale * q[r, h] . K[j, g]) V[j, g],  g = h / (n_heads / n_kv_heads).
  * q, out: rows [n_tokens, n_heads, head_dim].  scale: finite; 0 stands for head_dim^-1/2.  Single tokens, chunks
- * and both in one call.  Sums and softmax statistics are fp32. */
+ * and both in one call.  Sums and softmax statistics are fp32.  The result of a query row with a NaN is NaN, with an
+ * infinity NaN or 0; other rows and heads do not see it. */
 int sd_cache_attention(sd_cache *c, int layer, const sd_batch *batch, const sd_heads *q, float scale, const sd_heads *out);
 
-/* Synchronises the stream, reads the cache's status word and clears it.  Returns SD_ERR_DEVICE when it was not 0. */
+/* Synchronises the stream, reads the cache's status word and clears it (not to be called in a capture).  Bits: 16 a batch
+ * description that is wrong, 64 an appended element that is not finite, 2 a bounded wait inside a kernel that expired, the
+ * results of that call being wrong.  Returns SD_ERR_DEVICE when it was not 0. */
 int sd_cache_status(sd_cache *c, int32_t *device_status);
 
 void sd_cache_destroy(sd_cache *c);

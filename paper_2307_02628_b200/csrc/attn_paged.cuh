@@ -458,7 +458,7 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
     int tok, hd;
     place(r, tok, hd);
     if (used_splits == 1) {
-      store_elem(out, (long long)tok * out.row_stride + hd * out.head_stride + c, L > 0.f ? a / L : 0.f);
+      store_elem(out, (long long)tok * out.row_stride + hd * out.head_stride + c, normalised(a, L));
     } else {
       const size_t slot = ((size_t)tok * (group * b.n_kv_heads) + hd) * splits + z;
       __stcg(part_acc + slot * HD + c, a);
@@ -488,7 +488,7 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
       L += __ldcg(part_ml + (slot0 + s) * 2 + 1) * f;
       a += __ldcg(part_acc + (slot0 + s) * HD + c) * f;
     }
-    store_elem(out, (long long)tok * out.row_stride + hd * out.head_stride + c, L > 0.f ? a / L : 0.f);
+    store_elem(out, (long long)tok * out.row_stride + hd * out.head_stride + c, normalised(a, L));
   }
 }
 

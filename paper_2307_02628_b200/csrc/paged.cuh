@@ -208,6 +208,9 @@ __device__ __forceinline__ void store_elem(const Rows& t, long long i, float v) 
   else static_cast<__half*>(t.data)[i] = __float2half_rn(sat_f16_nan(v));
 }
 
+// A result from its weighted sum and the sum of its weights: 0 where no key was seen, NaN where the query was not a number.
+__device__ __forceinline__ float normalised(float a, float l) { return l > 0.f ? a / l : (l == 0.f ? 0.f : l); }
+
 // ---- codes ------------------------------------------------------------------------------------
 
 __device__ __forceinline__ uint32_t e4m3_pair(float lo, float hi) {
@@ -484,7 +487,7 @@ paged_attn_row_kernel(const BatchView b, const Rows q, const Rows out, const TC*
     float a = 0.f;
 #pragma unroll
     for (int w = 0; w < NW; ++w) a += sm_acc[w][c] * exp2_safe(sm_m[w], M);
-    store_elem(out, (long long)r * out.row_stride + h * out.head_stride + c, L > 0.f ? a / L : 0.f);
+    store_elem(out, (long long)r * out.row_stride + h * out.head_stride + c, normalised(a, L));
   }
 }
 
