@@ -17,6 +17,8 @@
 // The running maximum is raised only when it would be passed by 2^8 (weights then reach 256, well inside bf16 and the fp32
 // sums): O_t is rescaled in tensor memory in the first tiles and hardly ever after.
 //
+// Where there are fewer blocks than SMs the keys are split over several, each of which leaves its rows' shares to a second kernel.
+//
 // What bounds it: for 128 keys the 2 x 128 x 128 weights take 2048 clocks on the unit that computes exponentials, and the products
 // 2 x (768 + 512) clocks of the tensor core at HD = 128 (64 x 128 x 16 reads its operands for 48 clocks, not 32).
 //
@@ -128,16 +130,21 @@ __device__ __forceinline__ void to_bf16(uint32_t w, uint32_t& lo, uint32_t& hi, 
   hi = pack_bf16(b.x, b.y);
 }
 
+// Splits that have keys, of `keys` keys.
+__device__ __forceinline__ int splits_of(int keys, int chunk, int splits) { return min(splits, (int)(((long long)keys + chunk - 1) / chunk)); }
+
 }  // namespace ac
 
-// grid: blocks_per_seq * n_kv_heads * n_seqs.  Sequences with fewer than rows_from query rows are another kernel's.
+// grid (blocks_per_seq * n_kv_heads * n_seqs, splits).  Sequences with fewer than rows_from query rows are another kernel's.  Split z takes
+// keys [z * chunk, (z + 1) * chunk), the last one all that follow; several leave partial results (accumulator, maximum, sum) of their rows
+// to paged_attn_join_kernel.
 // map_k, map_v: the pools as [n_pages * n_kv_heads][page_len][HD] with boxes of a page by 64 elements (bf16 only; use_maps 0: not made).
 template <typename TC, int HD>
 __global__ void __launch_bounds__(ac::THREADS, 1)
 paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, int use_maps,
                         const BatchView b, const Rows q, const Rows out, const TC* __restrict__ Kp, const TC* __restrict__ Vp,
                         const float* __restrict__ Ksc, const float* __restrict__ Vsc, int group, float scale_log2, bool q_vec, bool out_vec,
-                        int blocks_per_seq, int rows_from) {
+                        int blocks_per_seq, int rows_from, int chunk, float* part_acc, float* part_ml) {
   using namespace ac;
   using L = Layout<HD>;
   constexpr bool SCALED = CacheType<TC>::TOP > 0.f;
@@ -177,14 +184,21 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   const int row0 = (blocks - 1 - blk) * ROWS;                   // the rows that see most keys first
   if (row0 < 0) return;
   const long long pos_first = (long long)b.len[seq] - (f1 - f0);
-  int n_keys[2], n_rows[2];
+  const int splits = gridDim.y, z = blockIdx.y, key0 = z * chunk;  // key numbers below count from key0
+  int n_keys[2], n_rows[2], used_splits = 1;
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     n_rows[t] = max(0, min(TILE_ROWS, rows_all - row0 - t * TILE_ROWS));
     const int last = (row0 + t * TILE_ROWS + n_rows[t] - 1) / group;
-    const int keys = n_rows[t] ? (int)min(max(pos_first + last + 1, 0ll), (long long)len) : 0;
+    int keys = n_rows[t] ? (int)min(max(pos_first + last + 1, 0ll), (long long)len) : 0;
+    if (splits > 1) {
+      used_splits = max(used_splits, splits_of(keys, chunk, splits));
+      keys = max(keys - key0, 0);
+      if (z < splits - 1) keys = min(keys, chunk);
+    }
     n_keys[t] = (keys + HALF - 1) / HALF;                       // halves of key tiles; a later tile of rows sees no fewer
   }
+  if (z >= used_splits) return;
   const int n_tiles = (max(n_keys[0], n_keys[1]) + 1) / 2;
 
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
@@ -225,7 +239,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     const uint32_t s_addr = tmem + lanes + t * 128, o_addr = tmem + lanes + L::O_COL + t * HD;
     const int row = row0 + t * TILE_ROWS + min(r, max(n_rows[t] - 1, 0));
     const int token = row / group, head = g_head * group + row % group;
-    const int row_last = (int)max(min(pos_first + token, (long long)len - 1), -1ll);        // last key this row sees
+    const int row_last = (int)max(min(pos_first + token, (long long)len - 1), -1ll) - key0; // last key this row sees
     const float scale = fabsf(scale_log2), sign = scale_log2 < 0.f ? -1.f : 1.f;            // a negative scale turns the queries round
     if (n_rows[t] > 0) {
       const long long at = (long long)(f0 + token) * q.row_stride + head * q.head_stride;
@@ -255,7 +269,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
 
     // the keys that all 32 rows of the warp see: tiles below need no mask
     const int first_token = (row0 + t * TILE_ROWS + min((warp & 3) * 32, max(n_rows[t] - 1, 0))) / group;
-    const int all_see = (int)max(min(pos_first + first_token, (long long)len - 1), -1ll);
+    const int all_see = (int)max(min(pos_first + first_token, (long long)len - 1), -1ll) - key0;
     float m = -INFINITY, l = 0.f;                                // m in the units of the scores (bf16) or base-2 (8 bits)
     const float unit = SCALED ? 1.f : scale;                     // base-2 units per unit of m
     bool ok = true;
@@ -362,7 +376,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         ok = __all_sync(0xffffffffu, tc::mbar_wait(odone + 8 * t, (n_keys[t] - 1) & 1, abort_flag, b.status));
         fence_after();
       }
-      if (ok) {
+      if (ok && used_splits == 1) {
         const float inv = l > 0.f ? 1.f / l : 0.f;
         const long long at = (long long)(f0 + token) * out.row_stride + head * out.head_stride;
 #pragma unroll 1
@@ -388,6 +402,23 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
             }
           }
         }
+      } else if (ok) {
+        // the row's share: sums relative to the maximum, in base-2 units
+        const size_t slot = ((size_t)(f0 + token) * (group * b.n_kv_heads) + head) * splits + z;
+#pragma unroll 1
+        for (int c0 = 0; c0 < HD; c0 += 32) {
+          uint32_t v[32] = {};
+          if (n_keys[t] > 0) {
+            tc::tmem_ld32(o_addr + c0, v);
+            tmem_wait_ld();
+          }
+          if (r < n_rows[t]) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4)
+              __stcg(reinterpret_cast<float4*>(part_acc + slot * HD + c0 + i), make_float4(__uint_as_float(v[i]), __uint_as_float(v[i + 1]), __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])));
+          }
+        }
+        if (r < n_rows[t]) __stcg(reinterpret_cast<float2*>(part_ml + slot * 2), make_float2(m * unit, l));
       }
     }
   } else if (warp < 12) {
@@ -398,11 +429,11 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     constexpr int E = sizeof(TC), PER_ROW = HD * E / 16;          // 16-byte pieces of a stored key
     constexpr int ROWS_AT_ONCE = 32 / PER_ROW;                    // of a warp
     constexpr int STEPS = KEYS / (4 * ROWS_AT_ONCE);
-    const int most = min(len, n_tiles * KEYS);                    // keys past it are filled with zeros
+    const int most = min(len - key0, n_tiles * KEYS);             // keys past it are filled with zeros
     // lane i < 16 looks up the page of keys [8 i, 8 i + 8) of a tile
     auto look_up = [&](int j) {
       const int key = j * KEYS + (lane & 15) * 8;
-      return j < n_tiles && key < most ? table[key >> b.page_shift] : 0;
+      return j < n_tiles && key < most ? table[(key0 + key) >> b.page_shift] : 0;
     };
     auto exists = [&](int j, int page) {
       return __ballot_sync(0xffffffffu, (unsigned)page < (unsigned)b.n_pages || j * KEYS + (lane & 15) * 8 >= most) & 0xffffu;
@@ -413,13 +444,13 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     auto source = [&](const TC* pool, int j, int key, int page, uint32_t pages_ok) -> const TC* {
       page = __shfl_sync(0xffffffffu, page, key >> 3);
       const bool on = j * KEYS + key < most && ((pages_ok >> (key >> 3)) & 1u);
-      return on ? pool + b.entry(page, g_head, j * KEYS + key) * HD + c * (16 / E) : nullptr;
+      return on ? pool + b.entry(page, g_head, key0 + j * KEYS + key) * HD + c * (16 / E) : nullptr;
     };
     // this thread's key's scales, zeros where there is none
     auto ask_scales = [&](int j, int page, uint32_t pages_ok) {
       page = __shfl_sync(0xffffffffu, page, (tid >> 3) & 15);
       if (!(j * KEYS + tid < most && ((pages_ok >> (tid >> 3)) & 1u))) return make_float2(0.f, 0.f);
-      const size_t e = b.entry(page, g_head, j * KEYS + tid);
+      const size_t e = b.entry(page, g_head, key0 + j * KEYS + tid);
       return make_float2(__ldg(Ksc + e), __ldg(Vsc + e));
     };
     auto begin_side = [&](int j, float2 scales, uint32_t pages_ok) {
@@ -623,6 +654,50 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
   }
+}
+
+// Adds the shares of a row's splits, in split order.  grid (n_tokens, heads / 8): one warp per row, lane s holds split s's maximum and sum.
+// A launch of its own (7..12 us), so that all SMs take part: joined by the last block of each unit, 64 tokens of 32 heads over 60 000
+// positions in 16 splits took 158 us instead of 83.
+template <int HD>
+__global__ void __launch_bounds__(256)
+paged_attn_join_kernel(const BatchView b, const Rows out, int group, int rows_from, int chunk, int splits, const float* __restrict__ part_acc,
+                       const float* __restrict__ part_ml) {
+  int seq, pos;
+  const int tok = blockIdx.x, where = locate_row(b, tok, seq, pos);
+  if (where == ROW_PADDING) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, heads = group * b.n_kv_heads, head = blockIdx.y * 8 + warp;
+  if (head >= heads) return;
+  // the keys that the block of this row went over: those of its last row
+  const int f0 = b.first[seq], f1 = b.first[seq + 1], n_new = min(f1 - f0, min(b.max_new, b.n_tokens - f0)), rows_all = n_new * group;
+  if (rows_all < rows_from) return;
+  const int row = (tok - f0) * group + head % group, last = (min((row / ac::ROWS + 1) * ac::ROWS, rows_all) - 1) / group;
+  const int keys = (int)min(max((long long)b.len[seq] - (f1 - f0) + last + 1, 0ll), (long long)b.seq_len(seq));
+  const int used = ac::splits_of(keys, chunk, splits);
+  if (used <= 1) return;                                         // written by its block
+  const size_t slot = ((size_t)tok * heads + head) * splits;
+  const float2 ml = lane < used ? __ldg(reinterpret_cast<const float2*>(part_ml) + slot + lane) : make_float2(-INFINITY, 0.f);
+  float top = ml.x;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - top);
+  constexpr int PER = HD / 32;
+  float sum = 0.f, x[PER] = {};
+#pragma unroll 8
+  for (int k = 0; k < used; ++k) {
+    const float w = __shfl_sync(0xffffffffu, f, k);
+    sum += w * __shfl_sync(0xffffffffu, ml.y, k);
+    const float* src = part_acc + (slot + k) * HD + lane * PER;
+    if constexpr (PER == 4) {
+      const float4 a = __ldg(reinterpret_cast<const float4*>(src));
+      x[0] += w * a.x; x[1] += w * a.y; x[2] += w * a.z; x[3] += w * a.w;
+    } else {
+      const float2 a = __ldg(reinterpret_cast<const float2*>(src));
+      x[0] += w * a.x; x[1] += w * a.y;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < PER; ++k) store_elem(out, (long long)tok * out.row_stride + head * out.head_stride + lane * PER + k, normalised(x[k], sum));
 }
 
 }  // namespace sd

@@ -246,6 +246,22 @@ bool pool_map(const sd_cache* c, void* pool, CUtensorMap* out) {
                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The same for the kernel for chunks, one block per SM, in units of what a key costs it (17 ns for 256 rows).  A block's start and
+// end cost as much as 450 keys, 800 where it leaves a share of its rows, and the joining launch 480 (8 us).  Measured, unsplit and as
+// chosen: 64 new tokens of 32 heads over 8 key heads at position 60 000 in bf16 902 and 83 us (16 splits); 512 at 30 000 467 and
+// 257 (2); 256 tokens of 32 heads at 4096 in int8 82 and 36 (4); 300 of 32 heads at 1500 33 us whole, 35 in 2.
+// No more than 32 splits, one per lane of the warp that joins them.
+constexpr int64_t kNoSplit = 0x7fffff80;
+int64_t pick_chunk_split(int64_t slots, int64_t units, int64_t rows, int64_t max_len) {
+  int64_t best = kNoSplit, best_cost = (units + slots - 1) / slots * (max_len + 450);
+  for (int splits = 2; splits <= 32 && rows * splits <= kPartSlots; ++splits) {
+    const int64_t chunk = (max_len + splits * 128 - 1) / (splits * 128) * 128;
+    const int64_t cost = (units * splits + slots - 1) / slots * (chunk + 800) + 480;
+    if (cost < best_cost) { best_cost = cost; best = chunk; }
+  }
+  return best;
+}
+
 template <typename TC, int HD>
 int attention_chunks(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale_log2, const sd_heads* out, int rows_from) {
   using L = sd::ac::Layout<HD>;
@@ -263,9 +279,18 @@ int attention_chunks(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, f
   const int blocks = (int)(((int64_t)b->max_new * c->group + sd::ac::ROWS - 1) / sd::ac::ROWS);
   const int64_t grid = (int64_t)blocks * c->cfg.n_kv_heads * b->n_seqs;
   if (grid > 0x7fffffff) return SD_ERR_ARG;
-  kernel<<<(unsigned)grid, sd::ac::THREADS, L::SMEM, c->stream>>>(
+  // blocks that can have rows: max_new is a bound for every sequence, n_tokens one for all of them
+  const int64_t units = std::min(grid, ((int64_t)b->n_tokens * c->group / sd::ac::ROWS + b->n_seqs) * c->cfg.n_kv_heads);
+  const int64_t rows = (int64_t)b->n_tokens * c->cfg.n_heads;
+  const int64_t max_len = b->max_len > 0 ? b->max_len : (int64_t)b->pages_per_seq * c->cfg.page_len;
+  const int64_t chunk = pick_chunk_split(c->sm_count, units, rows, max_len);
+  const int splits = chunk == kNoSplit ? 1 : (int)((max_len + chunk - 1) / chunk);
+  kernel<<<dim3((unsigned)grid, splits), sd::ac::THREADS, L::SMEM, c->stream>>>(
       mk, mv, use_maps, view_of(c, b), rows_of(q), rows_of(out), (const TC*)P.k, (const TC*)P.v, (const float*)P.ks, (const float*)P.vs, c->group, scale_log2, wide(q), wide(out),
-      blocks, rows_from);
+      blocks, rows_from, (int)chunk, c->at<float>(c->part_acc), c->at<float>(c->part_ml));
+  if (splits > 1)
+    sd::paged_attn_join_kernel<HD><<<dim3(b->n_tokens, (c->cfg.n_heads + 7) / 8), 256, 0, c->stream>>>(
+        view_of(c, b), rows_of(out), c->group, rows_from, (int)chunk, splits, c->at<float>(c->part_acc), c->at<float>(c->part_ml));
   return launched();
 }
 
@@ -448,6 +473,10 @@ int sd_extend(sd_handle* h, sd_cache* c, const sd_batch* b, const int32_t* d_tok
   if (rc != SD_OK) return rc;
   if (b->n_tokens > h->A.rows_max || b->n_seqs > m.max_batch) return SD_ERR_CAPACITY;
   if (b->n_tokens == 0) return SD_OK;
+  int device = 0;                                               // the default stream is a stream of every device
+  const int found = device_of(h->arena, &device);
+  if (found != SD_OK) return found;
+  if (device != c->device) return SD_ERR_ARG;
   DeviceGuard guard(c->device);
   if (!guard.ok) return SD_ERR_CUDA;
   return m.dtype == SD_DTYPE_BF16 ? extend_layers<bf16>(h, c, b, d_tokens, n_active, warmup, d_logits)

@@ -281,3 +281,48 @@ def test_no_wait_runs_out_when_the_gpu_is_full(cache_dtype, hd):
         assert torch.equal(cache.attention(0, dev, b, out=out), one)
     assert cache.status() == 0
     cache.close()
+
+
+@pytest.mark.parametrize("cache_dtype", ["bf16", "int8", "e4m3"])
+@pytest.mark.parametrize("hd,heads,page", [(64, 4, 16), (128, 7, 64)])
+def test_chunks_whose_keys_are_split(cache_dtype, hd, heads, page):
+    # few query rows over long sequences: keys split over blocks, rows that see fewer keys than others, a sequence that sees none of the
+    # later splits, and rows without a place
+    run(cache_dtype, "bf16", heads, 1, hd, page, [100, 40, 300, 9], [2900, 2049, 300, 4], seed=hd, start=2, tail=1)
+    run(cache_dtype, "bf16", heads, 1, hd, page, [65], [3333], seed=hd + 1)
+
+
+@pytest.mark.parametrize("cache_dtype", ["bf16", "e4m3"])
+def test_the_length_hint_only_splits(cache_dtype):
+    lay = P.Layout([70, 1, 50], [2600, 2000, 1100], 32, seed=1)
+    cache = P.make_cache(lay, 4, 1, 64, cache_dtype)
+    contents = P.fill(cache, lay, seed=2)
+    q = torch.randn(lay.n_tokens, 4, 64, generator=torch.Generator().manual_seed(3)).bfloat16()
+    want, parts = P.attention(q, contents, lay, 0.125, 4)
+    lim = P.bound(want, parts, *rels(64, cache_dtype, q.dtype, q.dtype), q.dtype)
+    for hint in (0, 1, 1024, 2600, 1 << 30):                    # unknown, far too short, too short, right, far too long
+        b = lay.batch(max_len=hint)
+        one = cache.attention(0, q.cuda(), b)
+        assert bool(((one.cpu().double() - want).abs() <= lim).all()), hint
+        for _ in range(20):
+            assert torch.equal(cache.attention(0, q.cuda(), b), one)
+    assert cache.status() == 0
+    cache.close()
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
+@pytest.mark.parametrize("new,length", [([1, 1], [70, 3]), ([50, 1], [60, 9]), ([40, 2], [2100, 2]), ([1], [3000])])
+def test_a_query_that_is_not_a_number_spoils_its_own_row_only(cache_dtype, new, length):
+    lay = P.Layout(new, length, 16, seed=7)
+    cache = P.make_cache(lay, 2, 2, 64, cache_dtype)
+    contents = P.fill(cache, lay, seed=8)
+    q = torch.randn(lay.n_tokens, 2, 64, generator=torch.Generator().manual_seed(9)).bfloat16()
+    want, parts = P.attention(q, contents, lay, 0.125, 1)
+    lim = P.bound(want, parts, *rels(64, cache_dtype, q.dtype, q.dtype), q.dtype)
+    q[0, 1, 5] = float("nan")
+    got = cache.attention(0, q.cuda(), lay.batch()).cpu().double()
+    assert bool(torch.isnan(got[0, 1]).all())
+    got[0, 1] = want[0, 1]
+    assert bool(((got - want).abs() <= lim).all())
+    assert cache.status() == 0
+    cache.close()
