@@ -148,7 +148,7 @@ int launched() { return cudaGetLastError() == cudaSuccess ? SD_OK : SD_ERR_CUDA;
 
 // Rows of a block of the copying kernels, as a power of two: two, so that neighbouring rows' codes and scales are touched together,
 // where eight blocks per SM are left (24 sequences of 900..1500 positions read in int8: 140 us with one, 131 with two, 128 with
-// four; 4300 rows appended from fp32: 50, 51, 52 us; read into fp32: 38, 37, 40 us).
+// four; 4005 rows appended from fp32: 50, 51, 52 us; read into fp32: 38, 37, 40 us).
 int row_shift(const sd_cache* c, const sd_batch* b) { return b->n_tokens >= 16 * c->sm_count ? 1 : 0; }
 static_assert(sd::MOST_ROWS == 2, "rows of a block");
 

@@ -17,6 +17,11 @@
 //      are told apart by counting.
 // min-p is a threshold on w: the mass above it is a plain sum of step 2.  All three cut a prefix of the same order, so the kept
 // mass is the smallest of the three, and the draw needs no list of kept tokens.
+//
+// What bounds it: 256 rows of 50 272 logits take 66 us, two rounds of blocks; the bytes would take 8.  Half of a block's 62 000 clocks is
+// step 2, bound by instruction issue: some forty per logit, a third of them in double precision at half rate (sums in fp32 would not
+// place a border as 64-bit floating point does).  33 rows of 1021: 11 us, one row of 50 272 in 8 blocks: 18 us, a chain of
+// barriers and searches.
 #pragma once
 #include <cooperative_groups.h>
 #include <cstdint>
