@@ -498,7 +498,7 @@ class Decoder:
                out: torch.Tensor | None = None) -> torch.Tensor:
         """One token per row with the row's own settings (CUDA tensors [B], fp32, top_k int32; None: off)."""
         B = logits.shape[0]
-        index = self.device.index
+        index = self.arena.get_device()
         if logits.dtype != torch.float32 or logits.shape != (B, self.shape.vocab) or not logits.is_contiguous() or logits.get_device() != index:
             raise ValueError(f"logits must be a contiguous fp32 [{B}, {self.shape.vocab}] on {self.device}")
         if out is None:
@@ -529,8 +529,11 @@ class Decoder:
             raise ValueError(f"tokens must be [{batch.n_tokens}]")
         if logits is None:
             logits = torch.empty(batch.c.n_seqs, self.shape.vocab, dtype=torch.float32, device=self.device)
-        elif logits.shape != (batch.c.n_seqs, self.shape.vocab) or logits.dtype != torch.float32 or not logits.is_contiguous():
-            raise ValueError(f"logits must be a contiguous fp32 [{batch.c.n_seqs}, {self.shape.vocab}]")
+        elif logits.shape != (batch.c.n_seqs, self.shape.vocab) or logits.dtype != torch.float32 or not logits.is_contiguous() or \
+                logits.get_device() != self.arena.get_device():
+            raise ValueError(f"logits must be a contiguous fp32 [{batch.c.n_seqs}, {self.shape.vocab}] on {self.device}")
+        if batch.index != self.arena.get_device():
+            raise ValueError(f"the batch must be on {self.device}")
         self._order()
         _check(lib().sd_extend(self.h, cache.h, C.byref(batch.c), tokens.data_ptr(), self.shape.n_layers if n_active is None else n_active, warmup,
                                logits.data_ptr()), "sd_extend")

@@ -211,3 +211,23 @@ def test_refusals():
     dec.extend(good, b, ids + shape.vocab)
     assert dec.status() == binding.STATUS_BAD_TOKEN
     dec.close()
+
+
+def test_tensors_elsewhere_are_refused_and_launches_are_counted():
+    shape = BF16
+    dec = binding.Decoder(shape, synth.make_weights(shape, seed=1), 2, 16, 8)
+    cache = binding.PagedCache(3, 4, 4, 64, 16, 8, 4, 64, dtype="bf16", stream=dec.stream)
+    b = Pages(2, 4, 8, 16).grow([3, 2])
+    ids = torch.zeros(5, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        dec.extend(cache, b, ids, logits=torch.empty(2, shape.vocab))              # host memory
+    dec.extend(cache, b, ids)
+    n0 = dec.launch_count()
+    dec.extend(cache, b, ids)
+    # rows, embedding; per layer two LayerNorms, four products, append, attention; LayerNorm and LM head
+    assert dec.launch_count() - n0 == 2 + 3 * 8 + 2
+    dec.extend(cache, b, ids, n_active=2)
+    assert dec.launch_count() - n0 == 2 * (2 + 2) + (3 + 2) * 8
+    assert dec.status() == 0 and cache.status() == 0
+    cache.close()
+    dec.close()
