@@ -158,6 +158,8 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_word;
 
+  pdl_launch_dependents();                                       // the kernel for few rows of the same call may begin beside this one's last blocks
+
   // the block's rows.  The longest sequences come first, so that no long block is left to the end: sequence number `turn` in
   // order of decreasing length (a block counts for each of up to THREADS sequences how many are longer; more keep their order)
   const int g_head = blockIdx.x % b.n_kv_heads, rest = blockIdx.x / b.n_kv_heads;

@@ -100,6 +100,13 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+// Keeps a block, on every way out, until the kernel before has ended.  A launch that was allowed to begin early must not end first:
+// what follows it in the stream waits for it alone.
+struct UntilPredecessorEnds {
+  bool on;
+  __device__ __forceinline__ ~UntilPredecessorEnds() { if (on) pdl_wait(); }
+};
+
 // N consecutive elements of a row, any type; vec: 16-byte accesses are allowed
 template <int N> __device__ __forceinline__ void load_run(const Rows& t, long long at, bool vec, float (&o)[N]) {
   if (vec) {
@@ -124,15 +131,18 @@ template <int N> __device__ __forceinline__ void load_run(const Rows& t, long lo
 // [z * chunk, (z + 1) * chunk), the last one all that follow.
 // Several splits leave partial results (accumulator, maximum, sum) of the rows they see and the block that arrives last at a
 // unit's counter adds them in split order, so the result does not depend on who came when.
+// early: launched to begin once the kernel for chunks of the same call has no block left to start, whose last blocks it runs beside
+// (33 sequences of 11..329 new tokens in e4m3: 213 us a call, 221 one after the other).
 template <typename TC, int HD>
 __global__ void __launch_bounds__(ap::THREADS)
 paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC* __restrict__ Kp, const TC* __restrict__ Vp,
                        const float* __restrict__ Ksc, const float* __restrict__ Vsc, int group, float scale_log2, bool q_vec,
-                       int tiles_per_seq, int rows_below, int chunk, float* part_acc, float* part_ml, int* __restrict__ counters) {
+                       int tiles_per_seq, int rows_below, int chunk, float* part_acc, float* part_ml, int* __restrict__ counters, bool early) {
   using namespace ap;
   using S = Shape<TC, HD>;
   extern __shared__ __align__(128) unsigned char ap_smem[];
   __shared__ int sm_last;
+  const UntilPredecessorEnds hold{early && blockIdx.x == 0 && blockIdx.y == 0};
 
   const int unit = blockIdx.x, tile = unit % tiles_per_seq, g_head = (unit / tiles_per_seq) % b.n_kv_heads, seq = unit / tiles_per_seq / b.n_kv_heads;
   const int splits = gridDim.y, z = blockIdx.y;

@@ -11,6 +11,7 @@ struct sd_cache {
   size_t minus_pos, last_row, part_acc, part_ml, counters, status_off, total;
   sd::EncodeTiledFn encode = nullptr;
   int tile_blocks[9] = {};   // blocks per SM of each form of the kernel for few rows
+  int64_t launches = 0;      // kernels launched
   unsigned long long tile_ready = 0;    // bit per kernel whose shared-memory size has been allowed on this device
   char* layer(int l) const { return arena + (size_t)l * layer_bytes; }
   template <typename T> T* at(size_t off) const { return reinterpret_cast<T*>(arena + off); }
@@ -144,7 +145,10 @@ template <typename F> int with_head_dim(int hd, F f) {
   return hd == 128 ? f(std::integral_constant<int, 128>{}) : hd == 64 ? f(std::integral_constant<int, 64>{}) : f(std::integral_constant<int, 32>{});
 }
 
-int launched() { return cudaGetLastError() == cudaSuccess ? SD_OK : SD_ERR_CUDA; }
+int launched(sd_cache* c, int n = 1) {
+  c->launches += n;
+  return cudaGetLastError() == cudaSuccess ? SD_OK : SD_ERR_CUDA;
+}
 
 // Rows of a block of the copying kernels, as a power of two: two, so that neighbouring rows' codes and scales are touched together,
 // where eight blocks per SM are left (24 sequences of 900..1500 positions read in int8: 140 us with one, 131 with two, 128 with
@@ -164,7 +168,7 @@ int cache_append(sd_cache* c, int l, const sd_batch* b, const sd_heads* k, const
         auto kernel = vec ? sd::cache_append_kernel<TS, TC, HD, true> : sd::cache_append_kernel<TS, TC, HD, false>;
         const int shift = row_shift(c, b);
         kernel<<<((b->n_tokens - 1) >> shift) + 1, 256, 0, c->stream>>>(view_of(c, b), shift, rows_of(k), rows_of(v), P.k, P.v, P.ks, P.vs);
-        return launched();
+        return launched(c);
       });
     });
   });
@@ -183,7 +187,7 @@ int cache_read(sd_cache* c, int l, const sd_batch* b, const sd_heads* k, const s
         const int shift = row_shift(c, b);
         kernel<<<((b->n_tokens - 1) >> shift) + 1, 256, 0, c->stream>>>(view_of(c, b), shift, rows_of(k), rows_of(v), (const TC*)P.k, (const TC*)P.v,
                                                    (const float*)P.ks, (const float*)P.vs);
-        return launched();
+        return launched(c);
       });
     });
   });
@@ -208,7 +212,7 @@ int pick_split(long slots, long units, long rows, int64_t max_len) {
 
 // Sequences of rows_below query rows per key head or more are left out (another kernel takes them).
 template <typename TC, int HD>
-int attention_tiles(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale_log2, const sd_heads* out, int64_t rows_below) {
+int attention_tiles(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale_log2, const sd_heads* out, int64_t rows_below, bool early = false) {
   using S = sd::ap::Shape<TC, HD>;
   constexpr int index = (HD == 128 ? 0 : HD == 64 ? 1 : 2) + 3 * (std::is_same<TC, bf16>::value ? 0 : std::is_same<TC, int8_t>::value ? 1 : 2);
   constexpr unsigned long long bit = 1ull << index;
@@ -228,10 +232,10 @@ int attention_tiles(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, fl
   const int max_len = b->max_len > 0 ? b->max_len : b->pages_per_seq * c->cfg.page_len;
   const int chunk = pick_split((long)c->tile_blocks[index] * c->sm_count, (long)units, (long)b->n_tokens * c->cfg.n_heads, max_len);
   const int splits = (int)(((int64_t)max_len + chunk - 1) / chunk);
-  kernel<<<dim3((unsigned)units, splits), sd::ap::THREADS, S::SMEM, c->stream>>>(
+  sd::launch_kernel(early, c->stream, kernel, dim3((unsigned)units, splits), dim3(sd::ap::THREADS), S::SMEM,
       view_of(c, b), rows_of(q), rows_of(out), (const TC*)P.k, (const TC*)P.v, (const float*)P.ks, (const float*)P.vs, c->group, scale_log2, wide(q),
-      tiles, (int)std::min<int64_t>(rows_below, 0x7fffffff), chunk, c->at<float>(c->part_acc), c->at<float>(c->part_ml), c->at<int>(c->counters));
-  return launched();
+      tiles, (int)std::min<int64_t>(rows_below, 0x7fffffff), chunk, c->at<float>(c->part_acc), c->at<float>(c->part_ml), c->at<int>(c->counters), early);
+  return launched(c);
 }
 
 // A bf16 pool as [n_pages * n_kv_heads][page_len][HD], boxes of one page by 64 elements (128 bytes, swizzled).
@@ -263,7 +267,7 @@ int64_t pick_chunk_split(int64_t slots, int64_t units, int64_t rows, int64_t max
 }
 
 template <typename TC, int HD>
-int attention_chunks(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale_log2, const sd_heads* out, int rows_from) {
+int attention_chunks(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale_log2, const sd_heads* out, int rows_from, bool* split) {
   using L = sd::ac::Layout<HD>;
   constexpr unsigned long long bit = 1ull << (32 + (HD == 128 ? 0 : 1) + 2 * (std::is_same<TC, bf16>::value ? 0 : std::is_same<TC, int8_t>::value ? 1 : 2));
   auto kernel = sd::paged_attn_chunk_kernel<TC, HD>;
@@ -291,7 +295,8 @@ int attention_chunks(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, f
   if (splits > 1)
     sd::paged_attn_join_kernel<HD><<<dim3(b->n_tokens, (c->cfg.n_heads + 7) / 8), 256, 0, c->stream>>>(
         view_of(c, b), rows_of(out), c->group, rows_from, (int)chunk, splits, c->at<float>(c->part_acc), c->at<float>(c->part_ml));
-  return launched();
+  *split = splits > 1;
+  return launched(c, splits > 1 ? 2 : 1);
 }
 
 constexpr int kChunkRows = 33;   // query rows per key head from which a sequence goes to the kernel for chunks
@@ -307,16 +312,18 @@ int cache_attention(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, fl
         const auto P = pools<TC>(c, l);
         sd::paged_attn_row_kernel<TC, HD><<<dim3(b->n_tokens, c->cfg.n_heads), 128, 0, c->stream>>>(
             view_of(c, b), rows_of(q), rows_of(out), (const TC*)P.k, (const TC*)P.v, (const float*)P.ks, (const float*)P.vs, c->group, scale_log2);
-        return launched();
+        return launched(c);
       } else {
         const int64_t most = (int64_t)b->max_new * c->group;
         if (most > 0x7fffff00) return (int)SD_ERR_ARG;
         if constexpr (HD >= 64) {
           if (most >= kChunkRows && out->dtype != SD_DTYPE_FP32) {
             // max_new is only a bound: which kernel takes a sequence is decided on the device, by its own rows
-            const int rc = attention_chunks<TC, HD>(c, l, b, q, scale_log2, out, b->n_seqs == 1 ? 1 : kChunkRows);
+            bool split = false;
+            const int rc = attention_chunks<TC, HD>(c, l, b, q, scale_log2, out, b->n_seqs == 1 ? 1 : kChunkRows, &split);
             if (rc != SD_OK || b->n_seqs == 1) return rc;
-            return attention_tiles<TC, HD>(c, l, b, q, scale_log2, out, kChunkRows);
+            // it may begin early where the two do not share the workspace for split keys
+            return attention_tiles<TC, HD>(c, l, b, q, scale_log2, out, kChunkRows, !split);
           }
         }
         return attention_tiles<TC, HD>(c, l, b, q, scale_log2, out, most + 1);
@@ -337,6 +344,7 @@ int extend_layers(sd_handle* h, sd_cache* c, const sd_batch* b, const int32_t* d
   float* qkv = h->at<float>(h->A.qkv);
   T* o = h->at<T>(h->A.o);
   T* y = h->at<T>(h->A.y);
+  const int64_t before = c->launches;
   sd::cache_rows_kernel<<<rows, 128, 0, h->stream>>>(view_of(c, b), c->at<int>(c->minus_pos), c->at<int>(c->last_row));
   Lc.end();
   const sd::RowMap map{1, 0, 0, nullptr, nullptr, c->at<int>(c->minus_pos)};
@@ -353,14 +361,13 @@ int extend_layers(sd_handle* h, sd_cache* c, const sd_batch* b, const int32_t* d
     norm(h->ln1_g[l], h->ln1_b[l]);
     launch_gemm<T>(Lc, SD_K_GEMM_QKV, u, (const T*)h->w_qkv[l], h->A.wp_qkv[l], (const T*)h->b_qkv[l], rows, 3 * d, d, qkv, 3 * d, sd::EPI_STORE_F32);
     if (cache_append(c, l, b, &k, &v) != SD_OK || cache_attention(c, l, b, &q, 0.f, &out) != SD_OK) return SD_ERR_CUDA;
-    Lc.count += 2;
     launch_gemm<T>(Lc, SD_K_GEMM_OUT, o, (const T*)h->w_o[l], h->A.wp_o[l], (const T*)h->b_o[l], rows, d, d, x, d, sd::EPI_RESIDUAL_F32);
     norm(h->ln2_g[l], h->ln2_b[l]);
     launch_gemm<T>(Lc, SD_K_GEMM_FC1, u, (const T*)h->w_fc1[l], h->A.wp_fc1[l], (const T*)h->b_fc1[l], rows, f, d, y, f * sd::Operand<T>::PARTS, sd::EPI_RELU_T);
     launch_gemm<T>(Lc, SD_K_GEMM_FC2, y, (const T*)h->w_fc2[l], h->A.wp_fc2[l], (const T*)h->b_fc2[l], rows, d, f, x, d, sd::EPI_RESIDUAL_F32);
   }
   enqueue_head<T>(Lc, b->n_seqs, c->at<int>(c->last_row), d_logits);
-  h->launches += Lc.count;
+  h->launches += Lc.count + (c->launches - before);
   return Lc.err;
 }
 

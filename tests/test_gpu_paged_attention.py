@@ -326,3 +326,33 @@ def test_a_query_that_is_not_a_number_spoils_its_own_row_only(cache_dtype, new, 
     assert bool(((got - want).abs() <= lim).all())
     assert cache.status() == 0
     cache.close()
+
+
+@pytest.mark.parametrize("cache_dtype", ["bf16", "int8"])
+@pytest.mark.parametrize("new", [[1, 1], [140, 33]])
+def test_pages_past_32_bits_of_elements_and_shared_pages(cache_dtype, new):
+    # the same contents in the first pages of a small cache and in the last of a pool with more than 2^32 elements; there the
+    # second sequence's first page is the first sequence's
+    heads, kv, hd, page = 8, 8, 128, 128
+    many = (1 << 32) // (kv * page * hd) + 40
+    length = [300, 260]
+    g = torch.Generator().manual_seed(1)
+    k, v = (torch.randn(sum(length), kv, hd, generator=g).bfloat16() for _ in range(2))
+    k[300:300 + page], v[300:300 + page] = k[:page], v[:page]
+    q = torch.randn(sum(new), heads, hd, generator=g).bfloat16().cuda()
+    out = []
+    for n_pages, table in ((6, [[0, 1, 2], [3, 4, 5]]), (many, [[many - 1, many - 9, many - 2], [many - 1, many - 30, many - 5]])):
+        cache = binding.PagedCache(1, heads, kv, hd, page, n_pages, 4, 600, dtype=cache_dtype)
+        i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+        for s in range(2):                                         # one sequence per call: the shared page is written twice, alike
+            rows = slice(0, 300) if s == 0 else slice(300, 560)
+            b = binding.CacheBatch(i32([table[s]]), i32([0, length[s]]), i32([length[s]]), length[s], length[s])
+            cache.append(0, k[rows].cuda(), v[rows].cuda(), b)
+            rk, rv = cache.read(0, b)
+            assert torch.equal(rk.cpu(), P.stored(k[rows].float(), cache_dtype)) and torch.equal(rv.cpu(), P.stored(v[rows].float(), cache_dtype))
+        b = binding.CacheBatch(i32(table), i32([0, new[0], sum(new)]), i32(length), sum(new), max(new), max(length))
+        out.append(cache.attention(0, q, b))
+        assert cache.status() == 0
+        cache.close()
+        del cache
+    assert torch.equal(out[0], out[1])
