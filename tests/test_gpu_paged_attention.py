@@ -356,3 +356,34 @@ def test_pages_past_32_bits_of_elements_and_shared_pages(cache_dtype, new):
         cache.close()
         del cache
     assert torch.equal(out[0], out[1])
+
+
+@pytest.mark.parametrize("graphed", [False, True])
+@pytest.mark.parametrize("new", [[300] * 12, [300, 1] * 6])
+def test_what_follows_on_the_stream_sees_all_results(graphed, new):
+    # the second launch of a call may begin, and have nothing to do, before the first has ended; a copy queued right behind it waits for both
+    lay = P.Layout(new, [900] * 12, 32, seed=1)
+    cache = P.make_cache(lay, 16, 16, 64, "bf16")
+    P.fill(cache, lay, seed=2)
+    q = torch.randn(lay.n_tokens, 16, 64, generator=torch.Generator().manual_seed(3)).bfloat16().cuda()
+    b = lay.batch()
+    want = cache.attention(0, q, b).clone()
+    out, copy = torch.empty_like(want), torch.empty_like(want)
+    torch.cuda.synchronize()
+
+    def step():
+        out.zero_()
+        cache.attention(0, q, b, out=out)
+        copy.copy_(out)
+
+    with torch.cuda.stream(cache.stream):
+        if graphed:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=cache.stream):
+                step()
+        for _ in range(100):
+            copy.zero_()
+            graph.replay() if graphed else step()
+            assert torch.equal(copy, want)
+    assert cache.status() == 0
+    cache.close()
