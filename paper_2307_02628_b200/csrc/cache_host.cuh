@@ -299,7 +299,13 @@ int attention_chunks(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, f
   return launched(c, splits > 1 ? 2 : 1);
 }
 
-constexpr int kChunkRows = 33;   // query rows per key head from which a sequence goes to the kernel for chunks
+// Query rows per key head from which a sequence goes to the kernel for chunks, whose time hardly depends on them up to 256; the kernel for few
+// rows reads the keys again for every 8.  Measured, chunks against few rows: bf16, 16 sequences of 1024 positions, 32 heads of 128, 12 rows
+// 70 and 131 us, 32 rows 71 and 133; 2 of 4096, 8 heads, 12 rows 18 and 28; one of 30 000, one key head, 12 rows 26 and 151; 8 of 300,
+// 12 heads of 64, 12 rows 10 and 8.  In 8 bits, where the few rows' kernel has less to read and this one codes to convert: int8,
+// 64 of 4096 over 2 key heads of 128, 16 rows 111 and 82, 32 rows 111 and 140; e4m3, 16 of 1024, 32 heads of 64, 24 rows 75 and 66,
+// 32 rows 75 and 116.
+template <typename TC> constexpr int kChunkRows = sd::CacheType<TC>::TOP > 0.f ? 25 : 9;
 
 int cache_attention(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale, const sd_heads* out) {
   if (scale == 0.f) scale = 1.f / sqrtf((float)c->cfg.head_dim);
@@ -317,13 +323,13 @@ int cache_attention(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, fl
         const int64_t most = (int64_t)b->max_new * c->group;
         if (most > 0x7fffff00) return (int)SD_ERR_ARG;
         if constexpr (HD >= 64) {
-          if (most >= kChunkRows && out->dtype != SD_DTYPE_FP32) {
+          if (most >= kChunkRows<TC> && out->dtype != SD_DTYPE_FP32) {
             // max_new is only a bound: which kernel takes a sequence is decided on the device, by its own rows
             bool split = false;
-            const int rc = attention_chunks<TC, HD>(c, l, b, q, scale_log2, out, b->n_seqs == 1 ? 1 : kChunkRows, &split);
+            const int rc = attention_chunks<TC, HD>(c, l, b, q, scale_log2, out, b->n_seqs == 1 ? 1 : kChunkRows<TC>, &split);
             if (rc != SD_OK || b->n_seqs == 1) return rc;
             // it may begin early where the two do not share the workspace for split keys
-            return attention_tiles<TC, HD>(c, l, b, q, scale_log2, out, kChunkRows, !split);
+            return attention_tiles<TC, HD>(c, l, b, q, scale_log2, out, kChunkRows<TC>, !split);
           }
         }
         return attention_tiles<TC, HD>(c, l, b, q, scale_log2, out, most + 1);

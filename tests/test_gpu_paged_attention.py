@@ -292,6 +292,14 @@ def test_chunks_whose_keys_are_split(cache_dtype, hd, heads, page):
     run(cache_dtype, "bf16", heads, 1, hd, page, [65], [3333], seed=hd + 1)
 
 
+@pytest.mark.parametrize("cache_dtype", ["bf16", "int8", "e4m3"])
+@pytest.mark.parametrize("heads,kv_heads,hd", [(2, 2, 64), (12, 1, 128), (24, 1, 64), (25, 1, 64), (64, 2, 128)])
+def test_numbers_of_rows_at_which_the_kernel_changes(cache_dtype, heads, kv_heads, hd):
+    group = heads // kv_heads
+    run(cache_dtype, "bf16", heads, kv_heads, hd, 16, [-(-n // group) for n in (8, 9, 16, 17, 24, 25, 32, 33)], [40, 50, 60, 17, 300, 25, 33, 900], seed=heads)
+    run(cache_dtype, "bf16", heads, kv_heads, hd, 16, [1, 1, 1], [1, 700, 64], seed=heads + 1)
+
+
 @pytest.mark.parametrize("cache_dtype", ["bf16", "e4m3"])
 def test_the_length_hint_only_splits(cache_dtype):
     lay = P.Layout([70, 1, 50], [2600, 2000, 1100], 32, seed=1)
