@@ -282,10 +282,11 @@ sample_rows_kernel(const float* __restrict__ logits, int vocab, int part, int fr
   }
 
   if (greedy || !(m > -INFINITY) || m == INFINITY) {
-    // the lowest index of the maximum; uniform over the cluster
+    // the lowest index of the maximum; uniform over the cluster.  Where that is minus infinity every logit is one, NaN among them
+    const bool any = !(m > -INFINITY);
     int best = 0x7fffffff;
     for (int i = tid; i < R.n; i += THREADS)
-      if (__ldg(R.src + i) == m) { best = R.id0 + i; break; }
+      if (any || __ldg(R.src + i) == m) { best = R.id0 + i; break; }
     best = __reduce_min_sync(0xffffffffu, best);
     if (lane == 0) sh.redi[warp] = best;
     __syncthreads();

@@ -157,3 +157,20 @@ def test_agrees_with_the_scalar_call_and_with_greedy():
     assert torch.equal(dec.sample(logits, u, temperature=full(0.0)), g)
     assert torch.equal(dec.sample(logits, u, top_k=torch.ones(n, dtype=torch.int32, device="cuda")), g)
     dec.close()
+
+
+@pytest.mark.parametrize("vocab", [5, 700, 50272])
+@pytest.mark.parametrize("temperature", [1.0, 0.0])
+def test_rows_of_nan_and_minus_infinity_answer_their_first_token(vocab, temperature):
+    # NaN counts as minus infinity, so every token attains the maximum: the lowest index is 0, wherever the first true infinity is
+    rows = torch.full((4, vocab), float("-inf"))
+    rows[0, 0] = float("nan")
+    rows[1, :vocab - 1] = float("nan")
+    rows[2, 1] = float("nan")
+    rows[3, :2] = float("nan")
+    dec = make(vocab, 4)
+    for u in (0.0, 0.9):
+        got = check(dec, rows, torch.full((4,), u), temperature=torch.full((4,), temperature))
+        assert got.tolist() == [0, 0, 0, 0]
+    assert dec.status() == 0
+    dec.close()
