@@ -302,7 +302,7 @@ typedef struct {
   const int32_t *pages;      /* [n_seqs, pages_per_seq] */
   const int32_t *first;      /* [n_seqs + 1], first[0] >= 0, not decreasing */
   const int32_t *len;        /* [n_seqs] */
-  int32_t n_seqs, pages_per_seq;
+  int32_t n_seqs, pages_per_seq;  /* pages_per_seq * page_len: at most 2^30 positions */
   int32_t n_tokens;          /* rows of the tensors; 0: the call does nothing */
   int32_t max_new;           /* most new tokens of a sequence */
   int32_t max_len;           /* longest len, or 0 when it is not known: pages_per_seq * page_len.  It only guides how the

@@ -135,9 +135,6 @@ __device__ __forceinline__ void to_bf16(uint32_t w, uint32_t& lo, uint32_t& hi, 
   hi = pack_bf16(b.x, b.y);
 }
 
-// Splits that have keys, of `keys` keys.
-__device__ __forceinline__ int splits_of(int keys, int chunk, int splits) { return min(splits, (int)(((long long)keys + chunk - 1) / chunk)); }
-
 }  // namespace ac
 
 // grid (blocks_per_seq * n_kv_heads * n_seqs, splits).  Sequences with fewer than rows_from query rows are another kernel's.  Split z takes
@@ -199,7 +196,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     const int last = (row0 + t * TILE_ROWS + n_rows[t] - 1) / group;
     int keys = n_rows[t] ? (int)min(max(pos_first + last + 1, 0ll), (long long)len) : 0;
     if (splits > 1) {
-      used_splits = max(used_splits, splits_of(keys, chunk, splits));
+      used_splits = max(used_splits, ap::splits_of(keys, chunk, splits));
       keys = max(keys - key0, 0);
       if (z < splits - 1) keys = min(keys, chunk);
     }
@@ -680,7 +677,7 @@ paged_attn_join_kernel(const BatchView b, const Rows out, int group, int rows_fr
   if (rows_all < rows_from) return;
   const int row = (tok - f0) * group + head % group, last = (min((row / ac::ROWS + 1) * ac::ROWS, rows_all) - 1) / group;
   const int keys = (int)min(max((long long)b.len[seq] - (f1 - f0) + last + 1, 0ll), (long long)b.seq_len(seq));
-  const int used = ac::splits_of(keys, chunk, splits);
+  const int used = ap::splits_of(keys, chunk, splits);
   if (used <= 1) return;                                         // written by its block
   const size_t slot = ((size_t)tok * heads + head) * splits;
   const float2 ml = lane < used ? __ldg(reinterpret_cast<const float2*>(part_ml) + slot + lane) : make_float2(-INFINITY, 0.f);

@@ -107,6 +107,9 @@ struct UntilPredecessorEnds {
   __device__ __forceinline__ ~UntilPredecessorEnds() { if (on) pdl_wait(); }
 };
 
+// Splits that have keys, of `keys` keys; chunk may come from a length that the caller only guessed, up to 2^31.
+__device__ __forceinline__ int splits_of(int keys, int chunk, int splits) { return min(splits, (int)(((long long)keys + chunk - 1) / chunk)); }
+
 // N consecutive elements of a row, any type; vec: 16-byte accesses are allowed
 template <int N> __device__ __forceinline__ void load_run(const Rows& t, long long at, bool vec, float (&o)[N]) {
   if (vec) {
@@ -161,7 +164,7 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
   const long long pos_first = (long long)b.len[seq] - (f1 - f0);            // position of the first new token, negative without a place
   const int last_token = (tile * ROWS + n_rows - 1) / group;
   const int key_end = (int)min(max(pos_first + last_token + 1, 0ll), (long long)len);      // keys that any row of the tile sees
-  const int used_splits = max(1, min(splits, (key_end + chunk - 1) / chunk));
+  const int used_splits = max(1, splits_of(key_end, chunk, splits));
   if (z >= used_splits) return;
   const int k0 = z * chunk, k1 = z == splits - 1 ? key_end : min(k0 + chunk, key_end);
 

@@ -21,6 +21,9 @@ struct sd_cache {
 namespace {
 
 constexpr int kPartSlots = 32768;      // 17 MB of head size 128
+// Positions that a table may reach.  Key numbers are 32-bit in the kernels, which round them up to whole tiles and look table entries
+// up some thousands of keys ahead: sums of a position below this and of such distances, or of two positions, do not wrap.
+constexpr int64_t kMostPositions = 1 << 30;
 
 // Makes `device` current for the length of a call.
 struct DeviceGuard {
@@ -85,7 +88,7 @@ bool carve_cache(const sd_cache_config& c, sd_cache& A) {
 int check_batch(const sd_cache* c, const sd_batch* b) {
   if (!b || !b->pages || !b->first || !b->len) return SD_ERR_ARG;
   if (b->n_seqs < 1 || b->pages_per_seq < 1 || b->n_tokens < 0 || b->max_len < 0) return SD_ERR_ARG;
-  if ((int64_t)b->pages_per_seq * c->cfg.page_len > 0x7fffffff) return SD_ERR_ARG;
+  if ((int64_t)b->pages_per_seq * c->cfg.page_len > kMostPositions) return SD_ERR_ARG;
   if (b->n_seqs > c->cfg.max_seqs || b->n_tokens > c->cfg.max_tokens) return SD_ERR_CAPACITY;
   if (b->n_tokens > 0 && (b->max_new < 1 || b->max_new > b->n_tokens)) return SD_ERR_ARG;
   return SD_OK;

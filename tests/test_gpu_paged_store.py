@@ -263,3 +263,33 @@ def test_refusals():
     assert cache.attention(0, q[:0], none).shape == (0, 4, 64)
     assert cache.status() == 0
     cache.close()
+
+
+@pytest.mark.parametrize("cache_dtype", ["fp32", "int8"])
+def test_tables_reach_at_most_two_to_the_thirtieth_positions(cache_dtype):
+    # key numbers are 32-bit in the kernels; the table's entries past the sequence's end are not read, so none have to be there
+    lay = P.Layout([2], [9], 16)
+    cache = P.make_cache(lay, 2, 2, 64, cache_dtype)
+    x = torch.ones(2, 2, 64, device="cuda")
+    L = binding.lib()
+    rows = binding.SdHeads(x.data_ptr(), x.stride(0), x.stride(1), binding.SD_DTYPE_FP32)
+    b = lay.batch()
+    cache.append(0, x, x, b)
+    for columns, code in (((1 << 30) // 16, binding.SD_OK), ((1 << 30) // 16 + 1, binding.SD_ERR_ARG), ((1 << 31) // 16 - 1, binding.SD_ERR_ARG)):
+        c = binding.SdBatch.from_buffer_copy(b.c)
+        c.pages_per_seq = columns
+        for call in (lambda: L.sd_cache_append(cache.h, 0, C.byref(c), C.byref(rows), C.byref(rows)),
+                     lambda: L.sd_cache_read(cache.h, 0, C.byref(c), C.byref(rows), C.byref(rows)),
+                     lambda: L.sd_cache_attention(cache.h, 0, C.byref(c), C.byref(rows), 0.0, C.byref(rows))):
+            assert call() == code
+    torch.cuda.synchronize()
+    # the length hint may be anything: it only guides how the work is split
+    pool = P.fill(cache, lay, seed=3)
+    q = torch.randn(2, 2, 64, generator=torch.Generator().manual_seed(4))
+    want, parts = P.attention(q, pool, lay, 0.125, 1)
+    lim = P.bound(want, parts, 2.0 ** -15, 2.0 ** -15, torch.float32)      # operands of 16 bits (2^-16), the sums' roundings below that
+    for hint in (0, 9, 2 ** 31 - 1):
+        got = cache.attention(0, q.cuda(), lay.batch(max_len=hint)).cpu().double()
+        assert bool(((got - want).abs() <= lim).all())
+    assert cache.status() == 0
+    cache.close()
