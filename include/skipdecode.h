@@ -278,7 +278,8 @@ int sd_sample(sd_handle *h, const float *d_logits, int B, const sd_sampling *set
  *
  * Streams and workspaces: work is enqueued on the stream given to sd_cache_create, calls return without synchronising,
  * and every call may be captured into a CUDA graph on that stream.  All calls of one object share its workspace:
- * they, and replays of graphs captured from them, must not run at the same time (one stream, or events between two). */
+ * they, and replays of graphs captured from them, must not run at the same time (one stream, or events between two).
+ * Threads: calls of one object may come from several threads; each is enqueued as a whole, one after the other. */
 typedef struct sd_cache sd_cache;
 
 typedef struct {

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import threading
 
 import torch
 
@@ -207,11 +208,21 @@ class CacheBatch:
         self.ref = C.addressof(self.c)
 
 
+class _Described(threading.local):
+    """The two tensors of a call as the library takes them: a pair for each thread, since other threads run between the filling and
+    the call (new structures for every call take 0.5 us longer)."""
+
+    def __init__(self):
+        self.pair = (SdHeads(), SdHeads())
+        self.refs = tuple(C.addressof(t) for t in self.pair)
+
+
 class PagedCache:
     """A paged KV cache (sd_cache) in an arena of its own.
 
     dtype: "fp32", "bf16", "int8" or "e4m3".  Calls are enqueued on `stream` (default: a stream of its own).  When torch's current
     stream is another one, the two are ordered around every call, so tensors can be used as if the call ran on the current one.
+    Several threads may call one cache; each call's work is enqueued as a whole.
     """
 
     def __init__(self, n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, page_len: int, n_pages: int,
@@ -237,8 +248,7 @@ class PagedCache:
         L = lib()
         self._append, self._read, self._attention = L.sd_cache_append, L.sd_cache_read, L.sd_cache_attention
         self._heads, self._kv_heads, self._head_dim = n_heads, n_kv_heads, head_dim
-        self._tensors = (SdHeads(), SdHeads())
-        self._refs = tuple(C.addressof(t) for t in self._tensors)
+        self._described = _Described()
 
     def layer(self, layer: int) -> dict:
         """Views of one layer's pools: k, v [n_pages, n_kv_heads, page_len, head_dim], in 8 bits also k_scale, v_scale."""
@@ -312,14 +322,14 @@ class PagedCache:
         except Exception:
             pass
 
-    # describes a tensor in one of the two structures that a call passes on (they are read during the call only)
+    # describes a tensor in one of this thread's two structures that a call passes on (they are read during the call only)
     def _rows(self, which: int, name: str, t: torch.Tensor, heads: int, batch: CacheBatch):
         code = _ROW_TYPES.get(t.dtype)
         if code is None or t.get_device() != self._index or batch.index != self._index:
             raise ValueError(f"{name} must be an fp32, bf16 or fp16 tensor on {self.device}, and so must the batch be there")
         if t.shape != (batch.n_tokens, heads, self._head_dim):
             raise ValueError(f"{name} must be [{batch.n_tokens}, {heads}, {self._head_dim}], got {tuple(t.shape)}")
-        r = self._tensors[which]
+        r = self._described.pair[which]
         r.row_stride, r.head_stride, step = t.stride()
         if step != 1 and t.numel():
             raise ValueError(f"{name}'s elements of a head must be adjacent, got strides {t.stride()}")
@@ -330,7 +340,8 @@ class PagedCache:
         other = _raw_stream(self._index) != self._raw
         if other:
             self._fork()
-        code = fn(self.h, layer, batch.ref, self._refs[0], *scale, self._refs[1])
+        first, second = self._described.refs
+        code = fn(self.h, layer, batch.ref, first, *scale, second)
         if code != SD_OK:
             raise SdError(code, name)
         if other:

@@ -1,7 +1,9 @@
 // Host side of the paged cache and of sd_extend: argument checks, arena carving, kernel choice.  Part of skipdecode.cu.
 #pragma once
+#include <mutex>
 
 struct sd_cache {
+  std::mutex busy;           // held while a call enqueues: the launches of one call share a workspace and stay together
   sd_cache_config cfg;
   int esize, page_shift, group, device, sm_count;
   bool scaled;
@@ -439,7 +441,9 @@ int sd_cache_append(sd_cache* c, int layer, const sd_batch* b, const sd_heads* k
   if (k->dtype != v->dtype) return SD_ERR_ARG;
   if (b->n_tokens == 0) return SD_OK;
   DeviceGuard guard(c->device);
-  return guard.ok ? cache_append(c, layer, b, k, v) : SD_ERR_CUDA;
+  if (!guard.ok) return SD_ERR_CUDA;
+  std::lock_guard<std::mutex> lock(c->busy);
+  return cache_append(c, layer, b, k, v);
 }
 
 int sd_cache_read(sd_cache* c, int layer, const sd_batch* b, const sd_heads* k, const sd_heads* v) {
@@ -451,7 +455,9 @@ int sd_cache_read(sd_cache* c, int layer, const sd_batch* b, const sd_heads* k, 
   if (k->dtype != v->dtype) return SD_ERR_ARG;
   if (b->n_tokens == 0) return SD_OK;
   DeviceGuard guard(c->device);
-  return guard.ok ? cache_read(c, layer, b, k, v) : SD_ERR_CUDA;
+  if (!guard.ok) return SD_ERR_CUDA;
+  std::lock_guard<std::mutex> lock(c->busy);
+  return cache_read(c, layer, b, k, v);
 }
 
 int sd_cache_attention(sd_cache* c, int layer, const sd_batch* b, const sd_heads* q, float scale, const sd_heads* out) {
@@ -462,14 +468,18 @@ int sd_cache_attention(sd_cache* c, int layer, const sd_batch* b, const sd_heads
   if (rc != SD_OK) return rc;
   if (b->n_tokens == 0) return SD_OK;
   DeviceGuard guard(c->device);
-  return guard.ok ? cache_attention(c, layer, b, q, scale, out) : SD_ERR_CUDA;
+  if (!guard.ok) return SD_ERR_CUDA;
+  std::lock_guard<std::mutex> lock(c->busy);
+  return cache_attention(c, layer, b, q, scale, out);
 }
 
 int sd_cache_status(sd_cache* c, int32_t* device_status) {
   if (!c) return SD_ERR_ARG;
   DeviceGuard guard(c->device);
   int32_t v = 0;
-  if (!guard.ok || cudaMemcpyAsync(&v, c->status(), 4, cudaMemcpyDeviceToHost, c->stream) != cudaSuccess ||
+  if (!guard.ok) return SD_ERR_CUDA;
+  std::lock_guard<std::mutex> lock(c->busy);                    // reading and clearing stay together
+  if (cudaMemcpyAsync(&v, c->status(), 4, cudaMemcpyDeviceToHost, c->stream) != cudaSuccess ||
       cudaMemsetAsync(c->status(), 0, 4, c->stream) != cudaSuccess || cudaStreamSynchronize(c->stream) != cudaSuccess) {
     cudaGetLastError();
     return SD_ERR_CUDA;
@@ -495,6 +505,7 @@ int sd_extend(sd_handle* h, sd_cache* c, const sd_batch* b, const int32_t* d_tok
   if (device != c->device) return SD_ERR_ARG;
   DeviceGuard guard(c->device);
   if (!guard.ok) return SD_ERR_CUDA;
+  std::lock_guard<std::mutex> lock(c->busy);
   return m.dtype == SD_DTYPE_BF16 ? extend_layers<bf16>(h, c, b, d_tokens, n_active, warmup, d_logits)
                                   : extend_layers<float>(h, c, b, d_tokens, n_active, warmup, d_logits);
 }

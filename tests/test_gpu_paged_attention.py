@@ -395,3 +395,35 @@ def test_what_follows_on_the_stream_sees_all_results(graphed, new):
             assert torch.equal(copy, want)
     assert cache.status() == 0
     cache.close()
+
+
+@pytest.mark.parametrize("cache_dtype", ["bf16", "int8"])
+def test_threads_may_share_a_cache(cache_dtype):
+    # calls of two launches that pass shares of split keys on through the cache's workspace: they must stay together
+    import threading
+    lay = P.Layout([70, 1], [2600, 900], 32, seed=1)
+    cache = P.make_cache(lay, 4, 1, 64, cache_dtype)
+    P.fill(cache, lay, seed=2)
+    g = torch.Generator().manual_seed(3)
+    b = lay.batch()
+    queries = [torch.randn(lay.n_tokens, 4, 64, generator=g).bfloat16().cuda() for _ in range(4)]
+    want = [cache.attention(0, q, b) for q in queries]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(i):
+        with torch.cuda.stream(cache.stream):
+            out = torch.empty_like(want[i])
+            for _ in range(100):
+                cache.attention(0, queries[i], b, out=out)
+                if not torch.equal(out, want[i]):
+                    wrong.append(i)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+    assert cache.status() == 0
+    cache.close()

@@ -109,3 +109,44 @@ def test_plain_selection_against_direct_enumeration():
                 want = i
                 break
         assert P.select(x, u, T, k, p, mp) == order[want]
+
+
+def test_threads_that_share_a_cache_hand_over_their_own_tensors(monkeypatch):
+    # the library's call is replaced by a function that looks at the pointers it is given; layer names the thread
+    from types import SimpleNamespace
+    import sys
+    import threading
+    monkeypatch.setattr(binding, "_raw_stream", lambda index: 0)
+    tensors = [(torch.zeros(2, 3, 4), torch.zeros(2, 3, 4)) for _ in range(4)]
+    wrong, calls = [], []
+
+    @C.CFUNCTYPE(C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p)
+    def append(h, layer, batch, k, v):
+        got = tuple(binding.SdHeads.from_address(p).data for p in (k, v))
+        calls.append(layer)
+        if got != tuple(t.data_ptr() for t in tensors[layer]):
+            wrong.append((layer, got))
+        return binding.SD_OK
+
+    cache = object.__new__(binding.PagedCache)
+    cache.h, cache._append, cache._index, cache._raw, cache.device = None, append, -1, 0, "cpu"
+    cache._kv_heads, cache._head_dim = 3, 4
+    cache._described = binding._Described()
+    batch = SimpleNamespace(n_tokens=2, index=-1, ref=0)
+
+    def work(i):
+        for _ in range(3000):
+            cache.append(i, *tensors[i], batch)
+
+    interval = sys.getswitchinterval()
+    sys.setswitchinterval(1e-6)
+    try:
+        threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+    finally:
+        sys.setswitchinterval(interval)
+    assert len(calls) == 12000
+    assert not wrong, (len(wrong), wrong[0])
