@@ -1,0 +1,92 @@
+"""Attention of chunks over a paged cache, held to a limit that one missing key exceeds (see paged_bounds): the kernel for many query
+rows, its split keys, masks, missing pages, scales and both ways in which pages reach it."""
+import pytest
+import torch
+
+import paged_bounds as B
+import paged_reference as P
+from paper_2307_02628_b200 import binding
+
+pytestmark = pytest.mark.gpu
+
+CACHES = ("bf16", "int8", "e4m3")
+
+
+def run(cache_dtype, heads, kv_heads, hd, page, new, length, scale=None, seed=0, io="bf16", out_dtype=None, gone=(), max_new=None, max_len=None, k_gain=1.0, **kw):
+    """gone: (sequence, column) of table entries that are made to name no page."""
+    lay = P.Layout(new, length, page, seed=seed, **kw)
+    cache = P.make_cache(lay, heads, kv_heads, hd, cache_dtype)
+    contents = P.fill(cache, lay, seed=seed + 1, k_gain=k_gain)
+    q = torch.randn(lay.n_tokens, heads, hd, generator=torch.Generator().manual_seed(seed + 2)).to(P.TORCH[io])
+    pages, exists = lay.pages.clone(), [torch.ones(l, dtype=torch.bool) for l in length]
+    for i, (s, column) in enumerate(gone):
+        pages[s, column] = (-1, lay.n_pages, 1 << 30)[i % 3]
+        exists[s][column * page:(column + 1) * page] = False
+    b = binding.CacheBatch(pages.cuda(), lay.first.cuda(), lay.len.cuda(), lay.n_tokens, max_new or max(new), max(length) if max_len is None else max_len)
+    out = torch.full(q.shape, 9.0, dtype=P.TORCH[out_dtype or io], device="cuda")
+    cache.attention(0, q.cuda(), b, scale=scale, out=out)
+    status = cache.status()
+    again = torch.full_like(out, 9.0)
+    cache.attention(0, q.cuda(), b, scale=scale, out=again)
+    assert torch.equal(out, again)
+    cache.close()
+    assert status == (binding.STATUS_BAD_BATCH if gone else 0)
+    want, R, terms = B.reference(q, contents, lay, hd ** -0.5 if scale is None else scale, heads // kv_heads, exists)
+    own = torch.zeros(lay.n_tokens, dtype=torch.bool)
+    for s in range(len(new)):
+        own[int(lay.first[s]):int(lay.first[s + 1])] = True
+    got = out.cpu()
+    assert bool((got[~own] == 9).all())
+    over = B.over(got, want, R, terms, hd, q.dtype)[own]
+    assert not bool(torch.isnan(over).any())
+    assert float(over.max()) <= 1, (float(over.max()), float(over.median()), int(over.argmax()))
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
+@pytest.mark.parametrize("hd,heads,page", [(64, 4, 16), (64, 4, 128), (128, 7, 64), (128, 4, 8)])
+def test_split_keys(cache_dtype, hd, heads, page):
+    run(cache_dtype, heads, 1, hd, page, [100, 40, 300, 9], [2900, 2049, 300, 4], seed=hd, start=2, tail=1)
+    run(cache_dtype, heads, 1, hd, page, [65], [3333], seed=hd + 1)
+    run(cache_dtype, heads, 1, hd, page, [33, 8], [4097, 2560], seed=hd + 2, max_len=1500)      # longer than the hint: the last split takes the rest
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("new,length", [([128], [128]), ([127], [255]), ([129], [129]), ([256, 1], [513, 511]), ([300], [700]), ([64, 257], [64, 258]),
+                                         ([65, 130, 191], [193, 320, 191])])
+def test_borders_of_tiles(cache_dtype, hd, new, length):
+    for page in (8, 32, 128):
+        run(cache_dtype, 2, 2, hd, page, new, length, seed=sum(new) + page)
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
+def test_chunks_beside_single_tokens(cache_dtype):
+    run(cache_dtype, 8, 4, 64, 16, [1] * 20 + [200] + [1] * 3 + [40, 0], [17 * i + 1 for i in range(20)] + [700, 1, 1000, 64, 41, 5], seed=3)
+    run(cache_dtype, 8, 2, 128, 32, [1, 150, 1], [2500, 190, 33], seed=4, tail=2)
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
+@pytest.mark.parametrize("hd", [64, 128])
+def test_one_sequence_of_few_rows_under_a_larger_bound(cache_dtype, hd):
+    run(cache_dtype, 2, 2, hd, 16, [3], [700], seed=5, tail=60, max_new=60)
+    run(cache_dtype, 2, 2, hd, 16, [1], [3001], seed=6, tail=60, max_new=60)
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("scale,k_gain", [(0.05, 1.0), (-0.3, 1.0), (-0.02, 3.0), (1.0, 0.5), (1e-7, 1e6), (3e4, 1e-6)])
+def test_scales(cache_dtype, hd, scale, k_gain):
+    run(cache_dtype, 2, 1, hd, 16, [40, 70, 1], [50, 300, 90], scale=scale, k_gain=k_gain, seed=11)
+    run(cache_dtype, 2, 1, hd, 64, [60], [2100], scale=scale, k_gain=k_gain, seed=12)
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("page", [8, 16, 64, 128])
+def test_pages_that_do_not_exist(cache_dtype, hd, page):
+    # in the first tile, between whole tiles, a whole tile, the one that holds a row's own key; nothing left for the first rows
+    n = 700 // page
+    run(cache_dtype, 2, 2, hd, page, [50, 60], [700, 90], gone=[(0, 0), (0, n // 2), (0, n)], seed=page)
+    run(cache_dtype, 2, 2, hd, page, [130], [700], gone=[(0, c) for c in range(128 // page, 256 // page)] + [(0, n)], seed=page + 1)
+    run(cache_dtype, 2, 2, hd, page, [150, 150], [150, 150], gone=[(0, c) for c in range(1 + 64 // page)] + [(1, 1)], seed=page + 2)
+    run(cache_dtype, 2, 2, hd, page, [40], [3000], gone=[(0, 1000 // page), (0, 2999 // page)], seed=page + 3)      # split keys
