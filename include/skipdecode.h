@@ -347,8 +347,8 @@ int sd_cache_read(sd_cache *c, int layer, const sd_batch *batch, const sd_heads 
  *   out[r, h] = sum_j softmax_j(scale * q[r, h] . K[j, g]) V[j, g],  g = h / (n_heads / n_kv_heads).
  * q, out: rows [n_tokens, n_heads, head_dim].  scale: finite; 0 stands for head_dim^-1/2.  Single tokens, chunks
  * and both in one call.  Sums and softmax statistics are fp32.  Over an fp32 cache nothing is rounded before the output; over the
- * others queries and weights enter the products with 16 bits or more where out is fp32, and may enter as bf16 where it is
- * not.  max_len, and how many rows a sequence brings, choose the kernel and the split: results of the same row under other values agree
+ * others queries and weights enter the products with 16 bits or more, except that the weights may enter as bf16 where
+ * both q and out are bf16.  max_len, and how many rows a sequence brings, choose the kernel and the split: results of the same row under other values agree
  * within that rounding, under the same values bit for bit.  The result of a query row with a NaN is NaN, with an
  * infinity NaN or 0; other rows and heads do not see it. */
 int sd_cache_attention(sd_cache *c, int layer, const sd_batch *batch, const sd_heads *q, float scale, const sd_heads *out);

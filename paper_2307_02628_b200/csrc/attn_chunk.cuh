@@ -1,6 +1,6 @@
 // Attention of chunks of new tokens over a paged cache in bf16 or 8 bits, on the fifth-generation tensor cores.
 //
-// One block per (sequence, key head, 256 query rows); a query row is a (token, head of the group) pair, so grouped heads share
+// One block per (sequence, key head, 256 query rows, or 128: see PAIRS below); a query row is a (token, head of the group) pair, so grouped heads share
 // the keys they read.  The 256 rows are two tiles of 128.  Keys come in tiles of 128; for every half i of one (64 keys) and each tile t:
 //     S_t,i = Q_t K_i^T    (both operands in shared memory, result in tensor memory)
 //     P_t,i = 2^(S - m)    (one thread per row: maximum, exponentials, sum; P in bf16 over S's own columns)
@@ -10,9 +10,13 @@
 // tensor core works through both tiles' softmax.  (Scores of 128 keys at a time leave no columns for a second set: every
 // softmax then waited for its two products, 1500 of 3700 clocks.)
 //
-// Operands are bf16: queries and weights are rounded once to 8 bits of significand, codes of 8-bit caches are bf16 numbers
-// exactly.  A result in 16 bits keeps no more; results wanted in fp32 go to the kernel for few rows.  A key's scale (8-bit
-// caches) multiplies its score in the softmax, a value's scale its weight, before the rounding.
+// Operands are bf16, the type of a bf16 cache; codes of 8-bit caches are bf16 numbers exactly.  Where queries and results are bf16 too, the only
+// rounding is that of the weights, once to 8 bits of significand: relative to 64-bit arithmetic results are 2.3e-3 off, of which their own
+// rounding is 1.7e-3.  Queries or results with more bits (fp32, fp16) take the form PAIRS: queries and weights are sums of two
+// bf16, 16 bits, in two products each; the weights' lower halves take the other 32 columns of their scores.  Twice the
+// products, and at HD = 128 one tile of rows instead of two: 4 chunks of 512 tokens at 2048, 32 heads of 128, bf16: 230 us from and to fp16, 90
+// from and to bf16; 2 x 1024 tokens, 32 heads of 64: 66 and 37.  fp32 results go to the kernel for few rows.  A key's scale
+// (8-bit caches) multiplies its score in the softmax, a value's scale its weight, before the rounding.
 //
 // The running maximum is raised only when it would be passed by 2^8 (weights then reach 256, well inside bf16 and the fp32
 // sums): O_t is rescaled in tensor memory in the first tiles and hardly ever after.
@@ -37,7 +41,7 @@
 namespace sd {
 namespace ac {
 
-constexpr int THREADS = 512, ROWS = 256, KEYS = 128, TILE_ROWS = 128, STAGES = 2, SIDE = 4, HALF = 64;
+constexpr int THREADS = 512, KEYS = 128, TILE_ROWS = 128, STAGES = 2, SIDE = 4, HALF = 64;
 constexpr float SLACK = 8.f;
 // Registers per thread of the softmax, the loader and the product warpgroups; the block is launched with 128 for each of its
 // 512 threads, and the shares add up to no more: 2 x 128 x 168 + 128 x 120 + 128 x 40 = 63 488.
@@ -45,9 +49,12 @@ constexpr int LAUNCH_REGS = 128, SOFTMAX_REGS = 168, LOADER_REGS = 120, PRODUCT_
 static_assert(2 * 128 * SOFTMAX_REGS + 128 * LOADER_REGS + 128 * PRODUCT_REGS <= THREADS * LAUNCH_REGS, "a larger share would wait forever");
 static_assert(SOFTMAX_REGS >= LAUNCH_REGS && LOADER_REGS <= LAUNCH_REGS && PRODUCT_REGS <= LAUNCH_REGS, "the first is raised, the others are lowered");
 
-template <int HD> struct Layout {
+template <int HD, bool PAIRS> struct Layout {
   static constexpr int TILE = 128 * HD * 2;                    // a tile of Q, K or V: blocks of 64 elements, 128 rows of 128 bytes each
-  static constexpr int Q = 0, K = 2 * TILE, V = K + STAGES * TILE, END = V + STAGES * TILE;
+  // tiles of query rows of a block; the lower halves of pairs lie behind the upper ones.  At HD = 128 two tiles of pairs leave no room for two
+  // stages of keys and values
+  static constexpr int TILES = PAIRS && HD == 128 ? 1 : 2, ROWS = TILES * TILE_ROWS, Q_LOW = TILES * TILE;
+  static constexpr int Q = 0, K = TILES * (PAIRS ? 2 : 1) * TILE, V = K + STAGES * TILE, END = V + STAGES * TILE;
   static constexpr int SIDE_OFF = END;                         // per key tile: 128 key scales, 128 value scales, mask of existing pages
   static constexpr int SIDE_BYTES = 2 * KEYS * 4 + 16;
   static constexpr int NEED = END + SIDE * SIDE_BYTES + 1024;  // + alignment
@@ -141,15 +148,17 @@ __device__ __forceinline__ void to_bf16(uint32_t w, uint32_t& lo, uint32_t& hi, 
 // keys [z * chunk, (z + 1) * chunk), the last one all that follow; several leave partial results (accumulator, maximum, sum) of their rows
 // to paged_attn_join_kernel.
 // map_k, map_v: the pools as [n_pages * n_kv_heads][page_len][HD] with boxes of a page by 64 elements (bf16 only; use_maps 0: not made).
-template <typename TC, int HD>
+// PAIRS: queries and weights enter as sums of two bf16.
+template <typename TC, int HD, bool PAIRS>
 __global__ void __launch_bounds__(ac::THREADS, 1)
 paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, int use_maps,
                         const BatchView b, const Rows q, const Rows out, const TC* __restrict__ Kp, const TC* __restrict__ Vp,
                         const float* __restrict__ Ksc, const float* __restrict__ Vsc, int group, float scale_log2, bool q_vec, bool out_vec,
                         int blocks_per_seq, int rows_from, int chunk, float* part_acc, float* part_ml) {
   using namespace ac;
-  using L = Layout<HD>;
+  using L = Layout<HD, PAIRS>;
   constexpr bool SCALED = CacheType<TC>::TOP > 0.f;
+  constexpr int ROWS = L::ROWS;
   extern __shared__ unsigned char ac_smem[];
   __shared__ uint64_t bars[4 * STAGES + 13 + SIDE];
   __shared__ uint32_t tmem_slot;
@@ -192,7 +201,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   int n_keys[2], n_rows[2], used_splits = 1;
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    n_rows[t] = max(0, min(TILE_ROWS, rows_all - row0 - t * TILE_ROWS));
+    n_rows[t] = t < L::TILES ? max(0, min(TILE_ROWS, rows_all - row0 - t * TILE_ROWS)) : 0;
     const int last = (row0 + t * TILE_ROWS + n_rows[t] - 1) / group;
     int keys = n_rows[t] ? (int)min(max(pos_first + last + 1, 0ll), (long long)len) : 0;
     if (splits > 1) {
@@ -248,7 +257,18 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     if (n_rows[t] > 0) {
       const long long at = (long long)(f0 + token) * q.row_stride + head * q.head_stride;
       const uint32_t dst = base + L::Q + t * L::TILE;
-      if (q_vec && q.dtype == DT_BF16) {
+      if constexpr (PAIRS) {
+#pragma unroll 4
+        for (int c = 0; c < HD / 8; ++c) {
+          float x[8];
+          uint32_t hi[4], lo[4];
+          ap::load_run<8>(q, at + c * 8, q_vec, x);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) ap::split(x[2 * i] * sign, x[2 * i + 1] * sign, hi[i], lo[i], __nv_bfloat16{});
+          sts16(dst + piece(r, c), hi[0], hi[1], hi[2], hi[3]);
+          sts16(dst + L::Q_LOW + piece(r, c), lo[0], lo[1], lo[2], lo[3]);
+        }
+      } else if (q_vec && q.dtype == DT_BF16) {
         const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(q.data) + at);
         const uint32_t turn = scale_log2 < 0.f ? 0x80008000u : 0u;
         uint4 x[HD / 8];                                          // all on their way together
@@ -342,7 +362,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       F2 sum[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        uint32_t w[16];
+        uint32_t w[16], w_lo[16];
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
           F2 x = f2(__uint_as_float(s[c][2 * k]), __uint_as_float(s[c][2 * k + 1]));
@@ -357,9 +377,11 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
             const float2 v = *reinterpret_cast<const float2*>(side + KEYS + c * 32 + 2 * k);
             un2(mul2(x, f2(v.x, v.y)), p0, p1);
           }
-          w[k] = pack_bf16(p0, p1);
+          if constexpr (PAIRS) ap::split(p0, p1, w[k], w_lo[k], __nv_bfloat16{});
+          else w[k] = pack_bf16(p0, p1);
         }
         tmem_st16(s_half + 16 * c, w);                           // over columns that have been read
+        if constexpr (PAIRS) tmem_st16(s_half + HALF / 2 + 16 * c, w_lo);
       }
       float a0, a1;
       un2(add2(sum[0], sum[1]), a0, a1);
@@ -591,20 +613,26 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         auto product_s = [&](int i) {
           const int h = i & 1;
           const uint64_t ka = tc::smem_desc(at + L::K + ((i >> 1) % STAGES) * L::TILE + h * (HALF * 128));
+#pragma unroll 1
+          for (int part = 0; part < (PAIRS ? 2 : 1); ++part) {
 #pragma unroll
-          for (int k = 0; k < HD / 16; ++k) {                     // descriptors count 16-byte units
-            const uint32_t off = ((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4;
-            mma_ss(tm + t * 128 + h * HALF, qa + off, ka + off, id_s, k > 0);
+            for (int k = 0; k < HD / 16; ++k) {                   // descriptors count 16-byte units
+              const uint32_t off = ((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4;
+              mma_ss(tm + t * 128 + h * HALF, qa + part * (L::Q_LOW >> 4) + off, ka + off, id_s, k > 0 ? 1u : (uint32_t)part);
+            }
           }
           tc::umma_commit(bar + (sfull - bar0) + 8 * (2 * t + h));
         };
         auto product_o = [&](int i) {
           const int h = i & 1;
           const uint64_t va = v_desc(at + L::V + ((i >> 1) % STAGES) * L::TILE + h * (HALF * 128), 128 * 128);
-          const uint32_t first = i > 0;
+#pragma unroll 1
+          for (int part = 0; part < (PAIRS ? 2 : 1); ++part) {
+            const uint32_t first = i + part > 0;
 #pragma unroll
-          for (int k = 0; k < HALF / 16; ++k)
-            mma_ts(tm + L::O_COL + t * HD, tm + t * 128 + h * HALF + k * 8, va + k * (2048 >> 4), id_o, k > 0 ? 1u : first);
+            for (int k = 0; k < HALF / 16; ++k)
+              mma_ts(tm + L::O_COL + t * HD, tm + t * 128 + h * HALF + part * (HALF / 2) + k * 8, va + k * (2048 >> 4), id_o, k > 0 ? 1u : first);
+          }
           tc::umma_commit(bar + (odone - bar0) + 8 * t);
         };
         auto announce = [&](uint32_t which) { tc::umma_commit(bar + (which - bar0)); };
@@ -665,7 +693,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
 // positions in 16 splits took 158 us instead of 83.
 template <int HD>
 __global__ void __launch_bounds__(256)
-paged_attn_join_kernel(const BatchView b, const Rows out, int group, int rows_from, int chunk, int splits, const float* __restrict__ part_acc,
+paged_attn_join_kernel(const BatchView b, const Rows out, int group, int rows_from, int block_rows, int chunk, int splits, const float* __restrict__ part_acc,
                        const float* __restrict__ part_ml) {
   int seq, pos;
   const int tok = blockIdx.x, where = locate_row(b, tok, seq, pos);
@@ -675,7 +703,7 @@ paged_attn_join_kernel(const BatchView b, const Rows out, int group, int rows_fr
   // the keys that the block of this row went over: those of its last row
   const int f0 = b.first[seq], f1 = b.first[seq + 1], n_new = min(f1 - f0, min(b.max_new, b.n_tokens - f0)), rows_all = n_new * group;
   if (rows_all < rows_from) return;
-  const int row = (tok - f0) * group + head % group, last = (min((row / ac::ROWS + 1) * ac::ROWS, rows_all) - 1) / group;
+  const int row = (tok - f0) * group + head % group, last = (min((row / block_rows + 1) * block_rows, rows_all) - 1) / group;
   const int keys = (int)min(max((long long)b.len[seq] - (f1 - f0) + last + 1, 0ll), (long long)b.seq_len(seq));
   const int used = ap::splits_of(keys, chunk, splits);
   if (used <= 1) return;                                         // written by its block

@@ -271,11 +271,11 @@ int64_t pick_chunk_split(int64_t slots, int64_t units, int64_t rows, int64_t max
   return best;
 }
 
-template <typename TC, int HD>
+template <typename TC, int HD, bool PAIRS>
 int attention_chunks(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale_log2, const sd_heads* out, int rows_from, bool* split) {
-  using L = sd::ac::Layout<HD>;
-  constexpr unsigned long long bit = 1ull << (32 + (HD == 128 ? 0 : 1) + 2 * (std::is_same<TC, bf16>::value ? 0 : std::is_same<TC, int8_t>::value ? 1 : 2));
-  auto kernel = sd::paged_attn_chunk_kernel<TC, HD>;
+  using L = sd::ac::Layout<HD, PAIRS>;
+  constexpr unsigned long long bit = 1ull << (32 + (HD == 128 ? 0 : 1) + 2 * (std::is_same<TC, bf16>::value ? 0 : std::is_same<TC, int8_t>::value ? 1 : 2) + (PAIRS ? 6 : 0));
+  auto kernel = sd::paged_attn_chunk_kernel<TC, HD, PAIRS>;
   if (!(c->tile_ready & bit)) {
     cudaFuncAttributes attr;                 // the warpgroups redistribute what the block is launched with: it must be that much
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM) != cudaSuccess ||
@@ -285,11 +285,11 @@ int attention_chunks(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, f
   const auto P = pools<TC>(c, l);
   CUtensorMap mk = {}, mv = {};
   const int use_maps = std::is_same<TC, bf16>::value && pool_map<HD>(c, P.k, &mk) && pool_map<HD>(c, P.v, &mv);
-  const int blocks = (int)(((int64_t)b->max_new * c->group + sd::ac::ROWS - 1) / sd::ac::ROWS);
+  const int blocks = (int)(((int64_t)b->max_new * c->group + L::ROWS - 1) / L::ROWS);
   const int64_t grid = (int64_t)blocks * c->cfg.n_kv_heads * b->n_seqs;
   if (grid > 0x7fffffff) return SD_ERR_ARG;
   // blocks that can have rows: max_new is a bound for every sequence, n_tokens one for all of them
-  const int64_t units = std::min(grid, ((int64_t)b->n_tokens * c->group / sd::ac::ROWS + b->n_seqs) * c->cfg.n_kv_heads);
+  const int64_t units = std::min(grid, ((int64_t)b->n_tokens * c->group / L::ROWS + b->n_seqs) * c->cfg.n_kv_heads);
   const int64_t rows = (int64_t)b->n_tokens * c->cfg.n_heads;
   const int64_t max_len = b->max_len > 0 ? b->max_len : (int64_t)b->pages_per_seq * c->cfg.page_len;
   const int64_t chunk = pick_chunk_split(c->sm_count, units, rows, max_len);
@@ -299,7 +299,7 @@ int attention_chunks(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, f
       blocks, rows_from, (int)chunk, c->at<float>(c->part_acc), c->at<float>(c->part_ml));
   if (splits > 1)
     sd::paged_attn_join_kernel<HD><<<dim3(b->n_tokens, (c->cfg.n_heads + 7) / 8), 256, 0, c->stream>>>(
-        view_of(c, b), rows_of(out), c->group, rows_from, (int)chunk, splits, c->at<float>(c->part_acc), c->at<float>(c->part_ml));
+        view_of(c, b), rows_of(out), c->group, rows_from, L::ROWS, (int)chunk, splits, c->at<float>(c->part_acc), c->at<float>(c->part_ml));
   *split = splits > 1;
   return launched(c, splits > 1 ? 2 : 1);
 }
@@ -309,8 +309,10 @@ int attention_chunks(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, f
 // 70 and 131 us, 32 rows 71 and 133; 2 of 4096, 8 heads, 12 rows 18 and 28; one of 30 000, one key head, 12 rows 26 and 151; 8 of 300,
 // 12 heads of 64, 12 rows 10 and 8.  In 8 bits, where the few rows' kernel has less to read and this one codes to convert: int8,
 // 64 of 4096 over 2 key heads of 128, 16 rows 111 and 82, 32 rows 111 and 140; e4m3, 16 of 1024, 32 heads of 64, 24 rows 75 and 66,
-// 32 rows 75 and 116.
-template <typename TC> constexpr int kChunkRows = sd::CacheType<TC>::TOP > 0.f ? 25 : 9;
+// 32 rows 75 and 116.  With pairs (results in fp16, few rows' time beside it): bf16, 16 of 1024, 32 heads of 64, 32 rows 133 and 74, 64 rows 135
+// and 133; 2 of 4096, 8 heads of 128, 32 rows 41 and 33, 48 rows 41 and 41; one of 30 000, one head, 32 rows 49 and 96; e4m3, 16 of 1024,
+// 8 heads of 128, 25 rows 49 and 67; 2 of 4096 41 and 45; 8 of 300, 12 heads of 64, 22 and 14.
+template <typename TC> constexpr int kChunkRows(bool pairs) { return sd::CacheType<TC>::TOP > 0.f ? 25 : pairs ? 41 : 9; }
 
 int cache_attention(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale, const sd_heads* out) {
   if (scale == 0.f) scale = 1.f / sqrtf((float)c->cfg.head_dim);
@@ -328,13 +330,18 @@ int cache_attention(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, fl
         const int64_t most = (int64_t)b->max_new * c->group;
         if (most > 0x7fffff00) return (int)SD_ERR_ARG;
         if constexpr (HD >= 64) {
-          if (most >= kChunkRows<TC> && out->dtype != SD_DTYPE_FP32) {
+          // one bf16 for a query or a weight only where the queries have no more and the results keep no more
+          const bool pairs = q->dtype != SD_DTYPE_BF16 || out->dtype != SD_DTYPE_BF16;
+          const int enough = kChunkRows<TC>(pairs);
+          if (most >= enough && out->dtype != SD_DTYPE_FP32) {
             // max_new is only a bound: which kernel takes a sequence is decided on the device, by its own rows
             bool split = false;
-            const int rc = attention_chunks<TC, HD>(c, l, b, q, scale_log2, out, b->n_seqs == 1 ? 1 : kChunkRows<TC>, &split);
+            const int rows_from = b->n_seqs == 1 ? 1 : enough;
+            const int rc = pairs ? attention_chunks<TC, HD, true>(c, l, b, q, scale_log2, out, rows_from, &split)
+                                 : attention_chunks<TC, HD, false>(c, l, b, q, scale_log2, out, rows_from, &split);
             if (rc != SD_OK || b->n_seqs == 1) return rc;
             // it may begin early where the two do not share the workspace for split keys
-            return attention_tiles<TC, HD>(c, l, b, q, scale_log2, out, kChunkRows<TC>, !split);
+            return attention_tiles<TC, HD>(c, l, b, q, scale_log2, out, enough, !split);
           }
         }
         return attention_tiles<TC, HD>(c, l, b, q, scale_log2, out, most + 1);

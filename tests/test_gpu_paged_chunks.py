@@ -90,3 +90,14 @@ def test_pages_that_do_not_exist(cache_dtype, hd, page):
     run(cache_dtype, 2, 2, hd, page, [130], [700], gone=[(0, c) for c in range(128 // page, 256 // page)] + [(0, n)], seed=page + 1)
     run(cache_dtype, 2, 2, hd, page, [150, 150], [150, 150], gone=[(0, c) for c in range(1 + 64 // page)] + [(1, 1)], seed=page + 2)
     run(cache_dtype, 2, 2, hd, page, [40], [3000], gone=[(0, 1000 // page), (0, 2999 // page)], seed=page + 3)      # split keys
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
+@pytest.mark.parametrize("io,out", [("fp16", "fp16"), ("fp32", "fp16"), ("fp32", "bf16"), ("fp16", "bf16"), ("bf16", "fp16")])
+@pytest.mark.parametrize("hd,heads,kv_heads,page", [(64, 4, 2, 16), (128, 3, 3, 64)])
+def test_types_that_keep_more_than_bf16(cache_dtype, io, out, hd, heads, kv_heads, page):
+    # queries or results with more bits than a bf16: queries and weights enter with 16 bits
+    run(cache_dtype, heads, kv_heads, hd, page, [1, 33, 140, 300, 5], [70, 600, 150, 900, 3], io=io, out_dtype=out, seed=hd, start=1, tail=2)
+    run(cache_dtype, heads, kv_heads, hd, page, [70], [2500], io=io, out_dtype=out, seed=hd + 1)                   # split keys
+    run(cache_dtype, heads, kv_heads, hd, page, [129, 128, 127], [129, 400, 255], io=io, out_dtype=out, scale=-0.5, seed=hd + 2)
+    run(cache_dtype, heads, kv_heads, hd, page, [60, 61], [700, 130], io=io, out_dtype=out, seed=hd + 3, gone=[(0, 0), (0, 200 // page), (1, 128 // page)])
