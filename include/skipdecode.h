@@ -358,6 +358,12 @@ int sd_cache_attention(sd_cache *c, int layer, const sd_batch *batch, const sd_h
  * results of that call being wrong.  Returns SD_ERR_DEVICE when it was not 0. */
 int sd_cache_status(sd_cache *c, int32_t *device_status);
 
+/* SD_CACHE_OPT_TEST_WAIT_EXPIRY: test hook, one shot.  1: in the next attention of chunks over a bf16 or 8-bit cache (16-bit results, more than
+ * 256 keys) a wait inside the kernel runs out after about a millisecond: sd_cache_status reports bit 2, the results of that
+ * call are garbage or as they were, nothing is left in flight and the cache stays usable.  Errors: SD_ERR_ARG. */
+enum { SD_CACHE_OPT_TEST_WAIT_EXPIRY = 1 };
+int sd_cache_set_option(sd_cache *c, int option, int value);
+
 void sd_cache_destroy(sd_cache *c);
 
 /* Runs the new tokens of a batch through the model over a paged cache in place of the handle's own: embedding at each

@@ -26,7 +26,7 @@ EXPORTS = ("sd_arena_bytes", "sd_create", "sd_schedule", "sd_schedule_compute", 
            "sd_prefill", "sd_decode_step", "sd_decode_step_static", "sd_rewind", "sd_launch_count", "sd_decode_step_host", "sd_greedy", "sd_sample_top_p", "sd_set_padding", "sd_set_rows", "sd_status", "sd_stats",
            "sd_set_option", "sd_kernel_time", "sd_kernel_time_reset", "sd_strerror", "sd_destroy",
            "sd_sample", "sd_cache_bytes", "sd_cache_create", "sd_cache_layer", "sd_cache_append", "sd_cache_read", "sd_cache_attention",
-           "sd_cache_status", "sd_cache_destroy", "sd_extend")
+           "sd_cache_status", "sd_cache_set_option", "sd_cache_destroy", "sd_extend")
 
 
 class SdConfig(C.Structure):
@@ -70,6 +70,7 @@ SD_DTYPE_FP32, SD_DTYPE_BF16, SD_DTYPE_FP16, SD_DTYPE_INT8, SD_DTYPE_E4M3 = 0, 1
 _CACHE_TYPES = {"fp32": (SD_DTYPE_FP32, torch.float32), "bf16": (SD_DTYPE_BF16, torch.bfloat16),
                 "int8": (SD_DTYPE_INT8, torch.int8), "e4m3": (SD_DTYPE_E4M3, torch.float8_e4m3fn)}
 _ROW_TYPES = {torch.float32: SD_DTYPE_FP32, torch.bfloat16: SD_DTYPE_BF16, torch.float16: SD_DTYPE_FP16}
+SD_CACHE_OPT_TEST_WAIT_EXPIRY = 1
 # bits of the status words
 STATUS_BAD_TOKEN, STATUS_WAIT_EXPIRED, STATUS_BAD_BATCH, STATUS_BAD_SETTING, STATUS_NOT_FINITE = 1, 2, 16, 32, 64
 
@@ -121,6 +122,7 @@ def lib() -> C.CDLL:
     L.sd_cache_read.argtypes = L.sd_cache_append.argtypes
     L.sd_cache_attention.argtypes = [vp, C.c_int, vp, vp, C.c_float, vp]
     L.sd_cache_status.argtypes = [vp, i32p]
+    L.sd_cache_set_option.argtypes = [vp, C.c_int, C.c_int]
     L.sd_cache_destroy.argtypes = [vp]
     L.sd_cache_destroy.restype = None
     L.sd_extend.argtypes = [vp, vp, C.POINTER(SdBatch), vp, C.c_int, C.c_int, vp]
@@ -308,6 +310,9 @@ class PagedCache:
         if code not in (SD_OK, SD_ERR_DEVICE):
             raise SdError(code, "sd_cache_status")
         return v.value
+
+    def set_option(self, option: int, value: int):
+        _check(lib().sd_cache_set_option(self.h, option, value), "sd_cache_set_option")
 
     def close(self):
         if getattr(self, "h", None) is not None and self.h.value:

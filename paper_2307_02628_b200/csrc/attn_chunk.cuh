@@ -149,12 +149,13 @@ __device__ __forceinline__ void to_bf16(uint32_t w, uint32_t& lo, uint32_t& hi, 
 // to paged_attn_join_kernel.
 // map_k, map_v: the pools as [n_pages * n_kv_heads][page_len][HD] with boxes of a page by 64 elements (bf16 only; use_maps 0: not made).
 // PAIRS: queries and weights enter as sums of two bf16.
+// test_expire: test hook, values are never given back and the loaders give up after about a millisecond, keys of the third tile on their way.
 template <typename TC, int HD, bool PAIRS>
 __global__ void __launch_bounds__(ac::THREADS, 1)
 paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, int use_maps,
                         const BatchView b, const Rows q, const Rows out, const TC* __restrict__ Kp, const TC* __restrict__ Vp,
                         const float* __restrict__ Ksc, const float* __restrict__ Vsc, int group, float scale_log2, bool q_vec, bool out_vec,
-                        int blocks_per_seq, int rows_from, int chunk, float* part_acc, float* part_ml) {
+                        int blocks_per_seq, int rows_from, int chunk, float* part_acc, float* part_ml, int test_expire) {
   using namespace ac;
   using L = Layout<HD, PAIRS>;
   constexpr bool SCALED = CacheType<TC>::TOP > 0.f;
@@ -491,7 +492,8 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       if (lane == 0) arrive(sidefull + 8 * (j % SIDE));
     };
     auto wait_free = [&](uint32_t bar, int j) {
-      return j < STAGES || __all_sync(0xffffffffu, tc::mbar_wait(bar + 8 * (j % STAGES), (j / STAGES - 1) & 1, abort_flag, b.status));
+      return j < STAGES || __all_sync(0xffffffffu, tc::mbar_wait(bar + 8 * (j % STAGES), (j / STAGES - 1) & 1, abort_flag, b.status,
+                                                                 test_expire ? 2000000ll : tc::kWaitLimit));
     };
     auto announce = [&](uint32_t bar, int j) {                    // plain stores or asynchronous copies that have landed
       fence_async();
@@ -510,19 +512,25 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         }
         pf_commit();
       };
-      // whole pages by tensor copies, a page's half (64 elements) per copy, lane i the page of keys [8 i, ...)
+      // whole pages by tensor copies, a page's half (64 elements) per copy, lane i the page of keys [8 i, ...).  The first warp announces
+      // for all four, so that a phase ends when its copies have landed, whatever the other warps do
       auto fetch = [&](const CUtensorMap* map, uint32_t dst, uint32_t bar, int j, int page) {
         const uint32_t full = bar + 8 * (j % STAGES);
         if (w == 0) {
-          if (lane == 0) tc::mbar_expect_tx(full, L::TILE);
+          if (lane == 0) {
+            tc::mbar_expect_tx(full, L::TILE);
+            arrive(full); arrive(full); arrive(full);
+          }
           __syncwarp();
           if (lane < 16 && ((lane * 8) & (b.page_len - 1)) == 0) {
 #pragma unroll
             for (int h = 0; h < HD / 64; ++h)
               tma_load_3d(dst + h * (128 * 128) + lane * 1024, map, h * 64, 0, page * b.n_kv_heads + g_head, full);
           }
-        } else if (lane == 0) arrive(full);
+        }
       };
+      int k_asked = 0, v_asked = 0;                               // tiles whose keys, values have been asked for
+      uint32_t wholes = 0u;                                       // bit i: tile k_asked - 1 - i came by tensor copies
       for (int j = 0; j < n_tiles; ++j) {
         const int page = page_next;
         page_next = look_up(j + 1);
@@ -533,7 +541,10 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         begin_side(j, make_float2(0.f, 0.f), pages_ok);
         if (whole) fetch(&map_k, kt, kfull, j, page);
         else copy(Kp, kt, j, page, pages_ok);
+        k_asked = j + 1;
+        wholes = wholes << 1 | (whole ? 1u : 0u);
         if (!(ok = wait_free(vempty, j))) break;
+        v_asked = j + 1;
         if (whole) fetch(&map_v, vt, vfull, j, page);
         else {
           copy(Vp, vt, j, page, pages_ok);
@@ -545,12 +556,16 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       }
       pf_wait<0>();
       if (!ok && w == 0) {
-        // giving up: tensor copies may still be on their way into this block's memory; wait (bounded) for every stage to come to rest
-        for (int i = 0; i < 2 * STAGES; ++i) {
-          const uint32_t full = (i < STAGES ? kfull : vfull) + 8 * (i % STAGES);
-          const long long t0 = clock64();
-          while (!(tc::mbar_try(full, 0) && tc::mbar_try(full, 1)) && clock64() - t0 < tc::kWaitLimit / 4) {}
-        }
+        // giving up: what tensor copies have been asked for must land before the block's memory goes; the last of each stage may be on its way
+        auto landed = [&](uint32_t bar, int asked) {
+          for (int j = max(asked - STAGES, 0); j < asked; ++j) {
+            const long long t0 = clock64();
+            if ((wholes >> (k_asked - 1 - j)) & 1u)
+              while (!tc::mbar_try(bar + 8 * (j % STAGES), (j / STAGES) & 1) && clock64() - t0 < tc::kWaitLimit) {}
+          }
+        };
+        landed(kfull, k_asked);
+        landed(vfull, v_asked);
       }
     } else {
       uint4 k[STEPS], v[STEPS];                                   // the next tile's codes, on their way
@@ -667,7 +682,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
             if (ok && 2 * j + 2 < halves) ok = next_s(2 * j + 2);
           }
           if (ok && 2 * j + 1 < halves) ok = next_o(2 * j + 1);
-          if (ok) announce(vempty + 8 * (j % STAGES));
+          if (ok && !test_expire) announce(vempty + 8 * (j % STAGES));
           if (ok && 2 * j + 3 < halves) ok = next_s(2 * j + 3);
           if (ok && j + 1 < tiles) announce(kempty + 8 * ((j + 1) % STAGES));
         }

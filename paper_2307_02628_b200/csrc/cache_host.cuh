@@ -14,6 +14,7 @@ struct sd_cache {
   sd::EncodeTiledFn encode = nullptr;
   int tile_blocks[9] = {};   // blocks per SM of each form of the kernel for few rows
   int64_t launches = 0;      // kernels launched
+  bool test_expire = false;  // test hook: the next launch for chunks makes a wait run out (one shot)
   unsigned long long tile_ready = 0;    // bit per kernel whose shared-memory size has been allowed on this device
   char* layer(int l) const { return arena + (size_t)l * layer_bytes; }
   template <typename T> T* at(size_t off) const { return reinterpret_cast<T*>(arena + off); }
@@ -296,7 +297,8 @@ int attention_chunks(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, f
   const int splits = chunk == kNoSplit ? 1 : (int)((max_len + chunk - 1) / chunk);
   kernel<<<dim3((unsigned)grid, splits), sd::ac::THREADS, L::SMEM, c->stream>>>(
       mk, mv, use_maps, view_of(c, b), rows_of(q), rows_of(out), (const TC*)P.k, (const TC*)P.v, (const float*)P.ks, (const float*)P.vs, c->group, scale_log2, wide(q), wide(out),
-      blocks, rows_from, (int)chunk, c->at<float>(c->part_acc), c->at<float>(c->part_ml));
+      blocks, rows_from, (int)chunk, c->at<float>(c->part_acc), c->at<float>(c->part_ml), c->test_expire ? 1 : 0);
+  c->test_expire = false;
   if (splits > 1)
     sd::paged_attn_join_kernel<HD><<<dim3(b->n_tokens, (c->cfg.n_heads + 7) / 8), 256, 0, c->stream>>>(
         view_of(c, b), rows_of(out), c->group, rows_from, L::ROWS, (int)chunk, splits, c->at<float>(c->part_acc), c->at<float>(c->part_ml));
@@ -493,6 +495,13 @@ int sd_cache_status(sd_cache* c, int32_t* device_status) {
   }
   if (device_status) *device_status = v;
   return v ? SD_ERR_DEVICE : SD_OK;
+}
+
+int sd_cache_set_option(sd_cache* c, int option, int value) {
+  if (!c || option != SD_CACHE_OPT_TEST_WAIT_EXPIRY || value < 0 || value > 1) return SD_ERR_ARG;
+  std::lock_guard<std::mutex> lock(c->busy);
+  c->test_expire = value != 0;
+  return SD_OK;
 }
 
 void sd_cache_destroy(sd_cache* c) { delete c; }

@@ -101,3 +101,33 @@ def test_types_that_keep_more_than_bf16(cache_dtype, io, out, hd, heads, kv_head
     run(cache_dtype, heads, kv_heads, hd, page, [70], [2500], io=io, out_dtype=out, seed=hd + 1)                   # split keys
     run(cache_dtype, heads, kv_heads, hd, page, [129, 128, 127], [129, 400, 255], io=io, out_dtype=out, scale=-0.5, seed=hd + 2)
     run(cache_dtype, heads, kv_heads, hd, page, [60, 61], [700, 130], io=io, out_dtype=out, seed=hd + 3, gone=[(0, 0), (0, 200 // page), (1, 128 // page)])
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
+@pytest.mark.parametrize("io", ["bf16", "fp16"])
+@pytest.mark.parametrize("new,length,page,heads", [([300], [1000], 64, 80), ([50, 1], [13000, 5], 16, 2), ([200, 50], [900, 820], 8, 80)])
+def test_a_wait_that_runs_out_is_reported_and_the_cache_stays_usable(cache_dtype, io, new, length, page, heads):
+    # the loaders give up with tensor copies (bf16) of a tile's keys on their way; they end with the copies, not with a time limit.  As many
+    # heads, or positions, as leave a block more tiles of keys than it has stages
+    import time
+    lay = P.Layout(new, length, page, seed=9)
+    cache = P.make_cache(lay, heads, heads, 128, cache_dtype)
+    P.fill(cache, lay, seed=10)
+    q = torch.randn(lay.n_tokens, heads, 128, generator=torch.Generator().manual_seed(11)).to(P.TORCH[io]).cuda()
+    b = lay.batch()
+    want = cache.attention(0, q, b)
+    assert cache.status() == 0
+    for value in (2, -1):
+        with pytest.raises(binding.SdError):
+            cache.set_option(binding.SD_CACHE_OPT_TEST_WAIT_EXPIRY, value)
+    with pytest.raises(binding.SdError):
+        cache.set_option(99, 1)
+    for _ in range(3):
+        cache.set_option(binding.SD_CACHE_OPT_TEST_WAIT_EXPIRY, 1)
+        t0 = time.perf_counter()
+        cache.attention(0, q, b)
+        assert cache.status() == binding.STATUS_WAIT_EXPIRED
+        assert time.perf_counter() - t0 < 0.5                   # a millisecond or two; the limit of a wait is two seconds
+        assert torch.equal(cache.attention(0, q, b), want)
+        assert cache.status() == 0
+    cache.close()

@@ -150,3 +150,8 @@ def test_threads_that_share_a_cache_hand_over_their_own_tensors(monkeypatch):
         sys.setswitchinterval(interval)
     assert len(calls) == 12000
     assert not wrong, (len(wrong), wrong[0])
+
+
+def test_options_of_a_cache_are_checked():
+    L = binding.lib()
+    assert L.sd_cache_set_option(None, binding.SD_CACHE_OPT_TEST_WAIT_EXPIRY, 1) == binding.SD_ERR_ARG
