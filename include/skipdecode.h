@@ -345,7 +345,7 @@ int sd_cache_read(sd_cache *c, int layer, const sd_batch *batch, const sd_heads 
 /* Attention of the new tokens, whose keys and values have been appended, over their sequences: the row at position p
  * attends to positions 0..p,
  *   out[r, h] = sum_j softmax_j(scale * q[r, h] . K[j, g]) V[j, g],  g = h / (n_heads / n_kv_heads).
- * q, out: rows [n_tokens, n_heads, head_dim].  scale: finite; 0 stands for head_dim^-1/2.  Single tokens, chunks
+ * q, out: rows [n_tokens, n_heads, head_dim].  scale: at most 2e38 in magnitude; 0 stands for head_dim^-1/2.  Single tokens, chunks
  * and both in one call.  Sums and softmax statistics are fp32.  Over an fp32 cache nothing is rounded before the output; over the
  * others queries and weights enter the products with 16 bits or more, except that the weights may enter as bf16 where
  * both q and out are bf16.  max_len, and how many rows a sequence brings, choose the kernel and the split: results of the same row under other values agree

@@ -294,8 +294,8 @@ class PagedCache:
         """Causal attention of the new tokens' queries [n_tokens, n_heads, head_dim] over their sequences; out: like q unless given."""
         if scale is None:
             scale = 0.0                                        # the library's default, head_dim^-1/2
-        elif not (scale == scale and abs(scale) != float("inf") and scale != 0):
-            raise ValueError("scale must be a finite number other than 0")
+        elif not 0 < abs(C.c_float(scale).value) < float("inf"):   # as the library gets it: 0 would stand for the default
+            raise ValueError("scale must be a number other than 0 within the range of fp32")
         n = self._heads
         if out is None:
             out = torch.empty(batch.n_tokens, n, self._head_dim, dtype=q.dtype, device=self.device)

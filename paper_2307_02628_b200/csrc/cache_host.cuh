@@ -470,7 +470,7 @@ int sd_cache_read(sd_cache* c, int layer, const sd_batch* b, const sd_heads* k, 
 }
 
 int sd_cache_attention(sd_cache* c, int layer, const sd_batch* b, const sd_heads* q, float scale, const sd_heads* out) {
-  if (!c || layer < 0 || layer >= c->cfg.n_layers || !std::isfinite(scale)) return SD_ERR_ARG;
+  if (!c || layer < 0 || layer >= c->cfg.n_layers || !(fabsf(scale) <= 2e38f)) return SD_ERR_ARG;   // its product with log2 e is finite too
   int rc = check_batch(c, b);
   if (rc == SD_OK) rc = check_rows(c, b, q, c->cfg.n_heads, false);
   if (rc == SD_OK) rc = check_rows(c, b, out, c->cfg.n_heads, true);

@@ -293,3 +293,21 @@ def test_tables_reach_at_most_two_to_the_thirtieth_positions(cache_dtype):
         assert bool(((got - want).abs() <= lim).all())
     assert cache.status() == 0
     cache.close()
+
+
+def test_scales_that_fp32_does_not_hold_are_refused():
+    # one that is 0 in fp32 would stand for the default
+    lay = P.Layout([2], [9], 16)
+    cache = P.make_cache(lay, 2, 2, 64, "bf16")
+    P.fill(cache, lay, seed=1)
+    q = torch.ones(2, 2, 64, device="cuda")
+    for scale in (1e-60, -1e-46, 1e39, float("inf"), 0.0, float("nan")):
+        with pytest.raises(ValueError):
+            cache.attention(0, q, lay.batch(), scale=scale)
+    with pytest.raises(binding.SdError) as e:
+        cache.attention(0, q, lay.batch(), scale=3e38)          # infinite once it is turned to base 2
+    assert e.value.code == binding.SD_ERR_ARG
+    tiny = cache.attention(0, q, lay.batch(), scale=1e-40)      # all keys alike
+    assert not torch.equal(tiny, cache.attention(0, q, lay.batch()))
+    assert cache.status() == 0
+    cache.close()
