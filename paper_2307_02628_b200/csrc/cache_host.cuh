@@ -199,7 +199,7 @@ int cache_read(sd_cache* c, int l, const sd_batch* b, const sd_heads* k, const s
   });
 }
 
-// Keys per split for `units` blocks over up to max_len keys each, `rows` query rows in all, `slots` blocks at a time on the device.
+// Keys per split for `units` blocks over up to max_len keys each, `rows` rows of partial results in all, `slots` blocks at a time on the device.
 // All of them should have work, and the last wave should not be long: three single tokens over 50 000..61 000 positions in
 // bf16 take 120 us with 12 splits (288 blocks, 296 slots), 135 with 18, 149 with 32; splitting stops at 256 keys, below which
 // a block's start and end outweigh its walk.
@@ -232,15 +232,16 @@ int attention_tiles(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, fl
     c->tile_ready |= bit;
   }
   const auto P = pools<TC>(c, l);
-  const int tiles = (int)((std::min((int64_t)b->max_new * c->group, rows_below - 1) + sd::ap::ROWS - 1) / sd::ap::ROWS);
+  const int64_t most = std::min((int64_t)b->max_new * c->group, rows_below - 1);       // rows of a sequence that this launch takes
+  const int tiles = (int)((most + sd::ap::ROWS - 1) / sd::ap::ROWS), slot_rows = (int)std::min<int64_t>(most, sd::ap::ROWS);
   const int64_t units = (int64_t)tiles * c->cfg.n_kv_heads * b->n_seqs;
   if (units > 0x7fffffff) return SD_ERR_ARG;
   const int max_len = b->max_len > 0 ? b->max_len : b->pages_per_seq * c->cfg.page_len;
-  const int chunk = pick_split((long)c->tile_blocks[index] * c->sm_count, (long)units, (long)b->n_tokens * c->cfg.n_heads, max_len);
+  const int chunk = pick_split((long)c->tile_blocks[index] * c->sm_count, (long)units, (long)units * slot_rows, max_len);
   const int splits = (int)(((int64_t)max_len + chunk - 1) / chunk);
   sd::launch_kernel(early, c->stream, kernel, dim3((unsigned)units, splits), dim3(sd::ap::THREADS), S::SMEM,
       view_of(c, b), rows_of(q), rows_of(out), (const TC*)P.k, (const TC*)P.v, (const float*)P.ks, (const float*)P.vs, c->group, scale_log2, wide(q),
-      tiles, (int)std::min<int64_t>(rows_below, 0x7fffffff), chunk, c->at<float>(c->part_acc), c->at<float>(c->part_ml), c->at<int>(c->counters), early);
+      tiles, (int)std::min<int64_t>(rows_below, 0x7fffffff), chunk, slot_rows, c->at<float>(c->part_acc), c->at<float>(c->part_ml), c->at<int>(c->counters), early);
   return launched(c);
 }
 

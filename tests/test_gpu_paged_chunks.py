@@ -66,6 +66,14 @@ def test_chunks_beside_single_tokens(cache_dtype):
 
 
 @pytest.mark.parametrize("cache_dtype", CACHES)
+@pytest.mark.parametrize("heads,kv_heads", [(4, 1), (4, 4), (7, 1)])
+def test_long_single_tokens_beside_a_chunk_are_split_too(cache_dtype, heads, kv_heads):
+    # the chunk's rows take none of the workspace of the few rows' partial results: all their splits are joined beside it
+    run(cache_dtype, heads, kv_heads, 128, 64, [1, 512, 1, 2, 8], [9000, 700, 20, 7777, 5001], seed=13)
+    run(cache_dtype, heads, kv_heads, 64, 16, [1, 1030, 3], [20001, 1030, 6000], seed=14, start=1, tail=3)
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
 @pytest.mark.parametrize("hd", [64, 128])
 def test_one_sequence_of_few_rows_under_a_larger_bound(cache_dtype, hd):
     run(cache_dtype, 2, 2, hd, 16, [3], [700], seed=5, tail=60, max_new=60)
