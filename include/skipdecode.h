@@ -348,9 +348,11 @@ int sd_cache_read(sd_cache *c, int layer, const sd_batch *batch, const sd_heads 
  * q, out: rows [n_tokens, n_heads, head_dim].  scale: at most 2e38 in magnitude; 0 stands for head_dim^-1/2.  Single tokens, chunks
  * and both in one call.  Sums and softmax statistics are fp32.  Over an fp32 cache nothing is rounded before the output; over the
  * others queries and weights enter the products with 16 bits or more, except that the weights may enter as bf16 where
- * both q and out are bf16.  max_len, and how many rows a sequence brings, choose the kernel and the split: results of the same row under other values agree
- * within that rounding, under the same values bit for bit.  The result of a query row with a NaN is NaN, with an
- * infinity NaN or 0; other rows and heads do not see it. */
+ * both q and out are bf16.  The numbers of sequences, tokens and rows and the bounds max_new and max_len choose the kernels and
+ * where the keys are split, and rows that are computed side by side raise their running maximum together: the same call (batch description,
+ * bounds and inputs) gives the same bits, the same row in another call agrees within that rounding.  The result of a query row
+ * with a NaN is NaN, with an infinity NaN or 0; other rows and heads do not see it beyond that rounding.  A weight before the
+ * division by their sum is at most 2^8, so the magnitudes of a sequence's values should add up to less than 2^119. */
 int sd_cache_attention(sd_cache *c, int layer, const sd_batch *batch, const sd_heads *q, float scale, const sd_heads *out);
 
 /* Synchronises the stream, reads the cache's status word and clears it (not to be called in a capture).  Bits: 16 a batch

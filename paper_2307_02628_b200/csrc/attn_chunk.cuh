@@ -27,8 +27,9 @@
 // 2 x (768 + 512) clocks of the tensor core at HD = 128 (64 x 128 x 16 reads its operands for 48 clocks, not 32).  A half takes about
 // 1750 clocks, exponentials 1024 of them; the rest is reading scores, maxima, packing and the hand-over between warps, and a block's
 // start and end cost as much as 450 keys.  Eight chunks of 1000..1024 tokens of 32 heads of 128 at 1024..4096 positions in bf16:
-// 255 us, 0.83 PFLOP/s.  33 sequences of 11..329 new tokens at 364..1471 positions, 32 heads of 64 in e4m3: 197 us; their last
-// blocks are half empty (166 of 256 rows on average) and the two scales add 2 x 32 packed products per row and half.
+// 255 us, 0.83 PFLOP/s.  33 sequences of 11..329 new tokens at 364..1471 positions, 32 heads of 64 in e4m3: 197 us; a block
+// has 129 of 256 rows on average, half of the blocks one tile only, whose products and softmax do not overlap, and 1050 keys, so that its start and
+// end are 30 % of it; the two scales add 2 x 32 packed products per row and half.
 // Exponentials by polynomial on the other units for an eighth to a half of the weights changed nothing (250..260 us).
 //
 // Warps: 0-3 and 4-7 softmax of tile 0 and 1 (one thread per row, which is a lane of tensor memory), 8-11 loaders (page

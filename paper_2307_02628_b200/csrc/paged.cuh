@@ -295,7 +295,7 @@ __device__ __forceinline__ void decode8(uint2 v, float s, float (&o)[8], e4m3) {
 // One block per few rows.  A group of HD / 8 lanes owns one (row, head, K or V): each lane holds eight elements, the largest
 // magnitude goes round the group by shuffles, and the codes leave as one 8-byte store per lane (16 or 32 bytes in bf16 or
 // fp32).  The bytes are read once and written once; there is no other work to speak of.  4005 rows of 32 heads of 128 from fp32 to
-// e4m3: 46 us, 3.6 TB/s (two codes per element: see encode8_fast); 8 rows of 12 heads of 64: 4.6 us, of which nearly all is
+// e4m3: 46 us, 3.6 TB/s (2000 short blocks, each behind a chain of look-ups before its first load); 8 rows of 12 heads of 64: 4.6 us, of which nearly all is
 // a launch and the chain of look-ups (owner, length, page) before the first load.
 template <typename TS, typename TC, int HD, bool VEC>
 __global__ void __launch_bounds__(256)
