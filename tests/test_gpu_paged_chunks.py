@@ -82,10 +82,11 @@ def test_one_sequence_of_few_rows_under_a_larger_bound(cache_dtype, hd):
 
 @pytest.mark.parametrize("cache_dtype", CACHES)
 @pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("io", ["bf16", "fp16"])
 @pytest.mark.parametrize("scale,k_gain", [(0.05, 1.0), (-0.3, 1.0), (-0.02, 3.0), (1.0, 0.5), (1e-7, 1e6), (3e4, 1e-6)])
-def test_scales(cache_dtype, hd, scale, k_gain):
-    run(cache_dtype, 2, 1, hd, 16, [40, 70, 1], [50, 300, 90], scale=scale, k_gain=k_gain, seed=11)
-    run(cache_dtype, 2, 1, hd, 64, [60], [2100], scale=scale, k_gain=k_gain, seed=12)
+def test_scales(cache_dtype, hd, io, scale, k_gain):
+    run(cache_dtype, 2, 1, hd, 16, [40, 70, 1], [50, 300, 90], scale=scale, k_gain=k_gain, seed=11, io=io)
+    run(cache_dtype, 2, 1, hd, 64, [60], [2100], scale=scale, k_gain=k_gain, seed=12, io=io)
 
 
 @pytest.mark.parametrize("cache_dtype", CACHES)
@@ -138,4 +139,73 @@ def test_a_wait_that_runs_out_is_reported_and_the_cache_stays_usable(cache_dtype
         assert time.perf_counter() - t0 < 0.5                   # a millisecond or two; the limit of a wait is two seconds
         assert torch.equal(cache.attention(0, q, b), want)
         assert cache.status() == 0
+    cache.close()
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
+@pytest.mark.parametrize("io", ["bf16", "fp16"])
+@pytest.mark.parametrize("new,length", [([3, 1, 70], [30, 17, 90]), ([74], [1500])])
+def test_strided_queries_and_outputs(cache_dtype, io, new, length):
+    # slices of wider rows, nothing 16-byte aligned, heads ahead of rows, one query for all heads; results into a strided tensor
+    lay = P.Layout(new, length, 16, seed=8)
+    H, hd, n = 4, 64, 74
+    cache = P.make_cache(lay, H, H, hd, cache_dtype)
+    contents = P.fill(cache, lay, seed=9)
+    g = torch.Generator().manual_seed(10)
+    draw = lambda *shape: torch.randn(*shape, generator=g).to(P.TORCH[io]).cuda()  # noqa: E731
+    for q in (draw(n, 3 * H * hd)[:, :H * hd].unflatten(1, (H, hd)), draw(n, H, hd + 3)[..., 3:], draw(H, n, hd).transpose(0, 1), draw(n, 1, hd).expand(n, H, hd)):
+        wide = torch.full((H, n, hd + 1), 5.0, dtype=q.dtype, device="cuda")
+        out = wide.transpose(0, 1)[..., 1:]
+        cache.attention(0, q, lay.batch(), out=out)
+        want, R, terms = B.reference(q.cpu(), contents, lay, hd ** -0.5, 1)
+        assert float(B.over(out.cpu(), want, R, terms, hd, q.dtype).max()) <= 1
+        assert bool((wide[..., 0] == 5).all())
+        assert torch.equal(out, cache.attention(0, q, lay.batch()))
+    assert cache.status() == 0
+    cache.close()
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
+@pytest.mark.parametrize("new,length", [([50, 60, 1], [60, 200, 9]), ([70], [3000])])
+def test_a_query_that_is_not_finite_spoils_its_own_row_only(cache_dtype, new, length):
+    lay = P.Layout(new, length, 16, seed=7)
+    cache = P.make_cache(lay, 2, 2, 64, cache_dtype)
+    contents = P.fill(cache, lay, seed=8)
+    q = torch.randn(lay.n_tokens, 2, 64, generator=torch.Generator().manual_seed(9)).half()
+    ref = B.reference(q, contents, lay, 0.125, 1)
+    for value in (float("nan"), float("inf"), float("-inf")):
+        bad = q.clone()
+        bad[7, 1, 5] = value
+        got = cache.attention(0, bad.cuda(), lay.batch()).cpu()
+        assert bool((torch.isnan(got[7, 1]) | ((got[7, 1] == 0) & (value == value))).all())
+        got[7, 1] = ref[0][7, 1].half()
+        assert float(B.over(got, *ref, 64, q.dtype).max()) <= 1
+    assert cache.status() == 0
+    cache.close()
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
+@pytest.mark.parametrize("new,length", [([300] * 4, [900] * 4), ([300, 1] * 3, [900, 2000] * 3), ([64], [4000])])
+def test_captured_calls_with_pairs(cache_dtype, new, length):
+    # one graph replayed with other queries in the same memory, a copy right behind each call
+    lay = P.Layout(new, length, 32, seed=1)
+    cache = P.make_cache(lay, 4, 2, 128, cache_dtype)
+    P.fill(cache, lay, seed=2)
+    b = lay.batch()
+    q = torch.zeros(lay.n_tokens, 4, 128, dtype=torch.float16, device="cuda")
+    out, copy = torch.zeros_like(q), torch.zeros_like(q)
+    with torch.cuda.stream(cache.stream):
+        cache.attention(0, q, b, out=out)
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=cache.stream):
+            cache.attention(0, q, b, out=out)
+            copy.copy_(out)
+        g = torch.Generator(device="cuda").manual_seed(3)
+        for _ in range(20):
+            q.normal_(generator=g)
+            graph.replay()
+            got = copy.clone()
+            assert torch.equal(got, cache.attention(0, q, b))
+    assert cache.status() == 0
     cache.close()
