@@ -347,8 +347,8 @@ int sd_cache_read(sd_cache *c, int layer, const sd_batch *batch, const sd_heads 
  *   out[r, h] = sum_j softmax_j(scale * q[r, h] . K[j, g]) V[j, g],  g = h / (n_heads / n_kv_heads).
  * q, out: rows [n_tokens, n_heads, head_dim].  scale: at most 2e38 in magnitude; 0 stands for head_dim^-1/2.  Single tokens, chunks
  * and both in one call.  Sums and softmax statistics are fp32.  Over an fp32 cache nothing is rounded before the output; over the
- * others queries and weights enter the products with 16 bits or more, except that the weights may enter as bf16 where
- * both q and out are bf16.  The numbers of sequences, tokens and rows and the bounds max_new and max_len choose the kernels and
+ * others queries and weights enter the products with 22 bits or more where out is fp32, with 16 or more where it is not, except that the
+ * weights may enter as bf16 where both q and out are bf16.  The numbers of sequences, tokens and rows and the bounds max_new and max_len choose the kernels and
  * where the keys are split, and rows that are computed side by side raise their running maximum together: the same call (batch description,
  * bounds and inputs) gives the same bits, the same row in another call agrees within that rounding.  The result of a query row
  * with a NaN is NaN, with an infinity NaN or 0; other rows and heads do not see it beyond that rounding.  A weight before the

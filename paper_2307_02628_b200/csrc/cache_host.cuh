@@ -12,7 +12,7 @@ struct sd_cache {
   size_t layer_bytes, v_off, ks_off, vs_off;   // K pool, V pool, K scales, V scales: offsets within a layer
   size_t minus_pos, last_row, part_acc, part_ml, counters, status_off, total;
   sd::EncodeTiledFn encode = nullptr;
-  int tile_blocks[9] = {};   // blocks per SM of each form of the kernel for few rows
+  int tile_blocks[12] = {};   // blocks per SM of each form of the kernel for few rows
   int64_t launches = 0;      // kernels launched
   bool test_expire = false;  // test hook: the next launch for chunks makes a wait run out (one shot)
   unsigned long long tile_ready = 0;    // bit per kernel whose shared-memory size has been allowed on this device
@@ -217,12 +217,12 @@ int pick_split(long slots, long units, long rows, int64_t max_len) {
 }
 
 // Sequences of rows_below query rows per key head or more are left out (another kernel takes them).
-template <typename TC, int HD>
+template <typename TC, int HD, bool THIRD>
 int attention_tiles(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale_log2, const sd_heads* out, int64_t rows_below, bool early = false) {
   using S = sd::ap::Shape<TC, HD>;
-  constexpr int index = (HD == 128 ? 0 : HD == 64 ? 1 : 2) + 3 * (std::is_same<TC, bf16>::value ? 0 : std::is_same<TC, int8_t>::value ? 1 : 2);
+  constexpr int index = (HD == 128 ? 0 : HD == 64 ? 1 : 2) + 3 * (THIRD ? 3 : std::is_same<TC, bf16>::value ? 0 : std::is_same<TC, int8_t>::value ? 1 : 2);
   constexpr unsigned long long bit = 1ull << index;
-  auto kernel = sd::paged_attn_tile_kernel<TC, HD>;
+  auto kernel = sd::paged_attn_tile_kernel<TC, HD, THIRD>;
   if (!(c->tile_ready & bit)) {
     int per_sm = 0;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) != cudaSuccess ||
@@ -344,10 +344,13 @@ int cache_attention(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, fl
                                  : attention_chunks<TC, HD, false>(c, l, b, q, scale_log2, out, rows_from, &split);
             if (rc != SD_OK || b->n_seqs == 1) return rc;
             // it may begin early where the two do not share the workspace for split keys
-            return attention_tiles<TC, HD>(c, l, b, q, scale_log2, out, enough, !split);
+            return attention_tiles<TC, HD, false>(c, l, b, q, scale_log2, out, enough, !split);
           }
         }
-        return attention_tiles<TC, HD>(c, l, b, q, scale_log2, out, most + 1);
+        if constexpr (std::is_same<TC, bf16>::value) {
+          if (out->dtype == SD_DTYPE_FP32) return attention_tiles<TC, HD, true>(c, l, b, q, scale_log2, out, most + 1);
+        }
+        return attention_tiles<TC, HD, false>(c, l, b, q, scale_log2, out, most + 1);
       }
     });
   });

@@ -427,3 +427,52 @@ def test_threads_may_share_a_cache(cache_dtype):
     assert not wrong
     assert cache.status() == 0
     cache.close()
+
+
+def two_keys(cache_dtype, hd, q, k, v, scale):
+    """Attention of single tokens over two keys each: q [seqs, heads, hd], k and v [2, hd] alike for all."""
+    seqs, heads = q.shape[:2]
+    cache = binding.PagedCache(1, heads, heads, hd, 8, seqs, seqs, 2 * seqs, dtype=cache_dtype)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    pages, length = i32([[s] for s in range(seqs)]), i32([2] * seqs)
+    both = binding.CacheBatch(pages, i32([2 * s for s in range(seqs + 1)]), length, 2 * seqs, 2, 2)
+    rows = lambda x: x.unsqueeze(1).expand(2, heads, hd).repeat(seqs, 1, 1).cuda()  # noqa: E731
+    cache.append(0, rows(k), rows(v), both)
+    out = cache.attention(0, q.cuda(), binding.CacheBatch(pages, i32(list(range(seqs + 1))), length, seqs, 1, 2), scale=scale).cpu().double()
+    assert out.dtype == torch.float64 and cache.status() == 0
+    cache.close()
+    return out
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
+@pytest.mark.parametrize("hd", [32, 64, 128])
+def test_fp32_results_keep_the_bits_of_fp32_queries(cache_dtype, hd):
+    # Scores 0 and -hd scale q with q = 1 + 2^-9 + 2^-18 in every element: the sums are exact in fp32, and parts of 8 + 8 bits would lose the
+    # last term.  The result is the second key's weight e^-10: the exponent of size 14.4 in base 2 is rounded three times (the scale in base 2, the
+    # product, the subtraction), 3 * 14.4 * 2^-24 * ln 2 = 1.8e-6, the key's scale in 8 bits and a query of 22 bits cost as much again,
+    # the exponential 2^-22, weights and division 2^-22 each: below 2^-17.  Without the last term it would be 10 * 2^-18 off.
+    # In 8 bits small weights lie on a fixed grid, each off by up to 2^-32 of the largest value (see paged_reference.bound): two keys, 2^-31.
+    q = torch.full((3, 5, hd), 1 + 2.0 ** -9 + 2.0 ** -18)
+    scale = float(torch.tensor(10.0 / hd))
+    k, v = torch.stack([torch.zeros(hd), -torch.ones(hd)]), torch.stack([torch.zeros(hd), torch.ones(hd)])
+    got = two_keys(cache_dtype, hd, q, k, v, scale)
+    s = -hd * scale * (1 + 2.0 ** -9 + 2.0 ** -18)
+    want = torch.exp(torch.tensor(s, dtype=torch.float64)) / (1 + torch.exp(torch.tensor(s, dtype=torch.float64)))
+    assert float((got - want).abs().max()) <= want * 2.0 ** -17 + (2.0 ** -31 if cache_dtype in P.TOP else 0)
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
+@pytest.mark.parametrize("hd", [32, 64, 128])
+def test_fp32_results_keep_the_bits_of_the_weights(cache_dtype, hd):
+    # Values 1 and -1 under nearly equal weights 1 and p = e^-s, s from 0.005 to 0.02: the result (1 - p) / (1 + p) is s / 2, and an error of p
+    # moves it by half of that error.  The exponential is off by 2^-22 at most, p as two parts of 11 or three of 8 bits by 2^-22, the sums of numbers
+    # near 1 by 2^-23, the exponent (below 2^-5) by less than 2^-27: 2^-21 in all.  Two parts of 8 bits would lose up to 2^-17.
+    g = torch.Generator().manual_seed(3)
+    q = torch.zeros(8, 16, hd)
+    q[..., 0] = 0.005 + 0.015 * torch.rand(8, 16, generator=g)
+    k = torch.zeros(2, hd)
+    k[1, 0] = -1.0
+    v = torch.stack([torch.ones(hd), -torch.ones(hd)])
+    got = two_keys(cache_dtype, hd, q, k, v, 1.0)
+    want = torch.tanh(q[..., :1].double() / 2)
+    assert float((got - want).abs().max()) <= 2.0 ** -21
