@@ -51,8 +51,8 @@ typedef enum {
 } sd_error;
 
 /* Element types.  A model's storage (sd_config.dtype) is one of the first two; the others are types of a paged
- * cache (fp32, bf16, int8, e4m3) or of the rows handed to its calls (fp32, bf16, fp16). */
-enum { SD_DTYPE_FP32 = 0, SD_DTYPE_BF16 = 1, SD_DTYPE_FP16 = 2, SD_DTYPE_INT8 = 3, SD_DTYPE_E4M3 = 4 };
+ * cache (fp32, bf16, int8, e4m3, e2m1) or of the rows handed to its calls (fp32, bf16, fp16). */
+enum { SD_DTYPE_FP32 = 0, SD_DTYPE_BF16 = 1, SD_DTYPE_FP16 = 2, SD_DTYPE_INT8 = 3, SD_DTYPE_E4M3 = 4, SD_DTYPE_E2M1 = 6 };
 
 /* Model and limits.  Plain data, copied by sd_create.
  * dtype selects the storage type of weights and the KV cache; the residual
@@ -271,9 +271,12 @@ int sd_sample(sd_handle *h, const float *d_logits, int B, const sd_sampling *set
 /* ---- paged cache ---------------------------------------------------------------------------
  *
  * A cache whose memory is handed out in pages, for sequences that come, grow and go at positions of their own (the
- * batching limitation of Section 5 does not apply to it), in fp32, bf16, or 8 bits with a scale for each token and head.
- * The object holds, per layer, a pool of K pages and one of V pages, [n_pages, n_kv_heads, page_len, head_dim], and in
- * 8 bits a scale pool [n_pages, n_kv_heads, page_len] of fp32 for each.  Which page belongs to which sequence is the
+ * batching limitation of Section 5 does not apply to it), in fp32, bf16, 8 bits with a scale for each token and head, or 4 bits with one
+ * more scale for every 16 elements of a head.
+ * The object holds, per layer, a pool of K pages and one of V pages, [n_pages, n_kv_heads, page_len, head_dim], in 8 and 4 bits
+ * a scale pool [n_pages, n_kv_heads, page_len] of fp32 for each, and in 4 bits (e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives, two codes
+ * to a byte, the even element in its lower half) a pool [n_pages, n_kv_heads, page_len, head_dim / 16] of e4m3 block scales; the value is
+ * code * block * scale.  Which page belongs to which sequence is the
  * caller's to decide: every call brings a table.
  *
  * Streams and workspaces: work is enqueued on the stream given to sd_cache_create, calls return without synchronising,
@@ -287,7 +290,7 @@ typedef struct {
   int32_t page_len;                                  /* positions per page: 8, 16, 32, 64 or 128 */
   int32_t n_pages;
   int32_t max_seqs, max_tokens;                      /* most sequences and most new tokens of one call */
-  int32_t dtype;                                     /* SD_DTYPE_FP32, BF16, INT8 or E4M3 */
+  int32_t dtype;                                     /* SD_DTYPE_FP32, BF16, INT8, E4M3 or E2M1 */
 } sd_cache_config;
 
 /* The sequences of one call and the new tokens each of them brings.  The first three are DEVICE arrays.  Row r of the new
@@ -326,12 +329,16 @@ int sd_cache_bytes(const sd_cache_config *cfg, size_t *out);
  * the pools are not.  Errors: SD_ERR_ARG, SD_ERR_CAPACITY (arena too small), SD_ERR_CUDA. */
 int sd_cache_create(const sd_cache_config *cfg, void *arena, size_t arena_bytes, void *stream, sd_cache **out);
 
-/* Device pointers of one layer's pools (scales NULL unless the cache is in 8 bits).  out pointers: host, may be NULL. */
+/* Device pointers of one layer's pools (scales NULL unless the cache is in 8 or 4 bits).  out pointers: host, may be NULL. */
 int sd_cache_layer(sd_cache *c, int layer, void **k, void **v, float **k_scale, float **v_scale);
+/* The same of the block scales (NULL unless the cache is in 4 bits). */
+int sd_cache_layer_blocks(sd_cache *c, int layer, uint8_t **k_block, uint8_t **v_block);
 
 /* Writes the new tokens' keys and values (rows [n_tokens, n_kv_heads, head_dim]) into their places, rounded to nearest,
  * ties to even.  In 8 bits the scale of a (token, head) is the largest magnitude of its head_dim elements divided by 127
- * (int8) or 448 (e4m3), in fp32, and a code is the nearest to x / scale, decided exactly.  In every type elements that are
+ * (int8), 448 (e4m3) or 2688 (e2m1), in fp32, and a code is the nearest to x / scale, decided exactly.  In 4 bits a block's scale is the
+ * e4m3 nearest to its largest magnitude / (6 scale) and a code the e2m1 nearest to x / (block scale * scale), both decided exactly; a block with
+ * an infinity takes the block scale of the row's largest.  In every type elements that are
  * not finite do not count for the scale and set the not-finite bit of the status word: infinities (and what rounds
  * to one) are stored as the largest finite value, NaN as 0, so that a masked key never puts a NaN into a sum.  Whoever writes
  * to the pools directly keeps to that.  Two rows of one call must

@@ -25,7 +25,7 @@ EXPORTS = ("sd_arena_bytes", "sd_create", "sd_schedule", "sd_schedule_compute", 
            "sd_schedule_custom", "sd_layer_capacity",
            "sd_prefill", "sd_decode_step", "sd_decode_step_static", "sd_rewind", "sd_launch_count", "sd_decode_step_host", "sd_greedy", "sd_sample_top_p", "sd_set_padding", "sd_set_rows", "sd_status", "sd_stats",
            "sd_set_option", "sd_kernel_time", "sd_kernel_time_reset", "sd_strerror", "sd_destroy",
-           "sd_sample", "sd_cache_bytes", "sd_cache_create", "sd_cache_layer", "sd_cache_append", "sd_cache_read", "sd_cache_attention",
+           "sd_sample", "sd_cache_bytes", "sd_cache_create", "sd_cache_layer", "sd_cache_layer_blocks", "sd_cache_append", "sd_cache_read", "sd_cache_attention",
            "sd_cache_status", "sd_cache_set_option", "sd_cache_destroy", "sd_extend")
 
 
@@ -66,9 +66,10 @@ class SdHeads(C.Structure):
 
 
 # element types of a paged cache and of the rows handed to its calls
-SD_DTYPE_FP32, SD_DTYPE_BF16, SD_DTYPE_FP16, SD_DTYPE_INT8, SD_DTYPE_E4M3 = 0, 1, 2, 3, 4
+SD_DTYPE_FP32, SD_DTYPE_BF16, SD_DTYPE_FP16, SD_DTYPE_INT8, SD_DTYPE_E4M3, SD_DTYPE_E2M1 = 0, 1, 2, 3, 4, 6
 _CACHE_TYPES = {"fp32": (SD_DTYPE_FP32, torch.float32), "bf16": (SD_DTYPE_BF16, torch.bfloat16),
-                "int8": (SD_DTYPE_INT8, torch.int8), "e4m3": (SD_DTYPE_E4M3, torch.float8_e4m3fn)}
+                "int8": (SD_DTYPE_INT8, torch.int8), "e4m3": (SD_DTYPE_E4M3, torch.float8_e4m3fn),
+                "e2m1": (SD_DTYPE_E2M1, torch.uint8)}
 _ROW_TYPES = {torch.float32: SD_DTYPE_FP32, torch.bfloat16: SD_DTYPE_BF16, torch.float16: SD_DTYPE_FP16}
 SD_CACHE_OPT_TEST_WAIT_EXPIRY = 1
 # bits of the status words
@@ -118,6 +119,7 @@ def lib() -> C.CDLL:
     L.sd_cache_bytes.argtypes = [C.POINTER(SdCacheConfig), C.POINTER(C.c_size_t)]
     L.sd_cache_create.argtypes = [C.POINTER(SdCacheConfig), vp, C.c_size_t, vp, C.POINTER(vp)]
     L.sd_cache_layer.argtypes = [vp, C.c_int, C.POINTER(vp), C.POINTER(vp), C.POINTER(vp), C.POINTER(vp)]
+    L.sd_cache_layer_blocks.argtypes = [vp, C.c_int, C.POINTER(vp), C.POINTER(vp)]
     L.sd_cache_append.argtypes = [vp, C.c_int, vp, vp, vp]          # structures by address
     L.sd_cache_read.argtypes = L.sd_cache_append.argtypes
     L.sd_cache_attention.argtypes = [vp, C.c_int, vp, vp, C.c_float, vp]
@@ -222,7 +224,7 @@ class _Described(threading.local):
 class PagedCache:
     """A paged KV cache (sd_cache) in an arena of its own.
 
-    dtype: "fp32", "bf16", "int8" or "e4m3".  Calls are enqueued on `stream` (default: a stream of its own).  When torch's current
+    dtype: "fp32", "bf16", "int8", "e4m3" or "e2m1" (4 bits).  Calls are enqueued on `stream` (default: a stream of its own).  When torch's current
     stream is another one, the two are ordered around every call, so tensors can be used as if the call ran on the current one.
     Several threads may call one cache; each call's work is enqueued as a whole.
     """
@@ -253,15 +255,20 @@ class PagedCache:
         self._described = _Described()
 
     def layer(self, layer: int) -> dict:
-        """Views of one layer's pools: k, v [n_pages, n_kv_heads, page_len, head_dim], in 8 bits also k_scale, v_scale."""
-        p = [C.c_void_p() for _ in range(4)]
-        _check(lib().sd_cache_layer(self.h, layer, *[C.byref(x) for x in p]), "sd_cache_layer")
+        """Views of one layer's pools: k, v [n_pages, n_kv_heads, page_len, head_dim], in 8 and 4 bits also k_scale, v_scale.  In 4 bits k, v
+        are bytes of two codes [.., head_dim / 2], and k_block, v_block [.., head_dim / 16] the block scales (e4m3)."""
+        p = [C.c_void_p() for _ in range(6)]
+        _check(lib().sd_cache_layer(self.h, layer, *[C.byref(x) for x in p[:4]]), "sd_cache_layer")
+        _check(lib().sd_cache_layer_blocks(self.h, layer, *[C.byref(x) for x in p[4:]]), "sd_cache_layer_blocks")
         c = self.cfg
         shape = (c.n_pages, c.n_kv_heads, c.page_len)
         dt = next(t for code, t in _CACHE_TYPES.values() if code == c.dtype)
         out = {}
-        for name, ptr, dtype, shp in (("k", p[0], dt, shape + (c.head_dim,)), ("v", p[1], dt, shape + (c.head_dim,)),
-                                      ("k_scale", p[2], torch.float32, shape), ("v_scale", p[3], torch.float32, shape)):
+        row = c.head_dim // 2 if c.dtype == SD_DTYPE_E2M1 else c.head_dim
+        blocks = shape + (c.head_dim // 16,)
+        for name, ptr, dtype, shp in (("k", p[0], dt, shape + (row,)), ("v", p[1], dt, shape + (row,)),
+                                      ("k_scale", p[2], torch.float32, shape), ("v_scale", p[3], torch.float32, shape),
+                                      ("k_block", p[4], torch.float8_e4m3fn, blocks), ("v_block", p[5], torch.float8_e4m3fn, blocks)):
             if ptr.value:
                 at = ptr.value - self.arena.data_ptr()
                 n = dtype.itemsize

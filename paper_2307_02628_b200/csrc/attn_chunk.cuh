@@ -10,7 +10,7 @@
 // tensor core works through both tiles' softmax.  (Scores of 128 keys at a time leave no columns for a second set: every
 // softmax then waited for its two products, 1500 of 3700 clocks.)
 //
-// Operands are bf16, the type of a bf16 cache; codes of 8-bit caches are bf16 numbers exactly.  Where queries and results are bf16 too, the only
+// Operands are bf16, the type of a bf16 cache; codes of 8-bit caches are bf16 numbers exactly, and so are 4-bit codes times their block's scale.  Where queries and results are bf16 too, the only
 // rounding is that of the weights, once to 8 bits of significand: relative to 64-bit arithmetic results are 2.3e-3 off, of which their own
 // rounding is 1.7e-3.  Queries or results with more bits (fp32, fp16) take the form PAIRS: queries and weights are sums of two
 // bf16, 16 bits, in two products each; the weights' lower halves take the other 32 columns of their scores.  Twice the
@@ -137,10 +137,27 @@ __device__ __forceinline__ void to_bf16(uint32_t w, uint32_t& lo, uint32_t& hi, 
   lo = int8_pair(__byte_perm(w, 0u, 0x4140));
   hi = int8_pair(__byte_perm(w, 0u, 0x4342));
 }
+__device__ __forceinline__ void to_bf16(uint32_t, uint32_t& lo, uint32_t& hi, e2m1) { lo = hi = 0u; }   // not reached: four_to_bf16
 __device__ __forceinline__ void to_bf16(uint32_t w, uint32_t& lo, uint32_t& hi, e4m3) {
   const float2 a = e4m3_widen(w & 0xffffu), b = e4m3_widen(w >> 16);
   lo = pack_bf16(a.x, a.y);
   hi = pack_bf16(b.x, b.y);
+}
+// Eight 4-bit codes (a word) to four bf16 pairs, times `unit`: their block's scale times 2^115, twice.  A code's three lower bits, read as the
+// last two of the exponent and the first of the fraction, are the code times 2^-126, subnormal or not, so that the product, exact, is
+// code times scale times 2^-11 (2^-126 and not its square would need a scale beyond the type's range).
+constexpr float FOUR_UNIT = 0x1p115f, FOUR_BACK = 2048.f;
+__device__ __forceinline__ uint32_t bmul2(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ void four_to_bf16(uint32_t w, uint32_t unit, uint32_t (&o)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t a = __byte_perm(w, 0u, 0x0444 | i << 12);                 // byte i, codes 2 i and 2 i + 1, in the uppermost eight bits
+    const uint32_t two = (a | a >> 12) & 0xf000f000u;                        // the odd one above the even one
+    o[i] = bmul2((two | two >> 6) & 0x81c081c0u, unit);                      // sign, and the other three bits as said
+  }
 }
 
 }  // namespace ac
@@ -155,7 +172,7 @@ template <typename TC, int HD, bool PAIRS>
 __global__ void __launch_bounds__(ac::THREADS, 1)
 paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, int use_maps,
                         const BatchView b, const Rows q, const Rows out, const TC* __restrict__ Kp, const TC* __restrict__ Vp,
-                        const float* __restrict__ Ksc, const float* __restrict__ Vsc, int group, float scale_log2, bool q_vec, bool out_vec,
+                        const float* __restrict__ Ksc, const float* __restrict__ Vsc, const uint8_t* __restrict__ Kb, const uint8_t* __restrict__ Vb, int group, float scale_log2, bool q_vec, bool out_vec,
                         int blocks_per_seq, int rows_from, int chunk, float* part_acc, float* part_ml, int test_expire) {
   using namespace ac;
   using L = Layout<HD, PAIRS>;
@@ -454,7 +471,8 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LOADER_REGS));
     const int w = warp - 8, tid = w * 32 + lane;
     const int* table = b.pages + (size_t)seq * b.pages_per_seq;
-    constexpr int E = sizeof(TC), PER_ROW = HD * E / 16;          // 16-byte pieces of a stored key
+    constexpr bool FOUR = kFour<TC>;
+    constexpr int E = sizeof(TC), PER_ROW = row_units<TC>(HD) * E / 16;   // 16-byte pieces of a stored key
     constexpr int ROWS_AT_ONCE = 32 / PER_ROW;                    // of a warp
     constexpr int STEPS = KEYS / (4 * ROWS_AT_ONCE);
     const int most = min(len - key0, n_tiles * KEYS);             // keys past it are filled with zeros
@@ -472,7 +490,11 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     auto source = [&](const TC* pool, int j, int key, int page, uint32_t pages_ok) -> const TC* {
       page = __shfl_sync(0xffffffffu, page, key >> 3);
       const bool on = j * KEYS + key < most && ((pages_ok >> (key >> 3)) & 1u);
-      return on ? pool + b.entry(page, g_head, key0 + j * KEYS + key) * HD + c * (16 / E) : nullptr;
+      return on ? pool + b.entry(page, g_head, key0 + j * KEYS + key) * row_units<TC>(HD) + c * (16 / E) : nullptr;
+    };
+    // the two block scales of such a piece (4 bits)
+    auto ask_blocks = [&](const TC* src, const TC* pool, const uint8_t* blocks) -> uint32_t {
+      return src ? __ldg(reinterpret_cast<const uint16_t*>(blocks + (src - pool) / (kBlock / 2))) : 0u;
     };
     // this thread's key's scales, zeros where there is none
     auto ask_scales = [&](int j, int page, uint32_t pages_ok) {
@@ -486,8 +508,8 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       if (tid == 0) *reinterpret_cast<uint32_t*>(side + 2 * KEYS) = pages_ok;
       if (pages_ok != 0xffffu && w == 0 && lane == 0) b.bad();
       if (SCALED) {
-        side[tid] = scales.x * fabsf(scale_log2);
-        side[KEYS + tid] = scales.y;
+        side[tid] = scales.x * fabsf(scale_log2) * (FOUR ? FOUR_BACK : 1.f);
+        side[KEYS + tid] = scales.y * (FOUR ? FOUR_BACK : 1.f);
       }
       __syncwarp();
       if (lane == 0) arrive(sidefull + 8 * (j % SIDE));
@@ -570,17 +592,31 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       }
     } else {
       uint4 k[STEPS], v[STEPS];                                   // the next tile's codes, on their way
-      auto request = [&](const TC* pool, uint4 (&x)[STEPS], int j, int page, uint32_t pages_ok) {
+      uint32_t kb[FOUR ? STEPS : 1], vb[FOUR ? STEPS : 1];        // and their block scales
+      auto request = [&](const TC* pool, uint4 (&x)[STEPS], const uint8_t* blocks, uint32_t (&xb)[FOUR ? STEPS : 1], int j, int page, uint32_t pages_ok) {
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
           const TC* src = source(pool, j, key_of(i), page, pages_ok);
           x[i] = src ? __ldg(reinterpret_cast<const uint4*>(src)) : make_uint4(0u, 0u, 0u, 0u);
+          if constexpr (FOUR) xb[i] = ask_blocks(src, pool, blocks);
         }
       };
-      auto convert = [&](const uint4 (&x)[STEPS], uint32_t dst) {
+      auto convert = [&](const uint4 (&x)[STEPS], const uint32_t (&xb)[FOUR ? STEPS : 1], uint32_t dst) {
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
           const int key = key_of(i);
+          if constexpr (FOUR) {
+            const float2 unit = e4m3_widen(xb[i]);
+            const uint32_t u[2] = {pack_bf16(unit.x * FOUR_UNIT, unit.x * FOUR_UNIT), pack_bf16(unit.y * FOUR_UNIT, unit.y * FOUR_UNIT)};
+            const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+              uint32_t o[4];
+              four_to_bf16(w[n], u[n >> 1], o);
+              sts16(dst + piece(key, 4 * c + n), o[0], o[1], o[2], o[3]);
+            }
+            continue;
+          }
           uint32_t o[8];
           to_bf16(x[i].x, o[0], o[1], TC{});
           to_bf16(x[i].y, o[2], o[3], TC{});
@@ -593,23 +629,23 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       int page = page_next;
       uint32_t pages_ok = exists(0, page);
       float2 scales = ask_scales(0, page, pages_ok);
-      request(Kp, k, 0, page, pages_ok);
-      request(Vp, v, 0, page, pages_ok);
+      request(Kp, k, Kb, kb, 0, page, pages_ok);
+      request(Vp, v, Vb, vb, 0, page, pages_ok);
       page_next = look_up(1);
       for (int j = 0; j < n_tiles; ++j) {
         const uint32_t pages_next = exists(j + 1, page_next);
         if (!(ok = wait_free(kempty, j))) break;
         begin_side(j, scales, pages_ok);
-        convert(k, base + L::K + (j % STAGES) * L::TILE);
+        convert(k, kb, base + L::K + (j % STAGES) * L::TILE);
         announce(kfull, j);
         if (j + 1 < n_tiles) {
           scales = ask_scales(j + 1, page_next, pages_next);
-          request(Kp, k, j + 1, page_next, pages_next);
+          request(Kp, k, Kb, kb, j + 1, page_next, pages_next);
         }
         if (!(ok = wait_free(vempty, j))) break;
-        convert(v, base + L::V + (j % STAGES) * L::TILE);
+        convert(v, vb, base + L::V + (j % STAGES) * L::TILE);
         announce(vfull, j);
-        if (j + 1 < n_tiles) request(Vp, v, j + 1, page_next, pages_next);
+        if (j + 1 < n_tiles) request(Vp, v, Vb, vb, j + 1, page_next, pages_next);
         page = page_next;
         pages_ok = pages_next;
         page_next = look_up(j + 2);

@@ -5,14 +5,14 @@
 struct sd_cache {
   std::mutex busy;           // held while a call enqueues: the launches of one call share a workspace and stay together
   sd_cache_config cfg;
-  int esize, page_shift, group, device, sm_count;
-  bool scaled;
+  int row_bytes, page_shift, group, device, sm_count;            // row_bytes: of a (token, head) in the pool
+  bool scaled, four;
   char* arena;
   cudaStream_t stream;
-  size_t layer_bytes, v_off, ks_off, vs_off;   // K pool, V pool, K scales, V scales: offsets within a layer
+  size_t layer_bytes, v_off, ks_off, vs_off, kb_off, vb_off;   // K pool, V pool, K and V scales, K and V block scales: offsets within a layer
   size_t minus_pos, last_row, part_acc, part_ml, counters, status_off, total;
   sd::EncodeTiledFn encode = nullptr;
-  int tile_blocks[12] = {};   // blocks per SM of each form of the kernel for few rows
+  int tile_blocks[15] = {};   // blocks per SM of each form of the kernel for few rows
   int64_t launches = 0;      // kernels launched
   bool test_expire = false;  // test hook: the next launch for chunks makes a wait run out (one shot)
   unsigned long long tile_ready = 0;    // bit per kernel whose shared-memory size has been allowed on this device
@@ -54,27 +54,31 @@ bool valid_cache_config(const sd_cache_config* c) {
   if (c->n_heads % c->n_kv_heads || c->n_heads > 65535) return false;                // heads are a grid dimension
   if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128) return false;
   if (c->page_len < 8 || c->page_len > 128 || (c->page_len & (c->page_len - 1))) return false;
-  return c->dtype == SD_DTYPE_FP32 || c->dtype == SD_DTYPE_BF16 || c->dtype == SD_DTYPE_INT8 || c->dtype == SD_DTYPE_E4M3;
+  return c->dtype == SD_DTYPE_FP32 || c->dtype == SD_DTYPE_BF16 || c->dtype == SD_DTYPE_INT8 || c->dtype == SD_DTYPE_E4M3 || c->dtype == SD_DTYPE_E2M1;
 }
 
 // Lays the arena out; false when a size does not fit 62 bits.
 bool carve_cache(const sd_cache_config& c, sd_cache& A) {
   A.cfg = c;
-  A.scaled = c.dtype == SD_DTYPE_INT8 || c.dtype == SD_DTYPE_E4M3;
-  A.esize = c.dtype == SD_DTYPE_FP32 ? 4 : c.dtype == SD_DTYPE_BF16 ? 2 : 1;
+  A.four = c.dtype == SD_DTYPE_E2M1;
+  A.scaled = c.dtype == SD_DTYPE_INT8 || c.dtype == SD_DTYPE_E4M3 || A.four;
+  A.row_bytes = A.four ? c.head_dim / 2 : c.head_dim * (c.dtype == SD_DTYPE_FP32 ? 4 : c.dtype == SD_DTYPE_BF16 ? 2 : 1);
   A.page_shift = 0;
   while ((1 << A.page_shift) < c.page_len) ++A.page_shift;
   A.group = c.n_heads / c.n_kv_heads;
   const unsigned __int128 entries = (unsigned __int128)c.n_pages * c.n_kv_heads * c.page_len;
-  const unsigned __int128 per_layer = 2 * entries * (c.head_dim * A.esize + (A.scaled ? 4 : 0)) + 4 * kAlign;
+  const int blocks = A.four ? c.head_dim / sd::kBlock : 0;
+  const unsigned __int128 per_layer = 2 * entries * (A.row_bytes + (A.scaled ? 4 : 0) + blocks) + 6 * kAlign;
   if (per_layer * c.n_layers > ((unsigned __int128)1 << 61)) return false;
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes); return o; };
-  const size_t values = (size_t)entries * c.head_dim * A.esize, scales = A.scaled ? (size_t)entries * 4 : 0;
+  const size_t values = (size_t)entries * A.row_bytes, scales = A.scaled ? (size_t)entries * 4 : 0;
   take(values);
   A.v_off = take(values);
   A.ks_off = take(scales);
   A.vs_off = take(scales);
+  A.kb_off = take((size_t)entries * blocks);
+  A.vb_off = take((size_t)entries * blocks);
   A.layer_bytes = off;
   off *= c.n_layers;
   A.minus_pos = take((size_t)c.max_tokens * 4);
@@ -127,12 +131,13 @@ sd::BatchView view_of(const sd_cache* c, const sd_batch* b) {
                        c->cfg.n_pages, c->cfg.page_len, c->page_shift, c->cfg.n_kv_heads, c->status()};
 }
 
-template <typename TC> struct LayerPools { TC *k, *v; float *ks, *vs; };
+template <typename TC> struct LayerPools { TC *k, *v; float *ks, *vs; uint8_t *kb, *vb; };
 template <typename TC>
 LayerPools<TC> pools(const sd_cache* c, int l) {
   char* p = c->layer(l);
   return {reinterpret_cast<TC*>(p), reinterpret_cast<TC*>(p + c->v_off), c->scaled ? reinterpret_cast<float*>(p + c->ks_off) : nullptr,
-          c->scaled ? reinterpret_cast<float*>(p + c->vs_off) : nullptr};
+          c->scaled ? reinterpret_cast<float*>(p + c->vs_off) : nullptr,
+          c->four ? reinterpret_cast<uint8_t*>(p + c->kb_off) : nullptr, c->four ? reinterpret_cast<uint8_t*>(p + c->vb_off) : nullptr};
 }
 
 // Calls f with a value of the cache's element type, resp. the rows' element type, resp. the head size as a constant.
@@ -141,6 +146,7 @@ template <typename F> int with_cache_type(int dtype, F f) {
     case SD_DTYPE_FP32: return f(float{});
     case SD_DTYPE_BF16: return f(bf16{});
     case SD_DTYPE_INT8: return f(int8_t{});
+    case SD_DTYPE_E2M1: return f(sd::e2m1{});
     default: return f(sd::e4m3{});
   }
 }
@@ -173,7 +179,7 @@ int cache_append(sd_cache* c, int l, const sd_batch* b, const sd_heads* k, const
         constexpr int HD = decltype(hd)::value;
         auto kernel = vec ? sd::cache_append_kernel<TS, TC, HD, true> : sd::cache_append_kernel<TS, TC, HD, false>;
         const int shift = row_shift(c, b);
-        kernel<<<((b->n_tokens - 1) >> shift) + 1, 256, 0, c->stream>>>(view_of(c, b), shift, rows_of(k), rows_of(v), P.k, P.v, P.ks, P.vs);
+        kernel<<<((b->n_tokens - 1) >> shift) + 1, 256, 0, c->stream>>>(view_of(c, b), shift, rows_of(k), rows_of(v), P.k, P.v, P.ks, P.vs, P.kb, P.vb);
         return launched(c);
       });
     });
@@ -192,7 +198,7 @@ int cache_read(sd_cache* c, int l, const sd_batch* b, const sd_heads* k, const s
         auto kernel = vec ? sd::cache_read_kernel<TO, TC, HD, true> : sd::cache_read_kernel<TO, TC, HD, false>;
         const int shift = row_shift(c, b);
         kernel<<<((b->n_tokens - 1) >> shift) + 1, 256, 0, c->stream>>>(view_of(c, b), shift, rows_of(k), rows_of(v), (const TC*)P.k, (const TC*)P.v,
-                                                   (const float*)P.ks, (const float*)P.vs);
+                                                   (const float*)P.ks, (const float*)P.vs, (const uint8_t*)P.kb, (const uint8_t*)P.vb);
         return launched(c);
       });
     });
@@ -217,10 +223,12 @@ int pick_split(long slots, long units, long rows, int64_t max_len) {
 }
 
 // Sequences of rows_below query rows per key head or more are left out (another kernel takes them).
+template <typename TC> constexpr int kTypeIndex = std::is_same<TC, bf16>::value ? 0 : std::is_same<TC, int8_t>::value ? 1 : std::is_same<TC, sd::e4m3>::value ? 2 : 4;
+
 template <typename TC, int HD, bool THIRD>
 int attention_tiles(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale_log2, const sd_heads* out, int64_t rows_below, bool early = false) {
   using S = sd::ap::Shape<TC, HD>;
-  constexpr int index = (HD == 128 ? 0 : HD == 64 ? 1 : 2) + 3 * (THIRD ? 3 : std::is_same<TC, bf16>::value ? 0 : std::is_same<TC, int8_t>::value ? 1 : 2);
+  constexpr int index = (HD == 128 ? 0 : HD == 64 ? 1 : 2) + 3 * (THIRD ? 3 : kTypeIndex<TC>);
   constexpr unsigned long long bit = 1ull << index;
   auto kernel = sd::paged_attn_tile_kernel<TC, HD, THIRD>;
   if (!(c->tile_ready & bit)) {
@@ -240,7 +248,7 @@ int attention_tiles(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, fl
   const int chunk = pick_split((long)c->tile_blocks[index] * c->sm_count, (long)units, (long)units * slot_rows, max_len);
   const int splits = (int)(((int64_t)max_len + chunk - 1) / chunk);
   sd::launch_kernel(early, c->stream, kernel, dim3((unsigned)units, splits), dim3(sd::ap::THREADS), S::SMEM,
-      view_of(c, b), rows_of(q), rows_of(out), (const TC*)P.k, (const TC*)P.v, (const float*)P.ks, (const float*)P.vs, c->group, scale_log2, wide(q),
+      view_of(c, b), rows_of(q), rows_of(out), (const TC*)P.k, (const TC*)P.v, (const float*)P.ks, (const float*)P.vs, (const uint8_t*)P.kb, (const uint8_t*)P.vb, c->group, scale_log2, wide(q),
       tiles, (int)std::min<int64_t>(rows_below, 0x7fffffff), chunk, slot_rows, c->at<float>(c->part_acc), c->at<float>(c->part_ml), c->at<int>(c->counters), early);
   return launched(c);
 }
@@ -276,7 +284,7 @@ int64_t pick_chunk_split(int64_t slots, int64_t units, int64_t rows, int64_t max
 template <typename TC, int HD, bool PAIRS>
 int attention_chunks(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale_log2, const sd_heads* out, int rows_from, bool* split) {
   using L = sd::ac::Layout<HD, PAIRS>;
-  constexpr unsigned long long bit = 1ull << (32 + (HD == 128 ? 0 : 1) + 2 * (std::is_same<TC, bf16>::value ? 0 : std::is_same<TC, int8_t>::value ? 1 : 2) + (PAIRS ? 6 : 0));
+  constexpr unsigned long long bit = 1ull << (32 + (HD == 128 ? 0 : 1) + 2 * (kTypeIndex<TC> == 4 ? 3 : kTypeIndex<TC>) + (PAIRS ? 8 : 0));
   auto kernel = sd::paged_attn_chunk_kernel<TC, HD, PAIRS>;
   if (!(c->tile_ready & bit)) {
     cudaFuncAttributes attr;                 // the warpgroups redistribute what the block is launched with: it must be that much
@@ -297,7 +305,7 @@ int attention_chunks(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, f
   const int64_t chunk = pick_chunk_split(c->sm_count, units, rows, max_len);
   const int splits = chunk == kNoSplit ? 1 : (int)((max_len + chunk - 1) / chunk);
   kernel<<<dim3((unsigned)grid, splits), sd::ac::THREADS, L::SMEM, c->stream>>>(
-      mk, mv, use_maps, view_of(c, b), rows_of(q), rows_of(out), (const TC*)P.k, (const TC*)P.v, (const float*)P.ks, (const float*)P.vs, c->group, scale_log2, wide(q), wide(out),
+      mk, mv, use_maps, view_of(c, b), rows_of(q), rows_of(out), (const TC*)P.k, (const TC*)P.v, (const float*)P.ks, (const float*)P.vs, (const uint8_t*)P.kb, (const uint8_t*)P.vb, c->group, scale_log2, wide(q), wide(out),
       blocks, rows_from, (int)chunk, c->at<float>(c->part_acc), c->at<float>(c->part_ml), c->test_expire ? 1 : 0);
   c->test_expire = false;
   if (splits > 1)
@@ -442,6 +450,14 @@ int sd_cache_layer(sd_cache* c, int layer, void** k, void** v, float** ks, float
   if (v) *v = P.v;
   if (ks) *ks = P.ks;
   if (vs) *vs = P.vs;
+  return SD_OK;
+}
+
+int sd_cache_layer_blocks(sd_cache* c, int layer, uint8_t** kb, uint8_t** vb) {
+  if (!c || layer < 0 || layer >= c->cfg.n_layers) return SD_ERR_ARG;
+  const auto P = pools<char>(c, layer);
+  if (kb) *kb = P.kb;
+  if (vb) *vb = P.vb;
   return SD_OK;
 }
 

@@ -1,10 +1,11 @@
-// Paged KV cache: storing new tokens' keys and values (fp32, bf16, or 8 bits with a scale per token and head), reading
-// them back, and the attention of one row at a time over it.  A pool is [n_pages, n_kv_heads, page_len, head_dim];
+// Paged KV cache: storing new tokens' keys and values (fp32, bf16, 8 bits with a scale per token and head, or 4 bits with one more
+// scale per 16 elements), reading them back, and the attention of one row at a time over it.  A pool is [n_pages, n_kv_heads, page_len, head_dim];
 // position p of sequence s is slot p % page_len of page pages[s * pages_per_seq + p / page_len].
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
+#include <cuda_fp4.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -15,13 +16,23 @@ namespace sd {
 enum : int { STATUS_BAD_BATCH = 16, STATUS_BAD_SETTING = 32, STATUS_NOT_FINITE = 64 };
 
 struct e4m3 { uint8_t bits; };
+struct e2m1 { uint8_t bits; };                // two codes, the even element in the lower half
 
-// TOP: largest code of the 8-bit types, 0 for the others.  MOST: largest finite value of the others.
+// TOP: largest code of the 8-bit types (largest code times largest block scale of e2m1), 0 for the others.  MOST: largest finite value
+// of the others.
 template <typename T> struct CacheType;
 template <> struct CacheType<float> { static constexpr float TOP = 0.f, MOST = 3.402823466e38f; };
 template <> struct CacheType<__nv_bfloat16> { static constexpr float TOP = 0.f, MOST = 3.389531390e38f; };   // (2 - 2^-7) 2^127
 template <> struct CacheType<int8_t> { static constexpr float TOP = 127.f, MOST = 0.f; };
 template <> struct CacheType<e4m3> { static constexpr float TOP = 448.f, MOST = 0.f; };
+template <> struct CacheType<e2m1> { static constexpr float TOP = 2688.f, MOST = 0.f; };
+
+// Four bits: value = code * block * scale, with a block scale in e4m3 for every 16 elements.  Code times block is at most 2 + 4 bits of
+// significand, a multiple of 2^-10 and at most 2688: exact in fp16, and in bf16.
+template <typename T> constexpr bool kFour = false;
+template <> inline constexpr bool kFour<e2m1> = true;
+template <typename T> __host__ __device__ constexpr int row_units(int hd) { return kFour<T> ? hd / 2 : hd; }        // elements of the pool's type per row
+constexpr int kBlock = 16;
 
 // A batch as the kernels see it: the caller's device arrays and the bounds that every index is held to.
 struct BatchView {
@@ -231,6 +242,79 @@ __device__ __noinline__ float quotient_sticky(float x, float s) {
   return (double)f == q ? f : __uint_as_float(__float_as_uint(f) | 1u);
 }
 
+// ---- four bits
+// The block scale nearest to t / (6 s), t the block's largest magnitude: t (24 bits) differs from a border (5 bits) times 6 s (26 bits) by at least
+// 2^-31 of itself or not at all, so that the 53-bit quotient decides.  The same for a code and x / (b s), 28 bits and a border of 3.
+__device__ __noinline__ uint32_t block_exact(float t, float s) {
+  const double q = (double)t / (6.0 * (double)s);
+  const float f = __double2float_rz(q);
+  return e4m3_pair((double)f == q ? f : __uint_as_float(__float_as_uint(f) | 1u), 0.f) & 0xffu;
+}
+__device__ __forceinline__ uint32_t e2m1_pair(float even, float odd) {
+  return (uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(even, odd), __NV_E2M1, cudaRoundNearest);
+}
+__device__ __noinline__ float quotient_sticky4(float x, float b, float s) {
+  const double q = (double)x / ((double)b * (double)s);
+  const float f = __double2float_rz(q);
+  return (double)f == q ? f : __uint_as_float(__float_as_uint(f) | 1u);
+}
+__device__ __forceinline__ uint32_t block_of(float t, float s, float inv) {        // inv: about 1 / s, or 0
+  if (s == 0.f) return 0u;
+  const float y = t * (inv * 0.16666667f);         // off by less than 2^-21 of itself
+  const uint32_t both = e4m3_pair(y * (1.f - 0x1p-21f), y * (1.f + 0x1p-21f));
+  if (inv != 0.f && (both & 0xffu) == both >> 8) return both & 0xffu;
+  return block_exact(t, s);
+}
+__device__ __forceinline__ float block_value(uint32_t b) { return e4m3_widen(b).x; }
+// Eight codes of x / (b s), the fast quotients where they decide.  NaN: 0.
+__device__ __forceinline__ uint32_t encode8_four(const float (&x)[8], float b, float s, bool finite) {
+  const float unit = b * s;
+  if (unit == 0.f && (b == 0.f || s == 0.f)) return 0u;
+  const float inv = unit > 1e-30f ? __fdiv_rn(1.f, unit) : 0.f;
+  uint32_t lo = 0u, hi = 0u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float e = x[2 * i] * inv, o = x[2 * i + 1] * inv;                        // off by less than 2^-21
+    lo |= e2m1_pair(e * (1.f - 0x1p-21f), o * (1.f - 0x1p-21f)) << (8 * i);
+    hi |= e2m1_pair(e * (1.f + 0x1p-21f), o * (1.f + 0x1p-21f)) << (8 * i);
+  }
+  if (finite && inv != 0.f && lo == hi) return lo;
+  uint32_t w = 0u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float e = x[2 * i] != x[2 * i] ? 0.f : quotient_sticky4(x[2 * i], b, s), o = x[2 * i + 1] != x[2 * i + 1] ? 0.f : quotient_sticky4(x[2 * i + 1], b, s);
+    w |= e2m1_pair(e, o) << (8 * i);
+  }
+  return w;
+}
+// two codes (a byte) as fp16, the even element first
+template <int BYTE> __device__ __forceinline__ uint32_t e2m1_widen(uint32_t w) {
+  uint32_t r;
+  if constexpr (BYTE == 0) asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %1;\n cvt.rn.f16x2.e2m1x2 %0, a;\n}" : "=r"(r) : "r"(w));
+  else if constexpr (BYTE == 1) asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %1;\n cvt.rn.f16x2.e2m1x2 %0, b;\n}" : "=r"(r) : "r"(w));
+  else if constexpr (BYTE == 2) asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %1;\n cvt.rn.f16x2.e2m1x2 %0, c;\n}" : "=r"(r) : "r"(w));
+  else asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %1;\n cvt.rn.f16x2.e2m1x2 %0, d;\n}" : "=r"(r) : "r"(w));
+  return r;
+}
+__device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
+  const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// the block scales of two bytes as fp16: (first, second)
+__device__ __forceinline__ uint32_t blocks_widen(uint32_t two) {
+  const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
+  return (uint32_t)r.x | ((uint32_t)r.y << 16);
+}
+__device__ __forceinline__ void decode8_four(uint32_t w, uint32_t block, float s, float (&o)[8]) {
+  const uint32_t b = __byte_perm(blocks_widen(block), 0u, 0x1010);
+  const uint32_t v[4] = {hmul2(e2m1_widen<0>(w), b), hmul2(e2m1_widen<1>(w), b), hmul2(e2m1_widen<2>(w), b), hmul2(e2m1_widen<3>(w), b)};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v[i]));
+    o[2 * i] = f.x * s; o[2 * i + 1] = f.y * s;
+  }
+}
+
 // Eight codes of x / s the exact way, for rows whose fast quotients do not decide, with a tiny scale or with elements that are not finite.
 __device__ __forceinline__ uint2 encode8_exact(const float (&x)[8], float s, int8_t) {
   uint32_t w[2] = {0u, 0u};
@@ -300,7 +384,7 @@ __device__ __forceinline__ void decode8(uint2 v, float s, float (&o)[8], e4m3) {
 template <typename TS, typename TC, int HD, bool VEC>
 __global__ void __launch_bounds__(256)
 cache_append_kernel(const BatchView b, int row_shift, const Rows ks, const Rows vs, TC* __restrict__ Kp, TC* __restrict__ Vp,
-                    float* __restrict__ Ksc, float* __restrict__ Vsc) {
+                    float* __restrict__ Ksc, float* __restrict__ Vsc, uint8_t* __restrict__ Kb, uint8_t* __restrict__ Vb) {
   constexpr int LANES = HD / 8;
   __shared__ Places place;
   const int rows = 1 << row_shift, r0 = blockIdx.x << row_shift, n = min(rows, b.n_tokens - r0);
@@ -331,7 +415,7 @@ cache_append_kernel(const BatchView b, int row_shift, const Rows ks, const Rows 
       const bool on = i < total && row < n && place.page[row] >= 0;
       const bool is_v = unit >= b.n_kv_heads;
       const size_t e = on ? b.entry(place.page[row], is_v ? unit - b.n_kv_heads : unit, place.pos[row]) : 0;
-      TC* dst = (is_v ? Vp : Kp) + e * HD + sub * 8;
+      TC* dst = (is_v ? Vp : Kp) + e * row_units<TC>(HD) + sub * row_units<TC>(8);
       float top = 0.f;                                           // of the finite elements
       bool finite = true;
 #pragma unroll
@@ -341,7 +425,22 @@ cache_append_kernel(const BatchView b, int row_shift, const Rows ks, const Rows 
         else finite = false;                                     // NaN too
       }
       if (!finite) atomicOr(b.status, STATUS_NOT_FINITE);
-      if constexpr (CacheType<TC>::TOP > 0.f) {
+      if constexpr (kFour<TC>) {
+        float part = top;                                        // of the block's 16 elements: this lane's and its neighbour's
+        const bool inf = fabsf(x[u][0]) == INFINITY || fabsf(x[u][1]) == INFINITY || fabsf(x[u][2]) == INFINITY || fabsf(x[u][3]) == INFINITY ||
+                         fabsf(x[u][4]) == INFINITY || fabsf(x[u][5]) == INFINITY || fabsf(x[u][6]) == INFINITY || fabsf(x[u][7]) == INFINITY;
+        part = fmaxf(part, inf ? INFINITY : 0.f);                // an infinity becomes the row's largest: the block's scale is the largest one
+        part = fmaxf(part, __shfl_xor_sync(0xffffffffu, part, 1));
+#pragma unroll
+        for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float s = __fdiv_rn(top, CacheType<TC>::TOP);
+        const uint32_t block = block_of(fminf(part, top), s, s > 1e-30f ? __fdiv_rn(1.f, s) : 0.f);
+        if (on) {
+          *reinterpret_cast<uint32_t*>(dst) = encode8_four(x[u], block_value(block), s, finite);
+          if ((sub & 1) == 0) (is_v ? Vb : Kb)[e * (HD / kBlock) + sub / 2] = (uint8_t)block;
+          if (sub == 0) (is_v ? Vsc : Ksc)[e] = s;
+        }
+      } else if constexpr (CacheType<TC>::TOP > 0.f) {
 #pragma unroll
         for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         const float s = __fdiv_rn(top, CacheType<TC>::TOP);
@@ -370,7 +469,7 @@ cache_append_kernel(const BatchView b, int row_shift, const Rows ks, const Rows 
 template <typename TO, typename TC, int HD, bool VEC>
 __global__ void __launch_bounds__(256)
 cache_read_kernel(const BatchView b, int row_shift, const Rows ko, const Rows vo, const TC* __restrict__ Kp, const TC* __restrict__ Vp,
-                  const float* __restrict__ Ksc, const float* __restrict__ Vsc) {
+                  const float* __restrict__ Ksc, const float* __restrict__ Vsc, const uint8_t* __restrict__ Kb, const uint8_t* __restrict__ Vb) {
   constexpr int LANES = HD / 8;
   __shared__ Places place;
   const int rows = 1 << row_shift, r0 = blockIdx.x << row_shift, n = min(rows, b.n_tokens - r0);
@@ -395,8 +494,12 @@ cache_read_kernel(const BatchView b, int row_shift, const Rows ko, const Rows vo
       if (i >= total || row >= n || place.page[row] < 0) continue;
       const bool is_v = unit >= b.n_kv_heads;
       const size_t e = b.entry(place.page[row], is_v ? unit - b.n_kv_heads : unit, place.pos[row]);
-      const TC* src = (is_v ? Vp : Kp) + e * HD + i % LANES * 8;
-      if constexpr (SCALED) {
+      const TC* src = (is_v ? Vp : Kp) + e * row_units<TC>(HD) + i % LANES * row_units<TC>(8);
+      if constexpr (kFour<TC>) {                                 // codes and their block's scale
+        code[u].x = __ldg(reinterpret_cast<const uint32_t*>(src));
+        code[u].y = __ldg((is_v ? Vb : Kb) + e * (HD / kBlock) + i % LANES / 2);
+        scale[u] = __ldg((is_v ? Vsc : Ksc) + e);
+      } else if constexpr (SCALED) {
         code[u] = __ldg(reinterpret_cast<const uint2*>(src));
         scale[u] = __ldg((is_v ? Vsc : Ksc) + e);
       } else {
@@ -409,7 +512,8 @@ cache_read_kernel(const BatchView b, int row_shift, const Rows ko, const Rows vo
       const int row = i / LANES & (rows - 1), unit = i / LANES >> row_shift;
       if (i >= total || row >= n || place.state[row] == ROW_PADDING) continue;
       const bool is_v = unit >= b.n_kv_heads;
-      if constexpr (SCALED) decode8(code[u], scale[u], x[u], TC{});
+      if constexpr (kFour<TC>) decode8_four(code[u].x, code[u].y, scale[u], x[u]);
+      else if constexpr (SCALED) decode8(code[u], scale[u], x[u], TC{});
       const Rows& dst = is_v ? vo : ko;
       store8<VEC>(static_cast<TO*>(dst.data) + (long long)(r0 + row) * dst.row_stride + (is_v ? unit - b.n_kv_heads : unit) * dst.head_stride + i % LANES * 8, x[u]);
     }
