@@ -362,8 +362,44 @@ int sd_cache_read(sd_cache *c, int layer, const sd_batch *batch, const sd_heads 
  * division by their sum is at most 2^8, so the magnitudes of a sequence's values should add up to less than 2^119. */
 int sd_cache_attention(sd_cache *c, int layer, const sd_batch *batch, const sd_heads *q, float scale, const sd_heads *out);
 
-/* Synchronises the stream, reads the cache's status word and clears it (not to be called in a capture).  Bits: 16 a batch
- * description that is wrong, 64 an appended element that is not finite, 2 a bounded wait inside a kernel that expired, the
+/* ---- pages: forking, growing, cutting and ending sequences, compacting the pool, copying pages
+ *
+ * The books of the sequences that live in a cache, the caller's DEVICE arrays.  The calls below read and write them on the stream, decide which pages are
+ * taken, shared, given back and moved, and copy pages in all layers; nothing waits for the host, and calls may be captured.  Before a pool is
+ * used, pages = -1, len = 0, refs = 0.  A caller that reserves pages for itself sets their refs to 1.
+ * A row of the table is as in sd_batch: position p of sequence s lives in page pages[s * pages_per_seq + p / page_len].  What the device finds
+ * wrong (row numbers, lengths beyond the table, page numbers out of range, a page given back that nobody was said to hold) sets the
+ * bad-batch bit of the cache's status word and is skipped, never read or written out of range; where there are not enough free pages, bit 128 is set. */
+typedef struct {
+  int32_t *pages;            /* [n_seqs, pages_per_seq] */
+  int32_t *len;              /* [n_seqs] */
+  int32_t *refs;             /* [n_pages]: how many rows of the table hold a page; 0: free */
+  int32_t n_seqs, pages_per_seq;  /* n_seqs at most max_seqs; pages_per_seq * page_len at most 2^30 positions */
+} sd_tables;
+
+/* Fork i makes row dst[i], which has to be empty (len 0), a sequence like row src[i]: whole pages are shared, the last one, where it is not full, is
+ * copied to a page of its own.  New pages are the lowest free ones, fork by fork.  Where there are not enough, the forks from the first one on that is
+ * short, as far as they need a page, leave their rows empty.  A row that several forks are for goes to the first of them.
+ * src, dst: device int32 [n], n at most n_seqs.  Errors: SD_ERR_ARG, SD_ERR_CAPACITY, SD_ERR_CUDA. */
+int sd_cache_fork(sd_cache *c, const sd_tables *t, const int32_t *src, const int32_t *dst, int n);
+
+/* Row s takes the length len[s] (device int32 [n_seqs]; 0 ends the sequence, its own length leaves it).  First all rows give back the pages past their new
+ * ends (table entries become -1).  Then, row by row, a page that the row keeps in part and other rows hold too is replaced by a copy, so that what is
+ * appended next is the row's own, and missing pages are added; both take the lowest free pages.  Where there are not enough, the rows from the first one on that
+ * is short, as far as they need pages, stay as they were; one that was to be cut is cut but still shares its last page, and has to be
+ * resized again before it is appended to.  Positions that a row gains hold nothing until they are appended. */
+int sd_cache_resize(sd_cache *c, const sd_tables *t, const int32_t *len);
+
+/* Renumbers the pages in use (refs not 0) so that they are the first ones: those from number `used` on move, in order, to the free ones below, in order; table,
+ * refs and contents follow.  A page in use that is in no table keeps its contents too, but the caller has to follow it.
+ * n_used: device int32 [1] or NULL, the number of pages in use. */
+int sd_cache_compact(sd_cache *c, const sd_tables *t, int32_t *n_used);
+
+/* Copies page src[i] to page dst[i] in all layers (device int32 [n]).  No destination may be another copy's source or destination. */
+int sd_cache_copy(sd_cache *c, const int32_t *src, const int32_t *dst, int n);
+
+/* Synchronises the stream, reads the cache's status word and clears it (not to be called in a capture).  Bits: 128 not enough free pages, 16 a batch
+ * description or books that are wrong, 64 an appended element that is not finite, 2 a bounded wait inside a kernel that expired, the
  * results of that call being wrong.  Returns SD_ERR_DEVICE when it was not 0. */
 int sd_cache_status(sd_cache *c, int32_t *device_status);
 

@@ -26,7 +26,7 @@ EXPORTS = ("sd_arena_bytes", "sd_create", "sd_schedule", "sd_schedule_compute", 
            "sd_prefill", "sd_decode_step", "sd_decode_step_static", "sd_rewind", "sd_launch_count", "sd_decode_step_host", "sd_greedy", "sd_sample_top_p", "sd_set_padding", "sd_set_rows", "sd_status", "sd_stats",
            "sd_set_option", "sd_kernel_time", "sd_kernel_time_reset", "sd_strerror", "sd_destroy",
            "sd_sample", "sd_cache_bytes", "sd_cache_create", "sd_cache_layer", "sd_cache_layer_blocks", "sd_cache_append", "sd_cache_read", "sd_cache_attention",
-           "sd_cache_status", "sd_cache_set_option", "sd_cache_destroy", "sd_extend")
+           "sd_cache_fork", "sd_cache_resize", "sd_cache_compact", "sd_cache_copy", "sd_cache_status", "sd_cache_set_option", "sd_cache_destroy", "sd_extend")
 
 
 class SdConfig(C.Structure):
@@ -61,6 +61,10 @@ class SdBatch(C.Structure):
                [(n, C.c_int32) for n in ("n_seqs", "pages_per_seq", "n_tokens", "max_new", "max_len")]
 
 
+class SdTables(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("pages", "len", "refs")] + [("n_seqs", C.c_int32), ("pages_per_seq", C.c_int32)]
+
+
 class SdHeads(C.Structure):
     _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64), ("dtype", C.c_int32)]
 
@@ -73,7 +77,7 @@ _CACHE_TYPES = {"fp32": (SD_DTYPE_FP32, torch.float32), "bf16": (SD_DTYPE_BF16, 
 _ROW_TYPES = {torch.float32: SD_DTYPE_FP32, torch.bfloat16: SD_DTYPE_BF16, torch.float16: SD_DTYPE_FP16}
 SD_CACHE_OPT_TEST_WAIT_EXPIRY = 1
 # bits of the status words
-STATUS_BAD_TOKEN, STATUS_WAIT_EXPIRED, STATUS_BAD_BATCH, STATUS_BAD_SETTING, STATUS_NOT_FINITE = 1, 2, 16, 32, 64
+STATUS_BAD_TOKEN, STATUS_WAIT_EXPIRED, STATUS_BAD_BATCH, STATUS_BAD_SETTING, STATUS_NOT_FINITE, STATUS_NO_PAGES = 1, 2, 16, 32, 64, 128
 
 
 class SdError(RuntimeError):
@@ -123,6 +127,10 @@ def lib() -> C.CDLL:
     L.sd_cache_append.argtypes = [vp, C.c_int, vp, vp, vp]          # structures by address
     L.sd_cache_read.argtypes = L.sd_cache_append.argtypes
     L.sd_cache_attention.argtypes = [vp, C.c_int, vp, vp, C.c_float, vp]
+    L.sd_cache_fork.argtypes = [vp, vp, vp, vp, C.c_int]
+    L.sd_cache_resize.argtypes = [vp, vp, vp]
+    L.sd_cache_compact.argtypes = [vp, vp, vp]
+    L.sd_cache_copy.argtypes = [vp, vp, vp, C.c_int]
     L.sd_cache_status.argtypes = [vp, i32p]
     L.sd_cache_set_option.argtypes = [vp, C.c_int, C.c_int]
     L.sd_cache_destroy.argtypes = [vp]
@@ -212,6 +220,28 @@ class CacheBatch:
         self.ref = C.addressof(self.c)
 
 
+class PageTables:
+    """The books of the sequences in a cache (sd_tables): pages [n_seqs, pages_per_seq], length [n_seqs], refs [n_pages] (how many rows hold a
+    page; 0: free), int32 CUDA tensors that the calls on pages read and write.  `empty` makes those of a cache without sequences."""
+
+    def __init__(self, pages: torch.Tensor, length: torch.Tensor, refs: torch.Tensor):
+        for name, t in (("pages", pages), ("length", length), ("refs", refs)):
+            if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous int32 CUDA tensor")
+        if pages.dim() != 2 or length.shape != (pages.shape[0],) or refs.dim() != 1:
+            raise ValueError("shapes must be pages [n, pages_per_seq], length [n], refs [n_pages]")
+        if not pages.device == length.device == refs.device:
+            raise ValueError("pages, length and refs must be on one device")
+        self.pages, self.length, self.refs, self.index = pages, length, refs, pages.device.index
+        self.c = SdTables(pages.data_ptr(), length.data_ptr(), refs.data_ptr(), pages.shape[0], pages.shape[1])
+        self.ref = C.addressof(self.c)
+
+    @classmethod
+    def empty(cls, cache: "PagedCache", n_seqs: int, pages_per_seq: int) -> "PageTables":
+        full = lambda shape, value: torch.full(shape, value, dtype=torch.int32, device=cache.device)  # noqa: E731
+        return cls(full((n_seqs, pages_per_seq), -1), full((n_seqs,), 0), full((cache.cfg.n_pages,), 0))
+
+
 class _Described(threading.local):
     """The two tensors of a call as the library takes them: a pair for each thread, since other threads run between the filling and
     the call (new structures for every call take 0.5 us longer)."""
@@ -252,6 +282,7 @@ class PagedCache:
         L = lib()
         self._append, self._read, self._attention = L.sd_cache_append, L.sd_cache_read, L.sd_cache_attention
         self._heads, self._kv_heads, self._head_dim = n_heads, n_kv_heads, head_dim
+        self._pages_calls = L.sd_cache_fork, L.sd_cache_resize, L.sd_cache_compact, L.sd_cache_copy
         self._described = _Described()
 
     def layer(self, layer: int) -> dict:
@@ -311,6 +342,35 @@ class PagedCache:
         self._call(self._attention, "sd_cache_attention", layer, batch, scale)
         return out
 
+    def fork(self, tables: PageTables, src: torch.Tensor, dst: torch.Tensor):
+        """Rows dst[i] of the tables, empty ones, become sequences like rows src[i]: whole pages shared, a last one that is not full copied."""
+        n = self._numbers("src", src)
+        if self._numbers("dst", dst) != n:
+            raise ValueError("src and dst must have one length")
+        self._on_pages(0, "sd_cache_fork", tables, src.data_ptr(), dst.data_ptr(), n)
+
+    def resize(self, tables: PageTables, length: torch.Tensor):
+        """Row s takes the length length[s]: pages are given back or added, a page kept in part that others hold too is copied."""
+        if self._numbers("length", length) != tables.c.n_seqs:
+            raise ValueError(f"length must be [{tables.c.n_seqs}]")
+        self._on_pages(1, "sd_cache_resize", tables, length.data_ptr())
+
+    def compact(self, tables: PageTables, used: torch.Tensor | None = None) -> torch.Tensor:
+        """Moves the pages in use to the numbers from 0 on; returns how many they are, int32 [1] on the device."""
+        if used is None:
+            used = torch.empty(1, dtype=torch.int32, device=self.device)
+        if self._numbers("used", used) != 1:
+            raise ValueError("used must be [1]")
+        self._on_pages(2, "sd_cache_compact", tables, used.data_ptr())
+        return used
+
+    def copy_pages(self, src: torch.Tensor, dst: torch.Tensor):
+        """Page src[i] to page dst[i], in all layers."""
+        n = self._numbers("src", src)
+        if self._numbers("dst", dst) != n:
+            raise ValueError("src and dst must have one length")
+        self._on_pages(3, "sd_cache_copy", None, src.data_ptr(), dst.data_ptr(), n)
+
     def status(self) -> int:
         v = C.c_int32(0)
         code = lib().sd_cache_status(self.h, C.byref(v))
@@ -354,6 +414,24 @@ class PagedCache:
             self._fork()
         first, second = self._described.refs
         code = fn(self.h, layer, batch.ref, first, *scale, second)
+        if code != SD_OK:
+            raise SdError(code, name)
+        if other:
+            self._join()
+
+    def _numbers(self, name: str, t: torch.Tensor) -> int:
+        if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.get_device() != self._index:
+            raise ValueError(f"{name} must be a contiguous int32 tensor of one dimension on {self.device}")
+        return t.shape[0]
+
+    def _on_pages(self, which: int, name: str, tables: PageTables | None, *args):
+        if tables is not None and (tables.index != self._index or tables.refs.shape[0] != self.cfg.n_pages):
+            raise ValueError(f"the tables must be on {self.device}, with refs [{self.cfg.n_pages}]")
+        other = _raw_stream(self._index) != self._raw
+        if other:
+            self._fork()
+        fn = self._pages_calls[which]
+        code = fn(self.h, *args) if tables is None else fn(self.h, tables.ref, *args)
         if code != SD_OK:
             raise SdError(code, name)
         if other:

@@ -11,6 +11,7 @@ struct sd_cache {
   cudaStream_t stream;
   size_t layer_bytes, v_off, ks_off, vs_off, kb_off, vb_off;   // K pool, V pool, K and V scales, K and V block scales: offsets within a layer
   size_t minus_pos, last_row, part_acc, part_ml, counters, status_off, total;
+  size_t plan, claim, copy_from, copy_to, place, totals;         // workspace of the calls on pages
   sd::EncodeTiledFn encode = nullptr;
   int tile_blocks[15] = {};   // blocks per SM of each form of the kernel for few rows
   int64_t launches = 0;      // kernels launched
@@ -87,6 +88,12 @@ bool carve_cache(const sd_cache_config& c, sd_cache& A) {
   A.part_acc = take((size_t)kPartSlots * c.head_dim * 4);
   A.part_ml = take((size_t)kPartSlots * 8);
   A.counters = take((size_t)kPartSlots * 4);
+  A.plan = take((size_t)c.max_seqs * 16);
+  A.claim = take((size_t)c.max_seqs * 4);
+  A.copy_from = take((size_t)c.n_pages * 4);
+  A.copy_to = take((size_t)c.n_pages * 4);
+  A.place = take((size_t)c.n_pages * 4);
+  A.totals = take(256);
   A.status_off = take(256);
   A.total = off;
   return true;
@@ -403,6 +410,47 @@ int extend_layers(sd_handle* h, sd_cache* c, const sd_batch* b, const int32_t* d
   return Lc.err;
 }
 
+// ---- pages
+
+int check_tables(const sd_cache* c, const sd_tables* t) {
+  if (!t || !t->pages || !t->len || !t->refs || t->n_seqs < 1 || t->pages_per_seq < 1) return SD_ERR_ARG;
+  if ((int64_t)t->pages_per_seq * c->cfg.page_len > kMostPositions) return SD_ERR_ARG;
+  return t->n_seqs > c->cfg.max_seqs ? SD_ERR_CAPACITY : SD_OK;
+}
+
+sd::Books books_of(const sd_cache* c, const sd_tables* t) {
+  return sd::Books{t ? t->pages : nullptr, t ? t->len : nullptr, t ? t->refs : nullptr, t ? t->n_seqs : 0, t ? t->pages_per_seq : 0, c->cfg.n_pages, c->page_shift, c->status()};
+}
+
+sd::PageWork page_work(const sd_cache* c) {
+  return sd::PageWork{c->at<int4>(c->plan), c->at<int>(c->claim), c->at<int>(c->copy_from), c->at<int>(c->copy_to), c->at<int>(c->place), c->at<int>(c->totals)};
+}
+
+// The second launch of a call on pages.  n_copies NULL: n copies of the caller's lists.  planned: behind a first launch, beside whose end it may begin.
+int copy_pages(sd_cache* c, const sd_tables* t, const int* from, const int* to, const int* n_copies, int n, bool remap, bool planned) {
+  sd::PageRuns runs = {};
+  const int64_t entries = (int64_t)c->cfg.n_kv_heads * c->cfg.page_len;
+  auto run = [&](int64_t offset, int64_t bytes) {
+    if (bytes == 0) return;
+    runs.offset[runs.n] = offset;
+    runs.words[runs.n] = (int)(bytes / 16);
+    runs.pieces[runs.n] = (int)((bytes / 16 + sd::PIECE - 1) / sd::PIECE);
+    runs.all_pieces += runs.pieces[runs.n++];
+  };
+  const int64_t scales = c->scaled ? entries * 4 : 0, blocks = c->four ? entries * (c->cfg.head_dim / sd::kBlock) : 0;
+  run(0, entries * c->row_bytes);
+  run((int64_t)c->v_off, entries * c->row_bytes);
+  run((int64_t)c->ks_off, scales);
+  run((int64_t)c->vs_off, scales);
+  run((int64_t)c->kb_off, blocks);
+  run((int64_t)c->vb_off, blocks);
+  const int64_t most = (int64_t)(n_copies ? c->cfg.n_pages : n) * c->cfg.n_layers * runs.all_pieces;
+  const int grid = (int)std::min<int64_t>(most, (int64_t)c->sm_count * 4);
+  sd::launch_kernel(planned, c->stream, sd::pages_copy_kernel, dim3(grid), dim3(256), 0, books_of(c, t), c->arena, (long long)c->layer_bytes, (int)c->cfg.n_layers, runs, from, to,
+                    n_copies, n, (const int*)c->at<int>(c->place), remap ? 1 : 0);
+  return launched(c);
+}
+
 }  // namespace
 
 extern "C" {
@@ -500,6 +548,57 @@ int sd_cache_attention(sd_cache* c, int layer, const sd_batch* b, const sd_heads
   if (!guard.ok) return SD_ERR_CUDA;
   std::lock_guard<std::mutex> lock(c->busy);
   return cache_attention(c, layer, b, q, scale, out);
+}
+
+int sd_cache_fork(sd_cache* c, const sd_tables* t, const int32_t* src, const int32_t* dst, int n) {
+  if (!c || n < 0) return SD_ERR_ARG;
+  const int rc = check_tables(c, t);
+  if (rc != SD_OK) return rc;
+  if (n == 0) return SD_OK;
+  if (!src || !dst || n > t->n_seqs) return SD_ERR_ARG;
+  DeviceGuard guard(c->device);
+  if (!guard.ok) return SD_ERR_CUDA;
+  std::lock_guard<std::mutex> lock(c->busy);
+  const sd::PageWork w = page_work(c);
+  sd::pages_fork_kernel<<<1, sd::pg::THREADS, 0, c->stream>>>(books_of(c, t), src, dst, n, w);
+  const int err = launched(c);
+  return err != SD_OK ? err : copy_pages(c, t, w.from, w.to, w.totals, 0, false, true);
+}
+
+int sd_cache_resize(sd_cache* c, const sd_tables* t, const int32_t* len) {
+  if (!c || !len) return SD_ERR_ARG;
+  const int rc = check_tables(c, t);
+  if (rc != SD_OK) return rc;
+  DeviceGuard guard(c->device);
+  if (!guard.ok) return SD_ERR_CUDA;
+  std::lock_guard<std::mutex> lock(c->busy);
+  const sd::PageWork w = page_work(c);
+  sd::pages_resize_kernel<<<1, sd::pg::THREADS, 0, c->stream>>>(books_of(c, t), len, w);
+  const int err = launched(c);
+  return err != SD_OK ? err : copy_pages(c, t, w.from, w.to, w.totals, 0, false, true);
+}
+
+int sd_cache_compact(sd_cache* c, const sd_tables* t, int32_t* n_used) {
+  if (!c) return SD_ERR_ARG;
+  const int rc = check_tables(c, t);
+  if (rc != SD_OK) return rc;
+  DeviceGuard guard(c->device);
+  if (!guard.ok) return SD_ERR_CUDA;
+  std::lock_guard<std::mutex> lock(c->busy);
+  const sd::PageWork w = page_work(c);
+  sd::pages_compact_kernel<<<1, sd::pg::THREADS, 0, c->stream>>>(books_of(c, t), n_used, w);
+  const int err = launched(c);
+  return err != SD_OK ? err : copy_pages(c, t, w.from, w.to, w.totals, 0, true, true);
+}
+
+int sd_cache_copy(sd_cache* c, const int32_t* src, const int32_t* dst, int n) {
+  if (!c || n < 0) return SD_ERR_ARG;
+  if (n == 0) return SD_OK;
+  if (!src || !dst) return SD_ERR_ARG;
+  DeviceGuard guard(c->device);
+  if (!guard.ok) return SD_ERR_CUDA;
+  std::lock_guard<std::mutex> lock(c->busy);
+  return copy_pages(c, nullptr, src, dst, nullptr, n, false, false);
 }
 
 int sd_cache_status(sd_cache* c, int32_t* device_status) {

@@ -1,0 +1,360 @@
+// Work on the pages of a paged cache: forking sequences, growing, cutting and ending them, compacting the pool, copying pages.  The
+// books are the caller's device arrays: a table of page numbers per sequence, lengths, and for every page how many tables hold it (0: free).
+//
+// A call is two launches.  The first, one block, works on the books: which pages are given back, taken or moved.  Everything is decided by order,
+// not by arrival: new pages are the lowest free ones, row by row.  It leaves a list of (source, destination) pages.  The second copies those pages in all
+// layers with all SMs; the number of copies stays on the device, so that neither launch waits for the host and both can be captured.
+#pragma once
+#include "paged.cuh"
+
+namespace sd {
+
+enum : int { STATUS_NO_PAGES = 128 };
+
+struct Books {
+  int *pages, *len, *refs;
+  int n_seqs, columns, n_pages, page_shift;
+  int* status;
+  __host__ __device__ __forceinline__ void say(int bit) const {
+#ifdef __CUDA_ARCH__
+    atomicOr(status, bit);
+#else
+    *status |= bit;                             // the index arithmetic is tested on the host
+#endif
+  }
+  __host__ __device__ __forceinline__ bool is_page(int p) const { return (unsigned)p < (unsigned)n_pages; }
+  __host__ __device__ __forceinline__ bool is_length(int l) const { return l >= 0 && (long long)l <= (long long)columns << page_shift; }
+  // Columns of the table that a sequence of l positions uses; l is a length.
+  __host__ __device__ __forceinline__ int columns_of(int l) const { return (int)(((long long)l + (1 << page_shift) - 1) >> page_shift); }
+  __host__ __device__ __forceinline__ int* row(int s) const { return pages + (size_t)s * columns; }
+};
+
+// What a resize does to a row: how many columns it has and shall have, and the column of the page that it keeps in part (-1: none).
+struct Resize {
+  int have, want, part;
+  bool ok;
+};
+__host__ __device__ __forceinline__ Resize resize_of(const Books& b, int length, int target) {
+  Resize r{0, 0, -1, b.is_length(length) && b.is_length(target)};
+  if (!r.ok) return r;
+  r.have = b.columns_of(length);
+  r.want = b.columns_of(target);
+  const int kept = length < target ? length : target;
+  if (kept & ((1 << b.page_shift) - 1)) r.part = kept >> b.page_shift;     // below have and want, so a column of the row
+  return r;
+}
+
+// Workspace of a call, in the cache's arena.
+struct PageWork {
+  int4* plan;          // [max_seqs] of a row (resize) or a fork
+  int* claim;          // [max_seqs] the fork that a row is for
+  int *from, *to;      // [n_pages] the copies
+  int* place;          // [n_pages] new numbers of pages that a compaction moves, -1: none (from the first number that is not kept on)
+  int* totals;         // number of copies, pages in use
+};
+
+namespace pg {
+
+constexpr int THREADS = 1024, WARPS = THREADS / 32, ROUNDS = 8, SPAN = WARPS * ROUNDS * 32;
+
+// Exclusive prefix sum of one number per thread, and the block's total.
+template <typename T> __device__ __forceinline__ T block_scan(T v, T& total, T* sm) {          // sm: [WARPS]
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  T x = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const T y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 31) sm[warp] = x;
+  __syncthreads();
+  if (warp == 0) {
+    T w = sm[lane];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const T y = __shfl_up_sync(0xffffffffu, w, o);
+      if (lane >= o) w += y;
+    }
+    sm[lane] = w;
+  }
+  __syncthreads();
+  total = sm[WARPS - 1];
+  const T before = warp ? sm[warp - 1] : T(0);
+  __syncthreads();                              // sm may be written again
+  return before + x - v;
+}
+
+// One span of pages from number p0 on: a warp's 256, of which its lanes see 32 in each round.  yes(p) says which count, at(p, k) is called
+// for each of them with its rank k.  Returns the rank after the span.
+template <typename Yes, typename At>
+__device__ __forceinline__ int rank_span(int p0, int n_pages, int rank, int* sm, Yes yes, At at) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first = p0 + warp * (ROUNDS * 32) + lane;
+  unsigned mask[ROUNDS];
+  bool on[ROUNDS];
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) on[r] = first + r * 32 < n_pages && yes(first + r * 32);
+  int count = 0;
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    mask[r] = __ballot_sync(0xffffffffu, on[r]);
+    count += __popc(mask[r]);
+  }
+  int total;
+  int k = rank + block_scan(lane == 0 ? count : 0, total, sm);
+  k = __shfl_sync(0xffffffffu, k, 0);
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    if (on[r]) at(first + r * 32, k + __popc(mask[r] & ((1u << lane) - 1)));
+    k += __popc(mask[r]);
+  }
+  return rank + total;
+}
+
+// The lowest `need` free pages to list[0..need), as far as there are so many; returns how many there are (up to the end of a span).
+__device__ __forceinline__ int find_free(const Books& b, int need, int* list, int* sm) {
+  int found = 0;
+  for (int p0 = 0; p0 < b.n_pages && found < need; p0 += SPAN)
+    found = rank_span(p0, b.n_pages, found, sm, [&](int p) { return __ldcg(b.refs + p) == 0; }, [&](int p, int k) { if (k < need) list[k] = p; });
+  __syncthreads();
+  return found;
+}
+
+__device__ __forceinline__ void add_copy(const PageWork& w, int from, int to) {
+  const int m = atomicAdd(&w.totals[0], 1);     // at most one copy per row: fewer than there are pages
+  w.from[m] = from;
+  w.to[m] = to;
+}
+
+}  // namespace pg
+
+// Fork i makes row dst[i], which has to be empty, a copy of row src[i]: whole pages are shared, the last one, where it is not full, is copied to a
+// new page.  A row that two forks are for goes to the first of them.
+__global__ void __launch_bounds__(pg::THREADS)
+pages_fork_kernel(const Books b, const int* __restrict__ src, const int* __restrict__ dst, int n, const PageWork w) {
+  using namespace pg;
+  __shared__ int sm[WARPS];
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (threadIdx.x == 0) w.totals[0] = 0;
+  for (int s = threadIdx.x; s < b.n_seqs; s += THREADS) w.claim[s] = 0x7fffffff;
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += THREADS)
+    if ((unsigned)dst[i] < (unsigned)b.n_seqs) atomicMin(&w.claim[dst[i]], i);
+  __syncthreads();
+  int need = 0;                                 // of all forks so far
+  for (int i0 = 0; i0 < n; i0 += THREADS) {
+    const int i = i0 + threadIdx.x;
+    int length = -1, part = 0;
+    if (i < n) {
+      const int from = src[i], to = dst[i];
+      if ((unsigned)from < (unsigned)b.n_seqs && (unsigned)to < (unsigned)b.n_seqs && from != to && __ldcg(w.claim + to) == i && b.len[to] == 0 && b.is_length(b.len[from])) {
+        length = b.len[from];
+        const int column = length >> b.page_shift;
+        part = (length & ((1 << b.page_shift) - 1)) && b.is_page(b.row(from)[column]);
+      } else {
+        b.say(STATUS_BAD_BATCH);
+      }
+    }
+    int total;
+    const int before = block_scan(part, total, sm);
+    if (i < n) w.plan[i] = make_int4(need + before, part, length, 0);
+    need += total;
+  }
+  const int found = find_free(b, need, w.to, sm);
+  // the list of free pages is the copies' destinations too: copies are numbered by rank, and what is not served comes last
+  const int served = min(found, need);
+  if (threadIdx.x == 0) w.totals[0] = served;
+  for (int i = warp; i < n; i += WARPS) {
+    const int4 plan = w.plan[i];
+    const int length = plan.z;
+    if (length < 0) continue;
+    if (plan.y && plan.x >= served) {
+      if (lane == 0) b.say(STATUS_NO_PAGES);
+      continue;
+    }
+    const int *from = b.row(src[i]);
+    int* to = b.row(dst[i]);
+    const int whole = length >> b.page_shift, used = b.columns_of(length);
+    for (int e = lane; e < whole; e += 32) {
+      const int p = from[e];
+      if (b.is_page(p)) atomicAdd(&b.refs[p], 1);
+      else b.say(STATUS_BAD_BATCH);
+      to[e] = b.is_page(p) ? p : -1;
+    }
+    if (lane == 0) {
+      if (plan.y) {
+        const int p = w.to[plan.x];
+        to[whole] = p;
+        b.refs[p] = 1;
+        w.from[plan.x] = from[whole];
+      } else if (used > whole) {
+        to[whole] = -1;
+        b.say(STATUS_BAD_BATCH);
+      }
+      b.len[dst[i]] = length;
+    }
+  }
+}
+
+// Row s takes the length target[s].  All rows first give back the pages past their new ends.  Then a page that a row keeps in part and others hold too is
+// replaced by a copy, and missing pages are added: the lowest free ones, row by row, a row's copy first.  From the first row on for which there are
+// not enough, rows that need any stay as they are (cut, but still sharing their last page, if they were to be cut).
+__global__ void __launch_bounds__(pg::THREADS)
+pages_resize_kernel(const Books b, const int* __restrict__ target, const PageWork w) {
+  using namespace pg;
+  __shared__ int sm[WARPS];
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (threadIdx.x == 0) w.totals[0] = 0;
+  for (int s = warp; s < b.n_seqs; s += WARPS) {
+    const Resize r = resize_of(b, b.len[s], target[s]);
+    if (!r.ok && lane == 0) b.say(STATUS_BAD_BATCH);
+    int* row = b.row(s);
+    for (int e = r.want + lane; e < r.have; e += 32) {
+      const int p = row[e];
+      row[e] = -1;
+      if (!b.is_page(p)) b.say(STATUS_BAD_BATCH);
+      else if (atomicSub(&b.refs[p], 1) <= 0) {                  // nobody was said to hold it
+        atomicAdd(&b.refs[p], 1);
+        b.say(STATUS_BAD_BATCH);
+      }
+    }
+  }
+  __syncthreads();
+  __shared__ long long sums[WARPS];
+  long long need = 0;                           // rows may ask for more than there can be
+  for (int s0 = 0; s0 < b.n_seqs; s0 += THREADS) {
+    const int s = s0 + threadIdx.x;
+    long long copy = 0, more = 0;
+    if (s < b.n_seqs) {
+      const Resize r = resize_of(b, b.len[s], target[s]);
+      more = r.want > r.have ? r.want - r.have : 0;
+      if (r.part >= 0) {
+        const int p = b.row(s)[r.part];
+        copy = b.is_page(p) && __ldcg(b.refs + p) > 1;
+      }
+    }
+    long long total;
+    const long long before = need + block_scan(copy + more, total, sums);
+    if (s < b.n_seqs) w.plan[s] = make_int4((int)min(before, 0x7fffffffll), (int)copy, (int)more, 0);
+    need += total;
+  }
+  int* list = w.place;
+  const int found = find_free(b, (int)min(need, (long long)b.n_pages), list, sm);
+  for (int s = warp; s < b.n_seqs; s += WARPS) {
+    const Resize r = resize_of(b, b.len[s], target[s]);
+    if (!r.ok) continue;
+    const int4 plan = w.plan[s];
+    int* row = b.row(s);
+    const bool served = plan.y + plan.z == 0 || (plan.x <= found && plan.y + plan.z <= found - plan.x);
+    if (!served && lane == 0) b.say(STATUS_NO_PAGES);
+    if (served && plan.y && lane == 0) {
+      const int p = list[plan.x], old = row[r.part];
+      row[r.part] = p;
+      b.refs[p] = 1;
+      atomicSub(&b.refs[old], 1);
+      add_copy(w, old, p);
+    }
+    if (served) {
+      for (int e = lane; e < plan.z; e += 32) {
+        const int p = list[plan.x + plan.y + e];
+        row[r.have + e] = p;
+        b.refs[p] = 1;
+      }
+    }
+    __syncwarp();                                                // all lanes have read the length
+    if (lane == 0 && (served || target[s] < b.len[s])) b.len[s] = target[s];
+  }
+}
+
+// The pages in use get the numbers from 0 on: those beyond move, in order, to the free ones below, in order.
+__global__ void __launch_bounds__(pg::THREADS)
+pages_compact_kernel(const Books b, int* __restrict__ n_used, const PageWork w) {
+  using namespace pg;
+  __shared__ int sm[WARPS];
+  pdl_launch_dependents();
+  int used = 0;
+  for (int p = threadIdx.x; p < b.n_pages; p += THREADS) used += b.refs[p] != 0;
+  int total;
+  block_scan(used, total, sm);
+  used = total;
+  int holes = 0, moves = 0;
+  for (int p0 = 0; p0 < b.n_pages; p0 += SPAN) {
+    if (p0 < used)
+      holes = rank_span(p0, used, holes, sm, [&](int p) { return b.refs[p] == 0; }, [&](int p, int k) { w.to[k] = p; });
+    __syncthreads();
+    if (p0 + SPAN > used) {
+      for (int p = max(p0, used) + threadIdx.x; p < min(p0 + SPAN, b.n_pages); p += THREADS) w.place[p] = -1;
+      __syncthreads();
+      moves = rank_span(p0, b.n_pages, moves, sm, [&](int p) { return p >= used && b.refs[p] != 0; },
+                        [&](int p, int k) { w.from[k] = p; w.place[p] = w.to[k]; });
+    }
+  }
+  __syncthreads();
+  for (int k = threadIdx.x; k < moves; k += THREADS) {
+    b.refs[w.to[k]] = b.refs[w.from[k]];
+    b.refs[w.from[k]] = 0;
+  }
+  if (threadIdx.x == 0) {
+    w.totals[0] = moves;
+    w.totals[1] = used;
+    if (n_used) *n_used = used;
+  }
+}
+
+// What a layer holds of a page: up to six runs of bytes (K, V, their scales, their block scales).
+struct PageRuns {
+  long long offset[6];     // of the pool within a layer
+  int words[6];            // 16-byte words of a page in it
+  int pieces[6];           // of PIECE words, the last one shorter
+  int n, all_pieces;
+};
+constexpr int PIECE = 2048;
+
+// Copies the listed pages in all layers, and gives the tables the new numbers where a compaction moved pages (books.pages not NULL).  A piece of 32 KB at a
+// time: eight 16-byte loads of a thread are on their way together.  What bounds it is memory.
+__global__ void __launch_bounds__(256)
+pages_copy_kernel(const Books b, char* __restrict__ arena, long long layer_bytes, int layers, const PageRuns runs, const int* __restrict__ from, const int* __restrict__ to,
+                  const int* __restrict__ n_copies, int n, const int* __restrict__ place, int remap) {
+  pdl_wait();
+  if (remap) {
+    const int used = n_copies[1];
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < (long long)b.n_seqs * b.columns; i += (long long)gridDim.x * blockDim.x) {
+      const int s = (int)(i / b.columns), e = (int)(i % b.columns);
+      const int l = b.len[s];
+      if (!b.is_length(l) || e >= b.columns_of(l)) continue;
+      const int p = b.pages[i];
+      if (b.is_page(p) && p < used) continue;
+      const int q = b.is_page(p) ? place[p] : -1;
+      if (q < 0) b.say(STATUS_BAD_BATCH);                        // no page, or one that nobody was said to hold
+      else b.pages[i] = q;
+    }
+  }
+  const long long copies = n_copies ? *n_copies : n;
+  for (long long i = blockIdx.x; i < copies * layers * runs.all_pieces; i += gridDim.x) {
+    int piece = (int)(i % runs.all_pieces);
+    const long long rest = i / runs.all_pieces;
+    const int layer = (int)(rest % layers), m = (int)(rest / layers);
+    int run = 0;
+    while (piece >= runs.pieces[run]) piece -= runs.pieces[run++];
+    const int f = from[m], t = to[m];
+    if (!b.is_page(f) || !b.is_page(t)) {
+      if (threadIdx.x == 0) b.say(STATUS_BAD_BATCH);
+      continue;
+    }
+    if (f == t) continue;
+    char* pool = arena + layer * layer_bytes + runs.offset[run];
+    const int words = min(PIECE, runs.words[run] - piece * PIECE);
+    const uint4* src = reinterpret_cast<const uint4*>(pool) + (long long)f * runs.words[run] + (long long)piece * PIECE;
+    uint4* dst = reinterpret_cast<uint4*>(pool) + (long long)t * runs.words[run] + (long long)piece * PIECE;
+    uint4 x[PIECE / 256];
+#pragma unroll
+    for (int u = 0; u < PIECE / 256; ++u)
+      if (u * 256 + (int)threadIdx.x < words) x[u] = __ldcs(src + u * 256 + threadIdx.x);
+#pragma unroll
+    for (int u = 0; u < PIECE / 256; ++u)
+      if (u * 256 + (int)threadIdx.x < words) __stcs(dst + u * 256 + threadIdx.x, x[u]);
+  }
+}
+
+}  // namespace sd
