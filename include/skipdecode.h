@@ -362,6 +362,23 @@ int sd_cache_read(sd_cache *c, int layer, const sd_batch *batch, const sd_heads 
  * division by their sum is at most 2^8, so the magnitudes of a sequence's values should add up to less than 2^119. */
 int sd_cache_attention(sd_cache *c, int layer, const sd_batch *batch, const sd_heads *q, float scale, const sd_heads *out);
 
+/* Changes to the scores of an attention, and which positions a row sees.  With x the scaled score of the row at position p and the key at position j,
+ *     x <- cap tanh(x / cap)                where cap > 0,
+ *     x <- x - slopes[h] |p - j|            where slopes is given,
+ * and row r attends to the positions j with  max(lo[r], p - window + 1) <= j <= hi[r],  j < len.  A row that sees nothing gives zeros. */
+typedef struct {
+  float cap;                 /* 0: off; else within 1e-30 and 1e30 */
+  const float *slopes;       /* DEVICE [n_heads], finite, or NULL */
+  int32_t window;            /* the last `window` positions, the row's own among them; 0: all */
+  const int32_t *lo, *hi;    /* DEVICE [n_tokens] or NULL: 0, and the row's own position.  Any numbers: lo below 0 counts as 0, hi beyond the sequence as
+                                its last position (hi >= p: a prefix that all of its rows see whole; lo: documents packed into one sequence) */
+} sd_scores;
+
+/* sd_cache_attention with changed scores and masks, rounded as documented there (a score's change in fp32, the cap to 2e-7 of the score).  Reads only the
+ * keys between the first and the last that some row of a tile of rows sees. */
+int sd_cache_attention_scores(sd_cache *c, int layer, const sd_batch *batch, const sd_heads *q, float scale, const sd_scores *scores,
+                              const sd_heads *out);
+
 /* ---- pages: forking, growing, cutting and ending sequences, compacting the pool, copying pages
  *
  * The books of the sequences that live in a cache, the caller's DEVICE arrays.  The calls below read and write them on the stream, decide which pages are

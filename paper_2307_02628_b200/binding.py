@@ -25,7 +25,7 @@ EXPORTS = ("sd_arena_bytes", "sd_create", "sd_schedule", "sd_schedule_compute", 
            "sd_schedule_custom", "sd_layer_capacity",
            "sd_prefill", "sd_decode_step", "sd_decode_step_static", "sd_rewind", "sd_launch_count", "sd_decode_step_host", "sd_greedy", "sd_sample_top_p", "sd_set_padding", "sd_set_rows", "sd_status", "sd_stats",
            "sd_set_option", "sd_kernel_time", "sd_kernel_time_reset", "sd_strerror", "sd_destroy",
-           "sd_sample", "sd_cache_bytes", "sd_cache_create", "sd_cache_layer", "sd_cache_layer_blocks", "sd_cache_append", "sd_cache_read", "sd_cache_attention",
+           "sd_sample", "sd_cache_bytes", "sd_cache_create", "sd_cache_layer", "sd_cache_layer_blocks", "sd_cache_append", "sd_cache_read", "sd_cache_attention", "sd_cache_attention_scores",
            "sd_cache_fork", "sd_cache_resize", "sd_cache_compact", "sd_cache_copy", "sd_cache_status", "sd_cache_set_option", "sd_cache_destroy", "sd_extend")
 
 
@@ -63,6 +63,10 @@ class SdBatch(C.Structure):
 
 class SdTables(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("pages", "len", "refs")] + [("n_seqs", C.c_int32), ("pages_per_seq", C.c_int32)]
+
+
+class SdScores(C.Structure):
+    _fields_ = [("cap", C.c_float), ("slopes", C.c_void_p), ("window", C.c_int32), ("lo", C.c_void_p), ("hi", C.c_void_p)]
 
 
 class SdHeads(C.Structure):
@@ -127,6 +131,7 @@ def lib() -> C.CDLL:
     L.sd_cache_append.argtypes = [vp, C.c_int, vp, vp, vp]          # structures by address
     L.sd_cache_read.argtypes = L.sd_cache_append.argtypes
     L.sd_cache_attention.argtypes = [vp, C.c_int, vp, vp, C.c_float, vp]
+    L.sd_cache_attention_scores.argtypes = [vp, C.c_int, vp, vp, C.c_float, vp, vp]
     L.sd_cache_fork.argtypes = [vp, vp, vp, vp, C.c_int]
     L.sd_cache_resize.argtypes = [vp, vp, vp]
     L.sd_cache_compact.argtypes = [vp, vp, vp]
@@ -220,6 +225,27 @@ class CacheBatch:
         self.ref = C.addressof(self.c)
 
 
+class Scores:
+    """What attention does to its scores, and which positions a row sees (sd_scores).
+
+    cap: scores x become cap tanh(x / cap) (0: off).  slopes [n_heads], fp32: slopes[h] |p - j| is taken off.  window: the last positions only (0: all).
+    lo, hi [n_tokens], int32: each row's first and last visible position (None: 0, and its own position).  The tensors are read by the
+    device at the call.
+    """
+
+    def __init__(self, cap: float = 0.0, slopes: torch.Tensor | None = None, window: int = 0, lo: torch.Tensor | None = None, hi: torch.Tensor | None = None):
+        for name, t, dt in (("slopes", slopes, torch.float32), ("lo", lo, torch.int32), ("hi", hi, torch.int32)):
+            if t is not None and (t.dtype != dt or not t.is_cuda or t.dim() != 1 or not t.is_contiguous()):
+                raise ValueError(f"{name} must be a contiguous {dt} CUDA tensor of one dimension")
+        self.slopes, self.lo, self.hi = slopes, lo, hi
+        self.indices = {t.device.index for t in (slopes, lo, hi) if t is not None}
+        self.n_heads = None if slopes is None else slopes.shape[0]
+        self.n_tokens = {t.shape[0] for t in (lo, hi) if t is not None}
+        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        self.c = SdScores(float(cap), ptr(slopes), int(window), ptr(lo), ptr(hi))
+        self.ref = C.addressof(self.c)
+
+
 class PageTables:
     """The books of the sequences in a cache (sd_tables): pages [n_seqs, pages_per_seq], length [n_seqs], refs [n_pages] (how many rows hold a
     page; 0: free), int32 CUDA tensors that the calls on pages read and write.  `empty` makes those of a cache without sequences."""
@@ -282,6 +308,7 @@ class PagedCache:
         L = lib()
         self._append, self._read, self._attention = L.sd_cache_append, L.sd_cache_read, L.sd_cache_attention
         self._heads, self._kv_heads, self._head_dim = n_heads, n_kv_heads, head_dim
+        self._attention_scores = L.sd_cache_attention_scores
         self._pages_calls = L.sd_cache_fork, L.sd_cache_resize, L.sd_cache_compact, L.sd_cache_copy
         self._described = _Described()
 
@@ -328,8 +355,10 @@ class PagedCache:
         self._call(self._read, "sd_cache_read", layer, batch)
         return k, v
 
-    def attention(self, layer: int, q: torch.Tensor, batch: CacheBatch, scale: float | None = None, out: torch.Tensor | None = None):
-        """Causal attention of the new tokens' queries [n_tokens, n_heads, head_dim] over their sequences; out: like q unless given."""
+    def attention(self, layer: int, q: torch.Tensor, batch: CacheBatch, scale: float | None = None, out: torch.Tensor | None = None,
+                  scores: Scores | None = None):
+        """Causal attention of the new tokens' queries [n_tokens, n_heads, head_dim] over their sequences; out: like q unless given.
+        scores: changes to the scores, and masks."""
         if scale is None:
             scale = 0.0                                        # the library's default, head_dim^-1/2
         elif not 0 < abs(C.c_float(scale).value) < float("inf"):   # as the library gets it: 0 would stand for the default
@@ -339,7 +368,12 @@ class PagedCache:
             out = torch.empty(batch.n_tokens, n, self._head_dim, dtype=q.dtype, device=self.device)
         self._rows(0, "q", q, n, batch)
         self._rows(1, "out", out, n, batch)
-        self._call(self._attention, "sd_cache_attention", layer, batch, scale)
+        if scores is None:
+            self._call(self._attention, "sd_cache_attention", layer, batch, scale)
+            return out
+        if scores.n_heads not in (None, n) or not scores.n_tokens <= {batch.n_tokens} or not scores.indices <= {self._index}:
+            raise ValueError(f"slopes must be [{n}], lo and hi [{batch.n_tokens}], on {self.device}")
+        self._call(self._attention_scores, "sd_cache_attention_scores", layer, batch, scale, scores.ref)
         return out
 
     def fork(self, tables: PageTables, src: torch.Tensor, dst: torch.Tensor):
@@ -408,12 +442,12 @@ class PagedCache:
         r.data = t.data_ptr()
         r.dtype = code
 
-    def _call(self, fn, name: str, layer: int, batch: CacheBatch, *scale):
+    def _call(self, fn, name: str, layer: int, batch: CacheBatch, *more):
         other = _raw_stream(self._index) != self._raw
         if other:
             self._fork()
         first, second = self._described.refs
-        code = fn(self.h, layer, batch.ref, first, *scale, second)
+        code = fn(self.h, layer, batch.ref, first, *more, second)
         if code != SD_OK:
             raise SdError(code, name)
         if other:

@@ -160,6 +160,68 @@ __device__ __forceinline__ void four_to_bf16(uint32_t w, uint32_t unit, uint32_t
   }
 }
 
+// A half's 64 scores of a row, in place, to base-2 units: scale (8 and 4 bits: done), cap, distance.  pos: the row's position, counted from the first
+// column; ahead: there may be visible keys behind the row's position.
+template <bool SCALED>
+__device__ __forceinline__ void change_scores(uint32_t (&s)[2][32], float scale, bool cap_on, float cap, float inv_cap, bool slope_on, float slope, int pos, int nearest, bool ahead) {
+  const F2 scale2 = f2(scale, scale);
+  auto get = [&](int k) { return f2(__uint_as_float(s[k >> 4][2 * k & 31]), __uint_as_float(s[k >> 4][(2 * k & 31) + 1])); };
+  auto put = [&](int k, F2 y) {
+    float a, b;
+    un2(y, a, b);
+    s[k >> 4][2 * k & 31] = __float_as_uint(a);
+    s[k >> 4][(2 * k & 31) + 1] = __float_as_uint(b);
+  };
+  if (cap_on) {
+    float top = 0.f;
+#pragma unroll
+    for (int k = 0; k < 64; k += 2) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(s[k >> 5][k & 31])), fabsf(__uint_as_float(s[k >> 5][(k & 31) + 1]))));
+    const float to_u = SCALED ? inv_cap : scale * inv_cap;
+    if (!__any_sync(0xffffffffu, top * to_u > 1.f)) {
+      const F2 to_u2 = f2(to_u, to_u);
+#pragma unroll
+      for (int k = 0; k < 32; ++k) {
+        const F2 x = get(k), u = mul2(x, to_u2), v = mul2(u, u);
+        F2 p = fma2(v, f2(TANH6, TANH6), f2(TANH5, TANH5));
+        p = fma2(v, p, f2(TANH4, TANH4));
+        p = fma2(v, p, f2(TANH3, TANH3));
+        p = fma2(v, p, f2(TANH2, TANH2));
+        p = fma2(v, p, f2(TANH1, TANH1));
+        p = fma2(v, p, f2(TANH0, TANH0));
+        put(k, mul2(SCALED ? x : mul2(x, scale2), p));
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 64; ++k) {
+        const float y = __uint_as_float(s[k >> 5][k & 31]) * (SCALED ? 1.f : scale);
+        s[k >> 5][k & 31] = __float_as_uint(capped(y, cap, inv_cap));
+      }
+    }
+  }
+  if (slope_on) {
+    if (!ahead || __all_sync(0xffffffffu, pos >= 63)) {            // -slope (pos - c - nearest) = slope c + begin
+      const float begin = -slope * (float)(pos - nearest);
+      const F2 slope2 = f2(slope, slope), begin2 = f2(begin, begin), two = f2(2.f, 2.f);
+      F2 c = f2(0.f, 1.f);
+#pragma unroll
+      for (int k = 0; k < 32; ++k) {
+        const F2 y = SCALED || cap_on ? add2(get(k), begin2) : fma2(get(k), scale2, begin2);
+        put(k, fma2(c, slope2, y));
+        c = add2(c, two);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 64; ++k) {
+        const float x = __uint_as_float(s[k >> 5][k & 31]), y = SCALED || cap_on ? x : x * scale;
+        s[k >> 5][k & 31] = __float_as_uint(fmaf(-slope, (float)(abs(pos - k) - nearest), y));
+      }
+    }
+  } else if (!SCALED && !cap_on) {
+#pragma unroll
+    for (int k = 0; k < 32; ++k) put(k, mul2(get(k), scale2));
+  }
+}
+
 }  // namespace ac
 
 // grid (blocks_per_seq * n_kv_heads * n_seqs, splits).  Sequences with fewer than rows_from query rows are another kernel's.  Split z takes
@@ -167,13 +229,16 @@ __device__ __forceinline__ void four_to_bf16(uint32_t w, uint32_t unit, uint32_t
 // to paged_attn_join_kernel.
 // map_k, map_v: the pools as [n_pages * n_kv_heads][page_len][HD] with boxes of a page by 64 elements (bf16 only; use_maps 0: not made).
 // PAIRS: queries and weights enter as sums of two bf16.
+// SC: scores are changed and keys masked as `sc` says; keys are counted from the tile of 128 that the first visible key of the block lies in, and a block
+// leaves the number of its splits for every row (part_used).  The change goes over pairs of scores: scale, the polynomial of paged.cuh while no score of
+// the warp passes the cap, the distance as a line (keys at or before the row) or an absolute value.
 // test_expire: test hook, values are never given back and the loaders give up after about a millisecond, keys of the third tile on their way.
-template <typename TC, int HD, bool PAIRS>
+template <typename TC, int HD, bool PAIRS, bool SC>
 __global__ void __launch_bounds__(ac::THREADS, 1)
 paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, int use_maps,
                         const BatchView b, const Rows q, const Rows out, const TC* __restrict__ Kp, const TC* __restrict__ Vp,
                         const float* __restrict__ Ksc, const float* __restrict__ Vsc, const uint8_t* __restrict__ Kb, const uint8_t* __restrict__ Vb, int group, float scale_log2, bool q_vec, bool out_vec,
-                        int blocks_per_seq, int rows_from, int chunk, float* part_acc, float* part_ml, int test_expire) {
+                        int blocks_per_seq, int rows_from, int chunk, float* part_acc, float* part_ml, int test_expire, const Scores sc, int* part_used) {
   using namespace ac;
   using L = Layout<HD, PAIRS>;
   constexpr bool SCALED = CacheType<TC>::TOP > 0.f;
@@ -216,16 +281,36 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   const int row0 = (blocks - 1 - blk) * ROWS;                   // the rows that see most keys first
   if (row0 < 0) return;
   const long long pos_first = (long long)b.len[seq] - (f1 - f0);
-  const int splits = gridDim.y, z = blockIdx.y, key0 = z * chunk;  // key numbers below count from key0
+  const int splits = gridDim.y, z = blockIdx.y;
+  int first_key = 0, ends[2] = {0, 0};                            // SC: where the block's keys begin, and end for each tile
+  if constexpr (SC) {
+    __shared__ int span_lo[THREADS / 32], span_hi[THREADS / 32];
+    const int t = threadIdx.x >> 8, tile_row = row0 + t * TILE_ROWS, rows = t < L::TILES ? min(TILE_ROWS, rows_all - tile_row) : 0;
+    const int token = tile_row / group + (threadIdx.x & 255);     // up to 129 of a tile
+    Span v{0, -1};
+    if (rows > 0 && token <= (tile_row + rows - 1) / group) v = visible(sc, f0 + token, pos_first + token, len);
+    const int from = __reduce_min_sync(0xffffffffu, v.lo <= v.hi ? v.lo : 0x7fffffff), to = __reduce_max_sync(0xffffffffu, v.hi + 1);
+    if ((threadIdx.x & 31) == 0) { span_lo[threadIdx.x >> 5] = from; span_hi[threadIdx.x >> 5] = to; }
+    __syncthreads();
+    first_key = 0x7fffffff;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+      first_key = min(first_key, span_lo[w]);
+      ends[w / 8] = max(ends[w / 8], span_hi[w]);
+    }
+    first_key = first_key == 0x7fffffff ? 0 : first_key & ~(KEYS - 1);
+  }
+  const int key0 = SC ? (int)min(first_key + (long long)z * chunk, 0x7fffffffll) : z * chunk;  // key numbers below count from key0
   int n_keys[2], n_rows[2], used_splits = 1;
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     n_rows[t] = t < L::TILES ? max(0, min(TILE_ROWS, rows_all - row0 - t * TILE_ROWS)) : 0;
     const int last = (row0 + t * TILE_ROWS + n_rows[t] - 1) / group;
     int keys = n_rows[t] ? (int)min(max(pos_first + last + 1, 0ll), (long long)len) : 0;
+    if (SC) keys = max(ends[t] - first_key, 0);
     if (splits > 1) {
       used_splits = max(used_splits, ap::splits_of(keys, chunk, splits));
-      keys = max(keys - key0, 0);
+      keys = max(keys - (key0 - first_key), 0);
       if (z < splits - 1) keys = min(keys, chunk);
     }
     n_keys[t] = (keys + HALF - 1) / HALF;                       // halves of key tiles; a later tile of rows sees no fewer
@@ -271,7 +356,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     const uint32_t s_addr = tmem + lanes + t * 128, o_addr = tmem + lanes + L::O_COL + t * HD;
     const int row = row0 + t * TILE_ROWS + min(r, max(n_rows[t] - 1, 0));
     const int token = row / group, head = g_head * group + row % group;
-    const int row_last = (int)max(min(pos_first + token, (long long)len - 1), -1ll) - key0; // last key this row sees
+    int row_last = (int)max(min(pos_first + token, (long long)len - 1), -1ll) - key0;        // last key this row sees
     const float scale = fabsf(scale_log2), sign = scale_log2 < 0.f ? -1.f : 1.f;            // a negative scale turns the queries round
     if (n_rows[t] > 0) {
       const long long at = (long long)(f0 + token) * q.row_stride + head * q.head_stride;
@@ -312,9 +397,27 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
 
     // the keys that all 32 rows of the warp see: tiles below need no mask
     const int first_token = (row0 + t * TILE_ROWS + min((warp & 3) * 32, max(n_rows[t] - 1, 0))) / group;
-    const int all_see = (int)max(min(pos_first + first_token, (long long)len - 1), -1ll) - key0;
+    int all_see = (int)max(min(pos_first + first_token, (long long)len - 1), -1ll) - key0;
+    int row_first = 0, all_from = 0, any_from = 0, any_see = 0;  // SC: the first key of this row, the keys that some row of the warp sees
+    int row_pos = 0, nearest = 0;                                // the row's position, counted as the keys; the distance of its nearest visible key
+    float slope = 0.f, cap = 0.f, inv_cap = 0.f;
+    if constexpr (SC) {
+      const Span v = visible(sc, f0 + token, pos_first + token, len);
+      row_first = v.lo - key0;
+      row_last = v.hi - key0;
+      all_from = __reduce_max_sync(0xffffffffu, row_first);
+      all_see = __reduce_min_sync(0xffffffffu, row_last);
+      any_from = __reduce_min_sync(0xffffffffu, v.lo <= v.hi ? row_first : 0x7fffffff);
+      any_see = __reduce_max_sync(0xffffffffu, row_last);
+      const int p = (int)min(max(pos_first + token, 0ll), 1ll << 30);
+      row_pos = p - key0;
+      nearest = abs(p - min(max(p, v.lo), v.hi));
+      if (sc.slopes && n_rows[t] > 0) slope = sc.slopes[head] * 1.4426950408889634f;
+      cap = sc.cap * 1.4426950408889634f;
+      inv_cap = sc.cap > 0.f ? 1.f / cap : 0.f;
+    }
     float m = -INFINITY, l = 0.f;                                // m in the units of the scores (bf16) or base-2 (8 bits)
-    const float unit = SCALED ? 1.f : scale;                     // base-2 units per unit of m
+    const float unit = SCALED || SC ? 1.f : scale;               // base-2 units per unit of m
     bool ok = true;
     for (int i = 0; i < n_keys[t]; ++i) {
       const int j = i >> 1, h = i & 1;
@@ -329,6 +432,22 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       side += h * HALF;
       const uint32_t s_half = s_addr + h * HALF;
 
+      if constexpr (SC) {
+        if (i * HALF + HALF - 1 < any_from || i * HALF > any_see) {              // nobody in this warp sees any of them
+          const uint32_t none[16] = {};
+#pragma unroll
+          for (int c = 0; c < (PAIRS ? 4 : 2); ++c) tmem_st16(s_half + 16 * c, none);
+          tmem_wait_st();
+          fence_before();
+          if (i > 0 && i + 1 == n_keys[t]) {                     // as below
+            ok = __all_sync(0xffffffffu, tc::mbar_wait(odone + 8 * t, (i - 1) & 1, abort_flag, b.status));
+            if (!ok) break;
+          }
+          __syncwarp();
+          if (lane == 0) arrive(pready + 8 * (2 * t + h));
+          continue;
+        }
+      }
       uint32_t s[2][32];
 #pragma unroll
       for (int c = 0; c < 2; ++c) tc::tmem_ld32(s_half + 32 * c, s[c]);
@@ -344,11 +463,12 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
           x[0] = __float_as_uint(y0); x[1] = __float_as_uint(y1); x[2] = __float_as_uint(y2); x[3] = __float_as_uint(y3);
         }
       }
-      if (i * HALF + HALF - 1 > all_see || pages_ok != 0xffu) {
-        const int left = row_last - i * HALF;                    // columns up to here are seen
+      if constexpr (SC) change_scores<SCALED>(s, scale, sc.cap > 0.f, cap, inv_cap, sc.slopes != nullptr, slope, row_pos - i * HALF, nearest, sc.hi != nullptr);
+      if (i * HALF + HALF - 1 > all_see || pages_ok != 0xffu || (SC && i * HALF < all_from)) {
+        const int left = row_last - i * HALF, right = SC ? row_first - i * HALF : 0;          // columns from `right` up to `left` are seen
 #pragma unroll
         for (int c = 0; c < HALF; ++c)
-          if (c > left || !((pages_ok >> (c >> 3)) & 1u)) s[c >> 5][c & 31] = 0xff800000u;
+          if (c > left || (SC && c < right) || !((pages_ok >> (c >> 3)) & 1u)) s[c >> 5][c & 31] = 0xff800000u;
       }
       float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -385,7 +505,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
           F2 x = f2(__uint_as_float(s[c][2 * k]), __uint_as_float(s[c][2 * k + 1]));
-          x = SCALED ? add2(x, mb2) : fma2(x, unit2, mb2);
+          x = SCALED || SC ? add2(x, mb2) : fma2(x, unit2, mb2);
           float p0, p1;
           un2(x, p0, p1);
           p0 = ex2(p0);
@@ -415,6 +535,9 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       }
       __syncwarp();
       if (lane == 0) arrive(pready + 8 * (2 * t + h));
+    }
+    if constexpr (SC) {
+      if (splits > 1 && z == 0 && r < n_rows[t]) part_used[(size_t)(f0 + token) * (group * b.n_kv_heads) + head] = used_splits;
     }
     if (n_rows[t] > 0 && ok) {
       if (n_keys[t] > 0) {
@@ -743,10 +866,11 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
 // Adds the shares of a row's splits, in split order.  grid (n_tokens, heads / 8): one warp per row, lane s holds split s's maximum and sum.
 // A launch of its own (7..12 us), so that all SMs take part: joined by the last block of each unit, 64 tokens of 32 heads over 60 000
 // positions in 16 splits took 158 us instead of 83.
+// part_used: how many splits each row has, where its keys alone do not say so; else NULL.
 template <int HD>
 __global__ void __launch_bounds__(256)
 paged_attn_join_kernel(const BatchView b, const Rows out, int group, int rows_from, int block_rows, int chunk, int splits, const float* __restrict__ part_acc,
-                       const float* __restrict__ part_ml) {
+                       const float* __restrict__ part_ml, const int* __restrict__ part_used) {
   int seq, pos;
   const int tok = blockIdx.x, where = locate_row(b, tok, seq, pos);
   if (where == ROW_PADDING) return;
@@ -757,7 +881,7 @@ paged_attn_join_kernel(const BatchView b, const Rows out, int group, int rows_fr
   if (rows_all < rows_from) return;
   const int row = (tok - f0) * group + head % group, last = (min((row / block_rows + 1) * block_rows, rows_all) - 1) / group;
   const int keys = (int)min(max((long long)b.len[seq] - (f1 - f0) + last + 1, 0ll), (long long)b.seq_len(seq));
-  const int used = ap::splits_of(keys, chunk, splits);
+  const int used = part_used ? min(part_used[(size_t)tok * heads + head], splits) : ap::splits_of(keys, chunk, splits);
   if (used <= 1) return;                                         // written by its block
   const size_t slot = ((size_t)tok * heads + head) * splits;
   const float2 ml = lane < used ? __ldg(reinterpret_cast<const float2*>(part_ml) + slot + lane) : make_float2(-INFINITY, 0.f);

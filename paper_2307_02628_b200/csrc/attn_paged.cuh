@@ -151,11 +151,12 @@ template <int N> __device__ __forceinline__ void load_run(const Rows& t, long lo
 // early: launched to begin once the kernel for chunks of the same call has no block left to start, whose last blocks it runs beside
 // (33 sequences of 11..329 new tokens in e4m3: 213 us a call, 221 one after the other).
 // THIRD: queries and weights are sums of three parts (bf16 caches, results in fp32), the third in products of its own.
-template <typename TC, int HD, bool THIRD>
+// SC: scores are changed and keys masked as `sc` says; split z counts from the first key that a row of the tile sees.
+template <typename TC, int HD, bool THIRD, bool SC>
 __global__ void __launch_bounds__(ap::THREADS)
 paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC* __restrict__ Kp, const TC* __restrict__ Vp,
                        const float* __restrict__ Ksc, const float* __restrict__ Vsc, const uint8_t* __restrict__ Kb, const uint8_t* __restrict__ Vb, int group, float scale_log2, bool q_vec,
-                       int tiles_per_seq, int rows_below, int chunk, int slot_rows, float* part_acc, float* part_ml, int* __restrict__ counters, bool early) {
+                       int tiles_per_seq, int rows_below, int chunk, int slot_rows, float* part_acc, float* part_ml, int* __restrict__ counters, bool early, const Scores sc) {
   using namespace ap;
   using S = Shape<TC, HD>;
   extern __shared__ __align__(128) unsigned char ap_smem[];
@@ -178,16 +179,36 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
   if (n_rows <= 0 || n_new * group >= rows_below) return;
   const long long pos_first = (long long)b.len[seq] - (f1 - f0);            // position of the first new token, negative without a place
   const int last_token = (tile * ROWS + n_rows - 1) / group;
-  const int key_end = (int)min(max(pos_first + last_token + 1, 0ll), (long long)len);      // keys that any row of the tile sees
-  const int used_splits = max(1, splits_of(key_end, chunk, splits));
-  if (z >= used_splits) return;
-  const int k0 = z * chunk, k1 = z == splits - 1 ? key_end : min(k0 + chunk, key_end);
-
   // this thread's query row (rows past the tile repeat the last one and are not stored) and the last key it sees
   const int row = tile * ROWS + min(g, n_rows - 1);
   const int token = row / group, head = g_head * group + row % group;
-  const int row_last = (int)max(min(pos_first + token, (long long)len - 1), -1ll);         // -1: none
-  const int all_see = (int)max(min(pos_first + (tile * ROWS) / group, (long long)len - 1), -1ll);   // the last key that every row sees
+  int key_end = (int)min(max(pos_first + last_token + 1, 0ll), (long long)len);            // keys that any row of the tile sees
+  int row_last = (int)max(min(pos_first + token, (long long)len - 1), -1ll);               // -1: none
+  int all_see = (int)max(min(pos_first + (tile * ROWS) / group, (long long)len - 1), -1ll);   // the last key that every row sees
+  int row_first = 0, all_from = 0, base = 0;                                                // the first ones; where the splits begin
+  if constexpr (SC) {
+    const Span v = visible(sc, f0 + token, pos_first + token, len);
+    row_first = v.lo;
+    row_last = v.hi;
+    int from = v.lo <= v.hi ? v.lo : 0x7fffffff, to = v.hi;
+    all_from = v.lo; all_see = v.hi;
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) {
+      from = min(from, __shfl_xor_sync(0xffffffffu, from, o));
+      to = max(to, __shfl_xor_sync(0xffffffffu, to, o));
+      all_from = max(all_from, __shfl_xor_sync(0xffffffffu, all_from, o));
+      all_see = min(all_see, __shfl_xor_sync(0xffffffffu, all_see, o));
+    }
+    key_end = to + 1;
+    base = key_end > 0 ? from & ~63 : 0;                                                    // chunks are multiples of 64
+  }
+  const int used_splits = max(1, splits_of(key_end - base, chunk, splits));
+  if (z >= used_splits) return;
+  const int k0 = base + z * chunk, k1 = z == splits - 1 ? key_end : (int)min((long long)k0 + chunk, (long long)key_end);
+  const float cap = SC ? sc.cap * 1.4426950408889634f : 0.f, inv_cap = SC && sc.cap > 0.f ? 1.f / cap : 0.f;
+  const float slope = SC && sc.slopes ? sc.slopes[head] * 1.4426950408889634f : 0.f;
+  const int row_pos = (int)min(max(pos_first + token, 0ll), 1ll << 30);
+  const int nearest = abs(row_pos - min(max(row_pos, row_first), row_last));                // distance of the nearest visible key, which bias is relative to
 
   float acc[S::NT][4];
 #pragma unroll
@@ -382,27 +403,38 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
       }
     }
     // this thread's four: keys n * 8 + 2 t + {0, 1}
-    float sc[2][2], vsc[2][2];
+    float sc_[2][2], vsc[2][2];
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
-      sc[n][0] = s[n][0] + (THIRD ? s[n][2] + s3[n][0] : s[n][2]);
-      sc[n][1] = s[n][1] + (THIRD ? s[n][3] + s3[n][1] : s[n][3]);
+      sc_[n][0] = s[n][0] + (THIRD ? s[n][2] + s3[n][0] : s[n][2]);
+      sc_[n][1] = s[n][1] + (THIRD ? s[n][3] + s3[n][1] : s[n][3]);
       if constexpr (S::SCALED) {
         const float2 k = lds_f32x2(sc_base + (n * 8 + 2 * t) * 4), v = lds_f32x2(sc_base + (KEYS + n * 8 + 2 * t) * 4);
-        sc[n][0] *= k.x; sc[n][1] *= k.y;
+        sc_[n][0] *= k.x; sc_[n][1] *= k.y;
         vsc[n][0] = v.x; vsc[n][1] = v.y;
       }
     }
+    if constexpr (SC) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float y = sc_[n][i] * row_scale;
+          if (sc.cap > 0.f) y = capped(y, cap, inv_cap);
+          if (sc.slopes) y -= slope * (float)(abs(row_pos - (kt * KEYS + n * 8 + 2 * t + i)) - nearest);
+          sc_[n][i] = y;
+        }
+    }
     const uint32_t ok = valid >> (2 * stage);
     uint32_t hidden = 0u, gone = 0u;                // of the four: keys that the row does not see, that are not there
-    if (kt * KEYS + KEYS - 1 > all_see || kt * KEYS + KEYS > k1 || (ok & 3u) != 3u) {
+    if (kt * KEYS + KEYS - 1 > all_see || kt * KEYS + KEYS > k1 || (ok & 3u) != 3u || (SC && kt * KEYS < all_from)) {
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int at = kt * KEYS + n * 8 + 2 * t + i;
           const bool there = at < k1 && ((ok >> n) & 1u);
-          if (!there || at > row_last) hidden |= 1u << (2 * n + i);
+          if (!there || at > row_last || (SC && at < row_first)) hidden |= 1u << (2 * n + i);
           if (!there) {                             // past the end or on a page that does not exist: it may be anything
             vsc[n][i] = 0.f;
             gone |= 1u << (2 * n + i);
@@ -416,7 +448,7 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
       for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          x[n][i] = fmaf(sc[n][i], row_scale, -mb);
+          x[n][i] = SC ? sc_[n][i] - mb : fmaf(sc_[n][i], row_scale, -mb);
           if (hidden && ((hidden >> (2 * n + i)) & 1u)) x[n][i] = -INFINITY;
         }
     };

@@ -410,7 +410,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
 // piece r * 8 + (c ^ (r & 7)); rows past N are zero.  Each bf16 weight is written as the fp16 with the same value:
 // exact for magnitudes in [2^-14, 65504] (every bf16 has at most 8 significant bits); smaller ones land on the fp16
 // subnormal grid (absolute error at most 2^-25), larger ones saturate and raise STATUS_WEIGHT_RANGE.
-__global__ void pack_tiles_kernel(const __nv_bfloat16* __restrict__ W, __nv_bfloat16* __restrict__ P, int N, int K, int* __restrict__ status) {
+static __global__ void pack_tiles_kernel(const __nv_bfloat16* __restrict__ W, __nv_bfloat16* __restrict__ P, int N, int K, int* __restrict__ status) {
   const int KB = K / BK;
   const int tn = blockIdx.x / KB, kb = blockIdx.x - tn * KB;
   uint4* dst = reinterpret_cast<uint4*>(P + (size_t)blockIdx.x * BM * BK);

@@ -442,7 +442,7 @@ inline cudaError_t launch_kernel(bool pdl, cudaStream_t stream, void (*kernel)(K
 }
 
 // next[b] = lowest index of the maximum of logits[b, :]
-__global__ void greedy_kernel(const float* __restrict__ logits, int vocab, int32_t* __restrict__ next) {
+static __global__ void greedy_kernel(const float* __restrict__ logits, int vocab, int32_t* __restrict__ next) {
   __shared__ float sv[32];
   __shared__ int si[32];
   const float* row = logits + (size_t)blockIdx.x * vocab;

@@ -133,6 +133,42 @@ __device__ __forceinline__ void locate_rows(const BatchView& b, int r0, int n, P
   __syncthreads();
 }
 
+// What attention does to its scores beside scaling them, and which keys a row sees.
+struct Scores {
+  float cap;                 // > 0: a score x becomes cap tanh(x / cap)
+  const float* slopes;       // [heads] or NULL: slope times the distance is taken off
+  int window;                // > 0: the last `window` positions only
+  const int *lo, *hi;        // [n_tokens] or NULL: a row's first and last visible position
+};
+struct Span { int lo, hi; };  // the keys lo..hi, none where lo > hi
+// What row r at position pos (below 0: no place) of a sequence of len positions sees.
+__host__ __device__ __forceinline__ Span visible(const Scores& sc, int r, long long pos, int len) {
+  if (pos < 0) return Span{0, -1};
+  const int p = (int)(pos < (1 << 30) ? pos : (1 << 30));
+  Span v{0, p};
+  if (sc.window > 0 && p >= sc.window) v.lo = p - sc.window + 1;
+  if (sc.lo && sc.lo[r] > v.lo) v.lo = sc.lo[r];
+  if (sc.hi) v.hi = sc.hi[r];
+  if (v.hi > len - 1) v.hi = len - 1;
+  if (v.lo > v.hi) return Span{0, -1};
+  return v;
+}
+// cap tanh(y / cap) of a score in any unit, inv = 1 / cap in that unit.  Up to |y| = cap the odd polynomial u P(u^2) whose largest relative error on [0, 1] is
+// smallest (fitted here: 5e-8, 1.6e-7 with fp32's roundings), beyond it 1 - 2 / (1 + e^(2 |u|)).
+constexpr float TANH0 = 0x1.fffffep-1f, TANH1 = -0x1.55540ap-2f, TANH2 = 0x1.10e672p-3f, TANH3 = -0x1.b5eb84p-5f, TANH4 = 0x1.4c6e58p-6f, TANH5 = -0x1.968b6ap-8f,
+                TANH6 = 0x1.10e5d2p-10f;
+__device__ __forceinline__ float tanh_large(float u) {           // |u| > 1
+  float e, d;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fabsf(u) * 2.8853901f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(1.f + e));
+  return copysignf(fmaf(-2.f, d, 1.f), u);
+}
+__device__ __forceinline__ float capped(float y, float cap, float inv) {
+  const float u = y * inv, v = u * u;
+  if (fabsf(u) > 1.f) return cap * tanh_large(u);
+  return y * fmaf(v, fmaf(v, fmaf(v, fmaf(v, fmaf(v, fmaf(v, TANH6, TANH5), TANH4), TANH3), TANH2), TANH1), TANH0);
+}
+
 // Rows handed in by the caller: [n_tokens, heads, head_dim] with strides in elements.
 struct Rows {
   void* data;
@@ -235,8 +271,8 @@ __device__ __forceinline__ float2 e4m3_widen(uint32_t pair) {          // exact:
 // The code nearest to x / s, ties to even.  The quotient of two 24-bit numbers is either a border or at least 2^-25 (relative) away from
 // it, so the 53-bit quotient decides exactly; on the way to e4m3 it passes through a float that is rounded to odd, which
 // keeps a later rounding to fewer bits correct.
-__device__ __noinline__ float quotient_int8(float x, float s) { return (float)fmin(fmax(rint((double)x / (double)s), -127.0), 127.0); }
-__device__ __noinline__ float quotient_sticky(float x, float s) {
+static __device__ __noinline__ float quotient_int8(float x, float s) { return (float)fmin(fmax(rint((double)x / (double)s), -127.0), 127.0); }
+static __device__ __noinline__ float quotient_sticky(float x, float s) {
   const double q = (double)x / (double)s;
   const float f = __double2float_rz(q);
   return (double)f == q ? f : __uint_as_float(__float_as_uint(f) | 1u);
@@ -245,7 +281,7 @@ __device__ __noinline__ float quotient_sticky(float x, float s) {
 // ---- four bits
 // The block scale nearest to t / (6 s), t the block's largest magnitude: t (24 bits) differs from a border (5 bits) times 6 s (26 bits) by at least
 // 2^-31 of itself or not at all, so that the 53-bit quotient decides.  The same for a code and x / (b s), 28 bits and a border of 3.
-__device__ __noinline__ uint32_t block_exact(float t, float s) {
+static __device__ __noinline__ uint32_t block_exact(float t, float s) {
   const double q = (double)t / (6.0 * (double)s);
   const float f = __double2float_rz(q);
   return e4m3_pair((double)f == q ? f : __uint_as_float(__float_as_uint(f) | 1u), 0.f) & 0xffu;
@@ -253,7 +289,7 @@ __device__ __noinline__ uint32_t block_exact(float t, float s) {
 __device__ __forceinline__ uint32_t e2m1_pair(float even, float odd) {
   return (uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(even, odd), __NV_E2M1, cudaRoundNearest);
 }
-__device__ __noinline__ float quotient_sticky4(float x, float b, float s) {
+static __device__ __noinline__ float quotient_sticky4(float x, float b, float s) {
   const double q = (double)x / ((double)b * (double)s);
   const float f = __double2float_rz(q);
   return (double)f == q ? f : __uint_as_float(__float_as_uint(f) | 1u);
@@ -525,17 +561,26 @@ cache_read_kernel(const BatchView b, int row_shift, const Rows ko, const Rows vo
 // A group of HD / 8 lanes owns a key at a time (eight elements per lane); every group runs its own base-2 online softmax,
 // merged by shuffles inside a warp and through shared memory across warps.  Every row reads its keys again (from L2): what bounds it is the
 // fused multiply-adds and shuffles.  It serves the fp32 configuration, whose sizes are small.
-template <typename TC, int HD>
+template <typename TC, int HD, bool SC>
 __global__ void __launch_bounds__(128)
 paged_attn_row_kernel(const BatchView b, const Rows q, const Rows out, const TC* __restrict__ Kp, const TC* __restrict__ Vp,
-                      const float* __restrict__ Ksc, const float* __restrict__ Vsc, int group, float scale_log2) {
+                      const float* __restrict__ Ksc, const float* __restrict__ Vsc, int group, float scale_log2, const Scores sc) {
   constexpr int LANES = HD / 8, GROUPS = 128 / LANES, NW = 4;
   __shared__ float sm_acc[NW][HD], sm_m[NW], sm_l[NW];
   const int r = blockIdx.x, h = blockIdx.y, g = h / group;
   int seq, pos;
   const int where = locate_row(b, r, seq, pos);
   if (where == ROW_PADDING) return;
-  const int n_keys = where == ROW_OK ? pos + 1 : 0;
+  int n_keys = where == ROW_OK ? pos + 1 : 0, first_key = 0, nearest = pos;
+  float slope = 0.f;
+  const float cap = SC ? sc.cap * 1.4426950408889634f : 0.f, inv_cap = SC && sc.cap > 0.f ? 1.f / cap : 0.f;
+  if constexpr (SC) {
+    const Span v = visible(sc, r, pos, b.seq_len(seq));
+    n_keys = v.hi + 1;
+    first_key = v.lo;
+    nearest = min(max(pos, v.lo), v.hi);                         // bias relative to the nearest visible key's: far ones lose nothing against each other
+    if (sc.slopes) slope = sc.slopes[h] * 1.4426950408889634f;
+  }
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = threadIdx.x % LANES, grp = threadIdx.x / LANES;
   float qv[8], acc[8], m = -INFINITY, l = 0.f;
 #pragma unroll
@@ -543,7 +588,7 @@ paged_attn_row_kernel(const BatchView b, const Rows q, const Rows out, const TC*
     qv[j] = load_elem(q, (long long)r * q.row_stride + h * q.head_stride + sub * 8 + j) * scale_log2;
     acc[j] = 0.f;
   }
-  for (int j0 = 0; j0 < n_keys; j0 += GROUPS) {                  // uniform bound: the shuffles need whole warps
+  for (int j0 = first_key; j0 < n_keys; j0 += GROUPS) {          // uniform bound: the shuffles need whole warps
     const int j = j0 + grp;
     float k[8], v[8];
     const int page = j < n_keys ? b.page_of(seq, j) : -1;
@@ -562,6 +607,10 @@ paged_attn_row_kernel(const BatchView b, const Rows q, const Rows out, const TC*
     }
 #pragma unroll
     for (int o = LANES / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if constexpr (SC) {
+      if (sc.cap > 0.f) s = capped(s, cap, inv_cap);
+      if (sc.slopes) s -= slope * (float)(abs(pos - j) - abs(pos - nearest));
+    }
     if (page >= 0) {
       const float mx = fmaxf(m, s);
       const float a = exp2_safe(m, mx), p = exp2f(s - mx);
@@ -602,7 +651,7 @@ paged_attn_row_kernel(const BatchView b, const Rows q, const Rows out, const TC*
 // ---- rows of a model call -----------------------------------------------------------------------
 // minus_pos[r]: minus the position of row r (0 for rows without one): RowMap takes learned positions as "slot minus
 // padding", so slot 0 with a padding of minus the position gives the position.  last_row[s]: the row of the sequence's last new token.
-__global__ void cache_rows_kernel(const BatchView b, int* __restrict__ minus_pos, int* __restrict__ last_row) {
+static __global__ void cache_rows_kernel(const BatchView b, int* __restrict__ minus_pos, int* __restrict__ last_row) {
   int seq, pos;
   const int r = blockIdx.x;
   const int where = locate_row(b, r, seq, pos);
