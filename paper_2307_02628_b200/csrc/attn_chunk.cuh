@@ -10,7 +10,11 @@
 // tensor core works through both tiles' softmax.  (Scores of 128 keys at a time leave no columns for a second set: every
 // softmax then waited for its two products, 1500 of 3700 clocks.)
 //
-// Operands are bf16, the type of a bf16 cache; codes of 8-bit caches are bf16 numbers exactly, and so are 4-bit codes times their block's scale.  Where queries and results are bf16 too, the only
+// Operands are bf16, the type of a bf16 cache; codes of 8-bit caches are bf16 numbers exactly.  Over 4-bit caches they are fp16: codes times their block's scale
+// are fp16 numbers exactly, two instructions a pair (six to bf16), and queries are brought near 1 by a power of two for each row.  A value's scale joins
+// its weight, relative to a power of two above all scales so far, times 2^7 (the weights stay below 2^15); where queries and results are bf16 it joins
+// the value instead, whose block scale times scale is then rounded to 11 bits, and the weight, of 11 bits too, is times 2^7 by itself: half as
+// many scales to read and multiply by in the softmax.  Where queries and results are bf16 too, the only
 // rounding is that of the weights, once to 8 bits of significand: relative to 64-bit arithmetic results are 2.3e-3 off, of which their own
 // rounding is 1.7e-3.  Queries or results with more bits (fp32, fp16) take the form PAIRS: queries and weights are sums of two
 // bf16, 16 bits, in two products each; the weights' lower halves take the other 32 columns of their scores.  Twice the
@@ -63,9 +67,9 @@ template <int HD, bool PAIRS> struct Layout {
   static constexpr int O_COL = 256;                            // tensor memory: S_0 at 0 and 64, S_1 at 128 and 192, O_0, O_1 from 256
 };
 
-// bf16 x bf16 -> fp32, 128 rows; b_mn: B is stored with its output axis contiguous
-__host__ __device__ constexpr uint32_t idesc(int n, bool b_mn) {
-  return (1u << 4) | (1u << 7) | (1u << 10) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
+// bf16 x bf16 (half: fp16 x fp16) -> fp32, 128 rows; b_mn: B is stored with its output axis contiguous
+__host__ __device__ constexpr uint32_t idesc(int n, bool b_mn, bool half) {
+  return (1u << 4) | (half ? 0u : (1u << 7) | (1u << 10)) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
 }
 // V as it lies: 64-element blocks `lead` bytes apart, groups of 8 keys 1024 bytes apart, 128-byte swizzle
 __device__ __forceinline__ uint64_t v_desc(uint32_t addr, uint32_t lead) {
@@ -123,6 +127,8 @@ __device__ __forceinline__ void un2(F2 x, float& a, float& b) { asm("mov.b64 {%0
 __device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
 __device__ __forceinline__ F2 add2(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
 __device__ __forceinline__ F2 mul2(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ uint32_t pack(float a, float b, __nv_bfloat16) { return pack_bf16(a, b); }
+__device__ __forceinline__ uint32_t pack(float a, float b, __half) { return pack_f16(a, b); }
 // byte offset of 16-byte piece c (8 elements) of row r in a tile
 __device__ __forceinline__ uint32_t piece(int r, int c) { return (uint32_t)((c >> 3) * (128 * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)); }
 
@@ -137,29 +143,21 @@ __device__ __forceinline__ void to_bf16(uint32_t w, uint32_t& lo, uint32_t& hi, 
   lo = int8_pair(__byte_perm(w, 0u, 0x4140));
   hi = int8_pair(__byte_perm(w, 0u, 0x4342));
 }
-__device__ __forceinline__ void to_bf16(uint32_t, uint32_t& lo, uint32_t& hi, e2m1) { lo = hi = 0u; }   // not reached: four_to_bf16
 __device__ __forceinline__ void to_bf16(uint32_t w, uint32_t& lo, uint32_t& hi, e4m3) {
   const float2 a = e4m3_widen(w & 0xffffu), b = e4m3_widen(w >> 16);
   lo = pack_bf16(a.x, a.y);
   hi = pack_bf16(b.x, b.y);
 }
-// Eight 4-bit codes (a word) to four bf16 pairs, times `unit`: their block's scale times 2^115, twice.  A code's three lower bits, read as the
-// last two of the exponent and the first of the fraction, are the code times 2^-126, subnormal or not, so that the product, exact, is
-// code times scale times 2^-11 (2^-126 and not its square would need a scale beyond the type's range).
-constexpr float FOUR_UNIT = 0x1p115f, FOUR_BACK = 2048.f;
-__device__ __forceinline__ uint32_t bmul2(uint32_t a, uint32_t b) {
-  const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
-  return *reinterpret_cast<const uint32_t*>(&r);
+// Which of 32 columns are within [right, left], a bit each.
+__device__ __forceinline__ uint32_t columns(int right, int left) {
+  const uint32_t below = left >= 31 ? 0xffffffffu : left < 0 ? 0u : (2u << left) - 1u;
+  return right <= 0 ? below : right > 31 ? 0u : below & (0xffffffffu << right);
 }
-__device__ __forceinline__ void four_to_bf16(uint32_t w, uint32_t unit, uint32_t (&o)[4]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t a = __byte_perm(w, 0u, 0x0444 | i << 12);                 // byte i, codes 2 i and 2 i + 1, in the uppermost eight bits
-    const uint32_t two = (a | a >> 12) & 0xf000f000u;                        // the odd one above the even one
-    o[i] = bmul2((two | two >> 6) & 0x81c081c0u, unit);                      // sign, and the other three bits as said
-  }
-}
+// Four bits to the four bytes of a word.
+__device__ __forceinline__ uint32_t bytes_of(uint32_t four) { return (((four & 15u) * 0x00204081u) & 0x01010101u) * 0xffu; }
 
+// as TANH0.. of paged.cuh, of degree 4 for [0, 0.7]
+constexpr float NEAR0 = 0x1.fffff6p-1f, NEAR1 = -0x1.554d28p-2f, NEAR2 = 0x1.0fff48p-3f, NEAR3 = -0x1.a07350p-5f, NEAR4 = 0x1.c35640p-7f;
 // A half's 64 scores of a row, in place, to base-2 units: scale (8 and 4 bits: done), cap, distance.  pos: the row's position, counted from the first
 // column; ahead: there may be visible keys behind the row's position.
 template <bool SCALED>
@@ -177,24 +175,36 @@ __device__ __forceinline__ void change_scores(uint32_t (&s)[2][32], float scale,
 #pragma unroll
     for (int k = 0; k < 64; k += 2) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(s[k >> 5][k & 31])), fabsf(__uint_as_float(s[k >> 5][(k & 31) + 1]))));
     const float to_u = SCALED ? inv_cap : scale * inv_cap;
-    if (!__any_sync(0xffffffffu, top * to_u > 1.f)) {
-      const F2 to_u2 = f2(to_u, to_u);
+    const F2 to_u2 = f2(to_u, to_u);
+    top = top * (SCALED ? 1.f : scale) * inv_cap;
+    if (!(to_u < 1e38f)) top = INFINITY;                             // queries beyond 10^30 and a cap below 10^-8, say
+    if (!__any_sync(0xffffffffu, top > 0.7f)) {                      // the polynomial of [0, 0.7]: 3e-7 of the score
+      const F2 c0 = f2(cap * NEAR0, cap * NEAR0), c1 = f2(cap * NEAR1, cap * NEAR1), c2 = f2(cap * NEAR2, cap * NEAR2), c3 = f2(cap * NEAR3, cap * NEAR3), c4 = f2(cap * NEAR4, cap * NEAR4);
 #pragma unroll
       for (int k = 0; k < 32; ++k) {
-        const F2 x = get(k), u = mul2(x, to_u2), v = mul2(u, u);
+        const F2 u = mul2(get(k), to_u2), v = mul2(u, u);
+        put(k, mul2(u, fma2(v, fma2(v, fma2(v, fma2(v, c4, c3), c2), c1), c0)));
+      }
+    } else if (!__any_sync(0xffffffffu, top > 1.f)) {
+#pragma unroll
+      for (int k = 0; k < 32; ++k) {
+        const F2 u = mul2(get(k), to_u2), v = mul2(u, u);
         F2 p = fma2(v, f2(TANH6, TANH6), f2(TANH5, TANH5));
         p = fma2(v, p, f2(TANH4, TANH4));
         p = fma2(v, p, f2(TANH3, TANH3));
         p = fma2(v, p, f2(TANH2, TANH2));
         p = fma2(v, p, f2(TANH1, TANH1));
         p = fma2(v, p, f2(TANH0, TANH0));
-        put(k, mul2(SCALED ? x : mul2(x, scale2), p));
+        put(k, mul2(mul2(u, f2(cap, cap)), p));
       }
-    } else {
+    } else {                                                       // 1 - 2 / (1 + e^(2 u)): off by 2^-21 of the cap at most, small scores too
+      const float to_e = inv_cap * 2.8853901f, twice = -2.f * cap;
 #pragma unroll
       for (int k = 0; k < 64; ++k) {
-        const float y = __uint_as_float(s[k >> 5][k & 31]) * (SCALED ? 1.f : scale);
-        s[k >> 5][k & 31] = __float_as_uint(capped(y, cap, inv_cap));
+        float e, d;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(__uint_as_float(s[k >> 5][k & 31]) * (SCALED ? 1.f : scale) * to_e));
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(1.f + e));
+        s[k >> 5][k & 31] = __float_as_uint(fmaf(twice, d, cap));
       }
     }
   }
@@ -241,7 +251,11 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
                         int blocks_per_seq, int rows_from, int chunk, float* part_acc, float* part_ml, int test_expire, const Scores sc, int* part_used) {
   using namespace ac;
   using L = Layout<HD, PAIRS>;
-  constexpr bool SCALED = CacheType<TC>::TOP > 0.f;
+  constexpr bool SCALED = CacheType<TC>::TOP > 0.f, FOUR = kFour<TC>;
+  using Op = std::conditional_t<FOUR, __half, __nv_bfloat16>;    // the products' operands
+  // 4 bits: from and to bf16 the values' scales are part of the operands (FOLD), else they join the weights
+  constexpr bool FOLD = FOUR && !PAIRS;
+  constexpr float LIFT = FOLD ? 16.f : 128.f, BACK = 1.f / LIFT;  // values, or weights, are relative to a power of two (ve) over LIFT
   constexpr int ROWS = L::ROWS;
   extern __shared__ unsigned char ac_smem[];
   __shared__ uint64_t bars[4 * STAGES + 13 + SIDE];
@@ -255,20 +269,24 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   const int g_head = blockIdx.x % b.n_kv_heads, rest = blockIdx.x / b.n_kv_heads;
   const int blk = rest % blocks_per_seq, turn = rest / blocks_per_seq;
   __shared__ int lens[THREADS];
-  __shared__ int turn_seq;
+  __shared__ int4 turn_seq;                                       // number, first row, behind its last row, length
+  int4 who;
   if (b.n_seqs > 1 && b.n_seqs <= THREADS) {
-    const int mine = threadIdx.x < b.n_seqs ? b.len[threadIdx.x] : 0;
+    int mine = 0, begin = 0, end = 0;
+    if (threadIdx.x < b.n_seqs) { mine = b.len[threadIdx.x]; begin = b.first[threadIdx.x]; end = b.first[threadIdx.x + 1]; }
     lens[threadIdx.x] = mine;
     __syncthreads();
     if (threadIdx.x < b.n_seqs) {
       int ahead = 0;
       for (int i = 0; i < b.n_seqs; ++i) ahead += lens[i] > mine || (lens[i] == mine && i < (int)threadIdx.x);
-      if (ahead == turn) turn_seq = threadIdx.x;
+      if (ahead == turn) turn_seq = make_int4(threadIdx.x, begin, end, mine);
     }
     __syncthreads();
+    who = turn_seq;
+  } else {
+    who = make_int4(turn, b.first[turn], b.first[turn + 1], b.len[turn]);
   }
-  const int seq = b.n_seqs > 1 && b.n_seqs <= THREADS ? turn_seq : turn;
-  const int f0 = b.first[seq], f1 = b.first[seq + 1], len = b.seq_len(seq);
+  const int seq = who.x, f0 = who.y, f1 = who.z, len = b.held_len(who.w);
   int n_new = f1 - f0;
   if (f0 < 0 || n_new < 0 || f1 > b.n_tokens || n_new > b.max_new) {
     if (threadIdx.x == 0) b.bad();
@@ -280,7 +298,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   const int blocks = (rows_all + ROWS - 1) / ROWS;
   const int row0 = (blocks - 1 - blk) * ROWS;                   // the rows that see most keys first
   if (row0 < 0) return;
-  const long long pos_first = (long long)b.len[seq] - (f1 - f0);
+  const long long pos_first = (long long)who.w - (f1 - f0);
   const int splits = gridDim.y, z = blockIdx.y;
   int first_key = 0, ends[2] = {0, 0};                            // SC: where the block's keys begin, and end for each tile
   if constexpr (SC) {
@@ -343,6 +361,92 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"((uint32_t)__cvta_generic_to_shared(&tmem_slot)), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  // Softmax warps: the thread's query row.  The rows are on their way while the barriers and the tensor memory are prepared.
+  const int t = warp >> 2 & 1, r = (warp & 3) * 32 + lane;
+  const int row = row0 + t * TILE_ROWS + min(r, max(n_rows[t] - 1, 0));
+  const int token = row / group, head = g_head * group + row % group;
+  int row_last = (int)max(min(pos_first + token, (long long)len - 1), -1ll) - key0;        // last key this row sees
+  const float sign = scale_log2 < 0.f ? -1.f : 1.f;             // a negative scale turns the queries round
+  float scale = SCALED ? 1.f : fabsf(scale_log2);               // base-2 units of a score, as it comes, that is 1 (8 and 4 bits: the keys' scales have the rest)
+  if (warp < 8 && n_rows[t] > 0) {
+    // The warp's 32 rows, PIECES lanes to a row, so that a request takes whole lines.  (A row to a thread, 32 lines to a request: 4000 clocks of a block at
+    // HD = 64 and 9000 at 128.)
+    constexpr int PIECES = HD / 8, AT_ONCE = 32 / PIECES;
+    const long long at = (long long)(f0 + token) * q.row_stride + head * q.head_stride;
+    const int mine = lane / PIECES, c = lane % PIECES;            // row of a round, piece
+    const uint32_t dst = base + L::Q + t * L::TILE;
+    auto place = [&](int i) { return dst + piece((warp & 3) * 32 + i * AT_ONCE + mine, c); };
+    auto start = [&](int i) { return __shfl_sync(0xffffffffu, at, i * AT_ONCE + mine) + c * 8; };
+    auto put = [&](int i, const float (&x)[8]) {
+      float turn = sign;
+      if constexpr (FOUR) {                                       // fp16 operands: the row is brought near 1 by a power of two
+        float top = 0.f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) top = fmaxf(top, fabsf(x[k]));
+#pragma unroll
+        for (int o = 1; o < PIECES; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const int e = min(max((int)((__float_as_uint(top) >> 23) & 0xff), 2), 252);
+        turn *= __uint_as_float((uint32_t)(254 - e) << 23);       // 2^(127 - e)
+        const float back = __shfl_sync(0xffffffffu, __uint_as_float((uint32_t)e << 23), lane % AT_ONCE * PIECES);
+        if (lane / AT_ONCE == i) scale = back;                    // 2^(e - 127), to the thread whose row it is
+      }
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if constexpr (PAIRS) ap::split(x[2 * k] * turn, x[2 * k + 1] * turn, hi[k], lo[k], Op{});
+        else hi[k] = pack(x[2 * k] * turn, x[2 * k + 1] * turn, Op{});
+      }
+      sts16(place(i), hi[0], hi[1], hi[2], hi[3]);
+      if constexpr (PAIRS) sts16(place(i) + L::Q_LOW, lo[0], lo[1], lo[2], lo[3]);
+    };
+    if (q_vec && q.dtype != DT_FP32) {
+      uint4 x[PIECES];                                            // all on their way together
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) x[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(q.data) + start(i)));
+      if (!PAIRS && !FOUR && q.dtype == DT_BF16) {
+        const uint32_t turn = scale_log2 < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) sts16(place(i), x[i].x ^ turn, x[i].y ^ turn, x[i].z ^ turn, x[i].w ^ turn);
+      } else {
+        const bool is_half = q.dtype == DT_FP16;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+          const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+          float y[8];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
+            y[2 * k] = is_half ? f.x : __uint_as_float(w[k] << 16);
+            y[2 * k + 1] = is_half ? f.y : __uint_as_float(w[k] & 0xffff0000u);
+          }
+          put(i, y);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i0 = 0; i0 < PIECES; i0 += 4) {                    // four rounds' loads on their way together
+        float x[4][8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const long long from = start(i0 + i);
+          if (q_vec) load8<true>(static_cast<const float*>(q.data) + from, x[i]);
+          else ap::load_run<8>(q, from, false, x[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) put(i0 + i, x[i]);
+      }
+    }
+    fence_async();
+  }
+  // loaders: the pages of the first tile of keys
+  const int* table = b.pages + (size_t)seq * b.pages_per_seq;
+  const int most = min(len - key0, n_tiles * KEYS);               // keys past it are filled with zeros
+  // lane i < 16 looks up the page of keys [8 i, 8 i + 8) of a tile
+  auto look_up = [&](int j) {
+    const int key = j * KEYS + (lane & 15) * 8;
+    return j < n_tiles && key < most ? table[(key0 + key) >> b.page_shift] : 0;
+  };
+  const int page_first = warp >= 8 && warp < 12 ? look_up(0) : 0;
   fence_before();
   __syncthreads();
   fence_after();
@@ -351,49 +455,9 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   if (warp < 8) {
     // ---- softmax: one thread per query row
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFTMAX_REGS));
-    const int t = warp >> 2, r = (warp & 3) * 32 + lane;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t s_addr = tmem + lanes + t * 128, o_addr = tmem + lanes + L::O_COL + t * HD;
-    const int row = row0 + t * TILE_ROWS + min(r, max(n_rows[t] - 1, 0));
-    const int token = row / group, head = g_head * group + row % group;
-    int row_last = (int)max(min(pos_first + token, (long long)len - 1), -1ll) - key0;        // last key this row sees
-    const float scale = fabsf(scale_log2), sign = scale_log2 < 0.f ? -1.f : 1.f;            // a negative scale turns the queries round
-    if (n_rows[t] > 0) {
-      const long long at = (long long)(f0 + token) * q.row_stride + head * q.head_stride;
-      const uint32_t dst = base + L::Q + t * L::TILE;
-      if constexpr (PAIRS) {
-#pragma unroll 4
-        for (int c = 0; c < HD / 8; ++c) {
-          float x[8];
-          uint32_t hi[4], lo[4];
-          ap::load_run<8>(q, at + c * 8, q_vec, x);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) ap::split(x[2 * i] * sign, x[2 * i + 1] * sign, hi[i], lo[i], __nv_bfloat16{});
-          sts16(dst + piece(r, c), hi[0], hi[1], hi[2], hi[3]);
-          sts16(dst + L::Q_LOW + piece(r, c), lo[0], lo[1], lo[2], lo[3]);
-        }
-      } else if (q_vec && q.dtype == DT_BF16) {
-        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(q.data) + at);
-        const uint32_t turn = scale_log2 < 0.f ? 0x80008000u : 0u;
-        uint4 x[HD / 8];                                          // all on their way together
-#pragma unroll
-        for (int c = 0; c < HD / 8; ++c) x[c] = __ldg(src + c);
-#pragma unroll
-        for (int c = 0; c < HD / 8; ++c) sts16(dst + piece(r, c), x[c].x ^ turn, x[c].y ^ turn, x[c].z ^ turn, x[c].w ^ turn);
-      } else {
-#pragma unroll 8
-        for (int c = 0; c < HD / 8; ++c) {
-          float x[8];
-          ap::load_run<8>(q, at + c * 8, q_vec, x);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] *= sign;
-          sts16(dst + piece(r, c), pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-        }
-      }
-    }
-    fence_async();
-    __syncwarp();
-    if (lane == 0) arrive(qfull);
+    if (lane == 0) arrive(qfull);                                 // the rows are in shared memory since before the block's barriers were
 
     // the keys that all 32 rows of the warp see: tiles below need no mask
     const int first_token = (row0 + t * TILE_ROWS + min((warp & 3) * 32, max(n_rows[t] - 1, 0))) / group;
@@ -416,8 +480,10 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       cap = sc.cap * 1.4426950408889634f;
       inv_cap = sc.cap > 0.f ? 1.f / cap : 0.f;
     }
-    float m = -INFINITY, l = 0.f;                                // m in the units of the scores (bf16) or base-2 (8 bits)
-    const float unit = SCALED || SC ? 1.f : scale;               // base-2 units per unit of m
+    float m = -INFINITY, l = 0.f;                                // m in the units of the scores (bf16, 4 bits), or base-2 (8 bits, changed scores)
+    const bool changed = SC && (sc.cap > 0.f || sc.slopes);
+    const float unit = changed ? 1.f : scale;                    // base-2 units per unit of m
+    float ve = 0.f;                                              // 4 bits: what values or their weights are relative to
     bool ok = true;
     for (int i = 0; i < n_keys[t]; ++i) {
       const int j = i >> 1, h = i & 1;
@@ -429,6 +495,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       fence_after();
       const float* side = reinterpret_cast<const float*>(base_ptr + L::SIDE_OFF + (j & (SIDE - 1)) * L::SIDE_BYTES);
       const uint32_t pages_ok = *reinterpret_cast<const uint32_t*>(side + 2 * KEYS) >> (8 * h) & 0xffu;
+      const float ve_now = FOUR ? side[2 * KEYS + 1] : 0.f;      // as large as that of any tile before
       side += h * HALF;
       const uint32_t s_half = s_addr + h * HALF;
 
@@ -463,12 +530,16 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
           x[0] = __float_as_uint(y0); x[1] = __float_as_uint(y1); x[2] = __float_as_uint(y2); x[3] = __float_as_uint(y3);
         }
       }
-      if constexpr (SC) change_scores<SCALED>(s, scale, sc.cap > 0.f, cap, inv_cap, sc.slopes != nullptr, slope, row_pos - i * HALF, nearest, sc.hi != nullptr);
+      if constexpr (SC) {
+        if (changed) change_scores<SCALED && !FOUR>(s, scale, sc.cap > 0.f, cap, inv_cap, sc.slopes != nullptr, slope, row_pos - i * HALF, nearest, sc.hi != nullptr);
+      }
       if (i * HALF + HALF - 1 > all_see || pages_ok != 0xffu || (SC && i * HALF < all_from)) {
         const int left = row_last - i * HALF, right = SC ? row_first - i * HALF : 0;          // columns from `right` up to `left` are seen
+        uint32_t see[2] = {columns(right, left), columns(right - 32, left - 32)};
+        if (pages_ok != 0xffu) { see[0] &= bytes_of(pages_ok); see[1] &= bytes_of(pages_ok >> 4); }
 #pragma unroll
         for (int c = 0; c < HALF; ++c)
-          if (c > left || (SC && c < right) || !((pages_ok >> (c >> 3)) & 1u)) s[c >> 5][c & 31] = 0xff800000u;
+          if (!(see[c >> 5] & (1u << (c & 31)))) s[c >> 5][c & 31] = 0xff800000u;
       }
       float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -476,10 +547,15 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
 #pragma unroll
         for (int c = 0; c < 4; ++c) mx[c] = fmaxf(mx[c], fmaxf(__uint_as_float(s[c >> 1][(c & 1) * 16 + k]), __uint_as_float(s[c >> 1][(c & 1) * 16 + k + 1])));
       const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-      if (__any_sync(0xffffffffu, (top - m) * unit > SLACK)) {   // -inf - -inf is NaN: not greater
-        const float m_new = fmaxf(m, top), a = m == -INFINITY ? 0.f : ex2((m - m_new) * unit);
+      if (__any_sync(0xffffffffu, (top - m) * unit > SLACK || (FOUR && ve_now > ve))) {   // -inf - -inf is NaN: not greater
+        const float m_new = fmaxf(m, top);
+        float a = m == -INFINITY ? 0.f : ex2((m - m_new) * unit);
         m = m_new;
         l *= a;
+        if (FOUR) {
+          a *= ve / ve_now;                                      // powers of two, or 0 over one
+          ve = ve_now;
+        }
         if (i > 0) {
           ok = __all_sync(0xffffffffu, tc::mbar_wait(odone + 8 * t, (i - 1) & 1, abort_flag, b.status));
           if (!ok) break;
@@ -496,7 +572,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
           tmem_wait_st();
         }
       }
-      const float mb = m == -INFINITY ? 0.f : -m * unit;
+      const float mb = (m == -INFINITY ? 0.f : -m * unit) + (FOLD ? 7.f : 0.f);      // weights and their sum times 2^7 where fp16 has to hold them
       const F2 unit2 = f2(unit, unit), mb2 = f2(mb, mb);
       F2 sum[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
 #pragma unroll
@@ -505,19 +581,19 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
           F2 x = f2(__uint_as_float(s[c][2 * k]), __uint_as_float(s[c][2 * k + 1]));
-          x = SCALED || SC ? add2(x, mb2) : fma2(x, unit2, mb2);
+          x = SCALED && !FOUR ? add2(x, mb2) : fma2(x, unit2, mb2);
           float p0, p1;
           un2(x, p0, p1);
           p0 = ex2(p0);
           p1 = ex2(p1);
           x = f2(p0, p1);
           sum[k & 1] = add2(sum[k & 1], x);
-          if (SCALED) {
+          if (SCALED && !FOLD) {
             const float2 v = *reinterpret_cast<const float2*>(side + KEYS + c * 32 + 2 * k);
             un2(mul2(x, f2(v.x, v.y)), p0, p1);
           }
-          if constexpr (PAIRS) ap::split(p0, p1, w[k], w_lo[k], __nv_bfloat16{});
-          else w[k] = pack_bf16(p0, p1);
+          if constexpr (PAIRS) ap::split(p0, p1, w[k], w_lo[k], Op{});
+          else w[k] = pack(p0, p1, Op{});
         }
         tmem_st16(s_half + 16 * c, w);                           // over columns that have been read
         if constexpr (PAIRS) tmem_st16(s_half + HALF / 2 + 16 * c, w_lo);
@@ -545,7 +621,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         fence_after();
       }
       if (ok && used_splits == 1) {
-        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const float inv = l > 0.f ? (FOUR ? ve * BACK : 1.f) / l : 0.f;
         const long long at = (long long)(f0 + token) * out.row_stride + head * out.head_stride;
 #pragma unroll 1
         for (int c0 = 0; c0 < HD; c0 += 32) {
@@ -573,6 +649,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       } else if (ok) {
         // the row's share: sums relative to the maximum, in base-2 units
         const size_t slot = ((size_t)(f0 + token) * (group * b.n_kv_heads) + head) * splits + z;
+        const float back = FOUR ? ve * BACK : 1.f;
 #pragma unroll 1
         for (int c0 = 0; c0 < HD; c0 += 32) {
           uint32_t v[32] = {};
@@ -583,7 +660,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
           if (r < n_rows[t]) {
 #pragma unroll
             for (int i = 0; i < 32; i += 4)
-              __stcg(reinterpret_cast<float4*>(part_acc + slot * HD + c0 + i), make_float4(__uint_as_float(v[i]), __uint_as_float(v[i + 1]), __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])));
+              __stcg(reinterpret_cast<float4*>(part_acc + slot * HD + c0 + i), make_float4(__uint_as_float(v[i]) * back, __uint_as_float(v[i + 1]) * back, __uint_as_float(v[i + 2]) * back, __uint_as_float(v[i + 3]) * back));
           }
         }
         if (r < n_rows[t]) __stcg(reinterpret_cast<float2*>(part_ml + slot * 2), make_float2(m * unit, l));
@@ -593,17 +670,9 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     // ---- loaders
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LOADER_REGS));
     const int w = warp - 8, tid = w * 32 + lane;
-    const int* table = b.pages + (size_t)seq * b.pages_per_seq;
-    constexpr bool FOUR = kFour<TC>;
     constexpr int E = sizeof(TC), PER_ROW = row_units<TC>(HD) * E / 16;   // 16-byte pieces of a stored key
     constexpr int ROWS_AT_ONCE = 32 / PER_ROW;                    // of a warp
     constexpr int STEPS = KEYS / (4 * ROWS_AT_ONCE);
-    const int most = min(len - key0, n_tiles * KEYS);             // keys past it are filled with zeros
-    // lane i < 16 looks up the page of keys [8 i, 8 i + 8) of a tile
-    auto look_up = [&](int j) {
-      const int key = j * KEYS + (lane & 15) * 8;
-      return j < n_tiles && key < most ? table[(key0 + key) >> b.page_shift] : 0;
-    };
     auto exists = [&](int j, int page) {
       return __ballot_sync(0xffffffffu, (unsigned)page < (unsigned)b.n_pages || j * KEYS + (lane & 15) * 8 >= most) & 0xffffu;
     };
@@ -615,10 +684,6 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       const bool on = j * KEYS + key < most && ((pages_ok >> (key >> 3)) & 1u);
       return on ? pool + b.entry(page, g_head, key0 + j * KEYS + key) * row_units<TC>(HD) + c * (16 / E) : nullptr;
     };
-    // the two block scales of such a piece (4 bits)
-    auto ask_blocks = [&](const TC* src, const TC* pool, const uint8_t* blocks) -> uint32_t {
-      return src ? __ldg(reinterpret_cast<const uint16_t*>(blocks + (src - pool) / (kBlock / 2))) : 0u;
-    };
     // this thread's key's scales, zeros where there is none
     auto ask_scales = [&](int j, int page, uint32_t pages_ok) {
       page = __shfl_sync(0xffffffffu, page, (tid >> 3) & 15);
@@ -626,13 +691,28 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       const size_t e = b.entry(page, g_head, key0 + j * KEYS + tid);
       return make_float2(__ldg(Ksc + e), __ldg(Vsc + e));
     };
+    // 4 bits: a power of two above all the values' scales so far.  Every warp looks at all 128 of a tile, four a lane, so that none waits for another.
+    float ve = 0.f;
+    auto ask_values = [&](int j, int page, uint32_t pages_ok) {
+      page = __shfl_sync(0xffffffffu, page, lane >> 1);
+      const int left = most - (j * KEYS + lane * 4);
+      if (left <= 0 || !((pages_ok >> (lane >> 1)) & 1u)) return 0.f;
+      const float4 v = __ldg(reinterpret_cast<const float4*>(Vsc + b.entry(page, g_head, key0 + j * KEYS + lane * 4)));
+      return fmaxf(fmaxf(v.x, left > 1 ? v.y : 0.f), fmaxf(left > 2 ? v.z : 0.f, left > 3 ? v.w : 0.f));
+    };
+    auto raise = [&](float top) {
+      const float all = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(fabsf(top))));
+      const int e = min(max((int)((__float_as_uint(all) >> 23) & 0xff) + 1, 14), 254);
+      ve = fmaxf(ve, __uint_as_float((uint32_t)e << 23));
+    };
     auto begin_side = [&](int j, float2 scales, uint32_t pages_ok) {
       float* side = reinterpret_cast<float*>(base_ptr + L::SIDE_OFF + (j & (SIDE - 1)) * L::SIDE_BYTES);
       if (tid == 0) *reinterpret_cast<uint32_t*>(side + 2 * KEYS) = pages_ok;
       if (pages_ok != 0xffffu && w == 0 && lane == 0) b.bad();
       if (SCALED) {
-        side[tid] = scales.x * fabsf(scale_log2) * (FOUR ? FOUR_BACK : 1.f);
-        side[KEYS + tid] = scales.y * (FOUR ? FOUR_BACK : 1.f);
+        side[tid] = scales.x * fabsf(scale_log2);
+        if (!FOLD) side[KEYS + tid] = FOUR ? scales.y * (LIFT / ve) : scales.y;
+        if (FOUR && tid == 0) side[2 * KEYS + 1] = ve;
       }
       __syncwarp();
       if (lane == 0) arrive(sidefull + 8 * (j % SIDE));
@@ -647,7 +727,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       if (lane == 0) arrive(bar + 8 * (j % STAGES));
     };
     bool ok = true;
-    int page_next = look_up(0);
+    int page_next = page_first;
     if constexpr (!SCALED) {
       auto copy = [&](const TC* pool, uint32_t dst, int j, int page, uint32_t pages_ok) {
 #pragma unroll 4
@@ -716,59 +796,98 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     } else {
       uint4 k[STEPS], v[STEPS];                                   // the next tile's codes, on their way
       uint32_t kb[FOUR ? STEPS : 1], vb[FOUR ? STEPS : 1];        // and their block scales
+      float vs[FOLD ? STEPS : 1];                                 // and, of the values, their scales
+      long long entry[FOUR ? STEPS : 1];                          // where the pieces lie, -1: nowhere
+      auto locate = [&](int j, int page, uint32_t pages_ok) {
+        if constexpr (FOUR) {
+#pragma unroll
+          for (int i = 0; i < STEPS; ++i) {
+            const int key = key_of(i), of = __shfl_sync(0xffffffffu, page, key >> 3);
+            entry[i] = j * KEYS + key < most && ((pages_ok >> (key >> 3)) & 1u) ? (long long)b.entry(of, g_head, key0 + j * KEYS + key) : -1;
+          }
+        }
+      };
       auto request = [&](const TC* pool, uint4 (&x)[STEPS], const uint8_t* blocks, uint32_t (&xb)[FOUR ? STEPS : 1], int j, int page, uint32_t pages_ok) {
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
-          const TC* src = source(pool, j, key_of(i), page, pages_ok);
-          x[i] = src ? __ldg(reinterpret_cast<const uint4*>(src)) : make_uint4(0u, 0u, 0u, 0u);
-          if constexpr (FOUR) xb[i] = ask_blocks(src, pool, blocks);
+          if constexpr (FOUR) {
+            x[i] = make_uint4(0u, 0u, 0u, 0u);
+            xb[i] = 0u;
+            if (entry[i] >= 0) {
+              x[i] = __ldg(reinterpret_cast<const uint4*>(pool + entry[i] * row_units<TC>(HD) + c * 16));
+              xb[i] = __ldg(reinterpret_cast<const uint16_t*>(blocks + entry[i] * (HD / kBlock) + c * 2));
+            }
+          } else {
+            const TC* src = source(pool, j, key_of(i), page, pages_ok);
+            x[i] = src ? __ldg(reinterpret_cast<const uint4*>(src)) : make_uint4(0u, 0u, 0u, 0u);
+          }
         }
       };
-      auto convert = [&](const uint4 (&x)[STEPS], const uint32_t (&xb)[FOUR ? STEPS : 1], uint32_t dst) {
+      auto request_scales = [&] {
+        if constexpr (FOLD) {
+#pragma unroll
+          for (int i = 0; i < STEPS; ++i) vs[i] = entry[i] >= 0 ? __ldg(Vsc + entry[i]) : 0.f;
+        }
+      };
+      // A key's pieces go to the two blocks of 64 elements, whose lines share their banks: lanes of the second block go over theirs in another order
+      const bool other = HD == 128 && c >= PER_ROW / 2;
+      auto convert = [&](const uint4 (&x)[STEPS], const uint32_t (&xb)[FOUR ? STEPS : 1], uint32_t dst, bool values) {
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
           const int key = key_of(i);
-          if constexpr (FOUR) {
-            const float2 unit = e4m3_widen(xb[i]);
-            const uint32_t u[2] = {pack_bf16(unit.x * FOUR_UNIT, unit.x * FOUR_UNIT), pack_bf16(unit.y * FOUR_UNIT, unit.y * FOUR_UNIT)};
-            const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-              uint32_t o[4];
-              four_to_bf16(w[n], u[n >> 1], o);
-              sts16(dst + piece(key, 4 * c + n), o[0], o[1], o[2], o[3]);
+          if constexpr (FOUR) {                                   // 32 codes: two blocks
+            uint32_t both = blocks_widen(xb[i]);
+            if (FOLD && values) {
+              const float2 b2 = e4m3_widen(xb[i]);
+              const float f = vs[i] * (LIFT / ve);
+              both = pack_f16(b2.x * f, b2.y * f);
             }
-            continue;
+            const uint32_t u[2] = {__byte_perm(both, 0u, other ? 0x3232 : 0x1010), __byte_perm(both, 0u, other ? 0x1010 : 0x3232)};
+            const uint32_t w[4] = {other ? x[i].z : x[i].x, other ? x[i].w : x[i].y, other ? x[i].x : x[i].z, other ? x[i].y : x[i].w};
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+              sts16(dst + piece(key, 4 * c + (n ^ (other ? 2 : 0))), hmul2(e2m1_widen<0>(w[n]), u[n >> 1]), hmul2(e2m1_widen<1>(w[n]), u[n >> 1]), hmul2(e2m1_widen<2>(w[n]), u[n >> 1]),
+                    hmul2(e2m1_widen<3>(w[n]), u[n >> 1]));
+          } else {
+            uint32_t o[8];
+            to_bf16(other ? x[i].z : x[i].x, o[0], o[1], TC{});
+            to_bf16(other ? x[i].w : x[i].y, o[2], o[3], TC{});
+            to_bf16(other ? x[i].x : x[i].z, o[4], o[5], TC{});
+            to_bf16(other ? x[i].y : x[i].w, o[6], o[7], TC{});
+            sts16(dst + piece(key, 2 * c + (other ? 1 : 0)), o[0], o[1], o[2], o[3]);
+            sts16(dst + piece(key, 2 * c + (other ? 0 : 1)), o[4], o[5], o[6], o[7]);
           }
-          uint32_t o[8];
-          to_bf16(x[i].x, o[0], o[1], TC{});
-          to_bf16(x[i].y, o[2], o[3], TC{});
-          to_bf16(x[i].z, o[4], o[5], TC{});
-          to_bf16(x[i].w, o[6], o[7], TC{});
-          sts16(dst + piece(key, 2 * c), o[0], o[1], o[2], o[3]);
-          sts16(dst + piece(key, 2 * c + 1), o[4], o[5], o[6], o[7]);
         }
       };
       int page = page_next;
       uint32_t pages_ok = exists(0, page);
       float2 scales = ask_scales(0, page, pages_ok);
+      float top = FOUR ? ask_values(0, page, pages_ok) : 0.f;
+      locate(0, page, pages_ok);
       request(Kp, k, Kb, kb, 0, page, pages_ok);
       request(Vp, v, Vb, vb, 0, page, pages_ok);
+      request_scales();
       page_next = look_up(1);
       for (int j = 0; j < n_tiles; ++j) {
         const uint32_t pages_next = exists(j + 1, page_next);
         if (!(ok = wait_free(kempty, j))) break;
+        if constexpr (FOUR) raise(top);
         begin_side(j, scales, pages_ok);
-        convert(k, kb, base + L::K + (j % STAGES) * L::TILE);
+        convert(k, kb, base + L::K + (j % STAGES) * L::TILE, false);
         announce(kfull, j);
         if (j + 1 < n_tiles) {
           scales = ask_scales(j + 1, page_next, pages_next);
+          if constexpr (FOUR) top = ask_values(j + 1, page_next, pages_next);
+          locate(j + 1, page_next, pages_next);
           request(Kp, k, Kb, kb, j + 1, page_next, pages_next);
         }
         if (!(ok = wait_free(vempty, j))) break;
-        convert(v, vb, base + L::V + (j % STAGES) * L::TILE);
+        convert(v, vb, base + L::V + (j % STAGES) * L::TILE, true);
         announce(vfull, j);
-        if (j + 1 < n_tiles) request(Vp, v, Vb, vb, j + 1, page_next, pages_next);
+        if (j + 1 < n_tiles) {
+          request(Vp, v, Vb, vb, j + 1, page_next, pages_next);
+          request_scales();
+        }
         page = page_next;
         pages_ok = pages_next;
         page_next = look_up(j + 2);
@@ -778,7 +897,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PRODUCT_REGS));
     if (warp < 14 && n_tiles > 0) {
       // ---- products: one warp per tile of rows, so that neither waits for the other's softmax
-      constexpr uint32_t id_s = idesc(HALF, false), id_o = idesc(HD, true);
+      constexpr uint32_t id_s = idesc(HALF, false, FOUR), id_o = idesc(HD, true, FOUR);
       const int t = warp - 12, tiles = uniform(n_tiles), halves = uniform(t ? n_keys[1] : n_keys[0]);
       const uint32_t tm = uniform(tmem), at = uniform(base), bar = uniform(bar0);
       auto wait = [&](uint32_t which, int phase) { return tc::mbar_wait(bar + (which - bar0), phase & 1, abort_flag, b.status); };

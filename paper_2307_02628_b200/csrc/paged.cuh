@@ -49,8 +49,8 @@ struct BatchView {
 #endif
   }
   // Positions a sequence can have: len, held to the table.
-  __host__ __device__ __forceinline__ int seq_len(int s) const {
-    const int l = len[s];
+  __host__ __device__ __forceinline__ int seq_len(int s) const { return held_len(len[s]); }
+  __host__ __device__ __forceinline__ int held_len(int l) const {
     const long long most = (long long)pages_per_seq << page_shift;
     if (l > most) { bad(); return (int)most; }
     return l > 0 ? l : 0;
