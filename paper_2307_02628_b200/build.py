@@ -12,7 +12,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libskipdecode.so")
 SOURCES = [os.path.join(CSRC, n) for n in ("skipdecode.cu", "attn_scores.cu")]
 HEADERS = [os.path.join(CSRC, n) for n in ("kernels.cuh", "gemm_tc.cuh", "sample.cuh", "attn_prefill.cuh", "gemm_persist.cuh", "attn_stream.cuh",
-                                              "paged.cuh", "pages.cuh", "attn_paged.cuh", "attn_chunk.cuh", "attn_launch.cuh", "sample_rows.cuh", "cache_host.cuh")] + \
+                                              "paged.cuh", "pages.cuh", "attn_paged.cuh", "attn_chunk.cuh", "attn_four.cuh", "attn_launch.cuh", "sample_rows.cuh", "cache_host.cuh")] + \
           [os.path.join(os.path.dirname(PKG), "include", "skipdecode.h")]
 
 

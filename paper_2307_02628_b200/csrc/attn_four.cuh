@@ -1,0 +1,427 @@
+// Attention of few query rows over a paged cache in 4 bits: the same division of the work as attn_paged.cuh (a block per sequence, key head, tile of 8
+// query rows and split of the keys, a ring of asynchronous copies per warp, partial results joined by the block that arrives last), with products
+// laid out for codes of which two make a byte.
+//
+// value = code * block scale * scale.  Code times block scale is an fp16 number exactly: one conversion and one multiplication for a pair.  A key's scale multiplies
+// its score, a value's scale its weight, relative to a power of two above all scales so far and times 2^7, as in 8 bits.
+//
+// What bounds it is instructions, not bytes: at 152 bytes a key and head of 128 the memory could deliver a key every 8 clocks to an SM, which four
+// schedulers have 32 slots for, and conversion alone takes 13 (a warp's instruction for 32 lanes: 256 values in pairs, two instructions each, plus the values' interleaving).
+// So the rest is kept small:
+//  - 32 keys of a warp go through the loop at a time, so that copies, waits and maxima are paid once for them;
+//  - scores are Q K^T with the queries as the 16-row operand (8 rows, and 8 more for what fp16 leaves of them, where that is anything); the results are, thread by thread,
+//    the weights' fragment of O^T = V^T P^T, in which the values are the 16-row operand: half as many products and accumulators as with the
+//    weights there, and the 8 rows fill the other side;
+//  - a values' operand pairs two keys: nibbles of the two are interleaved by masks, four words at a time, before they are converted, and not after;
+//  - queries and results in bf16 have weights of one fp16 (11 bits), others (FINE) of two.
+#pragma once
+#include "attn_paged.cuh"
+
+namespace sd {
+namespace a4 {
+
+constexpr int NW = 5, THREADS = 32 * NW, ROWS = 8, KEYS = 32, STAGES = 3;
+
+template <int HD> struct Shape {
+  static constexpr int ROW = HD / 2, PIECES = ROW / 16, SWZ = PIECES - 1;                  // bytes and 16-byte pieces of a key
+  static constexpr int EC = HD / 4, KS = HD / 16, MT = HD / 16;                            // elements of a key that a thread has; products for 8 keys, for 16 keys
+  static constexpr int BLOCKS = HD / kBlock;                                               // block scales of a key, a byte each
+  static constexpr int V = KEYS * ROW, SCALES = 2 * V, BLOCK = SCALES + 2 * KEYS * 4, STAGE = BLOCK + 2 * KEYS * BLOCKS;
+  static constexpr int MERGE = NW * ROWS * (HD + 2) * 4;
+  static constexpr int SMEM = NW * STAGES * STAGE > MERGE ? NW * STAGES * STAGE : MERGE;   // three blocks of 73 KB to an SM at HD = 128
+};
+__device__ __forceinline__ int swz(int key) { return key >> 1; }
+
+__device__ __forceinline__ uint32_t lds32(uint32_t addr) { uint32_t r[1]; ap::lds<4>(addr, r); return r[0]; }
+// a byte by its number, as two fp16
+__device__ __forceinline__ uint32_t widen(uint32_t w, int byte) {          // byte is a constant after unrolling
+  return byte == 0 ? e2m1_widen<0>(w) : byte == 1 ? e2m1_widen<1>(w) : byte == 2 ? e2m1_widen<2>(w) : e2m1_widen<3>(w);
+}
+
+}  // namespace a4
+
+// Arguments as those of paged_attn_tile_kernel.  FINE: weights of two fp16, and queries of two where they have more bits than one.
+template <int HD, bool FINE, bool SC>
+__global__ void __launch_bounds__(a4::THREADS, 3)
+paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2m1* __restrict__ Kp, const e2m1* __restrict__ Vp, const float* __restrict__ Ksc,
+                       const float* __restrict__ Vsc, const uint8_t* __restrict__ Kb, const uint8_t* __restrict__ Vb, int group, float scale_log2, bool q_vec, int tiles_per_seq,
+                       int rows_below, int chunk, int slot_rows, float* part_acc, float* part_ml, int* __restrict__ counters, bool early, const Scores sc) {
+  using namespace a4;
+  using S = Shape<HD>;
+  extern __shared__ __align__(128) unsigned char a4_smem[];
+  __shared__ int sm_last;
+  const ap::UntilPredecessorEnds hold{early && blockIdx.x == 0 && blockIdx.y == 0};
+
+  const int unit = blockIdx.x, tile = unit % tiles_per_seq, g_head = (unit / tiles_per_seq) % b.n_kv_heads, seq = unit / tiles_per_seq / b.n_kv_heads;
+  const int splits = gridDim.y, z = blockIdx.y;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+
+  // the sequence's rows; whatever does not fit the tensors is reported and left out
+  const int f0 = b.first[seq], f1 = b.first[seq + 1], raw_len = b.len[seq], len = b.held_len(raw_len);
+  int n_new = f1 - f0;
+  if (f0 < 0 || n_new < 0 || f1 > b.n_tokens || n_new > b.max_new) {
+    if (threadIdx.x == 0) b.bad();
+    if (f0 < 0 || n_new < 0) return;
+    n_new = min(n_new, min(b.max_new, b.n_tokens - f0));
+  }
+  const int n_rows = min(ROWS, n_new * group - tile * ROWS);
+  if (n_rows <= 0 || n_new * group >= rows_below) return;
+  const long long pos_first = (long long)raw_len - (f1 - f0);               // position of the first new token, negative without a place
+
+  // this thread's query row (rows past the tile repeat the last one and are not stored), the keys it sees, and those that any and every row of the tile sees
+  const int row = tile * ROWS + min(g, n_rows - 1);
+  const int token = row / group, head = g_head * group + row % group;
+  const Span seen = visible(sc, f0 + token, pos_first + token, len);
+  int key_begin = seen.lo <= seen.hi ? seen.lo : 0x7fffffff, key_end = seen.hi + 1, all_from = seen.lo, all_see = seen.hi;
+#pragma unroll
+  for (int o = 4; o < 32; o <<= 1) {
+    key_end = max(key_end, __shfl_xor_sync(0xffffffffu, key_end, o));
+    all_see = min(all_see, __shfl_xor_sync(0xffffffffu, all_see, o));
+    if constexpr (SC) {
+      key_begin = min(key_begin, __shfl_xor_sync(0xffffffffu, key_begin, o));
+      all_from = max(all_from, __shfl_xor_sync(0xffffffffu, all_from, o));
+    }
+  }
+  const int base = SC && key_end > 0 ? key_begin & ~63 : 0;                 // chunks are multiples of 64
+  const int used_splits = max(1, ap::splits_of(key_end - base, chunk, splits));
+  if (z >= used_splits) return;
+  const int k0 = base + z * chunk, k1 = z == splits - 1 ? key_end : (int)min((long long)k0 + chunk, (long long)key_end);
+  const float cap = SC ? sc.cap * 1.4426950408889634f : 0.f, inv_cap = SC && sc.cap > 0.f ? 1.f / cap : 0.f;
+  const float slope = SC && sc.slopes ? sc.slopes[head] * 1.4426950408889634f : 0.f;
+  const int row_pos = (int)min(max(pos_first + token, 0ll), 1ll << 30);
+  const int nearest = abs(row_pos - min(max(row_pos, seen.lo), seen.hi));   // distance of the nearest visible key, which bias is relative to
+
+  float acc[S::MT][4];                             // element 2 i (c0, c1) and 2 i + 1 (c2, c3) of run g, query rows 2 t and 2 t + 1
+#pragma unroll
+  for (int i = 0; i < S::MT; ++i) { acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f; }
+  float m = -INFINITY, l = 0.f;                    // the maximum is a row's, the sum is this thread's share
+  float ve = 0.f, inv_ve = 0.f;                    // 2^7 over it; 0: no value has had a scale yet
+
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(a4_smem) + warp * (STAGES * S::STAGE);
+  const int tile0 = k0 / KEYS + warp, n_tiles = (k1 + KEYS - 1) / KEYS;     // this warp's tiles: tile0, tile0 + NW, ...
+  const int* table = b.pages + (size_t)seq * b.pages_per_seq;
+  uint32_t valid = 0u;                             // four bits per stage: the groups of 8 keys whose page exists
+  // Table entries of this warp's next tiles (from number win on), 32 / parts of them: one round of loads instead of one per tile.
+  const int part_shift = min(b.page_shift, 5), parts_log = 5 - part_shift;  // a tile is 1, 2 or 4 pages or parts of one
+  int window = 0, win = 0, win_end = 0;
+  auto look_up = [&](int n) {                      // n: the warp's n-th tile, in order
+    if (n < win_end) return;
+    win = n;
+    win_end = n + (32 >> parts_log);
+    const long long key = ((long long)tile0 + (long long)(n + (lane >> parts_log)) * NW) * KEYS + ((lane & ((1 << parts_log) - 1)) << part_shift);
+    window = key < k1 ? table[key >> b.page_shift] : 0;
+  };
+  // copies: this lane's piece of the first keys of a tile, the others follow at fixed distances; scales, four keys a piece; block scales
+  const int lane_key = lane / S::PIECES, lane_piece = lane % S::PIECES;
+  constexpr int STEPS = KEYS * S::PIECES / 32, STEP_KEYS = 32 / S::PIECES, BP = KEYS * S::BLOCKS / 16, BKEYS = 16 / S::BLOCKS;   // pieces of block scales, keys of one
+  const int b_key = (lane % BP) * BKEYS, s_key = (lane & 7) * 4;
+  auto issue = [&](int n, int stage) {
+    look_up(n);
+    const int key0 = (tile0 + n * NW) * KEYS, slot = (n - win) << parts_log;
+    const uint32_t dst = ring + stage * S::STAGE;
+    const int page0 = __shfl_sync(0xffffffffu, window, slot);
+    if (parts_log == 0 && key0 + KEYS <= k1 && (unsigned)page0 < (unsigned)b.n_pages) {
+      const size_t e = b.entry(page0, g_head, key0);                        // a whole tile inside one page
+      const e2m1* ks = Kp + e * S::ROW + lane * 16;
+      const e2m1* vs = Vp + e * S::ROW + lane * 16;
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) {
+        const int key = lane_key + i * STEP_KEYS;
+        const uint32_t at = dst + key * S::ROW + ((lane_piece ^ (swz(key) & S::SWZ)) << 4);
+        pf_cp16(at, ks + i * 512, 16);
+        pf_cp16(at + S::V, vs + i * 512, 16);
+      }
+      if (lane < 16) pf_cp16(dst + S::SCALES + lane * 16, (lane < 8 ? Ksc : Vsc) + e + s_key, 16);
+      if (lane < 2 * BP) pf_cp16(dst + S::BLOCK + lane * 16, (lane < BP ? Kb : Vb) + e * S::BLOCKS + (lane % BP) * 16, 16);
+      valid |= 15u << (4 * stage);
+      return;
+    }
+    // The page of the part that a key lies in, -1: none or past the end.  What is not copied is what an earlier tile left: its keys are hidden, its
+    // values' weights and scales zero.
+    auto page_of = [&](int key) {
+      const int page = __shfl_sync(0xffffffffu, window, slot + (key >> part_shift));
+      return key0 + key < k1 && (unsigned)page < (unsigned)b.n_pages ? page : -1;
+    };
+    const int mine = page_of((lane & 3) * 8);
+    const uint32_t ok = __ballot_sync(0xffffffffu, mine >= 0 || key0 + (lane & 3) * 8 >= k1) & 15u;
+    if (ok != 15u && lane == 0) b.bad();
+    valid = (valid & ~(15u << (4 * stage))) | (ok << (4 * stage));
+#pragma unroll 1
+    for (int i = 0; i < STEPS; ++i) {
+      const int key = lane_key + i * STEP_KEYS, page = page_of(key);
+      if (page < 0) continue;                                               // no shuffle follows in this round
+      const size_t from = b.entry(page, g_head, key0 + key) * S::ROW + lane_piece * 16;
+      const uint32_t at = dst + key * S::ROW + ((lane_piece ^ (swz(key) & S::SWZ)) << 4);
+      pf_cp16(at, Kp + from, 16);
+      pf_cp16(at + S::V, Vp + from, 16);
+    }
+    __syncwarp();
+    const int ps = page_of(s_key), pb = page_of(b_key);
+    if (lane < 16 && ps >= 0) pf_cp16(dst + S::SCALES + lane * 16, (lane < 8 ? Ksc : Vsc) + b.entry(ps, g_head, key0 + s_key), 16);
+    if (lane < 2 * BP && pb >= 0) pf_cp16(dst + S::BLOCK + lane * 16, (lane < BP ? Kb : Vb) + b.entry(pb, g_head, key0 + b_key) * S::BLOCKS, 16);
+  };
+
+  // the query row is asked for, then the first keys, and both are on their way together
+  float q_raw[S::EC];
+  ap::load_run<S::EC>(q, (long long)(f0 + token) * q.row_stride + head * q.head_stride + t * S::EC, q_vec, q_raw);
+  const int mine = tile0 < n_tiles ? (n_tiles - tile0 + NW - 1) / NW : 0;   // this warp's tiles
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; ++s) {
+    if (s < mine) issue(s, s);
+    pf_commit();
+  }
+  uint32_t qf[S::KS][FINE ? 4 : 2];
+  float row_scale = scale_log2;
+  {
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < S::EC; ++i) top = fmaxf(top, fabsf(q_raw[i]));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const int e = min(max((int)((__float_as_uint(top) >> 23) & 0xff), 2), 252);
+    const float down = __uint_as_float((uint32_t)(254 - e) << 23);          // 2^(127 - e): queries enter as fp16, brought near 1
+    row_scale *= __uint_as_float((uint32_t)e << 23);                        // 2^(e - 127)
+#pragma unroll
+    for (int k = 0; k < S::KS; ++k) {
+      const float* v = q_raw + 4 * k;
+      if constexpr (FINE) {
+        ap::split(v[0] * down, v[1] * down, qf[k][0], qf[k][1], __half{});
+        ap::split(v[2] * down, v[3] * down, qf[k][2], qf[k][3], __half{});
+      } else {
+        qf[k][0] = pack_f16(v[0] * down, v[1] * down);
+        qf[k][1] = pack_f16(v[2] * down, v[3] * down);
+      }
+    }
+  }
+
+  int stage = 0, fill = STAGES - 1;
+  for (int n = 0; n < mine; ++n) {
+    const int key0 = (tile0 + n * NW) * KEYS;
+    if (n + STAGES - 1 < mine) issue(n + STAGES - 1, fill);
+    pf_commit();
+    fill = fill + 1 == STAGES ? 0 : fill + 1;
+    pf_wait<STAGES - 1>();
+    __syncwarp();
+    const uint32_t at = ring + stage * S::STAGE;
+
+    // scores: 8 query rows x 32 keys; this thread's eight: keys n * 8 + 2 t + {0, 1}
+    float x[4][2], vsc[4][2];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int key = j * 8 + g;
+      constexpr int B = S::EC / 2;                                          // bytes of the thread's elements
+      uint32_t w[B / 4];
+      const int off = t * B;
+      ap::lds<B>(at + key * S::ROW + (((off >> 4) ^ (swz(key) & S::SWZ)) << 4) + (off & 15), w);
+      uint32_t unit[2];                                                     // block scales of the first and the last 16 elements, twice each
+      if constexpr (HD == 128) {
+        uint32_t two[1];
+        ap::lds<2>(at + S::BLOCK + key * S::BLOCKS + 2 * t, two);
+        const uint32_t u = blocks_widen(two[0]);
+        unit[0] = __byte_perm(u, 0u, 0x1010); unit[1] = __byte_perm(u, 0u, 0x3232);
+      } else {
+        const int blk = t * S::EC / kBlock;
+        uint32_t two[1];
+        ap::lds<2>(at + S::BLOCK + key * S::BLOCKS + (blk & ~1), two);
+        unit[0] = unit[1] = __byte_perm(blocks_widen(two[0]), 0u, blk & 1 ? 0x3232 : 0x1010);
+      }
+      float c[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < S::KS; ++k) {                                     // two bytes: four elements
+        const uint32_t lo = hmul2(widen(w[k >> 1], 2 * (k & 1)), unit[k >> 2]), hi = hmul2(widen(w[k >> 1], 2 * (k & 1) + 1), unit[k >> 2]);
+        if constexpr (FINE) {
+          ap::mma(c, qf[k], lo, hi, __half{});
+        } else {
+          const uint32_t a[4] = {qf[k][0], 0u, qf[k][1], 0u};
+          ap::mma(c, a, lo, hi, __half{});
+        }
+      }
+      const float2 ks = ap::lds_f32x2(at + S::SCALES + (j * 8 + 2 * t) * 4), vs = ap::lds_f32x2(at + S::SCALES + (KEYS + j * 8 + 2 * t) * 4);
+      x[j][0] = (FINE ? c[0] + c[2] : c[0]) * ks.x;
+      x[j][1] = (FINE ? c[1] + c[3] : c[1]) * ks.y;
+      vsc[j][0] = vs.x; vsc[j][1] = vs.y;
+    }
+    if constexpr (SC) {
+      if (sc.cap > 0.f || sc.slopes) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            float y = x[j][i] * row_scale;
+            if (sc.cap > 0.f) y = capped(y, cap, inv_cap);
+            if (sc.slopes) y -= slope * (float)(abs(row_pos - (key0 + j * 8 + 2 * t + i)) - nearest);
+            x[j][i] = y;
+          }
+      }
+    }
+    const float unit_x = SC && (sc.cap > 0.f || sc.slopes) ? 1.f : row_scale;
+    const uint32_t ok = valid >> (4 * stage) & 15u;
+    uint32_t hidden = 0u, gone = 0u;               // of the eight: keys that the row does not see, that are not there
+    if (key0 + KEYS - 1 > all_see || key0 + KEYS > k1 || ok != 15u || (SC && key0 < all_from)) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int key = key0 + j * 8 + 2 * t + i;
+          const bool there = key < k1 && ((ok >> j) & 1u);
+          if (!there || key > seen.hi || (SC && key < seen.lo)) hidden |= 1u << (2 * j + i);
+          if (!there) {                            // past the end or on a page that does not exist: it may be anything
+            vsc[j][i] = 0.f;
+            gone |= 1u << (2 * j + i);
+          }
+        }
+    }
+    float mb = m == -INFINITY ? 0.f : m, top = -INFINITY, most = 0.f;
+    // scores relative to the maximum, base 2
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        x[j][i] = fmaf(x[j][i], unit_x, -mb);
+        if (hidden && ((hidden >> (2 * j + i)) & 1u)) x[j][i] = -INFINITY;
+        top = fmaxf(top, x[j][i]);
+        most = fmaxf(most, vsc[j][i]);
+      }
+    if (__any_sync(0xffffffffu, top > 8.f || m == -INFINITY || most > ve)) {
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const float m_new = fmaxf(m, top + mb);
+      float a = exp2_safe(m, m_new);
+      l *= a;
+      m = m_new;
+      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));            // the four lanes of a row see all 32 keys
+      if (most > ve) {
+        // the next power of two, kept where 2^7 over it is a normal number too
+        const int e = min(max((int)((__float_as_uint(most) >> 23) & 0xff) + 1, 14), 254);
+        const float ve_new = __uint_as_float((uint32_t)e << 23);
+        a *= ve / ve_new;
+        ve = ve_new;
+        inv_ve = __uint_as_float((uint32_t)(254 - e + 7) << 23);
+      }
+      const float a0 = __shfl_sync(0xffffffffu, a, 8 * t), a1 = __shfl_sync(0xffffffffu, a, 8 * t + 4);      // of rows 2 t and 2 t + 1
+#pragma unroll
+      for (int i = 0; i < S::MT; ++i) { acc[i][0] *= a0; acc[i][1] *= a1; acc[i][2] *= a0; acc[i][3] *= a1; }
+      const float mb_new = m == -INFINITY ? 0.f : m, shift = mb - mb_new;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { x[j][0] += shift; x[j][1] += shift; }
+    }
+    // weights: the sum's, and the ones that multiply the values
+    uint32_t pf[4], pl[FINE ? 4 : 1];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float p[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        p[i] = ap::ex2(x[j][i]);
+        l += p[i];
+        p[i] *= vsc[j][i] * inv_ve;
+      }
+      if constexpr (FINE) ap::split(p[0], p[1], pf[j], pl[j], __half{});
+      else pf[j] = pack_f16(p[0], p[1]);
+    }
+
+    // values, 16 keys at a time: this thread's four are 2 t, 2 t + 1, 2 t + 8, 2 t + 9, its elements run g of HD / 8
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      constexpr int B = HD / 16, W = B < 4 ? 4 : B;                         // bytes of a run, all of one block; a run of two is cut out of its word
+      uint32_t w[4][W / 4], blk[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int key = h * 16 + 2 * t + (i & 1) + (i >> 1) * 8, off = g * B;
+        ap::lds<W>(at + S::V + key * S::ROW + (((off >> 4) ^ (swz(key) & S::SWZ)) << 4) + (off & (16 - W)), w[i]);
+        if constexpr (B < 4) w[i][0] >>= (off & 2) * 8;
+        const int bl = g * (HD / 8) / kBlock;
+        uint32_t two[1];
+        ap::lds<2>(at + S::BLOCK + (KEYS + key) * S::BLOCKS + (bl & ~1), two);
+        blk[i] = gone && ((gone >> (4 * h + i)) & 1u) ? 0u : two[0];
+      }
+      const int sel = (g * (HD / 8) / kBlock) & 1 ? 0x0051 : 0x0040;         // the block's byte of the two
+      const uint32_t ua = blocks_widen(__byte_perm(blk[0], blk[1], sel)), ub = blocks_widen(__byte_perm(blk[2], blk[3], sel));
+#pragma unroll
+      for (int k = 0; k < W / 4; ++k) {
+        constexpr uint32_t LOW = 0x0f0f0f0fu;
+        const uint32_t a_even = (w[0][k] & LOW) | (w[1][k] << 4 & ~LOW), a_odd = (w[0][k] >> 4 & LOW) | (w[1][k] & ~LOW);
+        const uint32_t b_even = (w[2][k] & LOW) | (w[3][k] << 4 & ~LOW), b_odd = (w[2][k] >> 4 & LOW) | (w[3][k] & ~LOW);
+#pragma unroll
+        for (int i = 0; i < (B < 4 ? B : 4); ++i) {                         // elements 8 k + 2 i and 8 k + 2 i + 1
+          const uint32_t v[4] = {hmul2(widen(a_even, i), ua), hmul2(widen(a_odd, i), ua), hmul2(widen(b_even, i), ub), hmul2(widen(b_odd, i), ub)};
+          ap::mma(acc[4 * k + i], v, pf[2 * h], pf[2 * h + 1], __half{});
+          if constexpr (FINE) ap::mma(acc[4 * k + i], v, pl[2 * h], pl[2 * h + 1], __half{});
+        }
+      }
+    }
+    __syncwarp();                                                           // the stage is refilled in the next round
+    stage = stage + 1 == STAGES ? 0 : stage + 1;
+  }
+  pf_wait<0>();
+
+  // this warp's rows: accumulators and sums in units of 2^m, sums over the quad
+  l += __shfl_xor_sync(0xffffffffu, l, 1);
+  l += __shfl_xor_sync(0xffffffffu, l, 2);
+  const float back = ve * 0.0078125f;                                       // the unit of the values' weights
+  __syncthreads();                                                          // every warp is done with its ring
+  float* sm_acc = reinterpret_cast<float*>(a4_smem);                        // [NW][ROWS][HD]
+  float* sm_m = sm_acc + NW * ROWS * HD;                                    // [NW][ROWS]
+  float* sm_l = sm_m + NW * ROWS;
+#pragma unroll
+  for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) sm_acc[(warp * ROWS + 2 * t + (c & 1)) * HD + g * (HD / 8) + 2 * i + (c >> 1)] = acc[i][c] * back;
+  if (t == 0) { sm_m[warp * ROWS + g] = m; sm_l[warp * ROWS + g] = l; }
+  __syncthreads();
+
+  auto place = [&](int r, int& tok, int& hd) {
+    const int rr = tile * ROWS + r;
+    tok = f0 + rr / group;
+    hd = g_head * group + rr % group;
+  };
+  for (int i = threadIdx.x; i < n_rows * HD; i += THREADS) {
+    const int r = i / HD, c = i % HD;
+    float M = -INFINITY, L = 0.f, a = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) M = fmaxf(M, sm_m[w * ROWS + r]);
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float f = exp2_safe(sm_m[w * ROWS + r], M);
+      L += sm_l[w * ROWS + r] * f;
+      a += sm_acc[(w * ROWS + r) * HD + c] * f;
+    }
+    int tok, hd;
+    place(r, tok, hd);
+    if (used_splits == 1) {
+      store_elem(out, (long long)tok * out.row_stride + hd * out.head_stride + c, normalised(a, L));
+    } else {
+      const size_t slot = ((size_t)unit * slot_rows + r) * splits + z;
+      __stcg(part_acc + slot * HD + c, a);
+      if (c == 0) { __stcg(part_ml + slot * 2, M); __stcg(part_ml + slot * 2 + 1, L); }
+    }
+  }
+  if (used_splits == 1) return;
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const int done = atomicAdd(&counters[unit], 1);
+    sm_last = done == used_splits - 1;
+    if (sm_last) counters[unit] = 0;                                        // ready for the next launch
+  }
+  __syncthreads();
+  if (!sm_last) return;
+  __threadfence();
+  for (int i = threadIdx.x; i < n_rows * HD; i += THREADS) {
+    const int r = i / HD, c = i % HD;
+    int tok, hd;
+    place(r, tok, hd);
+    const size_t slot0 = ((size_t)unit * slot_rows + r) * splits;
+    float M = -INFINITY, L = 0.f, a = 0.f;
+    for (int s = 0; s < used_splits; ++s) M = fmaxf(M, __ldcg(part_ml + (slot0 + s) * 2));
+    for (int s = 0; s < used_splits; ++s) {
+      const float f = exp2_safe(__ldcg(part_ml + (slot0 + s) * 2), M);
+      L += __ldcg(part_ml + (slot0 + s) * 2 + 1) * f;
+      a += __ldcg(part_acc + (slot0 + s) * HD + c) * f;
+    }
+    store_elem(out, (long long)tok * out.row_stride + hd * out.head_stride + c, normalised(a, L));
+  }
+}
+
+}  // namespace sd

@@ -8,6 +8,7 @@
 
 #include "../../include/skipdecode.h"
 #include "attn_chunk.cuh"
+#include "attn_four.cuh"
 #include "attn_paged.cuh"
 #include "paged.cuh"
 
@@ -22,7 +23,7 @@ struct sd_cache {
   size_t minus_pos, last_row, part_acc, part_ml, part_used, counters, status_off, total;
   size_t plan, claim, copy_from, copy_to, place, totals;         // workspace of the calls on pages
   sd::EncodeTiledFn encode = nullptr;
-  int tile_blocks[2][15] = {};          // blocks per SM of each form of the kernel for few rows, without and with changed scores
+  int tile_blocks[2][18] = {};          // blocks per SM of each form of the kernel for few rows, without and with changed scores
   int64_t launches = 0;      // kernels launched
   bool test_expire = false;  // test hook: the next launch for chunks makes a wait run out (one shot)
   unsigned long long tile_ready[2] = {};   // bit per kernel whose shared-memory size has been allowed on this device
@@ -133,9 +134,52 @@ int attention_tiles(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, fl
   const int chunk = pick_split((long)c->tile_blocks[SC][index] * c->sm_count, (long)units, (long)units * slot_rows, max_len);
   const int splits = (int)(((int64_t)max_len + chunk - 1) / chunk);
   sd::launch_kernel(early, c->stream, kernel, dim3((unsigned)units, splits), dim3(sd::ap::THREADS), S::SMEM,
-      view_of(c, b), rows_of(q), rows_of(out), (const TC*)P.k, (const TC*)P.v, (const float*)P.ks, (const float*)P.vs, (const uint8_t*)P.kb, (const uint8_t*)P.vb, c->group, scale_log2, wide(q),
+      view_of(c, b), rows_of(q), rows_of(out), (const TC*)P.k, (const TC*)P.v, (const float*)P.ks, (const float*)P.vs, c->group, scale_log2, wide(q),
       tiles, (int)std::min<int64_t>(rows_below, 0x7fffffff), chunk, slot_rows, c->at<float>(c->part_acc), c->at<float>(c->part_ml), c->at<int>(c->counters), early, sc);
   return launched(c);
+}
+
+// The same over a cache in 4 bits.  A weight enters as one fp16 where queries and results are bf16, else as two.
+template <int HD, bool FINE, bool SC>
+int attention_four(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale_log2, const sd_heads* out, const sd::Scores& sc, int64_t rows_below, bool early) {
+  using S = sd::a4::Shape<HD>;
+  constexpr int index = 12 + (HD == 128 ? 0 : HD == 64 ? 1 : 2) + (FINE ? 3 : 0);
+  auto kernel = sd::paged_attn_four_kernel<HD, FINE, SC>;
+  if (!(c->tile_ready[SC] >> index & 1u)) {
+    int per_sm = 0;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) != cudaSuccess ||
+        cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 100) != cudaSuccess ||
+        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, sd::a4::THREADS, S::SMEM) != cudaSuccess) { cudaGetLastError(); return SD_ERR_CUDA; }
+    c->tile_blocks[SC][index] = std::max(per_sm, 1);
+    c->tile_ready[SC] |= 1ull << index;
+  }
+  const auto P = pools<sd::e2m1>(c, l);
+  const int64_t most = std::min((int64_t)b->max_new * c->group, rows_below - 1);       // rows of a sequence that this launch takes
+  const int tiles = (int)((most + sd::a4::ROWS - 1) / sd::a4::ROWS), slot_rows = (int)std::min<int64_t>(most, sd::a4::ROWS);
+  const int64_t units = (int64_t)tiles * c->cfg.n_kv_heads * b->n_seqs;
+  if (units > 0x7fffffff) return SD_ERR_ARG;
+  const int max_len = most_keys(c, b, sc, sd::a4::ROWS);
+  const int chunk = pick_split((long)c->tile_blocks[SC][index] * c->sm_count, (long)units, (long)units * slot_rows, max_len);
+  const int splits = (int)(((int64_t)max_len + chunk - 1) / chunk);
+  sd::launch_kernel(early, c->stream, kernel, dim3((unsigned)units, splits), dim3(sd::a4::THREADS), S::SMEM,
+      view_of(c, b), rows_of(q), rows_of(out), (const sd::e2m1*)P.k, (const sd::e2m1*)P.v, (const float*)P.ks, (const float*)P.vs, (const uint8_t*)P.kb, (const uint8_t*)P.vb, c->group,
+      scale_log2, wide(q), tiles, (int)std::min<int64_t>(rows_below, 0x7fffffff), chunk, slot_rows, c->at<float>(c->part_acc), c->at<float>(c->part_ml), c->at<int>(c->counters),
+      early, sc);
+  return launched(c);
+}
+
+// The kernel for few rows that a call's types take.
+template <typename TC, int HD, bool SC>
+int attention_few(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale_log2, const sd_heads* out, const sd::Scores& sc, int64_t rows_below, bool early = false) {
+  if constexpr (sd::kFour<TC>) {
+    return q->dtype == SD_DTYPE_BF16 && out->dtype == SD_DTYPE_BF16 ? attention_four<HD, false, SC>(c, l, b, q, scale_log2, out, sc, rows_below, early)
+                                                                    : attention_four<HD, true, SC>(c, l, b, q, scale_log2, out, sc, rows_below, early);
+  } else {
+    if constexpr (std::is_same<TC, bf16>::value) {
+      if (out->dtype == SD_DTYPE_FP32) return attention_tiles<TC, HD, true, SC>(c, l, b, q, scale_log2, out, sc, rows_below, early);
+    }
+    return attention_tiles<TC, HD, false, SC>(c, l, b, q, scale_log2, out, sc, rows_below, early);
+  }
 }
 
 // A bf16 pool as [n_pages * n_kv_heads][page_len][HD], boxes of one page by 64 elements (128 bytes, swizzled).
@@ -239,13 +283,10 @@ int cache_attention(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, fl
                                  : attention_chunks<TC, HD, false, SC>(c, l, b, q, scale_log2, out, sc, rows_from, &split);
             if (rc != SD_OK || b->n_seqs == 1) return rc;
             // it may begin early where the two do not share the workspace for split keys
-            return attention_tiles<TC, HD, false, SC>(c, l, b, q, scale_log2, out, sc, enough, !split);
+            return attention_few<TC, HD, SC>(c, l, b, q, scale_log2, out, sc, enough, !split);
           }
         }
-        if constexpr (std::is_same<TC, bf16>::value) {
-          if (out->dtype == SD_DTYPE_FP32) return attention_tiles<TC, HD, true, SC>(c, l, b, q, scale_log2, out, sc, most + 1);
-        }
-        return attention_tiles<TC, HD, false, SC>(c, l, b, q, scale_log2, out, sc, most + 1);
+        return attention_few<TC, HD, SC>(c, l, b, q, scale_log2, out, sc, most + 1);
       }
     });
   });

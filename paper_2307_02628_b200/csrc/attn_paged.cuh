@@ -12,7 +12,6 @@
 // 16 rows of a tile are the 8 query rows twice: once the upper and once the lower half of each query element (and of
 // each softmax weight), two 16-bit numbers that together keep 16 bits in bf16 and 22 in fp16, so the operands' rounding stays
 // near fp32 at no cost: with 8 rows or fewer the other half of the tile would be empty.  8-bit codes are fp16 numbers exactly.
-// 4-bit codes times their block's scale are fp16 numbers exactly too; the scale of the row is applied as in 8 bits.
 // bf16 caches multiply in bf16, and where results are fp32 with a third part of each operand, 24 bits, in products of their own (the form
 // THIRD): relative to 64-bit arithmetic 4.8e-7 instead of 3e-6.  64 single tokens at 1280, 32 heads of 128: 221 us (211 without the third
 // part), 3 of 32 heads over 8 at 65 000: 164 (156); 4 x 512 tokens at 2048, where the products are what it does, 975 (700).
@@ -38,17 +37,14 @@ constexpr int NW = 4, THREADS = 32 * NW, ROWS = 8, KEYS = 16;
 
 template <typename TC, int HD> struct Shape {
   static constexpr bool SCALED = CacheType<TC>::TOP > 0.f;
-  static constexpr bool FOUR = kFour<TC>;
-  static constexpr int ROW = FOUR ? HD / 2 : HD * (int)sizeof(TC);   // bytes of a key
+  static constexpr int E = sizeof(TC);
+  static constexpr int ROW = HD * E;                         // bytes of a key
   static constexpr int PIECES = ROW / 16;
   static constexpr int SWZ = PIECES < 8 ? PIECES - 1 : 7;
-  static constexpr int AT_ONCE = 16 * HD / ROW;                      // elements in 16 bytes
-  static constexpr int EC = AT_ONCE < HD / 4 ? AT_ONCE : HD / 4;     // elements a thread reads at a time for the scores
+  static constexpr int EC = 16 / E < HD / 4 ? 16 / E : HD / 4;   // elements a thread reads at a time for the scores
   static constexpr int NCH = HD / (4 * EC);
   static constexpr int KS = HD / 16, NT = HD / 8;
-  static constexpr int BLOCKS = FOUR ? HD / kBlock : 0;              // block scales of a key, a byte each; as many 16-byte pieces of a tile
-  static constexpr int BLOCK_OFF = 2 * KEYS * ROW + 2 * KEYS * 4;
-  static constexpr int STAGE = 2 * KEYS * ROW + (SCALED ? 2 * KEYS * 4 : 0) + 2 * KEYS * BLOCKS;
+  static constexpr int STAGE = 2 * KEYS * ROW + (SCALED ? 2 * KEYS * 4 : 0);
   // two blocks of 98 KB per SM (bf16, 128 elements), else three or four of 50 to 66 KB, as registers allow
   static constexpr int STAGES = STAGE >= 8192 ? 3 : STAGE >= 4096 ? 4 : 6;
   static constexpr int MERGE = NW * ROWS * (HD + 2) * 4;
@@ -93,7 +89,6 @@ __device__ __forceinline__ uint32_t widen(uint32_t w) {
   const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)w, __NV_E4M3);
   return (uint32_t)r.x | ((uint32_t)r.y << 16);
 }
-__device__ __forceinline__ uint32_t flip(uint32_t w, e2m1) { return w; }
 __device__ __forceinline__ uint32_t lower(uint32_t w, e4m3) { return widen(w & 0xffffu); }
 __device__ __forceinline__ uint32_t upper(uint32_t w, e4m3) { return widen(w >> 16); }
 
@@ -155,7 +150,7 @@ template <int N> __device__ __forceinline__ void load_run(const Rows& t, long lo
 template <typename TC, int HD, bool THIRD, bool SC>
 __global__ void __launch_bounds__(ap::THREADS)
 paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC* __restrict__ Kp, const TC* __restrict__ Vp,
-                       const float* __restrict__ Ksc, const float* __restrict__ Vsc, const uint8_t* __restrict__ Kb, const uint8_t* __restrict__ Vb, int group, float scale_log2, bool q_vec,
+                       const float* __restrict__ Ksc, const float* __restrict__ Vsc, int group, float scale_log2, bool q_vec,
                        int tiles_per_seq, int rows_below, int chunk, int slot_rows, float* part_acc, float* part_ml, int* __restrict__ counters, bool early, const Scores sc) {
   using namespace ap;
   using S = Shape<TC, HD>;
@@ -232,8 +227,8 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
   };
   // this lane's piece of the first keys of a tile: the others follow at fixed distances
   const int lane_key = lane / S::PIECES, lane_piece = lane % S::PIECES;
-  constexpr int STEPS = (KEYS * S::PIECES + 31) / 32, STEP_KEYS = 32 / S::PIECES;
-  static_assert(KEYS * S::PIECES % 32 == 0 || STEPS == 1, "whole warps of copies, or one in part");
+  constexpr int STEPS = KEYS * S::PIECES / 32, STEP_KEYS = 32 / S::PIECES;
+  static_assert(KEYS * S::PIECES % 32 == 0, "whole warps of copies");
   auto issue = [&](int n, int stage) {
     look_up(n);
     const int kt = tile0 + n * NW;
@@ -243,22 +238,17 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
     if (!split_tile && key0 + KEYS <= k1 && (unsigned)page[0] < (unsigned)b.n_pages) {
       // a whole tile inside one page
       const size_t e = b.entry(page[0], g_head, key0);
-      const TC* ks = Kp + e * row_units<TC>(HD) + lane * (16 / sizeof(TC));
-      const TC* vs = Vp + e * row_units<TC>(HD) + lane * (16 / sizeof(TC));
+      const TC* ks = Kp + e * HD + lane * (16 / S::E);
+      const TC* vs = Vp + e * HD + lane * (16 / S::E);
 #pragma unroll
       for (int i = 0; i < STEPS; ++i) {
         const int key = lane_key + i * STEP_KEYS;
         const uint32_t at = dst + key * S::ROW + ((lane_piece ^ (swz(key) & S::SWZ)) << 4);
-        if (S::PIECES * KEYS >= 32 || lane < S::PIECES * KEYS) {
-          pf_cp16(at, ks + i * 32 * (16 / sizeof(TC)), 16);
-          pf_cp16(at + KEYS * S::ROW, vs + i * 32 * (16 / sizeof(TC)), 16);
-        }
+        pf_cp16(at, ks + i * 32 * (16 / S::E), 16);
+        pf_cp16(at + KEYS * S::ROW, vs + i * 32 * (16 / S::E), 16);
       }
       if constexpr (S::SCALED) {
         if (lane < 8) pf_cp16(dst + 2 * KEYS * S::ROW + lane * 16, (lane < 4 ? Ksc : Vsc) + e + (lane & 3) * 4, 16);
-      }
-      if constexpr (S::FOUR) {                       // the keys' block scales, then the values'
-        if (lane < 2 * S::BLOCKS) pf_cp16(dst + S::BLOCK_OFF + lane * 16, (lane < S::BLOCKS ? Kb : Vb) + e * S::BLOCKS + lane % S::BLOCKS * 16, 16);
       }
       valid |= 3u << (2 * stage);
       return;
@@ -278,20 +268,10 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
     for (int i = 0; i < STEPS; ++i) {
       const int key = lane_key + i * STEP_KEYS, hf = key >> 3;
       const bool on = key0 + key < k1 && ((ok >> hf) & 1u);                  // off: zeros, nothing is read
-      const size_t src = on ? ((hf ? e[1] : e[0]) + (key & 7)) * row_units<TC>(HD) + lane_piece * (16 / sizeof(TC)) : 0;
+      const size_t src = on ? ((hf ? e[1] : e[0]) + (key & 7)) * HD + lane_piece * (16 / S::E) : 0;
       const uint32_t at = dst + key * S::ROW + ((lane_piece ^ (swz(key) & S::SWZ)) << 4);
-      if (S::PIECES * KEYS >= 32 || lane < S::PIECES * KEYS) {
-        pf_cp16(at, Kp + src, on ? 16 : 0);
-        pf_cp16(at + KEYS * S::ROW, Vp + src, on ? 16 : 0);
-      }
-    }
-    if constexpr (S::FOUR) {                         // half a tile's block scales are BLOCKS / 2 pieces; what lies past the end hides behind zero scales
-      if (lane < 2 * S::BLOCKS) {
-        const int i = lane % S::BLOCKS, hf = i / (S::BLOCKS / 2);
-        const bool on = key0 + 8 * hf < k1 && ((ok >> hf) & 1u);
-        const uint8_t* src = (lane < S::BLOCKS ? Kb : Vb) + (on ? (hf ? e[1] : e[0]) * S::BLOCKS + i % (S::BLOCKS / 2) * 16 : 0);
-        pf_cp16(dst + S::BLOCK_OFF + lane * 16, src, on ? 16 : 0);
-      }
+      pf_cp16(at, Kp + src, on ? 16 : 0);
+      pf_cp16(at + KEYS * S::ROW, Vp + src, on ? 16 : 0);
     }
     if constexpr (S::SCALED) {
       if (lane < 8) {                              // 16 scales of each: four pieces of four
@@ -365,31 +345,13 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
       const int key = n * 8 + g;
 #pragma unroll
       for (int c = 0; c < S::NCH; ++c) {
-        constexpr int B = S::EC * S::ROW / HD;                                // 16 bytes, 8 or 4
+        constexpr int B = S::EC * S::E;                                       // 16 bytes, or 8
         uint32_t w[B / 4];
         const int off = (t + 4 * c) * B;
         lds<B>(ks_base + key * S::ROW + (((off >> 4) ^ (swz(key) & S::SWZ)) << 4) + (off & 15), w);
-        uint32_t unit0 = 0u, unit1 = 0u;            // block scales of the thread's first and last 16 elements, twice each
-        if constexpr (S::FOUR) {
-          uint32_t two[1];
-          if constexpr (HD == 128) {
-            lds<2>(ks_base + S::BLOCK_OFF + key * S::BLOCKS + 2 * t, two);
-            const uint32_t u = blocks_widen(two[0]);
-            unit0 = __byte_perm(u, 0u, 0x1010); unit1 = __byte_perm(u, 0u, 0x3232);
-          } else {
-            const int blk = t * S::EC / kBlock;
-            lds<2>(ks_base + S::BLOCK_OFF + key * S::BLOCKS + (blk & ~1), two);
-            unit0 = __byte_perm(blocks_widen(two[0]), 0u, blk & 1 ? 0x3232 : 0x1010);
-          }
-        }
 #pragma unroll
         for (int k = 0; k < S::EC / 4; ++k) {
-          if constexpr (S::FOUR) {                  // two bytes, four elements of one block: (k / 4)-th of this thread's
-            const uint32_t unit = S::EC > kBlock && k >= 4 ? unit1 : unit0;
-            const uint32_t lo = hmul2(k & 1 ? e2m1_widen<2>(w[k >> 1]) : e2m1_widen<0>(w[k >> 1]), unit);
-            const uint32_t hi = hmul2(k & 1 ? e2m1_widen<3>(w[k >> 1]) : e2m1_widen<1>(w[k >> 1]), unit);
-            mma(s[n], qf[k], lo, hi, TC{});
-          } else if constexpr (S::SCALED) {
+          if constexpr (S::SCALED) {
             const uint32_t f = flip(w[k], TC{});
             mma(s[n], qf[c * (S::EC / 4) + k], lower(f, TC{}), upper(f, TC{}), TC{});
           } else {
@@ -426,7 +388,7 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
         }
     }
     const uint32_t ok = valid >> (2 * stage);
-    uint32_t hidden = 0u, gone = 0u;                // of the four: keys that the row does not see, that are not there
+    uint32_t hidden = 0u;                           // of the four: keys that the row does not see
     if (kt * KEYS + KEYS - 1 > all_see || kt * KEYS + KEYS > k1 || (ok & 3u) != 3u || (SC && kt * KEYS < all_from)) {
 #pragma unroll
       for (int n = 0; n < 2; ++n)
@@ -435,10 +397,7 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
           const int at = kt * KEYS + n * 8 + 2 * t + i;
           const bool there = at < k1 && ((ok >> n) & 1u);
           if (!there || at > row_last || (SC && at < row_first)) hidden |= 1u << (2 * n + i);
-          if (!there) {                             // past the end or on a page that does not exist: it may be anything
-            vsc[n][i] = 0.f;
-            gone |= 1u << (2 * n + i);
-          }
+          if (!there) vsc[n][i] = 0.f;              // past the end or on a page that does not exist: it may be anything
         }
     }
     float mb = m == -INFINITY ? 0.f : m;
@@ -498,32 +457,7 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
     }
 
     // values
-    if constexpr (S::FOUR) {
-      constexpr int B = HD / 16;                                              // bytes of a thread's run: elements [run * 2 B, +2 B), of one block
-      const int run = ((g & 1) << 2) | (g >> 1);
-      // A run of two bytes is cut out of its word: from a 16-bit load the compiler (12.9) made conversions whose results were zeros.
-      constexpr int W = B < 4 ? 4 : B;
-      uint32_t w[4][W / 4], blk[4][1];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int key = 2 * t + (i & 1) + (i >> 1) * 8, off = run * B;
-        lds<W>(vs_base + key * S::ROW + (((off >> 4) ^ (swz(key) & S::SWZ)) << 4) + (off & (16 - W)), w[i]);
-        if constexpr (B < 4) w[i][0] >>= (off & 2) * 8;
-        const int at = run * 2 * B / kBlock;
-        lds<2>(ks_base + S::BLOCK_OFF + (KEYS + key) * S::BLOCKS + (at & ~1), blk[i]);
-        blk[i][0] = at & 1 ? blk[i][0] >> 8 : blk[i][0];
-        if (gone && ((gone >> i) & 1u)) blk[i][0] = 0u;
-      }
-      const uint32_t ua = blocks_widen(__byte_perm(blk[0][0], blk[1][0], 0x0040)), ub = blocks_widen(__byte_perm(blk[2][0], blk[3][0], 0x0040));
-#pragma unroll
-      for (int k = 0; k < B; ++k) {                                           // byte k: elements 2 k and 2 k + 1 of four keys
-        uint32_t c[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) c[i] = (k & 3) == 0 ? e2m1_widen<0>(w[i][k >> 2]) : (k & 3) == 1 ? e2m1_widen<1>(w[i][k >> 2]) : (k & 3) == 2 ? e2m1_widen<2>(w[i][k >> 2]) : e2m1_widen<3>(w[i][k >> 2]);
-        mma(acc[2 * k], pf, hmul2(__byte_perm(c[0], c[1], 0x5410), ua), hmul2(__byte_perm(c[2], c[3], 0x5410), ub), TC{});
-        mma(acc[2 * k + 1], pf, hmul2(__byte_perm(c[0], c[1], 0x7632), ua), hmul2(__byte_perm(c[2], c[3], 0x7632), ub), TC{});
-      }
-    } else if constexpr (S::SCALED) {
+    if constexpr (S::SCALED) {
       constexpr int B = HD / 8;                                               // bytes of a thread's run: elements [run * B, +B)
       const int run = ((g & 1) << 2) | (g >> 1);
       uint32_t w[4][B / 4];
