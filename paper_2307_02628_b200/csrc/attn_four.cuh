@@ -95,7 +95,8 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
 #pragma unroll
   for (int i = 0; i < S::MT; ++i) { acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f; }
   float m = -INFINITY, l = 0.f;                    // the maximum is a row's, the sum is this thread's share
-  float ve = 0.f, inv_ve = 0.f;                    // 2^7 over it; 0: no value has had a scale yet
+  // Values' weights are relative to ve, times 2^7: 2^lift within the exponential, and what a lift of 60 does not reach, `rest`, by itself.
+  float ve = 0.f, lift = 0.f, rest = 1.f;          // 0: no value has had a scale yet
 
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(a4_smem) + warp * (STAGES * S::STAGE);
   const int tile0 = k0 / KEYS + warp, n_tiles = (k1 + KEYS - 1) / KEYS;     // this warp's tiles: tile0, tile0 + NW, ...
@@ -115,6 +116,8 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
   const int lane_key = lane / S::PIECES, lane_piece = lane % S::PIECES;
   constexpr int STEPS = KEYS * S::PIECES / 32, STEP_KEYS = 32 / S::PIECES, BP = KEYS * S::BLOCKS / 16, BKEYS = 16 / S::BLOCKS;   // pieces of block scales, keys of one
   const int b_key = (lane % BP) * BKEYS, s_key = (lane & 7) * 4;
+  static_assert(STEP_KEYS / 2 % (S::SWZ + 1) == 0, "a lane's pieces are swizzled alike");
+  const uint32_t lane_at = lane_key * S::ROW + ((lane_piece ^ (swz(lane_key) & S::SWZ)) << 4);
   auto issue = [&](int n, int stage) {
     look_up(n);
     const int key0 = (tile0 + n * NW) * KEYS, slot = (n - win) << parts_log;
@@ -126,10 +129,8 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
       const e2m1* vs = Vp + e * S::ROW + lane * 16;
 #pragma unroll
       for (int i = 0; i < STEPS; ++i) {
-        const int key = lane_key + i * STEP_KEYS;
-        const uint32_t at = dst + key * S::ROW + ((lane_piece ^ (swz(key) & S::SWZ)) << 4);
-        pf_cp16(at, ks + i * 512, 16);
-        pf_cp16(at + S::V, vs + i * 512, 16);
+        pf_cp16(dst + lane_at + i * 512, ks + i * 512, 16);
+        pf_cp16(dst + lane_at + i * 512 + S::V, vs + i * 512, 16);
       }
       if (lane < 16) pf_cp16(dst + S::SCALES + lane * 16, (lane < 8 ? Ksc : Vsc) + e + s_key, 16);
       if (lane < 2 * BP) pf_cp16(dst + S::BLOCK + lane * 16, (lane < BP ? Kb : Vb) + e * S::BLOCKS + (lane % BP) * 16, 16);
@@ -151,9 +152,8 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
       const int key = lane_key + i * STEP_KEYS, page = page_of(key);
       if (page < 0) continue;                                               // no shuffle follows in this round
       const size_t from = b.entry(page, g_head, key0 + key) * S::ROW + lane_piece * 16;
-      const uint32_t at = dst + key * S::ROW + ((lane_piece ^ (swz(key) & S::SWZ)) << 4);
-      pf_cp16(at, Kp + from, 16);
-      pf_cp16(at + S::V, Vp + from, 16);
+      pf_cp16(dst + lane_at + i * 512, Kp + from, 16);
+      pf_cp16(dst + lane_at + i * 512 + S::V, Vp + from, 16);
     }
     __syncwarp();
     const int ps = page_of(s_key), pb = page_of(b_key);
@@ -194,6 +194,16 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
     }
   }
 
+  // Where this thread's pieces lie within a stage, the others at fixed distances.  Keys: key g, EC elements from t on.  Values: key 2 t, run g.
+  constexpr int KB = S::EC / 2, VB = HD / 16, VW = VB < 4 ? 4 : VB;          // bytes of either; a run of two is cut out of its word
+  const int k_blk = t * S::EC / kBlock, v_blk = g * (HD / 8) / kBlock;
+  const uint32_t k_at = g * S::ROW + ((((t * KB) >> 4) ^ (swz(g) & S::SWZ)) << 4) + (t * KB & 15);
+  const uint32_t v_at = S::V + 2 * t * S::ROW + ((((g * VB) >> 4) ^ (t & S::SWZ)) << 4) + (g * VB & (16 - VW));
+  const uint32_t kb_at = S::BLOCK + g * S::BLOCKS + (k_blk & ~1), vb_at = S::BLOCK + (KEYS + 2 * t) * S::BLOCKS + (v_blk & ~1);
+  const uint32_t s_at = S::SCALES + 8 * t;
+  const int k_sel = k_blk & 1 ? 0x3232 : 0x1010, v_sel = v_blk & 1 ? 0x0051 : 0x0040;
+  static_assert(4 % (S::SWZ + 1) == 0, "keys 8 apart are swizzled alike");
+
   int stage = 0, fill = STAGES - 1;
   for (int n = 0; n < mine; ++n) {
     const int key0 = (tile0 + n * NW) * KEYS;
@@ -208,23 +218,12 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
     float x[4][2], vsc[4][2];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int key = j * 8 + g;
-      constexpr int B = S::EC / 2;                                          // bytes of the thread's elements
-      uint32_t w[B / 4];
-      const int off = t * B;
-      ap::lds<B>(at + key * S::ROW + (((off >> 4) ^ (swz(key) & S::SWZ)) << 4) + (off & 15), w);
-      uint32_t unit[2];                                                     // block scales of the first and the last 16 elements, twice each
-      if constexpr (HD == 128) {
-        uint32_t two[1];
-        ap::lds<2>(at + S::BLOCK + key * S::BLOCKS + 2 * t, two);
-        const uint32_t u = blocks_widen(two[0]);
-        unit[0] = __byte_perm(u, 0u, 0x1010); unit[1] = __byte_perm(u, 0u, 0x3232);
-      } else {
-        const int blk = t * S::EC / kBlock;
-        uint32_t two[1];
-        ap::lds<2>(at + S::BLOCK + key * S::BLOCKS + (blk & ~1), two);
-        unit[0] = unit[1] = __byte_perm(blocks_widen(two[0]), 0u, blk & 1 ? 0x3232 : 0x1010);
-      }
+      uint32_t w[KB / 4], two[1], unit[2];                                  // block scales of the first and the last 16 elements, twice each
+      ap::lds<KB>(at + k_at + j * 8 * S::ROW, w);
+      ap::lds<2>(at + kb_at + j * 8 * S::BLOCKS, two);
+      const uint32_t u = blocks_widen(two[0]);
+      unit[0] = __byte_perm(u, 0u, HD == 128 ? 0x1010 : k_sel);
+      unit[1] = __byte_perm(u, 0u, 0x3232);                                 // HD = 128
       float c[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < S::KS; ++k) {                                     // two bytes: four elements
@@ -236,7 +235,7 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
           ap::mma(c, a, lo, hi, __half{});
         }
       }
-      const float2 ks = ap::lds_f32x2(at + S::SCALES + (j * 8 + 2 * t) * 4), vs = ap::lds_f32x2(at + S::SCALES + (KEYS + j * 8 + 2 * t) * 4);
+      const float2 ks = ap::lds_f32x2(at + s_at + j * 32), vs = ap::lds_f32x2(at + s_at + KEYS * 4 + j * 32);
       x[j][0] = (FINE ? c[0] + c[2] : c[0]) * ks.x;
       x[j][1] = (FINE ? c[1] + c[3] : c[1]) * ks.y;
       vsc[j][0] = vs.x; vsc[j][1] = vs.y;
@@ -271,18 +270,21 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
           }
         }
     }
-    float mb = m == -INFINITY ? 0.f : m, top = -INFINITY, most = 0.f;
-    // scores relative to the maximum, base 2
+    const float mb = (m == -INFINITY ? 0.f : m) - lift;                       // scores relative to the maximum, base 2, and the lift
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        x[j][i] = fmaf(x[j][i], unit_x, -mb);
-        if (hidden && ((hidden >> (2 * j + i)) & 1u)) x[j][i] = -INFINITY;
-        top = fmaxf(top, x[j][i]);
-        most = fmaxf(most, vsc[j][i]);
-      }
-    if (__any_sync(0xffffffffu, top > 8.f || m == -INFINITY || most > ve)) {
+      for (int i = 0; i < 2; ++i) x[j][i] = fmaf(x[j][i], unit_x, -mb);
+    if (hidden) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if ((hidden >> (2 * j + i)) & 1u) x[j][i] = -INFINITY;
+    }
+    float top = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[1][0], x[1][1])), fmaxf(fmaxf(x[2][0], x[2][1]), fmaxf(x[3][0], x[3][1])));
+    float most = fmaxf(fmaxf(fmaxf(vsc[0][0], vsc[0][1]), fmaxf(vsc[1][0], vsc[1][1])), fmaxf(fmaxf(vsc[2][0], vsc[2][1]), fmaxf(vsc[3][0], vsc[3][1])));
+    if (__any_sync(0xffffffffu, top > 8.f + lift || m == -INFINITY || most > ve)) {
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
       const float m_new = fmaxf(m, top + mb);
@@ -293,58 +295,59 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
       most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));            // the four lanes of a row see all 32 keys
       if (most > ve) {
         // the next power of two, kept where 2^7 over it is a normal number too
-        const int e = min(max((int)((__float_as_uint(most) >> 23) & 0xff) + 1, 14), 254);
+        const int e = min(max((int)((__float_as_uint(most) >> 23) & 0xff) + 1, 14), 254), up = 134 - e, lift_new = min(max(up, -60), 60);
         const float ve_new = __uint_as_float((uint32_t)e << 23);
         a *= ve / ve_new;
         ve = ve_new;
-        inv_ve = __uint_as_float((uint32_t)(254 - e + 7) << 23);
+        l *= exp2f((float)lift_new - lift);                                 // up - lift_new is at most 60, and so is lift's change a power that fp32 holds
+        lift = (float)lift_new;
+        rest = __uint_as_float((uint32_t)(127 + up - lift_new) << 23);
       }
       const float a0 = __shfl_sync(0xffffffffu, a, 8 * t), a1 = __shfl_sync(0xffffffffu, a, 8 * t + 4);      // of rows 2 t and 2 t + 1
 #pragma unroll
       for (int i = 0; i < S::MT; ++i) { acc[i][0] *= a0; acc[i][1] *= a1; acc[i][2] *= a0; acc[i][3] *= a1; }
-      const float mb_new = m == -INFINITY ? 0.f : m, shift = mb - mb_new;
+      const float shift = mb - ((m == -INFINITY ? 0.f : m) - lift);
 #pragma unroll
       for (int j = 0; j < 4; ++j) { x[j][0] += shift; x[j][1] += shift; }
+    }
+    if (rest != 1.f) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { vsc[j][0] *= rest; vsc[j][1] *= rest; }
     }
     // weights: the sum's, and the ones that multiply the values
     uint32_t pf[4], pl[FINE ? 4 : 1];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      float p[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        p[i] = ap::ex2(x[j][i]);
-        l += p[i];
-        p[i] *= vsc[j][i] * inv_ve;
-      }
-      if constexpr (FINE) ap::split(p[0], p[1], pf[j], pl[j], __half{});
-      else pf[j] = pack_f16(p[0], p[1]);
+      const float p0 = ap::ex2(x[j][0]), p1 = ap::ex2(x[j][1]);
+      l += p0 + p1;
+      if constexpr (FINE) ap::split(p0 * vsc[j][0], p1 * vsc[j][1], pf[j], pl[j], __half{});
+      else pf[j] = pack_f16(p0 * vsc[j][0], p1 * vsc[j][1]);
     }
 
     // values, 16 keys at a time: this thread's four are 2 t, 2 t + 1, 2 t + 8, 2 t + 9, its elements run g of HD / 8
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      constexpr int B = HD / 16, W = B < 4 ? 4 : B;                         // bytes of a run, all of one block; a run of two is cut out of its word
-      uint32_t w[4][W / 4], blk[4];
+      uint32_t w[4][VW / 4], blk[4][1];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int key = h * 16 + 2 * t + (i & 1) + (i >> 1) * 8, off = g * B;
-        ap::lds<W>(at + S::V + key * S::ROW + (((off >> 4) ^ (swz(key) & S::SWZ)) << 4) + (off & (16 - W)), w[i]);
-        if constexpr (B < 4) w[i][0] >>= (off & 2) * 8;
-        const int bl = g * (HD / 8) / kBlock;
-        uint32_t two[1];
-        ap::lds<2>(at + S::BLOCK + (KEYS + key) * S::BLOCKS + (bl & ~1), two);
-        blk[i] = gone && ((gone >> (4 * h + i)) & 1u) ? 0u : two[0];
+        const int step = h * 16 + (i & 1) + (i >> 1) * 8;                   // keys from 2 t on
+        ap::lds<VW>(at + v_at + step * S::ROW, w[i]);
+        if constexpr (VB < 4) w[i][0] >>= (g * VB & 2) * 8;
+        ap::lds<2>(at + vb_at + step * S::BLOCKS, blk[i]);
       }
-      const int sel = (g * (HD / 8) / kBlock) & 1 ? 0x0051 : 0x0040;         // the block's byte of the two
-      const uint32_t ua = blocks_widen(__byte_perm(blk[0], blk[1], sel)), ub = blocks_widen(__byte_perm(blk[2], blk[3], sel));
+      if (gone >> (4 * h) & 15u) {
 #pragma unroll
-      for (int k = 0; k < W / 4; ++k) {
+        for (int i = 0; i < 4; ++i)
+          if ((gone >> (4 * h + i)) & 1u) blk[i][0] = 0u;
+      }
+      const uint32_t ua = blocks_widen(__byte_perm(blk[0][0], blk[1][0], v_sel)), ub = blocks_widen(__byte_perm(blk[2][0], blk[3][0], v_sel));   // this block's byte of the two
+#pragma unroll
+      for (int k = 0; k < VW / 4; ++k) {
         constexpr uint32_t LOW = 0x0f0f0f0fu;
         const uint32_t a_even = (w[0][k] & LOW) | (w[1][k] << 4 & ~LOW), a_odd = (w[0][k] >> 4 & LOW) | (w[1][k] & ~LOW);
         const uint32_t b_even = (w[2][k] & LOW) | (w[3][k] << 4 & ~LOW), b_odd = (w[2][k] >> 4 & LOW) | (w[3][k] & ~LOW);
 #pragma unroll
-        for (int i = 0; i < (B < 4 ? B : 4); ++i) {                         // elements 8 k + 2 i and 8 k + 2 i + 1
+        for (int i = 0; i < (VB < 4 ? VB : 4); ++i) {                         // elements 8 k + 2 i and 8 k + 2 i + 1
           const uint32_t v[4] = {hmul2(widen(a_even, i), ua), hmul2(widen(a_odd, i), ua), hmul2(widen(b_even, i), ub), hmul2(widen(b_odd, i), ub)};
           ap::mma(acc[4 * k + i], v, pf[2 * h], pf[2 * h + 1], __half{});
           if constexpr (FINE) ap::mma(acc[4 * k + i], v, pl[2 * h], pl[2 * h + 1], __half{});
@@ -359,6 +362,7 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
   // this warp's rows: accumulators and sums in units of 2^m, sums over the quad
   l += __shfl_xor_sync(0xffffffffu, l, 1);
   l += __shfl_xor_sync(0xffffffffu, l, 2);
+  l *= exp2f(-lift);
   const float back = ve * 0.0078125f;                                       // the unit of the values' weights
   __syncthreads();                                                          // every warp is done with its ring
   float* sm_acc = reinterpret_cast<float*>(a4_smem);                        // [NW][ROWS][HD]
