@@ -9,9 +9,9 @@
 // schedulers have 32 slots for, and conversion alone takes 13 (a warp's instruction for 32 lanes: 256 values in pairs, two instructions each, plus the values' interleaving).
 // So the rest is kept small:
 //  - 32 keys of a warp go through the loop at a time, so that copies, waits and maxima are paid once for them;
-//  - scores are Q K^T with the queries as the 16-row operand (8 rows, and 8 more for what fp16 leaves of them, where that is anything); the results are, thread by thread,
-//    the weights' fragment of O^T = V^T P^T, in which the values are the 16-row operand: half as many products and accumulators as with the
-//    weights there, and the 8 rows fill the other side;
+//  - scores are S^T = K Q^T with the keys as the 16-row operand, and O^T = V^T P^T has the values there: the 8 query rows fill the other side of both, so that
+//    either takes half the products, and half the accumulators, that it would take with the rows' operand padded.  A thread holds scores of two
+//    query rows, the rows of its accumulators; the weights' fragment is their transpose, one instruction for 8 keys;
 //  - a values' operand pairs two keys: nibbles of the two are interleaved by masks, four words at a time, before they are converted, and not after;
 //  - queries and results in bf16 have weights of one fp16 (11 bits), others (FINE) of two.
 #pragma once
@@ -32,7 +32,16 @@ template <int HD> struct Shape {
 };
 __device__ __forceinline__ int swz(int key) { return key >> 1; }
 
-__device__ __forceinline__ uint32_t lds32(uint32_t addr) { uint32_t r[1]; ap::lds<4>(addr, r); return r[0]; }
+__device__ __forceinline__ float lds_f32(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ uint32_t transpose(uint32_t pair) {             // 8 x 8 of 16 bits
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(pair));
+  return r;
+}
 // a byte by its number, as two fp16
 __device__ __forceinline__ uint32_t widen(uint32_t w, int byte) {          // byte is a constant after unrolling
   return byte == 0 ? e2m1_widen<0>(w) : byte == 1 ? e2m1_widen<1>(w) : byte == 2 ? e2m1_widen<2>(w) : e2m1_widen<3>(w);
@@ -68,13 +77,30 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
   if (n_rows <= 0 || n_new * group >= rows_below) return;
   const long long pos_first = (long long)raw_len - (f1 - f0);               // position of the first new token, negative without a place
 
-  // this thread's query row (rows past the tile repeat the last one and are not stored), the keys it sees, and those that any and every row of the tile sees
-  const int row = tile * ROWS + min(g, n_rows - 1);
-  const int token = row / group, head = g_head * group + row % group;
-  const Span seen = visible(sc, f0 + token, pos_first + token, len);
-  int key_begin = seen.lo <= seen.hi ? seen.lo : 0x7fffffff, key_end = seen.hi + 1, all_from = seen.lo, all_see = seen.hi;
+  // This thread's two query rows (rows past the tile repeat the last one and are not stored), the keys they see, and those that any and every row of the
+  // tile sees.
+  const float cap = SC ? sc.cap * 1.4426950408889634f : 0.f, inv_cap = SC && sc.cap > 0.f ? 1.f / cap : 0.f;
+  Span seen[2];
+  int row_pos[2], nearest[2];                      // position, and the distance of the nearest visible key, which bias is relative to
+  float slope[2];
+  int key_begin = 0x7fffffff, key_end = 0, all_from = 0, all_see = 0x7fffffff;
 #pragma unroll
-  for (int o = 4; o < 32; o <<= 1) {
+  for (int i = 0; i < 2; ++i) {
+    const int row = tile * ROWS + min(2 * t + i, n_rows - 1), token = row / group;
+    const Span v = visible(sc, f0 + token, pos_first + token, len);
+    seen[i] = v;
+    if (v.lo <= v.hi) key_begin = min(key_begin, v.lo);
+    key_end = max(key_end, v.hi + 1);
+    all_from = max(all_from, v.lo);
+    all_see = min(all_see, v.hi);
+    if constexpr (SC) {
+      row_pos[i] = (int)min(max(pos_first + token, 0ll), 1ll << 30);
+      nearest[i] = abs(row_pos[i] - min(max(row_pos[i], v.lo), v.hi));
+      slope[i] = sc.slopes ? sc.slopes[g_head * group + row % group] * 1.4426950408889634f : 0.f;
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < 4; o <<= 1) {
     key_end = max(key_end, __shfl_xor_sync(0xffffffffu, key_end, o));
     all_see = min(all_see, __shfl_xor_sync(0xffffffffu, all_see, o));
     if constexpr (SC) {
@@ -86,15 +112,11 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
   const int used_splits = max(1, ap::splits_of(key_end - base, chunk, splits));
   if (z >= used_splits) return;
   const int k0 = base + z * chunk, k1 = z == splits - 1 ? key_end : (int)min((long long)k0 + chunk, (long long)key_end);
-  const float cap = SC ? sc.cap * 1.4426950408889634f : 0.f, inv_cap = SC && sc.cap > 0.f ? 1.f / cap : 0.f;
-  const float slope = SC && sc.slopes ? sc.slopes[head] * 1.4426950408889634f : 0.f;
-  const int row_pos = (int)min(max(pos_first + token, 0ll), 1ll << 30);
-  const int nearest = abs(row_pos - min(max(row_pos, seen.lo), seen.hi));   // distance of the nearest visible key, which bias is relative to
 
   float acc[S::MT][4];                             // element 2 i (c0, c1) and 2 i + 1 (c2, c3) of run g, query rows 2 t and 2 t + 1
 #pragma unroll
   for (int i = 0; i < S::MT; ++i) { acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f; }
-  float m = -INFINITY, l = 0.f;                    // the maximum is a row's, the sum is this thread's share
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};   // of the two rows: the maximum is a row's, the sum is this thread's share
   // Values' weights are relative to ve, times 2^7: 2^lift within the exponential, and what a lift of 60 does not reach, `rest`, by itself.
   float ve = 0.f, lift = 0.f, rest = 1.f;          // 0: no value has had a scale yet
 
@@ -117,6 +139,9 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
   constexpr int STEPS = KEYS * S::PIECES / 32, STEP_KEYS = 32 / S::PIECES, BP = KEYS * S::BLOCKS / 16, BKEYS = 16 / S::BLOCKS;   // pieces of block scales, keys of one
   const int b_key = (lane % BP) * BKEYS, s_key = (lane & 7) * 4;
   static_assert(STEP_KEYS / 2 % (S::SWZ + 1) == 0, "a lane's pieces are swizzled alike");
+  const e2m1 *k_src = Kp + lane * 16, *v_src = Vp + lane * 16;              // a whole tile inside one page: this lane's sources, of the pool's first key
+  const float* s_src = (lane < 8 ? Ksc : Vsc) + s_key;
+  const uint8_t* b_src = (lane < BP ? Kb : Vb) + (lane % BP) * 16;
   const uint32_t lane_at = lane_key * S::ROW + ((lane_piece ^ (swz(lane_key) & S::SWZ)) << 4);
   auto issue = [&](int n, int stage) {
     look_up(n);
@@ -124,16 +149,15 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
     const uint32_t dst = ring + stage * S::STAGE;
     const int page0 = __shfl_sync(0xffffffffu, window, slot);
     if (parts_log == 0 && key0 + KEYS <= k1 && (unsigned)page0 < (unsigned)b.n_pages) {
-      const size_t e = b.entry(page0, g_head, key0);                        // a whole tile inside one page
-      const e2m1* ks = Kp + e * S::ROW + lane * 16;
-      const e2m1* vs = Vp + e * S::ROW + lane * 16;
+      const size_t e = b.entry(page0, g_head, key0);
+      const e2m1 *ks = k_src + e * S::ROW, *vs = v_src + e * S::ROW;
 #pragma unroll
       for (int i = 0; i < STEPS; ++i) {
         pf_cp16(dst + lane_at + i * 512, ks + i * 512, 16);
         pf_cp16(dst + lane_at + i * 512 + S::V, vs + i * 512, 16);
       }
-      if (lane < 16) pf_cp16(dst + S::SCALES + lane * 16, (lane < 8 ? Ksc : Vsc) + e + s_key, 16);
-      if (lane < 2 * BP) pf_cp16(dst + S::BLOCK + lane * 16, (lane < BP ? Kb : Vb) + e * S::BLOCKS + (lane % BP) * 16, 16);
+      if (lane < 16) pf_cp16(dst + S::SCALES + lane * 16, s_src + e, 16);
+      if (lane < 2 * BP) pf_cp16(dst + S::BLOCK + lane * 16, b_src + e * S::BLOCKS, 16);
       valid |= 15u << (4 * stage);
       return;
     }
@@ -162,16 +186,19 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
   };
 
   // the query row is asked for, then the first keys, and both are on their way together
-  float q_raw[S::EC];
-  ap::load_run<S::EC>(q, (long long)(f0 + token) * q.row_stride + head * q.head_stride + t * S::EC, q_vec, q_raw);
+  float q_raw[S::EC];                              // of row g: the products want another division than the softmax
+  {
+    const int row = tile * ROWS + min(g, n_rows - 1);
+    ap::load_run<S::EC>(q, (long long)(f0 + row / group) * q.row_stride + (g_head * group + row % group) * q.head_stride + t * S::EC, q_vec, q_raw);
+  }
   const int mine = tile0 < n_tiles ? (n_tiles - tile0 + NW - 1) / NW : 0;   // this warp's tiles
 #pragma unroll
   for (int s = 0; s < STAGES - 1; ++s) {
     if (s < mine) issue(s, s);
     pf_commit();
   }
-  uint32_t qf[S::KS][FINE ? 4 : 2];
-  float row_scale = scale_log2;
+  uint32_t qf[S::KS][2], ql[FINE ? S::KS : 1][2];
+  float row_scale[2];
   {
     float top = 0.f;
 #pragma unroll
@@ -180,13 +207,14 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
     const int e = min(max((int)((__float_as_uint(top) >> 23) & 0xff), 2), 252);
     const float down = __uint_as_float((uint32_t)(254 - e) << 23);          // 2^(127 - e): queries enter as fp16, brought near 1
-    row_scale *= __uint_as_float((uint32_t)e << 23);                        // 2^(e - 127)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) row_scale[i] = scale_log2 * __uint_as_float((uint32_t)__shfl_sync(0xffffffffu, e, 8 * t + 4 * i) << 23);   // 2^(e - 127)
 #pragma unroll
     for (int k = 0; k < S::KS; ++k) {
       const float* v = q_raw + 4 * k;
       if constexpr (FINE) {
-        ap::split(v[0] * down, v[1] * down, qf[k][0], qf[k][1], __half{});
-        ap::split(v[2] * down, v[3] * down, qf[k][2], qf[k][3], __half{});
+        ap::split(v[0] * down, v[1] * down, qf[k][0], ql[k][0], __half{});
+        ap::split(v[2] * down, v[3] * down, qf[k][1], ql[k][1], __half{});
       } else {
         qf[k][0] = pack_f16(v[0] * down, v[1] * down);
         qf[k][1] = pack_f16(v[2] * down, v[3] * down);
@@ -200,7 +228,7 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
   const uint32_t k_at = g * S::ROW + ((((t * KB) >> 4) ^ (swz(g) & S::SWZ)) << 4) + (t * KB & 15);
   const uint32_t v_at = S::V + 2 * t * S::ROW + ((((g * VB) >> 4) ^ (t & S::SWZ)) << 4) + (g * VB & (16 - VW));
   const uint32_t kb_at = S::BLOCK + g * S::BLOCKS + (k_blk & ~1), vb_at = S::BLOCK + (KEYS + 2 * t) * S::BLOCKS + (v_blk & ~1);
-  const uint32_t s_at = S::SCALES + 8 * t;
+  const uint32_t s_at = S::SCALES + 4 * g;
   const int k_sel = k_blk & 1 ? 0x3232 : 0x1010, v_sel = v_blk & 1 ? 0x0051 : 0x0040;
   static_assert(4 % (S::SWZ + 1) == 0, "keys 8 apart are swizzled alike");
 
@@ -214,67 +242,74 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
     __syncwarp();
     const uint32_t at = ring + stage * S::STAGE;
 
-    // scores: 8 query rows x 32 keys; this thread's eight: keys n * 8 + 2 t + {0, 1}
-    float x[4][2], vsc[4][2];
+    // scores: 32 keys x 8 query rows; this thread's eight: keys 8 j + g, rows 2 t and 2 t + 1
+    float x[4][2], vsc[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      uint32_t w[KB / 4], two[1], unit[2];                                  // block scales of the first and the last 16 elements, twice each
-      ap::lds<KB>(at + k_at + j * 8 * S::ROW, w);
-      ap::lds<2>(at + kb_at + j * 8 * S::BLOCKS, two);
-      const uint32_t u = blocks_widen(two[0]);
-      unit[0] = __byte_perm(u, 0u, HD == 128 ? 0x1010 : k_sel);
-      unit[1] = __byte_perm(u, 0u, 0x3232);                                 // HD = 128
+    for (int jj = 0; jj < 2; ++jj) {
+      uint32_t w[2][KB / 4], unit[2][2];                                    // block scales of the first and the last 16 elements, twice each
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        uint32_t two[1];
+        ap::lds<KB>(at + k_at + (jj * 16 + r * 8) * S::ROW, w[r]);
+        ap::lds<2>(at + kb_at + (jj * 16 + r * 8) * S::BLOCKS, two);
+        const uint32_t u = blocks_widen(two[0]);
+        unit[r][0] = __byte_perm(u, 0u, HD == 128 ? 0x1010 : k_sel);
+        unit[r][1] = __byte_perm(u, 0u, 0x3232);                            // HD = 128
+      }
       float c[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int k = 0; k < S::KS; ++k) {                                     // two bytes: four elements
-        const uint32_t lo = hmul2(widen(w[k >> 1], 2 * (k & 1)), unit[k >> 2]), hi = hmul2(widen(w[k >> 1], 2 * (k & 1) + 1), unit[k >> 2]);
-        if constexpr (FINE) {
-          ap::mma(c, qf[k], lo, hi, __half{});
-        } else {
-          const uint32_t a[4] = {qf[k][0], 0u, qf[k][1], 0u};
-          ap::mma(c, a, lo, hi, __half{});
-        }
+      for (int k = 0; k < S::KS; ++k) {                                     // two bytes of two keys: four elements of each
+        const uint32_t a[4] = {hmul2(widen(w[0][k >> 1], 2 * (k & 1)), unit[0][k >> 2]), hmul2(widen(w[1][k >> 1], 2 * (k & 1)), unit[1][k >> 2]),
+                               hmul2(widen(w[0][k >> 1], 2 * (k & 1) + 1), unit[0][k >> 2]), hmul2(widen(w[1][k >> 1], 2 * (k & 1) + 1), unit[1][k >> 2])};
+        ap::mma(c, a, qf[k][0], qf[k][1], __half{});
+        if constexpr (FINE) ap::mma(c, a, ql[k][0], ql[k][1], __half{});
       }
-      const float2 ks = ap::lds_f32x2(at + s_at + j * 32), vs = ap::lds_f32x2(at + s_at + KEYS * 4 + j * 32);
-      x[j][0] = (FINE ? c[0] + c[2] : c[0]) * ks.x;
-      x[j][1] = (FINE ? c[1] + c[3] : c[1]) * ks.y;
-      vsc[j][0] = vs.x; vsc[j][1] = vs.y;
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const float ks = lds_f32(at + s_at + (jj * 16 + r * 8) * 4);
+        vsc[2 * jj + r] = lds_f32(at + s_at + KEYS * 4 + (jj * 16 + r * 8) * 4);
+        x[2 * jj + r][0] = c[2 * r] * ks;
+        x[2 * jj + r][1] = c[2 * r + 1] * ks;
+      }
     }
+    const bool changed = SC && (sc.cap > 0.f || sc.slopes);
     if constexpr (SC) {
-      if (sc.cap > 0.f || sc.slopes) {
+      if (changed) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            float y = x[j][i] * row_scale;
+            float y = x[j][i] * row_scale[i];
             if (sc.cap > 0.f) y = capped(y, cap, inv_cap);
-            if (sc.slopes) y -= slope * (float)(abs(row_pos - (key0 + j * 8 + 2 * t + i)) - nearest);
+            if (sc.slopes) y -= slope[i] * (float)(abs(row_pos[i] - (key0 + j * 8 + g)) - nearest[i]);
             x[j][i] = y;
           }
       }
     }
-    const float unit_x = SC && (sc.cap > 0.f || sc.slopes) ? 1.f : row_scale;
     const uint32_t ok = valid >> (4 * stage) & 15u;
-    uint32_t hidden = 0u, gone = 0u;               // of the eight: keys that the row does not see, that are not there
+    uint32_t hidden = 0u, gone = 0u;               // of the eight: keys that a row does not see; of the eight whose values this thread takes: keys that are not there
     if (key0 + KEYS - 1 > all_see || key0 + KEYS > k1 || ok != 15u || (SC && key0 < all_from)) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < 4; ++j) {
+        const int key = key0 + j * 8 + g;
+        const bool there = key < k1 && ((ok >> j) & 1u);
+        if (!there) vsc[j] = 0.f;                  // past the end or on a page that does not exist: it may be anything
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int key = key0 + j * 8 + 2 * t + i;
-          const bool there = key < k1 && ((ok >> j) & 1u);
-          if (!there || key > seen.hi || (SC && key < seen.lo)) hidden |= 1u << (2 * j + i);
-          if (!there) {                            // past the end or on a page that does not exist: it may be anything
-            vsc[j][i] = 0.f;
-            gone |= 1u << (2 * j + i);
-          }
+          if (!there || key > seen[i].hi || (SC && key < seen[i].lo)) hidden |= 1u << (2 * j + i);
+          if (key0 + j * 8 + 2 * t + i >= k1 || !((ok >> j) & 1u)) gone |= 1u << (2 * j + i);
         }
+      }
     }
-    const float mb = (m == -INFINITY ? 0.f : m) - lift;                       // scores relative to the maximum, base 2, and the lift
+    // scores relative to the maximum, base 2, and the lift
+    float top[2], mb[2];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int i = 0; i < 2; ++i) {
+      mb[i] = (m[i] == -INFINITY ? 0.f : m[i]) - lift;
+      const float unit_x = changed ? 1.f : row_scale[i];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) x[j][i] = fmaf(x[j][i], unit_x, -mb);
+      for (int j = 0; j < 4; ++j) x[j][i] = fmaf(x[j][i], unit_x, -mb[i]);
+    }
     if (hidden) {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
@@ -282,46 +317,64 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
         for (int i = 0; i < 2; ++i)
           if ((hidden >> (2 * j + i)) & 1u) x[j][i] = -INFINITY;
     }
-    float top = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[1][0], x[1][1])), fmaxf(fmaxf(x[2][0], x[2][1]), fmaxf(x[3][0], x[3][1])));
-    float most = fmaxf(fmaxf(fmaxf(vsc[0][0], vsc[0][1]), fmaxf(vsc[1][0], vsc[1][1])), fmaxf(fmaxf(vsc[2][0], vsc[2][1]), fmaxf(vsc[3][0], vsc[3][1])));
-    if (__any_sync(0xffffffffu, top > 8.f + lift || m == -INFINITY || most > ve)) {
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      const float m_new = fmaxf(m, top + mb);
-      float a = exp2_safe(m, m_new);
-      l *= a;
-      m = m_new;
-      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
-      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));            // the four lanes of a row see all 32 keys
+#pragma unroll
+    for (int i = 0; i < 2; ++i) top[i] = fmaxf(fmaxf(x[0][i], x[1][i]), fmaxf(x[2][i], x[3][i]));
+    float most = fmaxf(fmaxf(vsc[0], vsc[1]), fmaxf(vsc[2], vsc[3]));
+    if (__any_sync(0xffffffffu, fmaxf(top[0], top[1]) > 8.f + lift || fminf(m[0], m[1]) == -INFINITY || most > ve)) {
+      float a[2], shift[2];
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) {                                    // the eight lanes of a pair of rows see all 32 keys
+        top[0] = fmaxf(top[0], __shfl_xor_sync(0xffffffffu, top[0], o));
+        top[1] = fmaxf(top[1], __shfl_xor_sync(0xffffffffu, top[1], o));
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float m_new = fmaxf(m[i], top[i] + mb[i]);
+        a[i] = exp2_safe(m[i], m_new);
+        l[i] *= a[i];
+        m[i] = m_new;
+      }
       if (most > ve) {
         // the next power of two, kept where 2^7 over it is a normal number too
         const int e = min(max((int)((__float_as_uint(most) >> 23) & 0xff) + 1, 14), 254), up = 134 - e, lift_new = min(max(up, -60), 60);
-        const float ve_new = __uint_as_float((uint32_t)e << 23);
-        a *= ve / ve_new;
+        const float ve_new = __uint_as_float((uint32_t)e << 23), more = exp2f((float)lift_new - lift);
+        a[0] *= ve / ve_new;
+        a[1] *= ve / ve_new;
         ve = ve_new;
-        l *= exp2f((float)lift_new - lift);                                 // up - lift_new is at most 60, and so is lift's change a power that fp32 holds
+        l[0] *= more;
+        l[1] *= more;
         lift = (float)lift_new;
-        rest = __uint_as_float((uint32_t)(127 + up - lift_new) << 23);
+        rest = __uint_as_float((uint32_t)(127 + up - lift_new) << 23);      // up - lift_new: 60 at most either way
       }
-      const float a0 = __shfl_sync(0xffffffffu, a, 8 * t), a1 = __shfl_sync(0xffffffffu, a, 8 * t + 4);      // of rows 2 t and 2 t + 1
 #pragma unroll
-      for (int i = 0; i < S::MT; ++i) { acc[i][0] *= a0; acc[i][1] *= a1; acc[i][2] *= a0; acc[i][3] *= a1; }
-      const float shift = mb - ((m == -INFINITY ? 0.f : m) - lift);
+      for (int i = 0; i < S::MT; ++i) { acc[i][0] *= a[0]; acc[i][1] *= a[1]; acc[i][2] *= a[0]; acc[i][3] *= a[1]; }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) { x[j][0] += shift; x[j][1] += shift; }
+      for (int i = 0; i < 2; ++i) {
+        shift[i] = mb[i] - ((m[i] == -INFINITY ? 0.f : m[i]) - lift);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j][i] += shift[i];
+      }
     }
     if (rest != 1.f) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) { vsc[j][0] *= rest; vsc[j][1] *= rest; }
+      for (int j = 0; j < 4; ++j) vsc[j] *= rest;
     }
     // weights: the sum's, and the ones that multiply the values
     uint32_t pf[4], pl[FINE ? 4 : 1];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const float p0 = ap::ex2(x[j][0]), p1 = ap::ex2(x[j][1]);
-      l += p0 + p1;
-      if constexpr (FINE) ap::split(p0 * vsc[j][0], p1 * vsc[j][1], pf[j], pl[j], __half{});
-      else pf[j] = pack_f16(p0 * vsc[j][0], p1 * vsc[j][1]);
+      l[0] += p0;
+      l[1] += p1;
+      if constexpr (FINE) {
+        uint32_t hi, lo;
+        ap::split(p0 * vsc[j], p1 * vsc[j], hi, lo, __half{});
+        pf[j] = transpose(hi);
+        pl[j] = transpose(lo);
+      } else {
+        pf[j] = transpose(pack_f16(p0 * vsc[j], p1 * vsc[j]));
+      }
     }
 
     // values, 16 keys at a time: this thread's four are 2 t, 2 t + 1, 2 t + 8, 2 t + 9, its elements run g of HD / 8
@@ -359,10 +412,14 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
   }
   pf_wait<0>();
 
-  // this warp's rows: accumulators and sums in units of 2^m, sums over the quad
-  l += __shfl_xor_sync(0xffffffffu, l, 1);
-  l += __shfl_xor_sync(0xffffffffu, l, 2);
-  l *= exp2f(-lift);
+  // this warp's rows: accumulators and sums in units of 2^m, sums over the eight lanes of a pair of rows
+  const float down = exp2f(-lift);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], o);
+    l[i] *= down;
+  }
   const float back = ve * 0.0078125f;                                       // the unit of the values' weights
   __syncthreads();                                                          // every warp is done with its ring
   float* sm_acc = reinterpret_cast<float*>(a4_smem);                        // [NW][ROWS][HD]
@@ -372,7 +429,10 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
   for (int i = 0; i < S::MT; ++i)
 #pragma unroll
     for (int c = 0; c < 4; ++c) sm_acc[(warp * ROWS + 2 * t + (c & 1)) * HD + g * (HD / 8) + 2 * i + (c >> 1)] = acc[i][c] * back;
-  if (t == 0) { sm_m[warp * ROWS + g] = m; sm_l[warp * ROWS + g] = l; }
+  if (g == 0) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) { sm_m[warp * ROWS + 2 * t + i] = m[i]; sm_l[warp * ROWS + 2 * t + i] = l[i]; }
+  }
   __syncthreads();
 
   auto place = [&](int r, int& tok, int& hd) {
