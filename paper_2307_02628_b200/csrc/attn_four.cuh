@@ -20,7 +20,10 @@
 namespace sd {
 namespace a4 {
 
-constexpr int NW = 5, THREADS = 32 * NW, ROWS = 8, KEYS = 32, STAGES = 3;
+// Warps of a block: fewer wait for one another where a block begins and ends, more have fewer shares of split keys to join.  Measured, 2, 3 and 5 warps (15 to an SM as
+// the ring of 14.6 KB a warp allows): 64 single tokens at 1280 positions, 32 heads of 128: 98, 96, 102 us; at 640: 59, 60, 67; 3 of 32 heads over 8 at
+// 20 000..65 521: 76, 75, 65; 200 at 100..600: 110, 116, 142.
+constexpr int NW = 3, THREADS = 32 * NW, ROWS = 8, KEYS = 32, STAGES = 3, PER_SM = 5;
 
 template <int HD> struct Shape {
   static constexpr int ROW = HD / 2, PIECES = ROW / 16, SWZ = PIECES - 1;                  // bytes and 16-byte pieces of a key
@@ -28,7 +31,7 @@ template <int HD> struct Shape {
   static constexpr int BLOCKS = HD / kBlock;                                               // block scales of a key, a byte each
   static constexpr int V = KEYS * ROW, SCALES = 2 * V, BLOCK = SCALES + 2 * KEYS * 4, STAGE = BLOCK + 2 * KEYS * BLOCKS;
   static constexpr int MERGE = NW * ROWS * (HD + 2) * 4;
-  static constexpr int SMEM = NW * STAGES * STAGE > MERGE ? NW * STAGES * STAGE : MERGE;   // three blocks of 73 KB to an SM at HD = 128
+  static constexpr int SMEM = NW * STAGES * STAGE > MERGE ? NW * STAGES * STAGE : MERGE;   // five blocks of 44 KB to an SM at HD = 128
 };
 __device__ __forceinline__ int swz(int key) { return key >> 1; }
 
@@ -42,6 +45,11 @@ __device__ __forceinline__ uint32_t transpose(uint32_t pair) {             // 8 
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(pair));
   return r;
 }
+// c = a b
+__device__ __forceinline__ void mma_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
+               : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
 // a byte by its number, as two fp16
 __device__ __forceinline__ uint32_t widen(uint32_t w, int byte) {          // byte is a constant after unrolling
   return byte == 0 ? e2m1_widen<0>(w) : byte == 1 ? e2m1_widen<1>(w) : byte == 2 ? e2m1_widen<2>(w) : e2m1_widen<3>(w);
@@ -51,7 +59,7 @@ __device__ __forceinline__ uint32_t widen(uint32_t w, int byte) {          // by
 
 // Arguments as those of paged_attn_tile_kernel.  FINE: weights of two fp16, and queries of two where they have more bits than one.
 template <int HD, bool FINE, bool SC>
-__global__ void __launch_bounds__(a4::THREADS, 3)
+__global__ void __launch_bounds__(a4::THREADS, a4::PER_SM)
 paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2m1* __restrict__ Kp, const e2m1* __restrict__ Vp, const float* __restrict__ Ksc,
                        const float* __restrict__ Vsc, const uint8_t* __restrict__ Kb, const uint8_t* __restrict__ Vb, int group, float scale_log2, bool q_vec, int tiles_per_seq,
                        int rows_below, int chunk, int slot_rows, float* part_acc, float* part_ml, int* __restrict__ counters, bool early, const Scores sc) {
@@ -76,6 +84,14 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
   const int n_rows = min(ROWS, n_new * group - tile * ROWS);
   if (n_rows <= 0 || n_new * group >= rows_below) return;
   const long long pos_first = (long long)raw_len - (f1 - f0);               // position of the first new token, negative without a place
+  // Token and head (of the group) of the tile's rows: the first one's, and what lies r < 8 rows on, a quotient below 2^17 that fp32 divides rightly.
+  const int token0 = tile * ROWS / group, member0 = tile * ROWS - token0 * group;
+  const float per_group = 1.f / (float)group;
+  auto place = [&](int r, int& tok, int& hd) {
+    const int member = member0 + r, more = (int)(((float)member + 0.5f) * per_group);
+    tok = token0 + more;
+    hd = g_head * group + member - more * group;
+  };
 
   // This thread's two query rows (rows past the tile repeat the last one and are not stored), the keys they see, and those that any and every row of the
   // tile sees.
@@ -86,7 +102,8 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
   int key_begin = 0x7fffffff, key_end = 0, all_from = 0, all_see = 0x7fffffff;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const int row = tile * ROWS + min(2 * t + i, n_rows - 1), token = row / group;
+    int token, head;
+    place(min(2 * t + i, n_rows - 1), token, head);
     const Span v = visible(sc, f0 + token, pos_first + token, len);
     seen[i] = v;
     if (v.lo <= v.hi) key_begin = min(key_begin, v.lo);
@@ -96,7 +113,7 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
     if constexpr (SC) {
       row_pos[i] = (int)min(max(pos_first + token, 0ll), 1ll << 30);
       nearest[i] = abs(row_pos[i] - min(max(row_pos[i], v.lo), v.hi));
-      slope[i] = sc.slopes ? sc.slopes[g_head * group + row % group] * 1.4426950408889634f : 0.f;
+      slope[i] = sc.slopes ? sc.slopes[head] * 1.4426950408889634f : 0.f;
     }
   }
 #pragma unroll
@@ -139,7 +156,8 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
   constexpr int STEPS = KEYS * S::PIECES / 32, STEP_KEYS = 32 / S::PIECES, BP = KEYS * S::BLOCKS / 16, BKEYS = 16 / S::BLOCKS;   // pieces of block scales, keys of one
   const int b_key = (lane % BP) * BKEYS, s_key = (lane & 7) * 4;
   static_assert(STEP_KEYS / 2 % (S::SWZ + 1) == 0, "a lane's pieces are swizzled alike");
-  const e2m1 *k_src = Kp + lane * 16, *v_src = Vp + lane * 16;              // a whole tile inside one page: this lane's sources, of the pool's first key
+  // a whole tile inside one page: this lane's sources, of the pool's first key (a pool has fewer than 2^32 keys)
+  const e2m1 *k_src = Kp + lane * 16, *v_src = Vp + lane * 16;
   const float* s_src = (lane < 8 ? Ksc : Vsc) + s_key;
   const uint8_t* b_src = (lane < BP ? Kb : Vb) + (lane % BP) * 16;
   const uint32_t lane_at = lane_key * S::ROW + ((lane_piece ^ (swz(lane_key) & S::SWZ)) << 4);
@@ -149,15 +167,15 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
     const uint32_t dst = ring + stage * S::STAGE;
     const int page0 = __shfl_sync(0xffffffffu, window, slot);
     if (parts_log == 0 && key0 + KEYS <= k1 && (unsigned)page0 < (unsigned)b.n_pages) {
-      const size_t e = b.entry(page0, g_head, key0);
-      const e2m1 *ks = k_src + e * S::ROW, *vs = v_src + e * S::ROW;
+      const uint32_t e = (((uint32_t)page0 * b.n_kv_heads + g_head) << b.page_shift) + (key0 & (b.page_len - 1));
+      const e2m1 *ks = k_src + (size_t)e * S::ROW, *vs = v_src + (size_t)e * S::ROW;
 #pragma unroll
       for (int i = 0; i < STEPS; ++i) {
         pf_cp16(dst + lane_at + i * 512, ks + i * 512, 16);
         pf_cp16(dst + lane_at + i * 512 + S::V, vs + i * 512, 16);
       }
       if (lane < 16) pf_cp16(dst + S::SCALES + lane * 16, s_src + e, 16);
-      if (lane < 2 * BP) pf_cp16(dst + S::BLOCK + lane * 16, b_src + e * S::BLOCKS, 16);
+      if (lane < 2 * BP) pf_cp16(dst + S::BLOCK + lane * 16, b_src + (size_t)e * S::BLOCKS, 16);
       valid |= 15u << (4 * stage);
       return;
     }
@@ -188,8 +206,9 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
   // the query row is asked for, then the first keys, and both are on their way together
   float q_raw[S::EC];                              // of row g: the products want another division than the softmax
   {
-    const int row = tile * ROWS + min(g, n_rows - 1);
-    ap::load_run<S::EC>(q, (long long)(f0 + row / group) * q.row_stride + (g_head * group + row % group) * q.head_stride + t * S::EC, q_vec, q_raw);
+    int token, head;
+    place(min(g, n_rows - 1), token, head);
+    ap::load_run<S::EC>(q, (long long)(f0 + token) * q.row_stride + head * q.head_stride + t * S::EC, q_vec, q_raw);
   }
   const int mine = tile0 < n_tiles ? (n_tiles - tile0 + NW - 1) / NW : 0;   // this warp's tiles
 #pragma unroll
@@ -232,6 +251,7 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
   const int k_sel = k_blk & 1 ? 0x3232 : 0x1010, v_sel = v_blk & 1 ? 0x0051 : 0x0040;
   static_assert(4 % (S::SWZ + 1) == 0, "keys 8 apart are swizzled alike");
 
+  const int all_end = min(all_see + 1, k1);        // tiles up to here need no mask
   int stage = 0, fill = STAGES - 1;
   for (int n = 0; n < mine; ++n) {
     const int key0 = (tile0 + n * NW) * KEYS;
@@ -256,12 +276,13 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
         unit[r][0] = __byte_perm(u, 0u, HD == 128 ? 0x1010 : k_sel);
         unit[r][1] = __byte_perm(u, 0u, 0x3232);                            // HD = 128
       }
-      float c[4] = {0.f, 0.f, 0.f, 0.f};
+      float c[4];
 #pragma unroll
       for (int k = 0; k < S::KS; ++k) {                                     // two bytes of two keys: four elements of each
         const uint32_t a[4] = {hmul2(widen(w[0][k >> 1], 2 * (k & 1)), unit[0][k >> 2]), hmul2(widen(w[1][k >> 1], 2 * (k & 1)), unit[1][k >> 2]),
                                hmul2(widen(w[0][k >> 1], 2 * (k & 1) + 1), unit[0][k >> 2]), hmul2(widen(w[1][k >> 1], 2 * (k & 1) + 1), unit[1][k >> 2])};
-        ap::mma(c, a, qf[k][0], qf[k][1], __half{});
+        if (k == 0) mma_first(c, a, qf[k][0], qf[k][1]);
+        else ap::mma(c, a, qf[k][0], qf[k][1], __half{});
         if constexpr (FINE) ap::mma(c, a, ql[k][0], ql[k][1], __half{});
       }
 #pragma unroll
@@ -288,7 +309,7 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
     }
     const uint32_t ok = valid >> (4 * stage) & 15u;
     uint32_t hidden = 0u, gone = 0u;               // of the eight: keys that a row does not see; of the eight whose values this thread takes: keys that are not there
-    if (key0 + KEYS - 1 > all_see || key0 + KEYS > k1 || ok != 15u || (SC && key0 < all_from)) {
+    if (key0 + KEYS > all_end || ok != 15u || (SC && key0 < all_from)) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int key = key0 + j * 8 + g;
@@ -422,43 +443,47 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
   }
   const float back = ve * 0.0078125f;                                       // the unit of the values' weights
   __syncthreads();                                                          // every warp is done with its ring
+  auto store4 = [&](int r, int c, float4 a, float L) {
+    int tok, hd;
+    place(r, tok, hd);
+    const long long to = (long long)(f0 + tok) * out.row_stride + hd * out.head_stride + c;
+    store_elem(out, to, normalised(a.x, L));
+    store_elem(out, to + 1, normalised(a.y, L));
+    store_elem(out, to + 2, normalised(a.z, L));
+    store_elem(out, to + 3, normalised(a.w, L));
+  };
   float* sm_acc = reinterpret_cast<float*>(a4_smem);                        // [NW][ROWS][HD]
   float* sm_m = sm_acc + NW * ROWS * HD;                                    // [NW][ROWS]
   float* sm_l = sm_m + NW * ROWS;
 #pragma unroll
-  for (int i = 0; i < S::MT; ++i)
+  for (int i = 0; i < 2; ++i) {
+    if (2 * t + i >= n_rows) continue;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) sm_acc[(warp * ROWS + 2 * t + (c & 1)) * HD + g * (HD / 8) + 2 * i + (c >> 1)] = acc[i][c] * back;
-  if (g == 0) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) { sm_m[warp * ROWS + 2 * t + i] = m[i]; sm_l[warp * ROWS + 2 * t + i] = l[i]; }
+    for (int k = 0; k < S::MT; ++k)
+      *reinterpret_cast<float2*>(sm_acc + (warp * ROWS + 2 * t + i) * HD + g * (HD / 8) + 2 * k) = make_float2(acc[k][i] * back, acc[k][2 + i] * back);
+    if (g == 0) { sm_m[warp * ROWS + 2 * t + i] = m[i]; sm_l[warp * ROWS + 2 * t + i] = l[i]; }
   }
   __syncthreads();
 
-  auto place = [&](int r, int& tok, int& hd) {
-    const int rr = tile * ROWS + r;
-    tok = f0 + rr / group;
-    hd = g_head * group + rr % group;
-  };
-  for (int i = threadIdx.x; i < n_rows * HD; i += THREADS) {
-    const int r = i / HD, c = i % HD;
-    float M = -INFINITY, L = 0.f, a = 0.f;
+  for (int i = threadIdx.x; i < n_rows * (HD / 4); i += THREADS) {          // four columns at a time
+    const int r = i / (HD / 4), c = i % (HD / 4) * 4;
+    float M = -INFINITY, L = 0.f;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int w = 0; w < NW; ++w) M = fmaxf(M, sm_m[w * ROWS + r]);
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
       const float f = exp2_safe(sm_m[w * ROWS + r], M);
+      const float4 v = *reinterpret_cast<const float4*>(sm_acc + (w * ROWS + r) * HD + c);
       L += sm_l[w * ROWS + r] * f;
-      a += sm_acc[(w * ROWS + r) * HD + c] * f;
+      a.x += v.x * f; a.y += v.y * f; a.z += v.z * f; a.w += v.w * f;
     }
-    int tok, hd;
-    place(r, tok, hd);
     if (used_splits == 1) {
-      store_elem(out, (long long)tok * out.row_stride + hd * out.head_stride + c, normalised(a, L));
+      store4(r, c, a, L);
     } else {
       const size_t slot = ((size_t)unit * slot_rows + r) * splits + z;
-      __stcg(part_acc + slot * HD + c, a);
-      if (c == 0) { __stcg(part_ml + slot * 2, M); __stcg(part_ml + slot * 2 + 1, L); }
+      __stcg(reinterpret_cast<float4*>(part_acc + slot * HD + c), a);
+      if (c == 0) __stcg(reinterpret_cast<float2*>(part_ml + slot * 2), make_float2(M, L));
     }
   }
   if (used_splits == 1) return;
@@ -472,19 +497,39 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
   __syncthreads();
   if (!sm_last) return;
   __threadfence();
-  for (int i = threadIdx.x; i < n_rows * HD; i += THREADS) {
-    const int r = i / HD, c = i % HD;
-    int tok, hd;
-    place(r, tok, hd);
+  // The shares are added in split order, sixteen splits' loads on their way together; a warp for each row finds its maximum and sum before.
+  float* sm_M = sm_m;
+  float* sm_L = sm_l;
+  for (int r = warp; r < n_rows; r += NW) {
+    const float2* ml = reinterpret_cast<const float2*>(part_ml) + ((size_t)unit * slot_rows + r) * splits;
+    float M = -INFINITY, L = 0.f;
+    for (int s = lane; s < used_splits; s += 32) {
+      const float2 v = __ldcg(ml + s);
+      const float top = fmaxf(M, v.x);
+      L = L * exp2_safe(M, top) + v.y * exp2_safe(v.x, top);
+      M = top;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const float M2 = __shfl_xor_sync(0xffffffffu, M, o), L2 = __shfl_xor_sync(0xffffffffu, L, o), top = fmaxf(M, M2);
+      L = L * exp2_safe(M, top) + L2 * exp2_safe(M2, top);
+      M = top;
+    }
+    if (lane == 0) { sm_M[r] = M; sm_L[r] = L; }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n_rows * (HD / 4); i += THREADS) {
+    const int r = i / (HD / 4), c = i % (HD / 4) * 4;
     const size_t slot0 = ((size_t)unit * slot_rows + r) * splits;
-    float M = -INFINITY, L = 0.f, a = 0.f;
-    for (int s = 0; s < used_splits; ++s) M = fmaxf(M, __ldcg(part_ml + (slot0 + s) * 2));
+    const float M = sm_M[r];
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 16
     for (int s = 0; s < used_splits; ++s) {
       const float f = exp2_safe(__ldcg(part_ml + (slot0 + s) * 2), M);
-      L += __ldcg(part_ml + (slot0 + s) * 2 + 1) * f;
-      a += __ldcg(part_acc + (slot0 + s) * HD + c) * f;
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(part_acc + (slot0 + s) * HD + c));
+      a.x += v.x * f; a.y += v.y * f; a.z += v.z * f; a.w += v.w * f;
     }
-    store_elem(out, (long long)tok * out.row_stride + hd * out.head_stride + c, normalised(a, L));
+    store4(r, c, a, sm_L[r]);
   }
 }
 

@@ -46,6 +46,7 @@ bool carve_cache(const sd_cache_config& c, sd_cache& A) {
   const int blocks = A.four ? c.head_dim / sd::kBlock : 0;
   const unsigned __int128 per_layer = 2 * entries * (A.row_bytes + (A.scaled ? 4 : 0) + blocks) + 6 * kAlign;
   if (per_layer * c.n_layers > ((unsigned __int128)1 << 61)) return false;
+  if (A.four && entries > 0xffffffffu) return false;            // beyond the device's memory; the kernels number its keys in 32 bits
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes); return o; };
   const size_t values = (size_t)entries * A.row_bytes, scales = A.scaled ? (size_t)entries * 4 : 0;
