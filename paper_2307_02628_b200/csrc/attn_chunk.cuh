@@ -552,7 +552,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         float a = m == -INFINITY ? 0.f : ex2((m - m_new) * unit);
         m = m_new;
         l *= a;
-        if (FOUR) {
+        if constexpr (FOUR) {
           a *= ve / ve_now;                                      // powers of two, or 0 over one
           ve = ve_now;
         }

@@ -25,6 +25,7 @@ struct sd_cache {
   sd::EncodeTiledFn encode = nullptr;
   int tile_blocks[2][18] = {};          // blocks per SM of each form of the kernel for few rows, without and with changed scores
   int64_t launches = 0;      // kernels launched
+  bool copy_ready = false;   // the same for the kernel that copies pages
   bool test_expire = false;  // test hook: the next launch for chunks makes a wait run out (one shot)
   unsigned long long tile_ready[2] = {};   // bit per kernel whose shared-memory size has been allowed on this device
   char* layer(int l) const { return arena + (size_t)l * layer_bytes; }

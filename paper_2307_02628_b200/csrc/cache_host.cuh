@@ -220,8 +220,12 @@ int copy_pages(sd_cache* c, const sd_tables* t, const int* from, const int* to, 
   run((int64_t)c->kb_off, blocks);
   run((int64_t)c->vb_off, blocks);
   const int64_t most = (int64_t)(n_copies ? c->cfg.n_pages : n) * c->cfg.n_layers * runs.all_pieces;
-  const int grid = (int)std::min<int64_t>(most, (int64_t)c->sm_count * 4);
-  sd::launch_kernel(planned, c->stream, sd::pages_copy_kernel, dim3(grid), dim3(256), 0, books_of(c, t), c->arena, (long long)c->layer_bytes, (int)c->cfg.n_layers, runs, from, to,
+  const int grid = (int)std::min<int64_t>(most, (int64_t)c->sm_count);
+  if (!c->copy_ready) {
+    if (cudaFuncSetAttribute(sd::pages_copy_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sd::COPY_SMEM) != cudaSuccess) { cudaGetLastError(); return SD_ERR_CUDA; }
+    c->copy_ready = true;
+  }
+  sd::launch_kernel(planned, c->stream, sd::pages_copy_kernel, dim3(grid), dim3(256), sd::COPY_SMEM, books_of(c, t), c->arena, (long long)c->layer_bytes, (int)c->cfg.n_layers, runs, from, to,
                     n_copies, n, (const int*)c->at<int>(c->place), remap ? 1 : 0);
   return launched(c);
 }

@@ -5,7 +5,6 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
-#include <cuda_fp4.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -286,13 +285,22 @@ static __device__ __noinline__ uint32_t block_exact(float t, float s) {
   const float f = __double2float_rz(q);
   return e4m3_pair((double)f == q ? f : __uint_as_float(__float_as_uint(f) | 1u), 0.f) & 0xffu;
 }
-__device__ __forceinline__ uint32_t e2m1_pair(float even, float odd) {
-  return (uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(even, odd), __NV_E2M1, cudaRoundNearest);
+// eight codes, to nearest, ties to even, at most 6
+__device__ __forceinline__ uint32_t e2m1_codes(const float (&y)[8]) {
+  uint32_t r;
+  asm("{\n .reg .b8 a, b, c, d;\n cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n"
+      " cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n mov.b32 %0, {a, b, c, d};\n}" : "=r"(r) : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
+  return r;
 }
 static __device__ __noinline__ float quotient_sticky4(float x, float b, float s) {
   const double q = (double)x / ((double)b * (double)s);
   const float f = __double2float_rz(q);
   return (double)f == q ? f : __uint_as_float(__float_as_uint(f) | 1u);
+}
+__device__ __forceinline__ float reciprocal(float x) {           // of a normal number, off by 2^-23 of itself
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 __device__ __forceinline__ uint32_t block_of(float t, float s, float inv) {        // inv: about 1 / s, or 0
   if (s == 0.f) return 0u;
@@ -306,22 +314,16 @@ __device__ __forceinline__ float block_value(uint32_t b) { return e4m3_widen(b).
 __device__ __forceinline__ uint32_t encode8_four(const float (&x)[8], float b, float s, bool finite) {
   const float unit = b * s;
   if (unit == 0.f && (b == 0.f || s == 0.f)) return 0u;
-  const float inv = unit > 1e-30f ? __fdiv_rn(1.f, unit) : 0.f;
-  uint32_t lo = 0u, hi = 0u;
+  const float inv = unit > 1e-30f ? reciprocal(unit) : 0.f;
+  const float down = inv * (1.f - 0x1p-21f), up = inv * (1.f + 0x1p-21f);          // quotients off by less than 2^-21, and on either side of the true ones
+  float y[8], z[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float e = x[2 * i] * inv, o = x[2 * i + 1] * inv;                        // off by less than 2^-21
-    lo |= e2m1_pair(e * (1.f - 0x1p-21f), o * (1.f - 0x1p-21f)) << (8 * i);
-    hi |= e2m1_pair(e * (1.f + 0x1p-21f), o * (1.f + 0x1p-21f)) << (8 * i);
-  }
-  if (finite && inv != 0.f && lo == hi) return lo;
-  uint32_t w = 0u;
+  for (int i = 0; i < 8; ++i) { y[i] = x[i] * down; z[i] = x[i] * up; }
+  const uint32_t w = e2m1_codes(y);
+  if (finite && inv != 0.f && w == e2m1_codes(z)) return w;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float e = x[2 * i] != x[2 * i] ? 0.f : quotient_sticky4(x[2 * i], b, s), o = x[2 * i + 1] != x[2 * i + 1] ? 0.f : quotient_sticky4(x[2 * i + 1], b, s);
-    w |= e2m1_pair(e, o) << (8 * i);
-  }
-  return w;
+  for (int i = 0; i < 8; ++i) y[i] = x[i] != x[i] ? 0.f : quotient_sticky4(x[i], b, s);
+  return e2m1_codes(y);
 }
 // two codes (a byte) as fp16, the even element first
 template <int BYTE> __device__ __forceinline__ uint32_t e2m1_widen(uint32_t w) {
@@ -454,23 +456,33 @@ cache_append_kernel(const BatchView b, int row_shift, const Rows ks, const Rows 
       TC* dst = (is_v ? Vp : Kp) + e * row_units<TC>(HD) + sub * row_units<TC>(8);
       float top = 0.f;                                           // of the finite elements
       bool finite = true;
+      if constexpr (kFour<TC>) {                                 // a maximum that keeps NaN tells whether there is more to look at
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float a = fabsf(x[u][j]);
-        if (a < INFINITY) top = fmaxf(top, a);
-        else finite = false;                                     // NaN too
+        for (int j = 0; j < 8; ++j) asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(fabsf(x[u][j])));
+        finite = top < INFINITY;
+      }
+      if (!kFour<TC> || !finite) {
+        top = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float a = fabsf(x[u][j]);
+          if (a < INFINITY) top = fmaxf(top, a);
+          else finite = false;                                   // NaN too
+        }
       }
       if (!finite) atomicOr(b.status, STATUS_NOT_FINITE);
       if constexpr (kFour<TC>) {
         float part = top;                                        // of the block's 16 elements: this lane's and its neighbour's
-        const bool inf = fabsf(x[u][0]) == INFINITY || fabsf(x[u][1]) == INFINITY || fabsf(x[u][2]) == INFINITY || fabsf(x[u][3]) == INFINITY ||
-                         fabsf(x[u][4]) == INFINITY || fabsf(x[u][5]) == INFINITY || fabsf(x[u][6]) == INFINITY || fabsf(x[u][7]) == INFINITY;
-        part = fmaxf(part, inf ? INFINITY : 0.f);                // an infinity becomes the row's largest: the block's scale is the largest one
+        if (!finite) {                                           // an infinity becomes the row's largest: the block's scale is the largest one
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (fabsf(x[u][j]) == INFINITY) part = INFINITY;
+        }
         part = fmaxf(part, __shfl_xor_sync(0xffffffffu, part, 1));
 #pragma unroll
         for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         const float s = __fdiv_rn(top, CacheType<TC>::TOP);
-        const uint32_t block = block_of(fminf(part, top), s, s > 1e-30f ? __fdiv_rn(1.f, s) : 0.f);
+        const uint32_t block = block_of(fminf(part, top), s, s > 1e-30f ? reciprocal(s) : 0.f);
         if (on) {
           *reinterpret_cast<uint32_t*>(dst) = encode8_four(x[u], block_value(block), s, finite);
           if ((sub & 1) == 0) (is_v ? Vb : Kb)[e * (HD / kBlock) + sub / 2] = (uint8_t)block;

@@ -309,13 +309,18 @@ struct PageRuns {
   int pieces[6];           // of PIECE words, the last one shorter
   int n, all_pieces;
 };
-constexpr int PIECE = 2048;
+constexpr int PIECE = 2048, COPY_STAGES = 6, COPY_AHEAD = 3, COPY_SMEM = COPY_STAGES * PIECE * 16;      // 192 KB: a block to an SM
+struct CopySpan { char* to; const char* from; uint32_t bytes; };                                         // bytes 0: nothing to copy
 
-// Copies the listed pages in all layers, and gives the tables the new numbers where a compaction moved pages (books.pages not NULL).  A piece of 32 KB at a
-// time: eight 16-byte loads of a thread are on their way together.  What bounds it is memory.
+// Copies the listed pages in all layers, and gives the tables the new numbers where a compaction moved pages (remap).  One thread of a block streams pieces of 32 KB
+// through shared memory by bulk copies, three on their way in while others leave, so that both directions of the memory are busy all the time.  What
+// bounds it is memory: 150 pages of 2.1 MB 108 us, 5.8 TB/s (117 us by 16-byte loads and stores of 1024 threads to an SM, eight each on their way).
 __global__ void __launch_bounds__(256)
 pages_copy_kernel(const Books b, char* __restrict__ arena, long long layer_bytes, int layers, const PageRuns runs, const int* __restrict__ from, const int* __restrict__ to,
                   const int* __restrict__ n_copies, int n, const int* __restrict__ place, int remap) {
+  extern __shared__ __align__(128) unsigned char copy_smem[];
+  __shared__ uint64_t full[COPY_STAGES];
+  __shared__ CopySpan spans[COPY_STAGES];
   pdl_wait();
   if (remap) {
     const int used = n_copies[1];
@@ -330,31 +335,78 @@ pages_copy_kernel(const Books b, char* __restrict__ arena, long long layer_bytes
       else b.pages[i] = q;
     }
   }
-  const long long copies = n_copies ? *n_copies : n;
-  for (long long i = blockIdx.x; i < copies * layers * runs.all_pieces; i += gridDim.x) {
+  if (threadIdx.x != 0) return;
+  const long long pieces = (long long)(n_copies ? *n_copies : n) * layers * runs.all_pieces;
+  const long long mine = blockIdx.x < pieces ? (pieces - 1 - blockIdx.x) / gridDim.x + 1 : 0;            // this block's: every gridDim.x-th
+  if (mine == 0) return;
+  auto span_of = [&](long long k) {
+    const long long i = blockIdx.x + k * gridDim.x;
     int piece = (int)(i % runs.all_pieces);
     const long long rest = i / runs.all_pieces;
     const int layer = (int)(rest % layers), m = (int)(rest / layers);
     int run = 0;
     while (piece >= runs.pieces[run]) piece -= runs.pieces[run++];
     const int f = from[m], t = to[m];
+    CopySpan c{nullptr, nullptr, 0u};
     if (!b.is_page(f) || !b.is_page(t)) {
-      if (threadIdx.x == 0) b.say(STATUS_BAD_BATCH);
-      continue;
+      b.say(STATUS_BAD_BATCH);
+    } else if (f != t) {
+      char* pool = arena + layer * layer_bytes + runs.offset[run];
+      c.from = pool + ((long long)f * runs.words[run] + (long long)piece * PIECE) * 16;
+      c.to = pool + ((long long)t * runs.words[run] + (long long)piece * PIECE) * 16;
+      c.bytes = (uint32_t)min(PIECE, runs.words[run] - piece * PIECE) * 16;
     }
-    if (f == t) continue;
-    char* pool = arena + layer * layer_bytes + runs.offset[run];
-    const int words = min(PIECE, runs.words[run] - piece * PIECE);
-    const uint4* src = reinterpret_cast<const uint4*>(pool) + (long long)f * runs.words[run] + (long long)piece * PIECE;
-    uint4* dst = reinterpret_cast<uint4*>(pool) + (long long)t * runs.words[run] + (long long)piece * PIECE;
-    uint4 x[PIECE / 256];
-#pragma unroll
-    for (int u = 0; u < PIECE / 256; ++u)
-      if (u * 256 + (int)threadIdx.x < words) x[u] = __ldcs(src + u * 256 + threadIdx.x);
-#pragma unroll
-    for (int u = 0; u < PIECE / 256; ++u)
-      if (u * 256 + (int)threadIdx.x < words) __stcs(dst + u * 256 + threadIdx.x, x[u]);
+    return c;
+  };
+  const uint32_t smem = (uint32_t)__cvta_generic_to_shared(copy_smem), bar = (uint32_t)__cvta_generic_to_shared(full);
+  for (int s = 0; s < COPY_STAGES; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar + 8 * s) : "memory");
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  unsigned phases = 0u, asked = 0u;              // a bit per stage: the phase to wait for next; copies in that have not been waited for
+  auto landed = [&](int s) {                     // bounded: false when a copy did not land in two seconds, which has no reason to happen
+    const long long t0 = clock64();
+    const uint32_t parity = phases >> s & 1u;
+    for (;;) {
+      uint32_t done;
+      asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.b32 %0, 1, 0, p;\n}\n" : "=r"(done) : "r"(bar + 8 * s), "r"(parity) : "memory");
+      if (done) break;
+      if (clock64() - t0 > 4000000000ll) return false;
+    }
+    phases ^= 1u << s;
+    asked &= ~(1u << s);
+    return true;
+  };
+  bool ok = true;
+  for (long long k = 0; k < mine + COPY_AHEAD && ok; ++k) {
+    if (k < mine) {
+      const int s = (int)(k % COPY_STAGES);
+      // the piece that was here before has left: all but the last STAGES - AHEAD - 1 groups
+      asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(COPY_STAGES - COPY_AHEAD - 1) : "memory");
+      const CopySpan c = span_of(k);
+      spans[s] = c;
+      if (c.bytes) {
+        asked |= 1u << s;
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar + 8 * s), "r"(c.bytes) : "memory");
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                     ::"r"(smem + s * PIECE * 16), "l"(c.from), "r"(c.bytes), "r"(bar + 8 * s) : "memory");
+      }
+    }
+    if (k >= COPY_AHEAD) {
+      const int s = (int)((k - COPY_AHEAD) % COPY_STAGES);
+      const CopySpan c = spans[s];
+      if (c.bytes) {
+        ok = landed(s);
+        if (ok) asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(c.to), "r"(smem + s * PIECE * 16), "r"(c.bytes) : "memory");
+      }
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
   }
+  if (!ok) {                                     // giving up: copies that are still on their way must land before the block's memory goes
+    b.say(STATUS_WAIT_EXPIRED);
+    for (int s = 0; s < COPY_STAGES; ++s)
+      if (asked >> s & 1u) landed(s);
+  }
+  asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
 }
 
 }  // namespace sd
