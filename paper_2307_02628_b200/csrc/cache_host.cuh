@@ -201,6 +201,9 @@ sd::PageWork page_work(const sd_cache* c) {
   return sd::PageWork{c->at<int4>(c->plan), c->at<int>(c->claim), c->at<int>(c->copy_from), c->at<int>(c->copy_to), c->at<int>(c->place), c->at<int>(c->totals)};
 }
 
+// Whether a small block is enough for the books: a round of its threads for the rows, a few for the pages.
+bool little(const sd_cache* c, const sd_tables* t) { return t->n_seqs <= sd::pg::SMALL && c->cfg.n_pages <= 4 * sd::pg::SPAN<sd::pg::SMALL>; }
+
 // The second launch of a call on pages.  n_copies NULL: n copies of the caller's lists.  planned: behind a first launch, beside whose end it may begin.
 int copy_pages(sd_cache* c, const sd_tables* t, const int* from, const int* to, const int* n_copies, int n, bool remap, bool planned) {
   sd::PageRuns runs = {};
@@ -357,7 +360,8 @@ int sd_cache_fork(sd_cache* c, const sd_tables* t, const int32_t* src, const int
   if (!guard.ok) return SD_ERR_CUDA;
   std::lock_guard<std::mutex> lock(c->busy);
   const sd::PageWork w = page_work(c);
-  sd::pages_fork_kernel<<<1, sd::pg::THREADS, 0, c->stream>>>(books_of(c, t), src, dst, n, w);
+  if (little(c, t)) sd::pages_fork_kernel<sd::pg::SMALL><<<1, sd::pg::SMALL, 0, c->stream>>>(books_of(c, t), src, dst, n, w);
+  else sd::pages_fork_kernel<sd::pg::LARGE><<<1, sd::pg::LARGE, 0, c->stream>>>(books_of(c, t), src, dst, n, w);
   const int err = launched(c);
   return err != SD_OK ? err : copy_pages(c, t, w.from, w.to, w.totals, 0, false, true);
 }
@@ -370,7 +374,8 @@ int sd_cache_resize(sd_cache* c, const sd_tables* t, const int32_t* len) {
   if (!guard.ok) return SD_ERR_CUDA;
   std::lock_guard<std::mutex> lock(c->busy);
   const sd::PageWork w = page_work(c);
-  sd::pages_resize_kernel<<<1, sd::pg::THREADS, 0, c->stream>>>(books_of(c, t), len, w);
+  if (little(c, t)) sd::pages_resize_kernel<sd::pg::SMALL><<<1, sd::pg::SMALL, 0, c->stream>>>(books_of(c, t), len, w);
+  else sd::pages_resize_kernel<sd::pg::LARGE><<<1, sd::pg::LARGE, 0, c->stream>>>(books_of(c, t), len, w);
   const int err = launched(c);
   return err != SD_OK ? err : copy_pages(c, t, w.from, w.to, w.totals, 0, false, true);
 }
@@ -383,7 +388,8 @@ int sd_cache_compact(sd_cache* c, const sd_tables* t, int32_t* n_used) {
   if (!guard.ok) return SD_ERR_CUDA;
   std::lock_guard<std::mutex> lock(c->busy);
   const sd::PageWork w = page_work(c);
-  sd::pages_compact_kernel<<<1, sd::pg::THREADS, 0, c->stream>>>(books_of(c, t), n_used, w);
+  if (little(c, t)) sd::pages_compact_kernel<sd::pg::SMALL><<<1, sd::pg::SMALL, 0, c->stream>>>(books_of(c, t), n_used, w);
+  else sd::pages_compact_kernel<sd::pg::LARGE><<<1, sd::pg::LARGE, 0, c->stream>>>(books_of(c, t), n_used, w);
   const int err = launched(c);
   return err != SD_OK ? err : copy_pages(c, t, w.from, w.to, w.totals, 0, true, true);
 }
