@@ -156,7 +156,8 @@ __device__ __forceinline__ uint32_t columns(int right, int left) {
 // Four bits to the four bytes of a word.
 __device__ __forceinline__ uint32_t bytes_of(uint32_t four) { return (((four & 15u) * 0x00204081u) & 0x01010101u) * 0xffu; }
 
-// as TANH0.. of paged.cuh, of degree 4 for [0, 0.7]
+// as TANH0.. of paged.cuh, of degree 3 for [0, 0.45] (3e-7 of the score) and of degree 4 for [0, 0.7]
+constexpr float CLOSE0 = 0x1.fffff8p-1f, CLOSE1 = -0x1.554b32p-2f, CLOSE2 = 0x1.0f14b2p-3f, CLOSE3 = -0x1.79101ep-5f;
 constexpr float NEAR0 = 0x1.fffff6p-1f, NEAR1 = -0x1.554d28p-2f, NEAR2 = 0x1.0fff48p-3f, NEAR3 = -0x1.a07350p-5f, NEAR4 = 0x1.c35640p-7f;
 // A half's 64 scores of a row, in place, to base-2 units: scale (8 and 4 bits: done), cap, distance.  pos: the row's position, counted from the first
 // column; ahead: there may be visible keys behind the row's position.
@@ -175,28 +176,32 @@ __device__ __forceinline__ void change_scores(uint32_t (&s)[2][32], float scale,
 #pragma unroll
     for (int k = 0; k < 64; k += 2) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(s[k >> 5][k & 31])), fabsf(__uint_as_float(s[k >> 5][(k & 31) + 1]))));
     const float to_u = SCALED ? inv_cap : scale * inv_cap;
-    const F2 to_u2 = f2(to_u, to_u);
     top = top * (SCALED ? 1.f : scale) * inv_cap;
-    if (!(to_u < 1e38f)) top = INFINITY;                             // queries beyond 10^30 and a cap below 10^-8, say
-    if (!__any_sync(0xffffffffu, top > 0.7f)) {                      // the polynomial of [0, 0.7]: 3e-7 of the score
-      const F2 c0 = f2(cap * NEAR0, cap * NEAR0), c1 = f2(cap * NEAR1, cap * NEAR1), c2 = f2(cap * NEAR2, cap * NEAR2), c3 = f2(cap * NEAR3, cap * NEAR3), c4 = f2(cap * NEAR4, cap * NEAR4);
+    // y = x (C0 + C1 x^2 + ..) with the cap and the unit within the numbers: five instructions a pair up to 0.45 of the cap, six up to 0.7, eight up to it
+    const float k2 = to_u * to_u, first = cap * to_u;
+    const bool fits = to_u > 0x1p-8f && to_u < 0x1p8f && first > 0x1p-19f && first < 0x1p19f;      // first to_u^12 is a normal number
+    auto polynomial = [&](auto... terms) {                           // the highest first
+      constexpr int N = sizeof...(terms);
+      const float number[N] = {terms...};
+      F2 c[N];
+      float power = first;
+#pragma unroll
+      for (int i = N - 1; i >= 0; --i) { c[i] = f2(number[i] * power, number[i] * power); power *= k2; }
 #pragma unroll
       for (int k = 0; k < 32; ++k) {
-        const F2 u = mul2(get(k), to_u2), v = mul2(u, u);
-        put(k, mul2(u, fma2(v, fma2(v, fma2(v, fma2(v, c4, c3), c2), c1), c0)));
-      }
-    } else if (!__any_sync(0xffffffffu, top > 1.f)) {
+        const F2 x = get(k), v = mul2(x, x);
+        F2 p = c[0];
 #pragma unroll
-      for (int k = 0; k < 32; ++k) {
-        const F2 u = mul2(get(k), to_u2), v = mul2(u, u);
-        F2 p = fma2(v, f2(TANH6, TANH6), f2(TANH5, TANH5));
-        p = fma2(v, p, f2(TANH4, TANH4));
-        p = fma2(v, p, f2(TANH3, TANH3));
-        p = fma2(v, p, f2(TANH2, TANH2));
-        p = fma2(v, p, f2(TANH1, TANH1));
-        p = fma2(v, p, f2(TANH0, TANH0));
-        put(k, mul2(mul2(u, f2(cap, cap)), p));
+        for (int i = 1; i < N; ++i) p = fma2(v, p, c[i]);
+        put(k, mul2(x, p));
       }
+    };
+    if (fits && !__any_sync(0xffffffffu, top > 0.45f)) {
+      polynomial(CLOSE3, CLOSE2, CLOSE1, CLOSE0);
+    } else if (fits && !__any_sync(0xffffffffu, top > 0.7f)) {
+      polynomial(NEAR4, NEAR3, NEAR2, NEAR1, NEAR0);
+    } else if (fits && !__any_sync(0xffffffffu, top > 1.f)) {
+      polynomial(TANH6, TANH5, TANH4, TANH3, TANH2, TANH1, TANH0);
     } else {                                                       // 1 - 2 / (1 + e^(2 u)): off by 2^-21 of the cap at most, small scores too
       const float to_e = inv_cap * 2.8853901f, twice = -2.f * cap;
 #pragma unroll
@@ -211,13 +216,15 @@ __device__ __forceinline__ void change_scores(uint32_t (&s)[2][32], float scale,
   if (slope_on) {
     if (!ahead || __all_sync(0xffffffffu, pos >= 63)) {            // -slope (pos - c - nearest) = slope c + begin
       const float begin = -slope * (float)(pos - nearest);
-      const F2 slope2 = f2(slope, slope), begin2 = f2(begin, begin), two = f2(2.f, 2.f);
-      F2 c = f2(0.f, 1.f);
+      const F2 slope2 = f2(slope, slope), begin2 = f2(begin, begin), step = f2(2.f * slope, 2.f * slope);
 #pragma unroll
-      for (int k = 0; k < 32; ++k) {
-        const F2 y = SCALED || cap_on ? add2(get(k), begin2) : fma2(get(k), scale2, begin2);
-        put(k, fma2(c, slope2, y));
-        c = add2(c, two);
+      for (int k8 = 0; k8 < 4; ++k8) {                               // a product for every eighth pair, sums between: as exact as a product for each
+        F2 bias = fma2(f2(16.f * k8, 16.f * k8 + 1.f), slope2, begin2);
+#pragma unroll
+        for (int k = 8 * k8; k < 8 * k8 + 8; ++k) {
+          put(k, SCALED || cap_on ? add2(get(k), bias) : fma2(get(k), scale2, bias));
+          bias = add2(bias, step);
+        }
       }
     } else {
 #pragma unroll
