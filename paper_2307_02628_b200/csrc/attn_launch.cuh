@@ -106,7 +106,7 @@ int pick_split(long slots, long units, long rows, int64_t max_len) {
 // the rounding of the first key to a tile.
 int most_keys(const sd_cache* c, const sd_batch* b, const sd::Scores& sc, int rows) {
   const int64_t len = b->max_len > 0 ? b->max_len : (int64_t)b->pages_per_seq * c->cfg.page_len;
-  return (int)(sc.window > 0 ? std::min(len, (int64_t)sc.window + rows + 128) : len);
+  return (int)(sc.window > 0 && !sc.hi ? std::min(len, (int64_t)sc.window + rows + 128) : len);
 }
 
 // Sequences of rows_below query rows per key head or more are left out (another kernel takes them).

@@ -125,6 +125,15 @@ def test_borders_of_windows(cache_dtype, window):
     run(cache_dtype, 4, 1, 128, 8, [130, 1], [131, 500], seed=window % 1000, window=window, slopes=alibi(4))
 
 
+@pytest.mark.parametrize("cache_dtype", ["bf16", "int8", "e2m1"])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_windows_whose_rows_see_far_ahead(cache_dtype, hd):
+    # many more keys than the window holds: they are split all the same, and none is left out
+    for window in (1, 64):
+        run(cache_dtype, 1, 1, hd, 16, [1500], [3000], seed=hd, window=window, hi=prefix(3000))
+        run(cache_dtype, 2, 1, hd, 64, [20, 2], [2500, 1999], seed=hd, window=window, hi=prefix(2500), slopes=alibi(2) / 16)
+
+
 @pytest.mark.parametrize("cache_dtype", ["bf16", "e2m1"])
 def test_blocks_whose_tiles_see_different_keys(cache_dtype):
     # the first tile of 128 rows sees many keys, the second few or none, and the other way round
