@@ -374,7 +374,8 @@ typedef struct {
                                 its last position (hi >= p: a prefix that all of its rows see whole; lo: documents packed into one sequence) */
 } sd_scores;
 
-/* sd_cache_attention with changed scores and masks, rounded as documented there (a score's change in fp32, the cap to 2e-7 of the score).  Reads only the
+/* sd_cache_attention with changed scores and masks, rounded as documented there (a score's change in fp32: where all scores that are computed together stay
+ * below the cap it is off by 3e-7 of the score, else by 2^-21 of the cap).  Reads only the
  * keys between the first and the last that some row of a tile of rows sees. */
 int sd_cache_attention_scores(sd_cache *c, int layer, const sd_batch *batch, const sd_heads *q, float scale, const sd_scores *scores,
                               const sd_heads *out);

@@ -177,9 +177,16 @@ __device__ __forceinline__ void change_scores(uint32_t (&s)[2][32], float scale,
     for (int k = 0; k < 64; k += 2) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(s[k >> 5][k & 31])), fabsf(__uint_as_float(s[k >> 5][(k & 31) + 1]))));
     const float to_u = SCALED ? inv_cap : scale * inv_cap;
     top = top * (SCALED ? 1.f : scale) * inv_cap;
-    // y = x (C0 + C1 x^2 + ..) with the cap and the unit within the numbers: five instructions a pair up to 0.45 of the cap, six up to 0.7, eight up to it
-    const float k2 = to_u * to_u, first = cap * to_u;
-    const bool fits = to_u > 0x1p-8f && to_u < 0x1p8f && first > 0x1p-19f && first < 0x1p19f;      // first to_u^12 is a normal number
+    // y = x (C0 + C1 x^2 + ..) with the cap and the unit within the numbers: five instructions a pair up to 0.45 of the cap, six up to 0.7.  Where
+    // the numbers would leave fp32's range, and up to the cap, u is a product of its own: nine.
+    const float k2 = to_u * to_u, first = SCALED ? 1.f : scale;
+    // Which form it is goes by the whole warp: the unit may be a row's own (4 bits), so it is part of the votes, which all lanes take.
+    const bool near_one = first > 0x1p-19f && first < 0x1p19f;
+    const bool linear = !__any_sync(0xffffffffu, top > 0x1p-12f);    // a third of the square is below a rounding
+    const bool close = !__any_sync(0xffffffffu, !(top <= 0.45f && near_one && to_u > 0x1p-15f && to_u < 0x1p15f));
+    const bool near = !__any_sync(0xffffffffu, !(top <= 0.7f && near_one && to_u > 0x1p-12f && to_u < 0x1p12f));
+    const bool below = !__any_sync(0xffffffffu, !(top <= 1.f && to_u < 1e38f));
+    const F2 to_u2 = f2(to_u, to_u), cap2 = f2(cap, cap);
     auto polynomial = [&](auto... terms) {                           // the highest first
       constexpr int N = sizeof...(terms);
       const float number[N] = {terms...};
@@ -196,12 +203,25 @@ __device__ __forceinline__ void change_scores(uint32_t (&s)[2][32], float scale,
         put(k, mul2(x, p));
       }
     };
-    if (fits && !__any_sync(0xffffffffu, top > 0.45f)) {
+    if (linear) {
+#pragma unroll
+      for (int k = 0; k < 32; ++k) put(k, mul2(get(k), f2(first, first)));
+    } else if (close) {
       polynomial(CLOSE3, CLOSE2, CLOSE1, CLOSE0);
-    } else if (fits && !__any_sync(0xffffffffu, top > 0.7f)) {
+    } else if (near) {
       polynomial(NEAR4, NEAR3, NEAR2, NEAR1, NEAR0);
-    } else if (fits && !__any_sync(0xffffffffu, top > 1.f)) {
-      polynomial(TANH6, TANH5, TANH4, TANH3, TANH2, TANH1, TANH0);
+    } else if (below) {
+#pragma unroll
+      for (int k = 0; k < 32; ++k) {
+        const F2 u = mul2(get(k), to_u2), v = mul2(u, u);
+        F2 p = fma2(v, f2(TANH6, TANH6), f2(TANH5, TANH5));
+        p = fma2(v, p, f2(TANH4, TANH4));
+        p = fma2(v, p, f2(TANH3, TANH3));
+        p = fma2(v, p, f2(TANH2, TANH2));
+        p = fma2(v, p, f2(TANH1, TANH1));
+        p = fma2(v, p, f2(TANH0, TANH0));
+        put(k, mul2(mul2(u, cap2), p));
+      }
     } else {                                                       // 1 - 2 / (1 + e^(2 u)): off by 2^-21 of the cap at most, small scores too
       const float to_e = inv_cap * 2.8853901f, twice = -2.f * cap;
 #pragma unroll

@@ -1,8 +1,8 @@
 """Attention over a paged cache with capped, biased and masked scores in plain 64-bit form, and how far the kernels may be off.
 
-The limits are those of paged_bounds, over the keys that a row sees.  Beside them a score may be off by cap 2^-21 where it is capped (the polynomial by 1.6e-7
-of the score, beyond the cap two approximations of 2^-22 in a term of at most 0.42 of it), and by 2^-22 of its bias, a product and a sum in fp32: a sum
-over keys weighted by their bias.
+The limits are those of paged_bounds, over the keys that a row sees.  Beside them a score may be off by 2^-21 of the cap, or of the largest score of the
+call where that is less (a polynomial to 3e-7 of the score up to the cap; beyond it two approximations of 2^-22 in a term of at most 0.42 of the cap),
+and by 2^-22 of its bias, a product and a sum in fp32: a sum over keys weighted by their bias.
 """
 from __future__ import annotations
 
@@ -28,9 +28,10 @@ def visible(layout, s, window=0, lo=None, hi=None):
 
 
 def reference(q, contents, layout, scale, group, exists=None, cap=0.0, slopes=None, window=0, lo=None, hi=None):
-    """(out, R, terms, Rb): as paged_bounds.reference, and R with every key's weight times its bias."""
+    """(out, R, terms, Rb, most): as paged_bounds.reference, R with every key's weight times its bias, the largest visible score before the cap."""
     out = torch.zeros(q.shape, dtype=torch.float64)
     R, terms, Rb = (torch.zeros(q.shape[:2], dtype=torch.float64) for _ in range(3))
+    largest = 0.0
     for s, (n, length) in enumerate(zip(layout.new, layout.length)):
         skip = max(0, n - length)                               # rows without a place
         if n == skip:
@@ -42,6 +43,7 @@ def reference(q, contents, layout, scale, group, exists=None, cap=0.0, slopes=No
         if exists is not None:
             seen = seen & exists[s]
         x = torch.einsum("rkgd,kjd->rkgj", qs, k) * scale
+        largest = max(largest, float(x.abs().max()))
         if cap:
             x = cap * torch.tanh(x / cap)
         far = torch.zeros_like(x)
@@ -56,10 +58,10 @@ def reference(q, contents, layout, scale, group, exists=None, cap=0.0, slopes=No
         most = (torch.einsum("rkgd,kjd->rkgj", qs.abs(), k.abs()) * abs(scale)).masked_fill(~seen[:, None, None], 0.0).amax(-1)
         out[r], R[r], terms[r] = o.flatten(1, 2), size(w).sqrt().flatten(1), most.flatten(1)
         Rb[r] = size(w * far.abs()).sqrt().flatten(1)
-    return out, R, terms, Rb
+    return out, R, terms, Rb, largest
 
 
-def over(got, want, R, terms, Rb, hd, q_dtype, cap=0.0):
+def over(got, want, R, terms, Rb, largest, hd, q_dtype, cap=0.0):
     """Error of each row and head over its limit."""
-    lim = B.limit(want, R, terms, *B.rels(hd, q_dtype, got.dtype), got.dtype) + 1.25 * (R * cap * 2.0 ** -21 + Rb * 2.0 ** -22)
+    lim = B.limit(want, R, terms, *B.rels(hd, q_dtype, got.dtype), got.dtype) + 1.25 * (R * min(cap, largest) * 2.0 ** -21 + Rb * 2.0 ** -22)
     return (got.double() - want).norm(dim=-1) / lim

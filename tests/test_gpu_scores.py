@@ -158,6 +158,16 @@ def test_caps_from_tiny_to_large(cache_dtype):
 
 
 @pytest.mark.parametrize("cache_dtype", CACHES)
+@pytest.mark.parametrize("io", ["bf16", "fp16"])
+def test_caps_against_scores_of_every_size(cache_dtype, io):
+    # scores below a thousandth of the cap, around 0.3, 0.6 and 0.9 of it, and beyond; keys and queries far from 1, so that the unit of a product is too
+    for q_gain, k_gain, scale in ((1.0, 1.0, 0.125), (1e3, 1e3, 1e-7), (1e-3, 1e-3, 1e5)):
+        size = 5.0 * 8.0 * q_gain * k_gain * scale             # about the largest score of 80 rows and 120 keys of 64 elements
+        for part in (1e-9, 1e-4, 0.3, 0.6, 0.9, 2.0):
+            run(cache_dtype, 2, 2, 64, 16, [80, 1], [120, 50], seed=2, cap=size / part, q_gain=q_gain, k_gain=k_gain, scale=scale, io=io)
+
+
+@pytest.mark.parametrize("cache_dtype", CACHES)
 def test_steep_slopes_over_far_keys(cache_dtype):
     # a mask that leaves only far keys: their differences count, not their distances
     slopes = torch.tensor([2.0, 0.01])
