@@ -19,8 +19,9 @@
 // rounding is 1.7e-3.  Queries or results with more bits (fp32, fp16) take the form PAIRS: queries and weights are sums of two
 // bf16, 16 bits, in two products each; the weights' lower halves take the other 32 columns of their scores.  Twice the
 // products, and at HD = 128 one tile of rows instead of two: 4 chunks of 512 tokens at 2048, 32 heads of 128, bf16: 230 us from and to fp16, 90
-// from and to bf16; 2 x 1024 tokens, 32 heads of 64: 66 and 37.  fp32 results go to the kernel for few rows.  A key's scale
-// (8-bit caches) multiplies its score in the softmax, a value's scale its weight, before the rounding.
+// from and to bf16; 2 x 1024 tokens, 32 heads of 64: 66 and 37.  fp32 results take 22 bits: over 4 bits, whose pairs are fp16, they
+// come here too (8 chunks of 3-1024 tokens at 1024-4096, 32 heads of 128, from and to fp32: 657 us, 2091 in the kernel for few rows), else they go to the
+// kernel for few rows, which has three bf16, or two fp16, for them.  A key's scale (8-bit caches) multiplies its score in the softmax, a value's scale its weight, before the rounding.
 //
 // The running maximum is raised only when it would be passed by 2^8 (weights then reach 256, well inside bf16 and the fp32
 // sums): O_t is rescaled in tensor memory in the first tiles and hardly ever after.
@@ -265,7 +266,7 @@ __device__ __forceinline__ void change_scores(uint32_t (&s)[2][32], float scale,
 // keys [z * chunk, (z + 1) * chunk), the last one all that follow; several leave partial results (accumulator, maximum, sum) of their rows
 // to paged_attn_join_kernel.
 // map_k, map_v: the pools as [n_pages * n_kv_heads][page_len][HD] with boxes of a page by 64 elements (bf16 only; use_maps 0: not made).
-// PAIRS: queries and weights enter as sums of two bf16.
+// PAIRS: queries and weights enter as sums of two bf16 (4 bits: of two fp16).
 // SC: scores are changed and keys masked as `sc` says; keys are counted from the tile of 128 that the first visible key of the block lies in, and a block
 // leaves the number of its splits for every row (part_used).  The change goes over pairs of scores: scale, the polynomial of paged.cuh while no score of
 // the warp passes the cap, the distance as a line (keys at or before the row) or an absolute value.
@@ -666,6 +667,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
               const long long e = at + c0 + i;
               if (out_vec && out.dtype == DT_BF16) store8<true>(static_cast<__nv_bfloat16*>(out.data) + e, x);
               else if (out_vec && out.dtype == DT_FP16) store8<true>(static_cast<__half*>(out.data) + e, x);
+              else if (out_vec) store8<true>(static_cast<float*>(out.data) + e, x);
               else {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) store_elem(out, e + k, x[k]);

@@ -253,8 +253,14 @@ int attention_chunks(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, f
 // 64 of 4096 over 2 key heads of 128, 16 rows 111 and 82, 32 rows 111 and 140; e4m3, 16 of 1024, 32 heads of 64, 24 rows 75 and 66,
 // 32 rows 75 and 116.  With pairs (results in fp16, few rows' time beside it): bf16, 16 of 1024, 32 heads of 64, 32 rows 133 and 74, 64 rows 135
 // and 133; 2 of 4096, 8 heads of 128, 32 rows 41 and 33, 48 rows 41 and 41; one of 30 000, one head, 32 rows 49 and 96; e4m3, 16 of 1024,
-// 8 heads of 128, 25 rows 49 and 67; 2 of 4096 41 and 45; 8 of 300, 12 heads of 64, 22 and 14.
-template <typename TC> constexpr int kChunkRows(bool pairs) { return sd::CacheType<TC>::TOP > 0.f ? 25 : pairs ? 41 : 9; }
+// 8 heads of 128, 25 rows 49 and 67; 2 of 4096 41 and 45; 8 of 300, 12 heads of 64, 22 and 14.  In 4 bits, where both kernels convert and the few rows' has a
+// half to read: bf16, 16 of 1024, 32 heads of 128, 40 rows 120 and 102, 56 rows 120 and 135; 64 of 4096 over 2 key heads, 32 rows 99 and 90, 48 rows 99 and 127; 2
+// of 4096, 8 heads, 40 and 37, 64 rows 40 and 39; 8 of 300, 12 heads of 64, 48 rows 22 and 14, 64 rows 22 and 21; fp32, 16 of 1024, 40 rows 149 and 135, 56 rows 150
+// and 179.  In 8 bits with pairs and changed scores, e4m3, results written in fp32 by both, the same, 40 rows 234 and 201, 56 rows 236 and 272; 2 of 4096 58 and 49, 58 and 64.
+template <typename TC, bool SC> constexpr int kChunkRows(bool pairs) {
+  constexpr bool scaled = sd::CacheType<TC>::TOP > 0.f;
+  return sd::kFour<TC> || (scaled && SC && pairs) ? 49 : scaled ? 25 : pairs ? 41 : 9;
+}
 
 template <bool SC>
 int cache_attention(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, float scale, const sd_heads* out, const sd::Scores& sc) {
@@ -275,8 +281,8 @@ int cache_attention(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, fl
         if constexpr (HD >= 64) {
           // one bf16 for a query or a weight only where the queries have no more and the results keep no more
           const bool pairs = q->dtype != SD_DTYPE_BF16 || out->dtype != SD_DTYPE_BF16;
-          const int enough = kChunkRows<TC>(pairs);
-          if (most >= enough && out->dtype != SD_DTYPE_FP32) {
+          const int enough = kChunkRows<TC, SC>(pairs);
+          if (most >= enough && (sd::kFour<TC> || out->dtype != SD_DTYPE_FP32)) {       // over 4 bits pairs are fp16 there too, 22 bits
             // max_new is only a bound: which kernel takes a sequence is decided on the device, by its own rows
             bool split = false;
             const int rows_from = b->n_seqs == 1 ? 1 : enough;

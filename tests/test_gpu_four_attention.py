@@ -15,13 +15,16 @@ from paper_2307_02628_b200 import binding
 pytestmark = pytest.mark.gpu
 
 
-def limit(want, parts, hd, out_dtype):
+def limit(want, parts, hd, out_dtype, fine=False):
+    """fine: queries and weights as two fp16.  A query's element is off by 2^-22 of itself or 2^-25 of the row's largest, which is 2^-20 of a score's terms
+    while the largest times the sum of the keys' magnitudes is at most 2^4 times theirs; a weight by 2^-22."""
     more = 0.0 if out_dtype == torch.float32 else 2.0 ** -8
-    lim = P.bound(want, parts, (hd + 10) * 2.0 ** -24 + 2.0 ** -16 + more, 2.0 ** -18 + 2.0 ** -16 + more, out_dtype)
+    pair = 2.0 ** -20 if fine else 2.0 ** -16
+    lim = P.bound(want, parts, (hd + 10) * 2.0 ** -24 + pair + more, 2.0 ** -18 + pair + more, out_dtype)
     return lim + parts[2].unsqueeze(-1) * 2.0 ** -31
 
 
-def run(io, heads, kv_heads, hd, page, new, length, scale=None, out_dtype=None, seed=0, k_gain=1.0, v_gain=1.0, max_len=None, **kw):
+def run(io, heads, kv_heads, hd, page, new, length, scale=None, out_dtype=None, seed=0, k_gain=1.0, v_gain=1.0, max_len=None, fine=False, **kw):
     lay = P.Layout(new, length, page, seed=seed, **kw)
     cache = P.make_cache(lay, heads, kv_heads, hd, "e2m1")
     contents = F.fill(cache, lay, seed=seed + 1, k_gain=k_gain, v_gain=v_gain)
@@ -38,7 +41,7 @@ def run(io, heads, kv_heads, hd, page, new, length, scale=None, out_dtype=None, 
         own[int(lay.first[s]):int(lay.first[s + 1])] = True
     assert bool((got[~own] == 9).all())                         # padding rows are left as they were
     assert not bool(torch.isnan(got).any())
-    err = ((got - want).abs() - limit(want, parts, hd, out_dtype))[own]
+    err = ((got - want).abs() - limit(want, parts, hd, out_dtype, fine))[own]
     assert float(err.max()) <= 0, (float(err.max()), float((got - want)[own].abs().max()))
     return got, want
 
@@ -86,6 +89,15 @@ def test_scales_and_magnitudes(scale, k_gain, v_gain, io):
 def test_output_types(io, out):
     run(io, 2, 2, 64, 16, [1, 70], [30, 100], out_dtype=out, seed=21)
     run(io, 2, 2, 128, 32, [1, 70], [30, 100], out_dtype=out, seed=22)
+
+
+@pytest.mark.parametrize("io", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_results_in_fp32_have_the_bits_of_two_fp16(io, hd):
+    # one, some and many rows, split and not, on rows that begin at any element
+    run(io, 2, 2, hd, 16, [1, 20, 70], [300, 200, 100], out_dtype="fp32", seed=31, fine=True)
+    run(io, 4, 1, hd, 64, [130], [700], out_dtype="fp32", seed=32, fine=True)
+    run(io, 2, 1, hd, 32, [49, 48, 47], [50, 333, 4000], out_dtype="fp32", seed=33, fine=True)
 
 
 @pytest.mark.parametrize("new,length", [([1, 2], [100, 40]), ([90, 1], [100, 40])])
