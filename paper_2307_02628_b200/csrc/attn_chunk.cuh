@@ -130,6 +130,16 @@ __device__ __forceinline__ F2 add2(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1,
 __device__ __forceinline__ F2 mul2(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
 __device__ __forceinline__ uint32_t pack(float a, float b, __nv_bfloat16) { return pack_bf16(a, b); }
 __device__ __forceinline__ uint32_t pack(float a, float b, __half) { return pack_f16(a, b); }
+// Query row of row r of the block's tile t, whose first row is row0 and whose tiles have n_rows: rows past the tile's end are its last one, and a tile without
+// rows has the block's first one, so that what is looked up for a row is always that of one of the caller's.
+__host__ __device__ __forceinline__ int tile_row(int row0, int t, int n_rows, int r) {
+  return n_rows > 0 ? row0 + t * TILE_ROWS + (r < n_rows ? r : n_rows - 1) : row0;
+}
+// Number i (0..255) of the tokens that a tile of rows > 0 rows from `first_row` on belongs to (up to 129 of them), -1: there is none.
+__host__ __device__ __forceinline__ int tile_token(int first_row, int rows, int group, int i) {
+  const int token = first_row / group + i;
+  return rows > 0 && token <= (first_row + rows - 1) / group ? token : -1;
+}
 // byte offset of 16-byte piece c (8 elements) of row r in a tile
 __device__ __forceinline__ uint32_t piece(int r, int c) { return (uint32_t)((c >> 3) * (128 * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)); }
 
@@ -331,10 +341,10 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   int first_key = 0, ends[2] = {0, 0};                            // SC: where the block's keys begin, and end for each tile
   if constexpr (SC) {
     __shared__ int span_lo[THREADS / 32], span_hi[THREADS / 32];
-    const int t = threadIdx.x >> 8, tile_row = row0 + t * TILE_ROWS, rows = t < L::TILES ? min(TILE_ROWS, rows_all - tile_row) : 0;
-    const int token = tile_row / group + (threadIdx.x & 255);     // up to 129 of a tile
+    const int t = threadIdx.x >> 8, start = row0 + t * TILE_ROWS;
+    const int token = tile_token(start, t < L::TILES ? min(TILE_ROWS, rows_all - start) : 0, group, threadIdx.x & 255);
     Span v{0, -1};
-    if (rows > 0 && token <= (tile_row + rows - 1) / group) v = visible(sc, f0 + token, pos_first + token, len);
+    if (token >= 0) v = visible(sc, f0 + token, pos_first + token, len);
     const int from = __reduce_min_sync(0xffffffffu, v.lo <= v.hi ? v.lo : 0x7fffffff), to = __reduce_max_sync(0xffffffffu, v.hi + 1);
     if ((threadIdx.x & 31) == 0) { span_lo[threadIdx.x >> 5] = from; span_hi[threadIdx.x >> 5] = to; }
     __syncthreads();
@@ -391,7 +401,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   }
   // Softmax warps: the thread's query row.  The rows are on their way while the barriers and the tensor memory are prepared.
   const int t = warp >> 2 & 1, r = (warp & 3) * 32 + lane;
-  const int row = row0 + t * TILE_ROWS + min(r, max(n_rows[t] - 1, 0));
+  const int row = tile_row(row0, t, n_rows[t], r);
   const int token = row / group, head = g_head * group + row % group;
   int row_last = (int)max(min(pos_first + token, (long long)len - 1), -1ll) - key0;        // last key this row sees
   const float sign = scale_log2 < 0.f ? -1.f : 1.f;             // a negative scale turns the queries round
@@ -488,7 +498,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     if (lane == 0) arrive(qfull);                                 // the rows are in shared memory since before the block's barriers were
 
     // the keys that all 32 rows of the warp see: tiles below need no mask
-    const int first_token = (row0 + t * TILE_ROWS + min((warp & 3) * 32, max(n_rows[t] - 1, 0))) / group;
+    const int first_token = tile_row(row0, t, n_rows[t], (warp & 3) * 32) / group;
     int all_see = (int)max(min(pos_first + first_token, (long long)len - 1), -1ll) - key0;
     int row_first = 0, all_from = 0, any_from = 0, any_see = 0;  // SC: the first key of this row, the keys that some row of the warp sees
     int row_pos = 0, nearest = 0;                                // the row's position, counted as the keys; the distance of its nearest visible key
