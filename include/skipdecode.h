@@ -375,8 +375,9 @@ typedef struct {
 } sd_scores;
 
 /* sd_cache_attention with changed scores and masks, rounded as documented there (a score's change in fp32: where all scores that are computed together stay
- * below the cap it is off by 3e-7 of the score, else by 2^-21 of the cap).  Reads only the
- * keys between the first and the last that some row of a tile of rows sees. */
+ * below the cap it is off by 3e-7 of the score, else by 2^-21 of the cap).  Rows that are computed together go over the keys between the first and the
+ * last that one of them sees.  What lies ahead of the first or behind the last position that some row of a sequence sees is not read: it may be anything,
+ * and table entries of pages that lie there as a whole need not name a page.  Positions between must have been written, seen or not. */
 int sd_cache_attention_scores(sd_cache *c, int layer, const sd_batch *batch, const sd_heads *q, float scale, const sd_scores *scores,
                               const sd_heads *out);
 

@@ -338,7 +338,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   if (row0 < 0) return;
   const long long pos_first = (long long)who.w - (f1 - f0);
   const int splits = gridDim.y, z = blockIdx.y;
-  int first_key = 0, ends[2] = {0, 0};                            // SC: where the block's keys begin, and end for each tile
+  int first_key = 0, first_seen = 0, ends[2] = {0, 0};            // SC: where the block's keys begin; the first that a row sees; where they end for each tile
   if constexpr (SC) {
     __shared__ int span_lo[THREADS / 32], span_hi[THREADS / 32];
     const int t = threadIdx.x >> 8, start = row0 + t * TILE_ROWS;
@@ -354,7 +354,8 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       first_key = min(first_key, span_lo[w]);
       ends[w / 8] = max(ends[w / 8], span_hi[w]);
     }
-    first_key = first_key == 0x7fffffff ? 0 : first_key & ~(KEYS - 1);
+    first_seen = first_key == 0x7fffffff ? 0 : first_key;
+    first_key = first_seen & ~(KEYS - 1);
   }
   const int key0 = SC ? (int)min(first_key + (long long)z * chunk, 0x7fffffffll) : z * chunk;  // key numbers below count from key0
   int n_keys[2], n_rows[2], used_splits = 1;
@@ -478,7 +479,8 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   }
   // loaders: the pages of the first tile of keys
   const int* table = b.pages + (size_t)seq * b.pages_per_seq;
-  const int most = min(len - key0, n_tiles * KEYS);               // keys past it are filled with zeros
+  // Keys from `most` on are filled with zeros, and with masks those ahead of `least`: no row sees them, they may be anything, and their pages need not exist.
+  const int most = min((SC ? max(ends[0], ends[1]) : len) - key0, n_tiles * KEYS), least = first_seen - key0;
   // lane i < 16 looks up the page of keys [8 i, 8 i + 8) of a tile
   auto look_up = [&](int j) {
     const int key = j * KEYS + (lane & 15) * 8;
@@ -713,20 +715,21 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     constexpr int ROWS_AT_ONCE = 32 / PER_ROW;                    // of a warp
     constexpr int STEPS = KEYS / (4 * ROWS_AT_ONCE);
     auto exists = [&](int j, int page) {
-      return __ballot_sync(0xffffffffu, (unsigned)page < (unsigned)b.n_pages || j * KEYS + (lane & 15) * 8 >= most) & 0xffffu;
+      const int key = j * KEYS + (lane & 15) * 8;
+      return __ballot_sync(0xffffffffu, (unsigned)page < (unsigned)b.n_pages || key >= most || (SC && key + 7 < least)) & 0xffffu;
     };
     // this thread's piece in step i: row `key`, piece c
     auto key_of = [&](int i) { return (i * 4 + w) * ROWS_AT_ONCE + lane / PER_ROW; };
     const int c = lane % PER_ROW;
     auto source = [&](const TC* pool, int j, int key, int page, uint32_t pages_ok) -> const TC* {
       page = __shfl_sync(0xffffffffu, page, key >> 3);
-      const bool on = j * KEYS + key < most && ((pages_ok >> (key >> 3)) & 1u);
+      const bool on = j * KEYS + key < most && !(SC && j * KEYS + key < least) && ((pages_ok >> (key >> 3)) & 1u);
       return on ? pool + b.entry(page, g_head, key0 + j * KEYS + key) * row_units<TC>(HD) + c * (16 / E) : nullptr;
     };
     // this thread's key's scales, zeros where there is none
     auto ask_scales = [&](int j, int page, uint32_t pages_ok) {
       page = __shfl_sync(0xffffffffu, page, (tid >> 3) & 15);
-      if (!(j * KEYS + tid < most && ((pages_ok >> (tid >> 3)) & 1u))) return make_float2(0.f, 0.f);
+      if (!(j * KEYS + tid < most && !(SC && j * KEYS + tid < least) && ((pages_ok >> (tid >> 3)) & 1u))) return make_float2(0.f, 0.f);
       const size_t e = b.entry(page, g_head, key0 + j * KEYS + tid);
       return make_float2(__ldg(Ksc + e), __ldg(Vsc + e));
     };
@@ -734,10 +737,10 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     float ve = 0.f;
     auto ask_values = [&](int j, int page, uint32_t pages_ok) {
       page = __shfl_sync(0xffffffffu, page, lane >> 1);
-      const int left = most - (j * KEYS + lane * 4);
-      if (left <= 0 || !((pages_ok >> (lane >> 1)) & 1u)) return 0.f;
-      const float4 v = __ldg(reinterpret_cast<const float4*>(Vsc + b.entry(page, g_head, key0 + j * KEYS + lane * 4)));
-      return fmaxf(fmaxf(v.x, left > 1 ? v.y : 0.f), fmaxf(left > 2 ? v.z : 0.f, left > 3 ? v.w : 0.f));
+      const int key = j * KEYS + lane * 4, left = most - key;
+      if (left <= 0 || (SC && key + 3 < least) || !((pages_ok >> (lane >> 1)) & 1u)) return 0.f;
+      const float4 v = __ldg(reinterpret_cast<const float4*>(Vsc + b.entry(page, g_head, key0 + key)));
+      return fmaxf(fmaxf((SC && key < least) ? 0.f : v.x, left > 1 && !(SC && key + 1 < least) ? v.y : 0.f), fmaxf(left > 2 && !(SC && key + 2 < least) ? v.z : 0.f, left > 3 ? v.w : 0.f));
     };
     auto raise = [&](float top) {
       const float all = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(fabsf(top))));
@@ -800,7 +803,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         const int page = page_next;
         page_next = look_up(j + 1);
         const uint32_t pages_ok = exists(j, page);
-        const bool whole = use_maps && (j + 1) * KEYS <= most && pages_ok == 0xffffu;
+        const bool whole = use_maps && (j + 1) * KEYS <= most && !(SC && j * KEYS < least) && pages_ok == 0xffffu;
         const uint32_t kt = base + L::K + (j % STAGES) * L::TILE, vt = base + L::V + (j % STAGES) * L::TILE;
         if (!(ok = wait_free(kempty, j))) break;
         begin_side(j, make_float2(0.f, 0.f), pages_ok);
@@ -842,7 +845,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
 #pragma unroll
           for (int i = 0; i < STEPS; ++i) {
             const int key = key_of(i), of = __shfl_sync(0xffffffffu, page, key >> 3);
-            entry[i] = j * KEYS + key < most && ((pages_ok >> (key >> 3)) & 1u) ? (long long)b.entry(of, g_head, key0 + j * KEYS + key) : -1;
+            entry[i] = j * KEYS + key < most && !(SC && j * KEYS + key < least) && ((pages_ok >> (key >> 3)) & 1u) ? (long long)b.entry(of, g_head, key0 + j * KEYS + key) : -1;
           }
         }
       };

@@ -125,7 +125,8 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
       all_from = max(all_from, __shfl_xor_sync(0xffffffffu, all_from, o));
     }
   }
-  const int base = SC && key_end > 0 ? key_begin & ~63 : 0;                 // chunks are multiples of 64
+  if (!SC || key_end == 0) key_begin = 0;
+  const int base = key_begin & ~63;                                         // chunks are multiples of 64
   const int used_splits = max(1, ap::splits_of(key_end - base, chunk, splits));
   if (z >= used_splits) return;
   const int k0 = base + z * chunk, k1 = z == splits - 1 ? key_end : (int)min((long long)k0 + chunk, (long long)key_end);
@@ -161,12 +162,13 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
   const float* s_src = (lane < 8 ? Ksc : Vsc) + s_key;
   const uint8_t* b_src = (lane < BP ? Kb : Vb) + (lane % BP) * 16;
   const uint32_t lane_at = lane_key * S::ROW + ((lane_piece ^ (swz(lane_key) & S::SWZ)) << 4);
+  // Keys ahead of key_begin are seen by no row: they may be anything, and their pages need not exist.
   auto issue = [&](int n, int stage) {
     look_up(n);
     const int key0 = (tile0 + n * NW) * KEYS, slot = (n - win) << parts_log;
     const uint32_t dst = ring + stage * S::STAGE;
     const int page0 = __shfl_sync(0xffffffffu, window, slot);
-    if (parts_log == 0 && key0 + KEYS <= k1 && (unsigned)page0 < (unsigned)b.n_pages) {
+    if (parts_log == 0 && key0 + KEYS <= k1 && !(SC && key0 < key_begin) && (unsigned)page0 < (unsigned)b.n_pages) {
       const uint32_t e = (((uint32_t)page0 * b.n_kv_heads + g_head) << b.page_shift) + (key0 & (b.page_len - 1));
       const e2m1 *ks = k_src + (size_t)e * S::ROW, *vs = v_src + (size_t)e * S::ROW;
 #pragma unroll
@@ -179,26 +181,26 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
       valid |= 15u << (4 * stage);
       return;
     }
-    // The page of the part that a key lies in, -1: none or past the end.  What is not copied is what an earlier tile left: its keys are hidden, its
-    // values' weights and scales zero.
-    auto page_of = [&](int key) {
+    // The page of `some` keys from one on, of one part, -1: none, or no row sees them.  What is not copied is what an earlier tile left: its keys are
+    // hidden, its values' weights and scales zero.
+    auto page_of = [&](int key, int some) {
       const int page = __shfl_sync(0xffffffffu, window, slot + (key >> part_shift));
-      return key0 + key < k1 && (unsigned)page < (unsigned)b.n_pages ? page : -1;
+      return key0 + key < k1 && !(SC && key0 + key + some - 1 < key_begin) && (unsigned)page < (unsigned)b.n_pages ? page : -1;
     };
-    const int mine = page_of((lane & 3) * 8);
-    const uint32_t ok = __ballot_sync(0xffffffffu, mine >= 0 || key0 + (lane & 3) * 8 >= k1) & 15u;
+    const int eight = (lane & 3) * 8, mine = page_of(eight, 8);
+    const uint32_t ok = __ballot_sync(0xffffffffu, mine >= 0 || key0 + eight >= k1 || (SC && key0 + eight + 7 < key_begin)) & 15u;
     if (ok != 15u && lane == 0) b.bad();
     valid = (valid & ~(15u << (4 * stage))) | (ok << (4 * stage));
 #pragma unroll 1
     for (int i = 0; i < STEPS; ++i) {
-      const int key = lane_key + i * STEP_KEYS, page = page_of(key);
+      const int key = lane_key + i * STEP_KEYS, page = page_of(key, 1);
       if (page < 0) continue;                                               // no shuffle follows in this round
       const size_t from = b.entry(page, g_head, key0 + key) * S::ROW + lane_piece * 16;
       pf_cp16(dst + lane_at + i * 512, Kp + from, 16);
       pf_cp16(dst + lane_at + i * 512 + S::V, Vp + from, 16);
     }
     __syncwarp();
-    const int ps = page_of(s_key), pb = page_of(b_key);
+    const int ps = page_of(s_key, 4), pb = page_of(b_key, BKEYS);
     if (lane < 16 && ps >= 0) pf_cp16(dst + S::SCALES + lane * 16, (lane < 8 ? Ksc : Vsc) + b.entry(ps, g_head, key0 + s_key), 16);
     if (lane < 2 * BP && pb >= 0) pf_cp16(dst + S::BLOCK + lane * 16, (lane < BP ? Kb : Vb) + b.entry(pb, g_head, key0 + b_key) * S::BLOCKS, 16);
   };
@@ -313,12 +315,13 @@ paged_attn_four_kernel(const BatchView b, const Rows q, const Rows out, const e2
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int key = key0 + j * 8 + g;
-        const bool there = key < k1 && ((ok >> j) & 1u);
-        if (!there) vsc[j] = 0.f;                  // past the end or on a page that does not exist: it may be anything
+        const bool there = key < k1 && !(SC && key < key_begin) && ((ok >> j) & 1u);
+        if (!there) vsc[j] = 0.f;                  // outside what the rows see or on a page that does not exist: it may be anything
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           if (!there || key > seen[i].hi || (SC && key < seen[i].lo)) hidden |= 1u << (2 * j + i);
-          if (key0 + j * 8 + 2 * t + i >= k1 || !((ok >> j) & 1u)) gone |= 1u << (2 * j + i);
+          const int of = key0 + j * 8 + 2 * t + i;
+          if (of >= k1 || (SC && of < key_begin) || !((ok >> j) & 1u)) gone |= 1u << (2 * j + i);
         }
       }
     }

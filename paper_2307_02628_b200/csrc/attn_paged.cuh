@@ -180,7 +180,7 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
   int key_end = (int)min(max(pos_first + last_token + 1, 0ll), (long long)len);            // keys that any row of the tile sees
   int row_last = (int)max(min(pos_first + token, (long long)len - 1), -1ll);               // -1: none
   int all_see = (int)max(min(pos_first + (tile * ROWS) / group, (long long)len - 1), -1ll);   // the last key that every row sees
-  int row_first = 0, all_from = 0, base = 0;                                                // the first ones; where the splits begin
+  int row_first = 0, all_from = 0, key_begin = 0, base = 0;                                 // the first ones; where the splits begin
   if constexpr (SC) {
     const Span v = visible(sc, f0 + token, pos_first + token, len);
     row_first = v.lo;
@@ -195,7 +195,8 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
       all_see = min(all_see, __shfl_xor_sync(0xffffffffu, all_see, o));
     }
     key_end = to + 1;
-    base = key_end > 0 ? from & ~63 : 0;                                                    // chunks are multiples of 64
+    key_begin = key_end > 0 ? from : 0;
+    base = key_begin & ~63;                                                                 // chunks are multiples of 64
   }
   const int used_splits = max(1, splits_of(key_end - base, chunk, splits));
   if (z >= used_splits) return;
@@ -229,13 +230,14 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
   const int lane_key = lane / S::PIECES, lane_piece = lane % S::PIECES;
   constexpr int STEPS = KEYS * S::PIECES / 32, STEP_KEYS = 32 / S::PIECES;
   static_assert(KEYS * S::PIECES % 32 == 0, "whole warps of copies");
+  // Keys ahead of key_begin are seen by no row: they may be anything, and their pages need not exist.
   auto issue = [&](int n, int stage) {
     look_up(n);
     const int kt = tile0 + n * NW;
     const int page[2] = {__shfl_sync(0xffffffffu, window[0], n - win), __shfl_sync(0xffffffffu, window[1], n - win)};
     const uint32_t dst = ring + stage * S::STAGE;
     const int key0 = kt * KEYS;
-    if (!split_tile && key0 + KEYS <= k1 && (unsigned)page[0] < (unsigned)b.n_pages) {
+    if (!split_tile && key0 + KEYS <= k1 && !(SC && key0 < key_begin) && (unsigned)page[0] < (unsigned)b.n_pages) {
       // a whole tile inside one page
       const size_t e = b.entry(page[0], g_head, key0);
       const TC* ks = Kp + e * HD + lane * (16 / S::E);
@@ -259,7 +261,7 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
     for (int hf = 0; hf < 2; ++hf) {
       const int key = key0 + 8 * hf;
       const bool there = (unsigned)page[hf] < (unsigned)b.n_pages;
-      if (!there && key < k1 && lane == 0) b.bad();
+      if (!there && key < k1 && !(SC && key + 7 < key_begin) && lane == 0) b.bad();
       e[hf] = there ? b.entry(page[hf], g_head, key) : 0;
       ok |= there ? 1u << hf : 0u;
     }
@@ -267,7 +269,7 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
 #pragma unroll 1
     for (int i = 0; i < STEPS; ++i) {
       const int key = lane_key + i * STEP_KEYS, hf = key >> 3;
-      const bool on = key0 + key < k1 && ((ok >> hf) & 1u);                  // off: zeros, nothing is read
+      const bool on = key0 + key < k1 && !(SC && key0 + key < key_begin) && ((ok >> hf) & 1u);                  // off: zeros, nothing is read
       const size_t src = on ? ((hf ? e[1] : e[0]) + (key & 7)) * HD + lane_piece * (16 / S::E) : 0;
       const uint32_t at = dst + key * S::ROW + ((lane_piece ^ (swz(key) & S::SWZ)) << 4);
       pf_cp16(at, Kp + src, on ? 16 : 0);
@@ -276,7 +278,7 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
     if constexpr (S::SCALED) {
       if (lane < 8) {                              // 16 scales of each: four pieces of four
         const int key = (lane & 3) * 4, hf = key >> 3;
-        const bool on = key0 + key < k1 && ((ok >> hf) & 1u);
+        const bool on = key0 + key < k1 && !(SC && key0 + key + 3 < key_begin) && ((ok >> hf) & 1u);
         const float* src = (lane < 4 ? Ksc : Vsc) + (on ? (hf ? e[1] : e[0]) + (key & 7) : 0);
         pf_cp16(dst + 2 * KEYS * S::ROW + lane * 16, src, on ? 16 : 0);
       }
@@ -395,9 +397,9 @@ paged_attn_tile_kernel(const BatchView b, const Rows q, const Rows out, const TC
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int at = kt * KEYS + n * 8 + 2 * t + i;
-          const bool there = at < k1 && ((ok >> n) & 1u);
+          const bool there = at < k1 && !(SC && at < key_begin) && ((ok >> n) & 1u);
           if (!there || at > row_last || (SC && at < row_first)) hidden |= 1u << (2 * n + i);
-          if (!there) vsc[n][i] = 0.f;              // past the end or on a page that does not exist: it may be anything
+          if (!there) vsc[n][i] = 0.f;              // outside what the rows see or on a page that does not exist: it may be anything
         }
     }
     float mb = m == -INFINITY ? 0.f : m;
