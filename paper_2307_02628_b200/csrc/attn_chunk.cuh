@@ -245,16 +245,18 @@ __device__ __forceinline__ void change_scores(uint32_t (&s)[2][32], float scale,
     }
   }
   if (slope_on) {
-    if (!ahead || __all_sync(0xffffffffu, pos >= 63)) {            // -slope (pos - c - nearest) = slope c + begin
-      const float begin = -slope * (float)(pos - nearest);
-      const F2 slope2 = f2(slope, slope), begin2 = f2(begin, begin), step = f2(2.f * slope, 2.f * slope);
+    if (!ahead || __all_sync(0xffffffffu, pos >= 63)) {            // -slope (pos - c - nearest) = slope away, away = c - (pos - nearest)
+      // The distances are whole numbers, counted on two at a time: a bias is rounded once, with its sum where that is one instruction.  (Sums of slopes in
+      // their place save a product where there is neither scale nor cap, and were off by roundings of the largest bias in the half.)
+      const float begin = (float)(nearest - pos);
+      const F2 slope2 = f2(slope, slope), two = f2(2.f, 2.f);
 #pragma unroll
-      for (int k8 = 0; k8 < 4; ++k8) {                               // a product for every eighth pair, sums between: as exact as a product for each
-        F2 bias = fma2(f2(16.f * k8, 16.f * k8 + 1.f), slope2, begin2);
+      for (int k8 = 0; k8 < 4; ++k8) {
+        F2 away = add2(f2(begin, begin), f2(16.f * k8, 16.f * k8 + 1.f));
 #pragma unroll
         for (int k = 8 * k8; k < 8 * k8 + 8; ++k) {
-          put(k, SCALED || cap_on ? add2(get(k), bias) : fma2(get(k), scale2, bias));
-          bias = add2(bias, step);
+          put(k, SCALED || cap_on ? fma2(away, slope2, get(k)) : fma2(get(k), scale2, mul2(away, slope2)));
+          away = add2(away, two);
         }
       }
     } else {
