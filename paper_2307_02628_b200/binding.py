@@ -237,6 +237,11 @@ class Scores:
         for name, t, dt in (("slopes", slopes, torch.float32), ("lo", lo, torch.int32), ("hi", hi, torch.int32)):
             if t is not None and (t.dtype != dt or not t.is_cuda or t.dim() != 1 or not t.is_contiguous()):
                 raise ValueError(f"{name} must be a contiguous {dt} CUDA tensor of one dimension")
+        # as the library gets them: a window of 2^32 would stand for none, a cap that rounds to 0 for off
+        if not -2 ** 31 <= window < 2 ** 31 or int(window) != window:
+            raise ValueError("window must be a whole number of 32 bits")
+        if cap != 0 and C.c_float(cap).value == 0:
+            raise ValueError("cap must be 0, or a number that fp32 holds")
         self.slopes, self.lo, self.hi = slopes, lo, hi
         self.indices = {t.device.index for t in (slopes, lo, hi) if t is not None}
         self.n_heads = None if slopes is None else slopes.shape[0]

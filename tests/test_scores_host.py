@@ -55,3 +55,18 @@ def test_the_limit_notices_a_wrong_mask_cap_or_slope():
         got = S.reference(q, contents, lay, 0.125, 2, **wrong)[0].bfloat16()
         assert float(S.over(got, *out, 64, q.dtype, 6.0).max()) > 1, wrong
     assert float(S.over(out[0].bfloat16(), *out, 64, q.dtype, 6.0).max()) < 1
+
+
+@pytest.mark.parametrize("bad", [dict(window=2 ** 32), dict(window=2 ** 31), dict(window=2 ** 32 + 5), dict(window=-(2 ** 31) - 1), dict(window=0.5), dict(window=2.5), dict(window=float("inf")), dict(window=float("nan")),
+                                 dict(cap=1e-46), dict(cap=-1e-50)])
+def test_numbers_that_would_arrive_as_others_are_refused(bad):
+    """A window of 2^32 would be none, a cap of 1e-46 off: the library sees 32 bits of either."""
+    with pytest.raises(ValueError):
+        binding.Scores(**bad)
+
+
+def test_numbers_that_arrive_as_they_are():
+    for kw in (dict(window=2 ** 31 - 1), dict(window=-1), dict(window=2048.0), dict(cap=0.0), dict(cap=1e-35), dict(cap=float("inf")), dict(cap=-1.0)):
+        c = binding.Scores(**kw).c                             # what is out of its range is the library's to refuse
+        for name, value in kw.items():
+            assert getattr(c, name) == pytest.approx(value, rel=2.0 ** -24, abs=0)
