@@ -354,8 +354,9 @@ int sd_cache_read(sd_cache *c, int layer, const sd_batch *batch, const sd_heads 
  *   out[r, h] = sum_j softmax_j(scale * q[r, h] . K[j, g]) V[j, g],  g = h / (n_heads / n_kv_heads).
  * q, out: rows [n_tokens, n_heads, head_dim].  scale: at most 2e38 in magnitude; 0 stands for head_dim^-1/2.  Single tokens, chunks
  * and both in one call.  Sums and softmax statistics are fp32.  Over an fp32 cache nothing is rounded before the output; over the
- * others queries and weights enter the products with 22 bits or more where out is fp32, with 16 or more where it is not, except that the
- * weights may enter as bf16 where both q and out are bf16.  The numbers of sequences, tokens and rows and the bounds max_new and max_len choose the kernels and
+ * others queries and weights enter the products with 22 bits or more where out is fp32, with 16 or more where it is not, except that, where
+ * both q and out are bf16, the weights may enter as bf16 (over 4 bits with 11 bits), and over 4 bits a value may be rounded to 11 bits twice: the
+ * product of its two scales, and that times its code.  The numbers of sequences, tokens and rows and the bounds max_new and max_len choose the kernels and
  * where the keys are split, and rows that are computed side by side raise their running maximum together: the same call (batch description,
  * bounds and inputs) gives the same bits, the same row in another call agrees within that rounding.  The result of a query row
  * with a NaN is NaN, with an infinity NaN or 0; other rows and heads do not see it beyond that rounding.  A weight before the
@@ -375,7 +376,7 @@ typedef struct {
 } sd_scores;
 
 /* sd_cache_attention with changed scores and masks, rounded as documented there (a score's change in fp32: where all scores that are computed together stay
- * below the cap it is off by 3e-7 of the score, else by 2^-21 of the cap).  Rows that are computed together go over the keys between the first and the
+ * below the cap it is off by 2^-21 of the score, else by 2^-21 of the cap).  Rows that are computed together go over the keys between the first and the
  * last that one of them sees.  What lies ahead of the first or behind the last position that some row of a sequence sees is not read: it may be anything,
  * and table entries of pages that lie there as a whole need not name a page.  Positions between must have been written, seen or not. */
 int sd_cache_attention_scores(sd_cache *c, int layer, const sd_batch *batch, const sd_heads *q, float scale, const sd_scores *scores,
@@ -422,8 +423,8 @@ int sd_cache_copy(sd_cache *c, const int32_t *src, const int32_t *dst, int n);
  * results of that call being wrong.  Returns SD_ERR_DEVICE when it was not 0. */
 int sd_cache_status(sd_cache *c, int32_t *device_status);
 
-/* SD_CACHE_OPT_TEST_WAIT_EXPIRY: test hook, one shot.  1: in the next attention of chunks over a bf16 or 8-bit cache (16-bit results, more than
- * 256 keys) a wait inside the kernel runs out after about a millisecond: sd_cache_status reports bit 2, the results of that
+/* SD_CACHE_OPT_TEST_WAIT_EXPIRY: test hook, one shot.  1: in the next attention of chunks over a bf16 or 8-bit cache with 16-bit results, or over a
+ * 4-bit cache (more than 256 keys), a wait inside the kernel runs out after about a millisecond: sd_cache_status reports bit 2, the results of that
  * call are garbage or as they were, nothing is left in flight and the cache stays usable.  Errors: SD_ERR_ARG. */
 enum { SD_CACHE_OPT_TEST_WAIT_EXPIRY = 1 };
 int sd_cache_set_option(sd_cache *c, int option, int value);

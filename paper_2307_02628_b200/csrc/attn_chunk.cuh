@@ -13,14 +13,14 @@
 // Operands are bf16, the type of a bf16 cache; codes of 8-bit caches are bf16 numbers exactly.  Over 4-bit caches they are fp16: codes times their block's scale
 // are fp16 numbers exactly, two instructions a pair (six to bf16), and queries are brought near 1 by a power of two for each row.  A value's scale joins
 // its weight, relative to a power of two above all scales so far, times 2^7 (the weights stay below 2^15); where queries and results are bf16 it joins
-// the value instead, whose block scale times scale is then rounded to 11 bits, and the weight, of 11 bits too, is times 2^7 by itself: half as
-// many scales to read and multiply by in the softmax.  Where queries and results are bf16 too, the only
+// the value instead, whose block scale times scale is then rounded to 11 bits, and once more times a code of 1.5, 3 or 6 (2^-10 of a value at most, both), and the
+// weight, of 11 bits too, is times 2^7 by itself: half as many scales to read and multiply by in the softmax.  Where queries and results are bf16 too, the only
 // rounding is that of the weights, once to 8 bits of significand: relative to 64-bit arithmetic results are 2.3e-3 off, of which their own
 // rounding is 1.7e-3.  Queries or results with more bits (fp32, fp16) take the form PAIRS: queries and weights are sums of two
 // bf16, 16 bits, in two products each; the weights' lower halves take the other 32 columns of their scores.  Twice the
 // products, and at HD = 128 one tile of rows instead of two: 4 chunks of 512 tokens at 2048, 32 heads of 128, bf16: 230 us from and to fp16, 90
 // from and to bf16; 2 x 1024 tokens, 32 heads of 64: 66 and 37.  fp32 results take 22 bits: over 4 bits, whose pairs are fp16, they
-// come here too (8 chunks of 3-1024 tokens at 1024-4096, 32 heads of 128, from and to fp32: 657 us, 2091 in the kernel for few rows), else they go to the
+// come here too (8 chunks of 3-1024 tokens at 1024-4096, 32 heads of 128, from and to fp32: 652 us, 2091 in the kernel for few rows), else they go to the
 // kernel for few rows, which has three bf16, or two fp16, for them.  A key's scale (8-bit caches) multiplies its score in the softmax, a value's scale its weight, before the rounding.
 //
 // The running maximum is raised only when it would be passed by 2^8 (weights then reach 256, well inside bf16 and the fp32
@@ -167,7 +167,7 @@ __device__ __forceinline__ uint32_t columns(int right, int left) {
 // Four bits to the four bytes of a word.
 __device__ __forceinline__ uint32_t bytes_of(uint32_t four) { return (((four & 15u) * 0x00204081u) & 0x01010101u) * 0xffu; }
 
-// as TANH0.. of paged.cuh, of degree 3 for [0, 0.45] (3e-7 of the score) and of degree 4 for [0, 0.7]
+// as TANH0.. of paged.cuh, of degree 3 for [0, 0.45] and of degree 4 for [0, 0.7]: off by 2.5e-7 and 3.1e-7, with fp32's roundings 4.0e-7 and 4.7e-7
 constexpr float CLOSE0 = 0x1.fffff8p-1f, CLOSE1 = -0x1.554b32p-2f, CLOSE2 = 0x1.0f14b2p-3f, CLOSE3 = -0x1.79101ep-5f;
 constexpr float NEAR0 = 0x1.fffff6p-1f, NEAR1 = -0x1.554d28p-2f, NEAR2 = 0x1.0fff48p-3f, NEAR3 = -0x1.a07350p-5f, NEAR4 = 0x1.c35640p-7f;
 // A half's 64 scores of a row, in place, to base-2 units: scale (8 and 4 bits: done), cap, distance.  pos: the row's position, counted from the first

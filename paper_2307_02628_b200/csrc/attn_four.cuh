@@ -5,9 +5,10 @@
 // value = code * block scale * scale.  Code times block scale is an fp16 number exactly: one conversion and one multiplication for a pair.  A key's scale multiplies
 // its score, a value's scale its weight, relative to a power of two above all scales so far and times 2^7, as in 8 bits.
 //
-// What bounds it is instructions, not bytes: at 152 bytes a key and head of 128 the memory could deliver a key every 8 clocks to an SM, which four
-// schedulers have 32 slots for, and conversion alone takes 13 (a warp's instruction for 32 lanes: 256 values in pairs, two instructions each, plus the values' interleaving).
-// So the rest is kept small:
+// At 152 bytes a key and head of 128 the memory could deliver a key every 8 clocks to an SM, which four schedulers have 32 slots for, and conversion alone
+// takes 13 (a warp's instruction for 32 lanes: 256 values in pairs, two instructions each, plus the values' interleaving).  Nothing is full (64 single tokens at
+// 1024..1536: issue and ALU 53 %, memory 48 %): 15 warps to an SM, each a chain of copies, products, maxima and exponentials, do not cover one another's
+// waits, and a block's start and end are a fifth of it.  So instructions and steps are kept few:
 //  - 32 keys of a warp go through the loop at a time, so that copies, waits and maxima are paid once for them;
 //  - scores are S^T = K Q^T with the keys as the 16-row operand, and O^T = V^T P^T has the values there: the 8 query rows fill the other side of both, so that
 //    either takes half the products, and half the accumulators, that it would take with the rows' operand padded.  A thread holds scores of two

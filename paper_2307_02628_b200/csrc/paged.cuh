@@ -153,7 +153,7 @@ __host__ __device__ __forceinline__ Span visible(const Scores& sc, int r, long l
   return v;
 }
 // cap tanh(y / cap) of a score in any unit, inv = 1 / cap in that unit.  Up to |y| = cap the odd polynomial u P(u^2) whose largest relative error on [0, 1] is
-// smallest (fitted here: 5e-8, 1.6e-7 with fp32's roundings), beyond it 1 - 2 / (1 + e^(2 |u|)).
+// smallest (fitted here: 7e-8, 1.9e-7 with fp32's roundings, 2.7e-7 where u cap is a product of its own), beyond it 1 - 2 / (1 + e^(2 |u|)).
 constexpr float TANH0 = 0x1.fffffep-1f, TANH1 = -0x1.55540ap-2f, TANH2 = 0x1.10e672p-3f, TANH3 = -0x1.b5eb84p-5f, TANH4 = 0x1.4c6e58p-6f, TANH5 = -0x1.968b6ap-8f,
                 TANH6 = 0x1.10e5d2p-10f;
 __device__ __forceinline__ float tanh_large(float u) {           // |u| > 1
