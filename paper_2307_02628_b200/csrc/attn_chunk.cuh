@@ -20,7 +20,7 @@
 // bf16, 16 bits, in two products each; the weights' lower halves take the other 32 columns of their scores.  Twice the
 // products, and at HD = 128 one tile of rows instead of two: 4 chunks of 512 tokens at 2048, 32 heads of 128, bf16: 230 us from and to fp16, 90
 // from and to bf16; 2 x 1024 tokens, 32 heads of 64: 66 and 37.  fp32 results take 22 bits: over 4 bits, whose pairs are fp16, they
-// come here too (8 chunks of 3-1024 tokens at 1024-4096, 32 heads of 128, from and to fp32: 652 us, 2091 in the kernel for few rows), else they go to the
+// come here too (8 chunks of 3-1024 tokens at 1024-4096, 32 heads of 128, from and to fp32: 694 us, 2091 in the kernel for few rows), else they go to the
 // kernel for few rows, which has three bf16, or two fp16, for them.  A key's scale (8-bit caches) multiplies its score in the softmax, a value's scale its weight, before the rounding.
 //
 // The running maximum is raised only when it would be passed by 2^8 (weights then reach 256, well inside bf16 and the fp32
@@ -49,6 +49,7 @@ namespace ac {
 
 constexpr int THREADS = 512, KEYS = 128, TILE_ROWS = 128, STAGES = 2, SIDE = 4, HALF = 64;
 constexpr float SLACK = 8.f;
+constexpr int SUM_HALVES = 4;            // halves after which O joins a sum of its own, where results are fp32: a power of two
 // Registers per thread of the softmax, the loader and the product warpgroups; the block is launched with 128 for each of its
 // 512 threads, and the shares add up to no more: 2 x 128 x 168 + 128 x 120 + 128 x 40 = 63 488.
 constexpr int LAUNCH_REGS = 128, SOFTMAX_REGS = 168, LOADER_REGS = 120, PRODUCT_REGS = 40;
@@ -65,7 +66,8 @@ template <int HD, bool PAIRS> struct Layout {
   static constexpr int SIDE_BYTES = 2 * KEYS * 4 + 16;
   static constexpr int NEED = END + SIDE * SIDE_BYTES + 1024;  // + alignment
   static constexpr int SMEM = NEED > 116 * 1024 ? NEED : 116 * 1024;   // one block per SM: each takes all of the tensor memory
-  static constexpr int O_COL = 256;                            // tensor memory: S_0 at 0 and 64, S_1 at 128 and 192, O_0, O_1 from 256
+  static constexpr int O_COL = 256;                            // tensor memory: S_0 at 0 and 64, S_1 at 128 and 192, O_0, O_1 from 256,
+  static constexpr int SUM_COL = O_COL + 128;                  // and with pairs sums of O_0, O_1
 };
 
 // bf16 x bf16 (half: fp16 x fp16) -> fp32, 128 rows; b_mn: B is stored with its output axis contiguous
@@ -297,6 +299,10 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   constexpr bool FOLD = FOUR && !PAIRS;
   constexpr float LIFT = FOLD ? 16.f : 128.f, BACK = 1.f / LIFT;  // values, or weights, are relative to a power of two (ve) over LIFT
   constexpr int ROWS = L::ROWS;
+  // The tensor core's additions truncate, so a long sum comes out smaller (16 384 equal values 3.1e-5, random ones 1e-5): results in fp32
+  // have theirs in parts of 256 keys, which are added to nearest (1e-6; 8 chunks of 3-1024 tokens at 1024-4096, 32 heads of 128: 652 us without, 694 with).
+  constexpr bool SUMS = FOUR && PAIRS;
+  const int sum_mask = SUMS && out.dtype == DT_FP32 ? SUM_HALVES - 1 : 0x7fffffff;
   extern __shared__ unsigned char ac_smem[];
   __shared__ uint64_t bars[4 * STAGES + 13 + SIDE];
   __shared__ uint32_t tmem_slot;
@@ -527,6 +533,27 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     const float unit = changed ? 1.f : scale;                    // base-2 units per unit of m
     float ve = 0.f;                                              // 4 bits: what values or their weights are relative to
     bool ok = true;
+    // Results in fp32: O of every SUM_HALVES halves is added to a sum beside it, whose unit is behind by `since`.  The product of half i begins anew.
+    const uint32_t sum_addr = tmem + lanes + L::SUM_COL + t * HD;
+    float since = 1.f;
+    auto join = [&](int i) {
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(odone + 8 * t, (i - 1) & 1, abort_flag, b.status));
+      if (!ok) return false;
+      fence_after();
+#pragma unroll 1
+      for (int c0 = 0; c0 < HD; c0 += 16) {
+        uint32_t v[32], old[32], sum[16];
+        tc::tmem_ld16(o_addr + c0, v);
+        if (i > SUM_HALVES) tc::tmem_ld16(sum_addr + c0, old);
+        tmem_wait_ld();
+#pragma unroll
+        for (int k = 0; k < 16; ++k) sum[k] = i > SUM_HALVES ? __float_as_uint(fmaf(__uint_as_float(old[k]), since, __uint_as_float(v[k]))) : v[k];
+        tmem_st16(sum_addr + c0, sum);
+      }
+      tmem_wait_st();
+      since = 1.f;
+      return true;
+    };
     for (int i = 0; i < n_keys[t]; ++i) {
       const int j = i >> 1, h = i & 1;
       // scales and mask have a barrier of their own; it cannot run a phase ahead of this wait, because the loaders reach tile
@@ -547,6 +574,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
 #pragma unroll
           for (int c = 0; c < (PAIRS ? 4 : 2); ++c) tmem_st16(s_half + 16 * c, none);
           tmem_wait_st();
+          if (SUMS && i > 0 && (i & sum_mask) == 0 && !join(i)) break;
           fence_before();
           if (i > 0 && i + 1 == n_keys[t]) {                     // as below
             ok = __all_sync(0xffffffffu, tc::mbar_wait(odone + 8 * t, (i - 1) & 1, abort_flag, b.status));
@@ -598,6 +626,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
           a *= ve / ve_now;                                      // powers of two, or 0 over one
           ve = ve_now;
         }
+        since *= a;
         if (i > 0) {
           ok = __all_sync(0xffffffffu, tc::mbar_wait(odone + 8 * t, (i - 1) & 1, abort_flag, b.status));
           if (!ok) break;
@@ -644,6 +673,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       un2(add2(sum[0], sum[1]), a0, a1);
       l += a0 + a1;
       tmem_wait_st();
+      if (SUMS && i > 0 && (i & sum_mask) == 0 && !join(i)) break;
       fence_before();
       // The last half waits here for the product before its own, so that the wait after the loop is for the phase in progress or
       // the one before: a wait looks at a phase's parity only, and one for a phase two back would never end.
@@ -662,16 +692,26 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         ok = __all_sync(0xffffffffu, tc::mbar_wait(odone + 8 * t, (n_keys[t] - 1) & 1, abort_flag, b.status));
         fence_after();
       }
+      const bool joined = SUMS && n_keys[t] > SUM_HALVES && sum_mask == SUM_HALVES - 1;
+      auto load = [&](int c0, uint32_t (&v)[32]) {               // 32 columns of the row's sums
+        tc::tmem_ld32(o_addr + c0, v);
+        if (joined) {
+          uint32_t old[32];
+          tc::tmem_ld32(sum_addr + c0, old);
+          tmem_wait_ld();
+#pragma unroll
+          for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(fmaf(__uint_as_float(old[k]), since, __uint_as_float(v[k])));
+        } else {
+          tmem_wait_ld();
+        }
+      };
       if (ok && used_splits == 1) {
         const float inv = l > 0.f ? (FOUR ? ve * BACK : 1.f) / l : 0.f;
         const long long at = (long long)(f0 + token) * out.row_stride + head * out.head_stride;
 #pragma unroll 1
         for (int c0 = 0; c0 < HD; c0 += 32) {
           uint32_t v[32];
-          if (n_keys[t] > 0) {
-            tc::tmem_ld32(o_addr + c0, v);
-            tmem_wait_ld();
-          }
+          if (n_keys[t] > 0) load(c0, v);
           if (r < n_rows[t]) {
 #pragma unroll
             for (int i = 0; i < 32; i += 8) {
@@ -696,10 +736,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
 #pragma unroll 1
         for (int c0 = 0; c0 < HD; c0 += 32) {
           uint32_t v[32] = {};
-          if (n_keys[t] > 0) {
-            tc::tmem_ld32(o_addr + c0, v);
-            tmem_wait_ld();
-          }
+          if (n_keys[t] > 0) load(c0, v);
           if (r < n_rows[t]) {
 #pragma unroll
             for (int i = 0; i < 32; i += 4)
@@ -966,7 +1003,7 @@ paged_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
           const uint64_t va = v_desc(at + L::V + ((i >> 1) % STAGES) * L::TILE + h * (HALF * 128), 128 * 128);
 #pragma unroll 1
           for (int part = 0; part < (PAIRS ? 2 : 1); ++part) {
-            const uint32_t first = i + part > 0;
+            const uint32_t first = (SUMS ? i & sum_mask : i) + part > 0;
 #pragma unroll
             for (int k = 0; k < HALF / 16; ++k)
               mma_ts(tm + L::O_COL + t * HD, tm + t * 128 + h * HALF + part * (HALF / 2) + k * 8, va + k * (2048 >> 4), id_o, k > 0 ? 1u : first);
