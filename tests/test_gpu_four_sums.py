@@ -1,9 +1,10 @@
 """Results in fp32 over many keys: sums that do not shrink.
 
 Queries are zeros and all values one number, so that every weight is 1 and their sum a whole number: what a result is off by is its sum over the values.  A
-tensor core's addition truncates, by at most 2^-23 of the sum so far.  In the kernel for chunks at most 32 follow one another (4 x 64 keys, 16 at a time, a weight's two
-parts one after the other), of a sum that grows evenly: half of 32 * 2^-23.  Then sums of 256 keys are added, rounded to nearest: half of n / 256 * 2^-24; the weight's second
-part is rounded to 2^-23, and two more products to 2^-24 each.
+tensor core's addition of 16 products truncates each of them, and the sum so far, to a multiple of the last place: 2^-23 of the sum at most.  The kernel for chunks makes a
+sum of 256 keys of 16 additions of the weights' first parts and as many of their second ones.  A first part (11 bits) times 2688 (21 * 2^7) has 16 bits, of a sum of at most 256
+such products all 24: nothing is lost but by the sum so far, 32 times.  Of a second part's products each may lose as much: 16 * 16.  Half of it all, as the sum grows evenly.
+Then sums of 256 keys are added, rounded to nearest: half of n / 256 * 2^-24; the weight's second part is rounded to 2^-23, and two more products to 2^-24 each.
 """
 import pytest
 import torch
@@ -31,5 +32,5 @@ def test_sums_over_many_keys(hd, heads, new, length, value, masked):
     out = cache.attention(0, torch.zeros(new, heads, hd, device="cuda"), lay.batch(), scores=sc).cpu().double()
     assert cache.status() == 0
     want = 2688 * scale * (1 if value > 0 else -1)
-    limit = 16 * 2.0 ** -23 + length / 512 * 2.0 ** -24 + 2.0 ** -22
+    limit = (16 * 16 + 32) / 2 * 2.0 ** -23 + length / 512 * 2.0 ** -24 + 2.0 ** -22
     assert float((out / want - 1).abs().max()) <= limit, (float((out / want - 1).abs().max()), limit)
