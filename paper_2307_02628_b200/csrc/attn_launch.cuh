@@ -102,6 +102,15 @@ int pick_split(long slots, long units, long rows, int64_t max_len) {
   return (int)std::min<int64_t>((max_len + best * 64 - 1) / (best * 64) * 64, 0x7fffffc0);
 }
 
+// The tensor core's additions truncate, so that a sum over many keys comes out smaller; joining splits rounds to nearest.  Where results are fp32 a split has
+// no more than this many keys, as far as there is room for the partial results: 1000 single rows of 5 heads over 65 536 positions in bf16 were 1.5e-5 off in one.
+constexpr int64_t kSumKeys = 8192;
+int split_sums(int chunk, long units, long rows, int64_t max_len) {
+  if (chunk <= kSumKeys || units > kPartSlots) return chunk;
+  const int64_t splits = std::min<int64_t>((max_len + kSumKeys - 1) / kSumKeys, kPartSlots / rows);
+  return splits < 2 ? chunk : (int)std::min<int64_t>(chunk, (max_len + splits * 64 - 1) / (splits * 64) * 64);
+}
+
 // Bound on the keys that a block of `rows` query rows goes over.  A window leaves, beside its own length, a token for each row (tokens of one head) and
 // the rounding of the first key to a tile.
 int most_keys(const sd_cache* c, const sd_batch* b, const sd::Scores& sc, int rows) {
@@ -132,7 +141,8 @@ int attention_tiles(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, fl
   const int64_t units = (int64_t)tiles * c->cfg.n_kv_heads * b->n_seqs;
   if (units > 0x7fffffff) return SD_ERR_ARG;
   const int max_len = most_keys(c, b, sc, sd::ap::ROWS);
-  const int chunk = pick_split((long)c->tile_blocks[SC][index] * c->sm_count, (long)units, (long)units * slot_rows, max_len);
+  int chunk = pick_split((long)c->tile_blocks[SC][index] * c->sm_count, (long)units, (long)units * slot_rows, max_len);
+  if (out->dtype == SD_DTYPE_FP32) chunk = split_sums(chunk, (long)units, (long)units * slot_rows, max_len);
   const int splits = (int)(((int64_t)max_len + chunk - 1) / chunk);
   sd::launch_kernel(early, c->stream, kernel, dim3((unsigned)units, splits), dim3(sd::ap::THREADS), S::SMEM,
       view_of(c, b), rows_of(q), rows_of(out), (const TC*)P.k, (const TC*)P.v, (const float*)P.ks, (const float*)P.vs, c->group, scale_log2, wide(q),
@@ -160,7 +170,8 @@ int attention_four(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, flo
   const int64_t units = (int64_t)tiles * c->cfg.n_kv_heads * b->n_seqs;
   if (units > 0x7fffffff) return SD_ERR_ARG;
   const int max_len = most_keys(c, b, sc, sd::a4::ROWS);
-  const int chunk = pick_split((long)c->tile_blocks[SC][index] * c->sm_count, (long)units, (long)units * slot_rows, max_len);
+  int chunk = pick_split((long)c->tile_blocks[SC][index] * c->sm_count, (long)units, (long)units * slot_rows, max_len);
+  if (out->dtype == SD_DTYPE_FP32) chunk = split_sums(chunk, (long)units, (long)units * slot_rows, max_len);
   const int splits = (int)(((int64_t)max_len + chunk - 1) / chunk);
   sd::launch_kernel(early, c->stream, kernel, dim3((unsigned)units, splits), dim3(sd::a4::THREADS), S::SMEM,
       view_of(c, b), rows_of(q), rows_of(out), (const sd::e2m1*)P.k, (const sd::e2m1*)P.v, (const float*)P.ks, (const float*)P.vs, (const uint8_t*)P.kb, (const uint8_t*)P.vb, c->group,
