@@ -267,7 +267,7 @@ int attention_chunks(sd_cache* c, int l, const sd_batch* b, const sd_heads* q, f
 // 8 heads of 128, 25 rows 49 and 67; 2 of 4096 41 and 45; 8 of 300, 12 heads of 64, 22 and 14.  In 4 bits, where both kernels convert and the few rows' has a
 // half to read: bf16, 16 of 1024, 32 heads of 128, 40 rows 120 and 102, 56 rows 120 and 135; 64 of 4096 over 2 key heads, 32 rows 99 and 90, 48 rows 99 and 127; 2
 // of 4096, 8 heads, 40 and 37, 64 rows 40 and 39; 8 of 300, 12 heads of 64, 48 rows 22 and 14, 64 rows 22 and 21; fp32, 16 of 1024, 40 rows 149 and 135, 56 rows 150
-// and 179.  In 8 bits with pairs and changed scores, e4m3, results written in fp32 by both, the same, 40 rows 234 and 201, 56 rows 236 and 272; 2 of 4096 58 and 49, 58 and 64.
+// and 179 (158 since sums are in parts, the few rows' kernel 159 at 48).  In 8 bits with pairs and changed scores, e4m3, results written in fp32 by both, the same, 40 rows 234 and 201, 56 rows 236 and 272; 2 of 4096 58 and 49, 58 and 64.
 template <typename TC, bool SC> constexpr int kChunkRows(bool pairs) {
   constexpr bool scaled = sd::CacheType<TC>::TOP > 0.f;
   return sd::kFour<TC> || (scaled && SC && pairs) ? 49 : scaled ? 25 : pairs ? 41 : 9;
